@@ -375,6 +375,140 @@ turnopd_status turnopd_vocab_shard_loss_grad(const void *z_student, const void *
                                              turnopd_stream_t stream);
 
 /*
+ * ---- Log probabilities of given tokens ----
+ *
+ * turnopd_token_logprobs -- log probability of one given token per row, the
+ * row's entropy and its most probable tokens (Sec. 3: the log probabilities
+ * log pi(y_i | .) of the sampled tokens that the one-token estimator and
+ * importance ratios take, under student or teacher; natural log throughout,
+ * softmax of the raw logits).
+ *
+ * For every supervised token i (loss_mask[i] = 1; all tokens if loss_mask is
+ * NULL) with row r = row_of_token[i] (or i when row_of_token is NULL), z = row r,
+ * m = max_v z_v and S = sum_v exp(z_v - m):
+ *   logprob_out[i]   = (z_y - m) - log S, y = token_ids[i]
+ *   entropy_out[i]   = -sum_v p_v log p_v,  p_v = exp(z_v - m) / S
+ *   stats_out[i]     = (m, log S): log p_v = (z_v - m) - log S for every v
+ *   top_ids_out[i], top_logprob_out[i] = the n_top ids of largest logit, the
+ *                      lower id first among equal logits (+0 and -0 are equal),
+ *                      and their log probabilities
+ * A logit of -inf (a forbidden token) has probability 0 and log probability
+ * -inf, and adds nothing to the entropy.
+ * Inputs:
+ *   logits       [num_rows, ld] row-major, in_dtype (F32 or BF16), any element
+ *                 alignment; columns [vocab, ld) are not read.
+ *   row_of_token  int32[num_tokens] or NULL (then num_rows >= num_tokens);
+ *                 several tokens may name one row.
+ *   token_ids     int32[num_tokens], or NULL (then logprob_out is NULL too).
+ *   loss_mask     uint8[num_tokens] or NULL.
+ *   n_top         0 (no alternatives) to min(vocab, TURNOPD_TOP_ALTERNATIVES_MAX).
+ * Outputs (each nullable, but not all; the two top arrays are needed if n_top > 0):
+ *   logprob_out, entropy_out  float32[num_tokens]; 0 for masked tokens
+ *   stats_out      float32[num_tokens, 2]; (0, 0) for masked tokens
+ *   top_ids_out    int32[num_tokens, n_top], -1 for masked tokens;
+ *   top_logprob_out float32[num_tokens, n_top], 0 for masked tokens.
+ * Workspace: turnopd_token_logprobs_workspace_bytes(num_tokens) bytes, 256-byte
+ *   aligned; NULL and 0 will do when loss_mask is NULL.
+ * Device errors (the token's outputs are those of a masked one, its stats (-inf, 0)):
+ *   TURNOPD_ERR_TOKEN_RANGE (row or token id), TURNOPD_ERR_NONFINITE (a row that holds
+ *   NaN or +inf, or no logit above -1.2e38).
+ * Precision: fp32 arithmetic on exact inputs.  The sums leave y out and add its
+ *   term at the end, so that logprob_out and entropy_out keep their relative
+ *   precision where y is all but certain.
+ */
+#define TURNOPD_TOP_ALTERNATIVES_MAX 32
+turnopd_status turnopd_token_logprobs(const void *logits, int32_t in_dtype, int64_t ld, int64_t vocab,
+                                      int64_t num_rows, const int32_t *row_of_token,
+                                      const int32_t *token_ids, const uint8_t *loss_mask,
+                                      int64_t num_tokens, int32_t n_top, float *logprob_out,
+                                      float *entropy_out, float *stats_out, int32_t *top_ids_out,
+                                      float *top_logprob_out, void *workspace, size_t workspace_bytes,
+                                      int32_t *dev_status, turnopd_stream_t stream);
+
+size_t turnopd_token_logprobs_workspace_bytes(int64_t num_tokens);
+
+/*
+ * turnopd_token_logprobs_bwd -- the gradient of any function of the log
+ * probabilities and entropies (a policy-gradient term, an entropy bonus) with
+ * respect to the logits.  With gl = d_logprob[i], gh = d_entropy[i]:
+ *   grad[r, v] = gl (delta_vy - p_v) - gh p_v (log p_v + H_i)
+ * Inputs: logits, row_of_token, token_ids, loss_mask as in the forward call; stats,
+ *   logprob and entropy are its outputs (logprob and token_ids are needed if
+ *   d_logprob is given, entropy if d_entropy is); d_logprob, d_entropy
+ *   float32[num_tokens], either nullable.
+ * Output: grad_out [num_rows, ld] of grad_dtype (F32 or BF16).  Rows of supervised
+ *   tokens get the gradient (zeros where the forward call found no distribution),
+ *   columns [vocab, ld) and other rows are not written unless
+ *   TURNOPD_ZERO_MASKED_GRAD, which zero-fills columns [0, vocab) of masked tokens'
+ *   rows.  grad_out may be the logits themselves (grad_dtype = in_dtype), else it
+ *   may not overlap them.  A row belongs to one supervised token at most.
+ * Flags: TURNOPD_ZERO_MASKED_GRAD only.  Workspace as in the forward call.
+ * Device errors: TURNOPD_ERR_TOKEN_RANGE (row or token id; token skipped).
+ * Precision: 1 - p_y is -expm1(logprob[i]), so it keeps its relative precision.
+ */
+turnopd_status turnopd_token_logprobs_bwd(const void *logits, int32_t in_dtype, int64_t ld, int64_t vocab,
+                                          int64_t num_rows, const int32_t *row_of_token,
+                                          const int32_t *token_ids, const uint8_t *loss_mask,
+                                          int64_t num_tokens, const float *stats, const float *logprob,
+                                          const float *entropy, const float *d_logprob,
+                                          const float *d_entropy, void *grad_out, int32_t grad_dtype,
+                                          uint32_t flags, void *workspace, size_t workspace_bytes,
+                                          int32_t *dev_status, turnopd_stream_t stream);
+
+/*
+ * ---- The norm before the LM head ----
+ *
+ * turnopd_norm_fwd -- layer norm or root-mean-square norm of hidden states: what
+ * stands between a model's last block and its LM head (its bf16 output is h_s of
+ * turnopd_fused_lmhead_fwd_bwd).  For every supervised token i (all tokens if
+ * loss_mask is NULL), x = row i, over its d columns:
+ *   mu = mean x (0 for TURNOPD_RMS_NORM),  r = 1 / sqrt(mean (x - mu)^2 + eps)
+ *   y_out[i, j] = (x_j - mu) r gamma_j + beta_j
+ * Inputs:
+ *   x       [num_tokens, ldx] row-major, x_dtype (F32 or BF16), any element alignment
+ *   gamma   [d] of param_dtype (F32 or BF16); beta [d] of param_dtype or NULL (0)
+ *   loss_mask uint8[num_tokens] or NULL: rows of masked tokens are not read.
+ * Outputs:
+ *   y_out    [num_tokens, ldy] of y_dtype; rows of masked tokens are zero;
+ *            columns [d, ldy) are not written; may not overlap x.
+ *   mean_out, rstd_out  float32[num_tokens], each nullable: mu and r, both 0 for
+ *            masked tokens; turnopd_norm_bwd takes them.
+ * Device errors (the token is treated as masked): TURNOPD_ERR_NONFINITE (mu or r is
+ *   not finite: NaN or inf in the row, or squares beyond fp32).
+ * Precision: fp32; the variance is summed over x - mu.
+ */
+enum { TURNOPD_LAYER_NORM = 0, TURNOPD_RMS_NORM = 1 };            /* norm kind     */
+turnopd_status turnopd_norm_fwd(const void *x, int32_t x_dtype, int64_t ldx, const void *gamma,
+                                const void *beta, int32_t param_dtype, const uint8_t *loss_mask,
+                                int64_t num_tokens, int64_t d, int32_t kind, double eps, void *y_out,
+                                int32_t y_dtype, int64_t ldy, float *mean_out, float *rstd_out,
+                                int32_t *dev_status, turnopd_stream_t stream);
+
+/*
+ * turnopd_norm_bwd -- its backward pass.  With xh = (x - mu) r and g = dy gamma:
+ *   dx_out[i, j]  = r (g_j - mean g - xh_j mean(g xh))   (RMS norm: without mean g)
+ *   dgamma_out[j] = sum_i dy_ij xh_ij,   dbeta_out[j] = sum_i dy_ij
+ * over the supervised tokens that the forward call found finite (rstd[i] > 0).
+ * Inputs: x, gamma, loss_mask, kind as in the forward call, mean and rstd its outputs
+ *   (mean is not read and may be NULL for TURNOPD_RMS_NORM); dy [num_tokens, lddy] of
+ *   dy_dtype (dh_s_out of turnopd_fused_lmhead_fwd_bwd, for one); rows of masked
+ *   tokens are not read.
+ * Outputs (each nullable, but not all): dx_out [num_tokens, lddx] of dx_dtype, zero
+ *   rows for masked tokens, columns [d, lddx) not written, may not overlap x or dy;
+ *   dgamma_out, dbeta_out float32[d] (overwritten, not accumulated; fixed-order sums).
+ * Workspace: turnopd_norm_bwd_workspace_bytes(num_tokens, d) bytes, 256-byte aligned;
+ *   NULL and 0 will do when dgamma_out and dbeta_out are NULL.
+ */
+turnopd_status turnopd_norm_bwd(const void *x, int32_t x_dtype, int64_t ldx, const void *gamma,
+                                int32_t param_dtype, const uint8_t *loss_mask, int64_t num_tokens,
+                                int64_t d, int32_t kind, const float *mean, const float *rstd,
+                                const void *dy, int32_t dy_dtype, int64_t lddy, void *dx_out,
+                                int32_t dx_dtype, int64_t lddx, float *dgamma_out, float *dbeta_out,
+                                void *workspace, size_t workspace_bytes, turnopd_stream_t stream);
+
+size_t turnopd_norm_bwd_workspace_bytes(int64_t num_tokens, int64_t d);
+
+/*
  * ---- Adaptive rollout-depth controller and loss-allocation diagnostics ----
  * (Sec. 4.1 "Adaptive Rollout-Depth Budgeting", Algorithm 1, and the
  * loss-allocation diagnostics of Sec. 3).  Host functions: every pointer is

@@ -31,6 +31,9 @@ __all__ = [
     "turnopd_depth_coverage", "turnopd_turn_diagnostics",
     "turnopd_vocab_stats_bytes", "turnopd_vocab_shard_stats", "turnopd_vocab_stats_merge",
     "turnopd_vocab_shard_loss_grad",
+    "TURNOPD_TOP_ALTERNATIVES_MAX", "TURNOPD_LAYER_NORM", "TURNOPD_RMS_NORM",
+    "turnopd_token_logprobs", "turnopd_token_logprobs_bwd", "turnopd_token_logprobs_workspace_bytes",
+    "turnopd_norm_fwd", "turnopd_norm_bwd", "turnopd_norm_bwd_workspace_bytes",
 ]
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -45,6 +48,8 @@ TURNOPD_MAX_TURNS = 4096
 TURNOPD_STATIC_MAX_TOKENS = 65536
 TURNOPD_TOPK_MAX = 1024
 TURNOPD_TOPK_MAX_VOCAB = 737280
+TURNOPD_TOP_ALTERNATIVES_MAX = 32
+TURNOPD_LAYER_NORM, TURNOPD_RMS_NORM = 0, 1
 
 STATUS_NAMES = {
     0: "TURNOPD_OK", 1: "TURNOPD_ERR_NULL", 2: "TURNOPD_ERR_SHAPE", 3: "TURNOPD_ERR_OFFSETS",
@@ -106,6 +111,12 @@ def load():
         "turnopd_selftest_wait_timeout": [u32, P, P],
         "turnopd_vocab_shard_loss_grad": [P, P, i32, i64, i64, i64, P, P, P, i64, P, P, i32, u32, P, P, P,
                                           sz, P, P],
+        "turnopd_token_logprobs": [P, i32, i64, i64, i64, P, P, P, i64, i32, P, P, P, P, P, P, sz, P, P],
+        "turnopd_token_logprobs_bwd": [P, i32, i64, i64, i64, P, P, P, i64, P, P, P, P, P, P, i32, u32, P, sz,
+                                       P, P],
+        "turnopd_norm_fwd": [P, i32, i64, P, P, i32, P, i64, i64, i32, f64, P, i32, i64, P, P, P, P],
+        "turnopd_norm_bwd": [P, i32, i64, P, i32, P, i64, i64, i32, P, P, P, i32, i64, P, i32, i64, P, P, P, sz,
+                             P],
     })
     for name, args in sig.items():
         fn = getattr(lib, name)
@@ -124,6 +135,10 @@ def load():
     lib.turnopd_turn_floor.argtypes = [i64, i32, f64]
     lib.turnopd_turn_floor.restype = i32
     lib.turnopd_depth_default_params.restype = None
+    lib.turnopd_token_logprobs_workspace_bytes.argtypes = [i64]
+    lib.turnopd_token_logprobs_workspace_bytes.restype = sz
+    lib.turnopd_norm_bwd_workspace_bytes.argtypes = [i64, i64]
+    lib.turnopd_norm_bwd_workspace_bytes.restype = sz
     lib.turnopd_vocab_stats_bytes.argtypes = [i64]
     lib.turnopd_vocab_stats_bytes.restype = sz
     lib.turnopd_status_string.argtypes = [ctypes.c_int]
@@ -435,6 +450,145 @@ def turnopd_vocab_shard_loss_grad(z_student, z_teacher, row_of_token, loss_mask,
         _ptr(row_of_token), _ptr(loss_mask), _ptr(w), T, _ptr(merged_stats), _ptr(grad_shard), gdt, int(flags),
         _ptr(token_loss_out), _ptr(loss_out), _ptr(workspace), workspace.numel() * workspace.element_size(),
         _ptr(dev_status), _stream(stream)), "turnopd_vocab_shard_loss_grad")
+
+
+# ---------------------------------------------------------------- log probabilities of given tokens
+
+def _rows_2d(t, name, like=None):
+    """(row stride) of a 2-D CUDA tensor with unit column stride."""
+    if not t.is_cuda or t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] > 1):
+        raise ValueError(f"{name} must be a 2-D CUDA tensor with unit column stride")
+    if like is not None and (t.shape != like.shape or t.stride(0) != like.stride(0)):
+        raise ValueError(f"{name} must match the logits in shape and row stride")
+    return max(t.stride(0), t.shape[1]) if t.shape[0] < 2 else t.stride(0)
+
+
+def turnopd_token_logprobs_workspace_bytes(num_tokens: int) -> int:
+    return int(load().turnopd_token_logprobs_workspace_bytes(int(num_tokens)))
+
+
+def _num_tokens(logits, row_of_token, token_ids, loss_mask):
+    for t in (loss_mask, token_ids, row_of_token):
+        if t is not None:
+            return t.numel()
+    return logits.shape[0]
+
+
+def _ws(workspace):
+    return 0 if workspace is None else workspace.numel() * workspace.element_size()
+
+
+def turnopd_token_logprobs(logits, vocab, row_of_token, token_ids, loss_mask, n_top, logprob_out, entropy_out,
+                           stats_out, top_ids_out, top_logprob_out, workspace, dev_status, stream=None):
+    """Log probability of token_ids[i] in its row, the row's entropy, (m, log S) and the n_top best ids.
+    logits [num_rows, ld]; row_of_token, token_ids int32 [T] or None; loss_mask uint8 [T] or None (every
+    token; workspace may be None then); the outputs float32 [T] / [T, 2] / int32 and float32 [T, n_top], or None."""
+    import torch
+
+    ld = _rows_2d(logits, "logits")
+    T = _num_tokens(logits, row_of_token, token_ids, loss_mask)
+    _need(row_of_token, "row_of_token", torch.int32, T)
+    _need(token_ids, "token_ids", torch.int32, T)
+    _need(loss_mask, "loss_mask", torch.uint8, T)
+    _need(logprob_out, "logprob_out", torch.float32, T)
+    _need(entropy_out, "entropy_out", torch.float32, T)
+    _need(stats_out, "stats_out", torch.float32, 2 * T)
+    _need(top_ids_out, "top_ids_out", torch.int32, T * int(n_top))
+    _need(top_logprob_out, "top_logprob_out", torch.float32, T * int(n_top))
+    _need(workspace, "workspace")
+    _need(dev_status, "dev_status", torch.int32, 1)
+    if vocab > logits.shape[1]:
+        raise ValueError("vocab is larger than the rows of logits")
+    _check(load().turnopd_token_logprobs(
+        _ptr(logits), _dtype_code(logits, "logits"), ld, int(vocab), logits.shape[0], _ptr(row_of_token),
+        _ptr(token_ids), _ptr(loss_mask), T, int(n_top), _ptr(logprob_out), _ptr(entropy_out), _ptr(stats_out),
+        _ptr(top_ids_out), _ptr(top_logprob_out), _ptr(workspace), _ws(workspace), _ptr(dev_status),
+        _stream(stream)), "turnopd_token_logprobs")
+
+
+def turnopd_token_logprobs_bwd(logits, vocab, row_of_token, token_ids, loss_mask, stats, logprob, entropy, d_logprob,
+                               d_entropy, grad_out, flags, workspace, dev_status, stream=None):
+    """Gradient with respect to the logits from d_logprob and / or d_entropy (float32 [T] or None);
+    stats, logprob and entropy are the forward call's outputs; grad_out is shaped like the logits, or is
+    the logits."""
+    import torch
+
+    ld = _rows_2d(logits, "logits")
+    _rows_2d(grad_out, "grad_out", logits)
+    T = _num_tokens(logits, row_of_token, token_ids, loss_mask)
+    _need(row_of_token, "row_of_token", torch.int32, T)
+    _need(token_ids, "token_ids", torch.int32, T)
+    _need(loss_mask, "loss_mask", torch.uint8, T)
+    _need(stats, "stats", torch.float32, 2 * T)
+    _need(logprob, "logprob", torch.float32, T)
+    _need(entropy, "entropy", torch.float32, T)
+    _need(d_logprob, "d_logprob", torch.float32, T)
+    _need(d_entropy, "d_entropy", torch.float32, T)
+    _need(workspace, "workspace")
+    _need(dev_status, "dev_status", torch.int32, 1)
+    if vocab > logits.shape[1]:
+        raise ValueError("vocab is larger than the rows of logits")
+    _check(load().turnopd_token_logprobs_bwd(
+        _ptr(logits), _dtype_code(logits, "logits"), ld, int(vocab), logits.shape[0], _ptr(row_of_token),
+        _ptr(token_ids), _ptr(loss_mask), T, _ptr(stats), _ptr(logprob), _ptr(entropy), _ptr(d_logprob),
+        _ptr(d_entropy), _ptr(grad_out), _dtype_code(grad_out, "grad_out"), int(flags), _ptr(workspace),
+        _ws(workspace), _ptr(dev_status), _stream(stream)), "turnopd_token_logprobs_bwd")
+
+
+# ---------------------------------------------------------------- the norm before the LM head
+
+def _norm_checks(T, d, gamma, beta, loss_mask, mean, rstd):
+    import torch
+
+    _need(gamma, "gamma", None, d)
+    if beta is not None and beta.dtype != gamma.dtype:
+        raise ValueError("gamma and beta must have one dtype")
+    _need(beta, "beta", None, d)
+    _need(loss_mask, "loss_mask", torch.uint8, T)
+    _need(mean, "mean", torch.float32, T)
+    _need(rstd, "rstd", torch.float32, T)
+
+
+def turnopd_norm_fwd(x, gamma, beta, loss_mask, kind, eps, y_out, mean_out, rstd_out, dev_status, stream=None):
+    """x [T, d] -> y_out [T, d] (rows any stride); gamma, beta [d] (beta or None); loss_mask uint8 [T] or None;
+    mean_out, rstd_out float32 [T] or None; kind TURNOPD_LAYER_NORM or TURNOPD_RMS_NORM."""
+    import torch
+
+    ldx, ldy = _rows_2d(x, "x"), _rows_2d(y_out, "y_out")
+    T, d = x.shape
+    if y_out.shape != x.shape:
+        raise ValueError("y_out must match x in shape")
+    _norm_checks(T, d, gamma, beta, loss_mask, mean_out, rstd_out)
+    _need(dev_status, "dev_status", torch.int32, 1)
+    _check(load().turnopd_norm_fwd(
+        _ptr(x), _dtype_code(x, "x"), ldx, _ptr(gamma), _ptr(beta), _dtype_code(gamma, "gamma"), _ptr(loss_mask), T, d,
+        int(kind), float(eps), _ptr(y_out), _dtype_code(y_out, "y_out"), ldy, _ptr(mean_out), _ptr(rstd_out),
+        _ptr(dev_status), _stream(stream)), "turnopd_norm_fwd")
+
+
+def turnopd_norm_bwd_workspace_bytes(num_tokens: int, d: int) -> int:
+    return int(load().turnopd_norm_bwd_workspace_bytes(int(num_tokens), int(d)))
+
+
+def turnopd_norm_bwd(x, gamma, loss_mask, kind, mean, rstd, dy, dx_out, dgamma_out, dbeta_out, workspace, stream=None):
+    """dx_out [T, d] (or None), dgamma_out and dbeta_out float32 [d] (or None) from dy [T, d]; mean (None for the
+    root-mean-square norm) and rstd are the forward call's."""
+    import torch
+
+    ldx, lddy = _rows_2d(x, "x"), _rows_2d(dy, "dy")
+    T, d = x.shape
+    if dy.shape != x.shape or (dx_out is not None and dx_out.shape != x.shape):
+        raise ValueError("dy and dx_out must match x in shape")
+    lddx = _rows_2d(dx_out, "dx_out") if dx_out is not None else d
+    _norm_checks(T, d, gamma, None, loss_mask, mean, rstd)
+    _need(dgamma_out, "dgamma_out", torch.float32, d)
+    _need(dbeta_out, "dbeta_out", torch.float32, d)
+    _need(workspace, "workspace")
+    _check(load().turnopd_norm_bwd(
+        _ptr(x), _dtype_code(x, "x"), ldx, _ptr(gamma), _dtype_code(gamma, "gamma"), _ptr(loss_mask), T, d, int(kind),
+        _ptr(mean), _ptr(rstd), _ptr(dy), _dtype_code(dy, "dy"), lddy, _ptr(dx_out),
+        TURNOPD_F32 if dx_out is None else _dtype_code(dx_out, "dx_out"), lddx, _ptr(dgamma_out), _ptr(dbeta_out),
+        _ptr(workspace), _ws(workspace), _stream(stream)), "turnopd_norm_bwd")
 
 
 # ---------------------------------------------------------------- rollout-depth controller (host)

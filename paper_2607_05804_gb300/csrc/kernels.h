@@ -98,7 +98,8 @@ struct RowIn {
 int device_sm_count();
 cudaError_t launch_wait_selftest(uint32_t limit, int32_t *status, cudaStream_t stream);
 
-// Pieces of the loss path reused by the fused LM-head path.
+// Pieces of the loss path reused by the fused LM-head path and by the token log
+// probabilities (which have no weights and no token losses: a.w and a.token_loss may be null).
 cudaError_t launch_compaction(const LossArgs &a, int4 *rows, int32_t *blk_count, int32_t *nvalid,
                               cudaStream_t stream);
 void launch_loss_sum(const double *row_wl, int32_t *nvalid, double *loss, int32_t *status,
@@ -189,5 +190,82 @@ cudaError_t launch_rows_f32_ragged(const RowIn &p, bool fp32_grad, cudaStream_t 
 // Split-row kernel (clusters of CTAs stream each row twice) for fp32 rows longer than a
 // cluster holds, vocab and ld multiples of 4.
 cudaError_t launch_row_split(const RowIn &p, bool fp32_grad, cudaStream_t stream);
+
+// Log probabilities of given tokens, and their gradient.
+struct LogprobCall {
+    const void *logits;
+    int32_t in_dtype;
+    int64_t ld, vocab, num_rows;
+    const int32_t *row_of_token, *token_ids;
+    const uint8_t *mask;
+    int64_t T;
+    int32_t n_top;
+    float *logprob, *entropy, *stats;
+    int32_t *top_ids;
+    float *top_logprob;
+    void *workspace;
+    int32_t *status;
+};
+
+struct LogprobGradCall {
+    const void *logits;
+    int32_t in_dtype;
+    int64_t ld, vocab, num_rows;
+    const int32_t *row_of_token, *token_ids;
+    const uint8_t *mask;
+    int64_t T;
+    const float *stats, *logprob, *entropy, *d_logprob, *d_entropy;
+    void *grad;
+    int32_t grad_dtype;
+    uint32_t flags;
+    void *workspace;
+    int32_t *status;
+};
+
+size_t logprob_workspace_bytes(int64_t T);
+cudaError_t launch_token_logprobs(const LogprobCall &c, cudaStream_t stream);
+cudaError_t launch_token_logprobs_bwd(const LogprobGradCall &c, cudaStream_t stream);
+
+// Final norm and its backward pass.
+struct NormCall {
+    const void *x;
+    int32_t x_dtype;
+    int64_t ldx;
+    const void *gamma, *beta;
+    int32_t param_dtype;
+    const uint8_t *mask;
+    int64_t T, d;
+    int32_t kind;
+    float eps;
+    void *y;
+    int32_t y_dtype;
+    int64_t ldy;
+    float *mean, *rstd;
+    int32_t *status;
+};
+
+struct NormGradCall {
+    const void *x;
+    int32_t x_dtype;
+    int64_t ldx;
+    const void *gamma;
+    int32_t param_dtype;
+    const uint8_t *mask;
+    int64_t T, d;
+    int32_t kind;
+    const float *mean, *rstd;
+    const void *dy;
+    int32_t dy_dtype;
+    int64_t lddy;
+    void *dx;
+    int32_t dx_dtype;
+    int64_t lddx;
+    float *dgamma, *dbeta;
+    void *workspace;
+};
+
+size_t norm_bwd_workspace_bytes(int64_t T, int64_t d);
+cudaError_t launch_norm_fwd(const NormCall &c, cudaStream_t stream);
+cudaError_t launch_norm_bwd(const NormGradCall &c, cudaStream_t stream);
 
 }  // namespace turnopd

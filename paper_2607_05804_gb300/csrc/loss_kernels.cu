@@ -113,7 +113,7 @@ __global__ void k_compact_count(CompactIn c, int32_t *__restrict__ blk_count)
         set_status(c.status, TURNOPD_ERR_TOKEN_RANGE);
 #pragma unroll
     for (int k = 0; k < kPerThread; ++k)
-        if (i0 + k < c.T && !((t.valid >> k) & 1u))
+        if (c.token_loss && i0 + k < c.T && !((t.valid >> k) & 1u))
             c.token_loss[i0 + k] = 0.f;
     int n = warp_sum_i32(__popc(t.valid));
     if ((threadIdx.x & 31) == 0)
@@ -142,7 +142,7 @@ __global__ void k_compact_scatter(CompactIn c, const int32_t *__restrict__ blk_c
     float wv[kPerThread];
 #pragma unroll
     for (int k = 0; k < kPerThread; ++k)
-        wv[k] = ((t.valid >> k) & 1u) ? c.w[i0 + k] : 0.f;
+        wv[k] = c.w && ((t.valid >> k) & 1u) ? c.w[i0 + k] : 0.f;
     asm volatile("griddepcontrol.wait;" ::: "memory");  // every block's count is written
     // exclusive prefix over the preceding blocks
     int64_t pre = 0;

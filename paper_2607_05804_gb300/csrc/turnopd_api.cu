@@ -434,6 +434,146 @@ turnopd_status turnopd_fused_lmhead_fwd_bwd(const void *h_s, const void *W_s, in
     return cuda_status(launch_fused(c, s));
 }
 
+size_t turnopd_token_logprobs_workspace_bytes(int64_t num_tokens)
+{
+    if (num_tokens < 0)
+        return 0;
+    return logprob_workspace_bytes(num_tokens);
+}
+
+static bool is_dtype(int32_t t) { return t == TURNOPD_F32 || t == TURNOPD_BF16; }
+static size_t dtype_size(int32_t t) { return t == TURNOPD_BF16 ? 2 : 4; }
+
+static bool bad_logit_shape(const void *logits, int32_t in_dtype, int64_t ld, int64_t vocab, int64_t num_rows,
+                            const int32_t *row_of_token, int64_t num_tokens)
+{
+    return num_tokens < 0 || num_tokens > INT32_MAX || vocab < 1 || vocab > INT32_MAX || ld < vocab ||
+           num_rows < 0 || (!row_of_token && num_rows < num_tokens) || misaligned(logits, dtype_size(in_dtype));
+}
+
+turnopd_status turnopd_token_logprobs(const void *logits, int32_t in_dtype, int64_t ld, int64_t vocab,
+                                      int64_t num_rows, const int32_t *row_of_token, const int32_t *token_ids,
+                                      const uint8_t *loss_mask, int64_t num_tokens, int32_t n_top,
+                                      float *logprob_out, float *entropy_out, float *stats_out,
+                                      int32_t *top_ids_out, float *top_logprob_out, void *workspace,
+                                      size_t workspace_bytes, int32_t *dev_status, turnopd_stream_t stream)
+{
+    NvtxRange nvtx("turnopd_token_logprobs");
+    if (!dev_status || (num_tokens > 0 && !logits))
+        return TURNOPD_ERR_NULL;
+    if (num_tokens > 0 && ((!logprob_out && !entropy_out && !stats_out && n_top == 0) || (logprob_out && !token_ids) ||
+                           (n_top > 0 && (!top_ids_out || !top_logprob_out))))
+        return TURNOPD_ERR_NULL;
+    if (!is_dtype(in_dtype))
+        return TURNOPD_ERR_UNSUPPORTED;
+    if (bad_logit_shape(logits, in_dtype, ld, vocab, num_rows, row_of_token, num_tokens) || n_top < 0 ||
+        n_top > TURNOPD_TOP_ALTERNATIVES_MAX || n_top > vocab)
+        return TURNOPD_ERR_SHAPE;
+    if (misaligned(logprob_out, 4) || misaligned(entropy_out, 4) || misaligned(stats_out, 4) ||
+        misaligned(top_ids_out, 4) || misaligned(top_logprob_out, 4))
+        return TURNOPD_ERR_SHAPE;
+    if (loss_mask && (!workspace || misaligned(workspace, 256) || workspace_bytes < logprob_workspace_bytes(num_tokens)))
+        return TURNOPD_ERR_WORKSPACE;
+    if (num_tokens == 0)
+        return TURNOPD_OK;
+    LogprobCall c{logits, in_dtype, ld, vocab, num_rows, row_of_token, token_ids, loss_mask, num_tokens, n_top,
+                  logprob_out, entropy_out, stats_out, top_ids_out, top_logprob_out, workspace, dev_status};
+    return cuda_status(launch_token_logprobs(c, (cudaStream_t)stream));
+}
+
+turnopd_status turnopd_token_logprobs_bwd(const void *logits, int32_t in_dtype, int64_t ld, int64_t vocab,
+                                          int64_t num_rows, const int32_t *row_of_token, const int32_t *token_ids,
+                                          const uint8_t *loss_mask, int64_t num_tokens, const float *stats,
+                                          const float *logprob, const float *entropy, const float *d_logprob,
+                                          const float *d_entropy, void *grad_out, int32_t grad_dtype,
+                                          uint32_t flags, void *workspace, size_t workspace_bytes,
+                                          int32_t *dev_status, turnopd_stream_t stream)
+{
+    NvtxRange nvtx("turnopd_token_logprobs_bwd");
+    if (!dev_status || (num_tokens > 0 && (!logits || !grad_out || !stats)))
+        return TURNOPD_ERR_NULL;
+    if (num_tokens > 0 &&
+        ((!d_logprob && !d_entropy) || (d_logprob && (!logprob || !token_ids)) || (d_entropy && !entropy)))
+        return TURNOPD_ERR_NULL;
+    if (!is_dtype(in_dtype) || !is_dtype(grad_dtype) || (flags & ~(uint32_t)TURNOPD_ZERO_MASKED_GRAD) ||
+        (grad_out == logits && grad_out && grad_dtype != in_dtype))
+        return TURNOPD_ERR_UNSUPPORTED;
+    if (bad_logit_shape(logits, in_dtype, ld, vocab, num_rows, row_of_token, num_tokens) ||
+        misaligned(grad_out, dtype_size(grad_dtype)) || misaligned(stats, 4) || misaligned(logprob, 4) ||
+        misaligned(entropy, 4) || misaligned(d_logprob, 4) || misaligned(d_entropy, 4))
+        return TURNOPD_ERR_SHAPE;
+    if (loss_mask && (!workspace || misaligned(workspace, 256) || workspace_bytes < logprob_workspace_bytes(num_tokens)))
+        return TURNOPD_ERR_WORKSPACE;
+    if (num_tokens == 0)
+        return TURNOPD_OK;
+    LogprobGradCall c{logits, in_dtype, ld, vocab, num_rows, row_of_token, token_ids, loss_mask, num_tokens, stats,
+                      logprob, entropy, d_logprob, d_entropy, grad_out, grad_dtype, flags, workspace, dev_status};
+    return cuda_status(launch_token_logprobs_bwd(c, (cudaStream_t)stream));
+}
+
+turnopd_status turnopd_norm_fwd(const void *x, int32_t x_dtype, int64_t ldx, const void *gamma, const void *beta,
+                                int32_t param_dtype, const uint8_t *loss_mask, int64_t num_tokens, int64_t d,
+                                int32_t kind, double eps, void *y_out, int32_t y_dtype, int64_t ldy,
+                                float *mean_out, float *rstd_out, int32_t *dev_status, turnopd_stream_t stream)
+{
+    NvtxRange nvtx("turnopd_norm_fwd");
+    if (!dev_status || !gamma || (num_tokens > 0 && (!x || !y_out)))
+        return TURNOPD_ERR_NULL;
+    if (!is_dtype(x_dtype) || !is_dtype(y_dtype) || !is_dtype(param_dtype) ||
+        (kind != TURNOPD_LAYER_NORM && kind != TURNOPD_RMS_NORM))
+        return TURNOPD_ERR_UNSUPPORTED;
+    if (num_tokens < 0 || num_tokens > INT32_MAX || d < 1 || d > INT32_MAX || ldx < d || ldy < d ||
+        !(eps >= 0.0 && eps <= 3e38) || misaligned(x, dtype_size(x_dtype)) || misaligned(y_out, dtype_size(y_dtype)) ||
+        misaligned(gamma, dtype_size(param_dtype)) || misaligned(beta, dtype_size(param_dtype)) ||
+        misaligned(mean_out, 4) || misaligned(rstd_out, 4))
+        return TURNOPD_ERR_SHAPE;
+    if (num_tokens == 0)
+        return TURNOPD_OK;
+    NormCall c{x, x_dtype, ldx, gamma, beta, param_dtype, loss_mask, num_tokens, d, kind, (float)eps,
+               y_out, y_dtype, ldy, mean_out, rstd_out, dev_status};
+    return cuda_status(launch_norm_fwd(c, (cudaStream_t)stream));
+}
+
+size_t turnopd_norm_bwd_workspace_bytes(int64_t num_tokens, int64_t d)
+{
+    if (num_tokens < 0 || d < 1)
+        return 0;
+    return norm_bwd_workspace_bytes(num_tokens, d);
+}
+
+turnopd_status turnopd_norm_bwd(const void *x, int32_t x_dtype, int64_t ldx, const void *gamma, int32_t param_dtype,
+                                const uint8_t *loss_mask, int64_t num_tokens, int64_t d, int32_t kind,
+                                const float *mean, const float *rstd, const void *dy, int32_t dy_dtype, int64_t lddy,
+                                void *dx_out, int32_t dx_dtype, int64_t lddx, float *dgamma_out, float *dbeta_out,
+                                void *workspace, size_t workspace_bytes, turnopd_stream_t stream)
+{
+    NvtxRange nvtx("turnopd_norm_bwd");
+    if (!gamma || (num_tokens > 0 && (!x || !dy || !rstd || (kind == TURNOPD_LAYER_NORM && !mean))) ||
+        (!dx_out && !dgamma_out && !dbeta_out))
+        return TURNOPD_ERR_NULL;
+    if (!is_dtype(x_dtype) || !is_dtype(dy_dtype) || (dx_out && !is_dtype(dx_dtype)) || !is_dtype(param_dtype) ||
+        (kind != TURNOPD_LAYER_NORM && kind != TURNOPD_RMS_NORM))
+        return TURNOPD_ERR_UNSUPPORTED;
+    if (num_tokens < 0 || num_tokens > INT32_MAX || d < 1 || d > INT32_MAX || ldx < d || lddy < d ||
+        (dx_out && lddx < d) || misaligned(x, dtype_size(x_dtype)) || misaligned(dy, dtype_size(dy_dtype)) ||
+        (dx_out && misaligned(dx_out, dtype_size(dx_dtype))) || misaligned(gamma, dtype_size(param_dtype)) ||
+        misaligned(mean, 4) || misaligned(rstd, 4) || misaligned(dgamma_out, 4) || misaligned(dbeta_out, 4))
+        return TURNOPD_ERR_SHAPE;
+    if ((dgamma_out || dbeta_out) &&
+        (!workspace || misaligned(workspace, 256) || workspace_bytes < norm_bwd_workspace_bytes(num_tokens, d)))
+        return TURNOPD_ERR_WORKSPACE;
+    cudaStream_t s = (cudaStream_t)stream;
+    if (num_tokens == 0) {
+        cudaError_t e = dgamma_out ? cudaMemsetAsync(dgamma_out, 0, sizeof(float) * (size_t)d, s) : cudaSuccess;
+        if (e == cudaSuccess && dbeta_out)
+            e = cudaMemsetAsync(dbeta_out, 0, sizeof(float) * (size_t)d, s);
+        return cuda_status(e);
+    }
+    NormGradCall c{x, x_dtype, ldx, gamma, param_dtype, loss_mask, num_tokens, d, kind, mean, rstd, dy, dy_dtype, lddy,
+                   dx_out, dx_dtype, lddx, dgamma_out, dbeta_out, workspace};
+    return cuda_status(launch_norm_bwd(c, s));
+}
+
 turnopd_status turnopd_turn_stats(const float *token_loss, const int32_t *turn_id,
                                   const uint8_t *loss_mask, const int64_t *traj_offsets,
                                   int32_t num_traj, int64_t num_tokens, int32_t max_turns,
