@@ -138,6 +138,11 @@ template <typename TIn> struct Logits;
 template <> struct Logits<__nv_bfloat16> {
     static constexpr int N = 8;
     static constexpr uint32_t kHole = 0xff80ff80u;  // -inf
+    __device__ static float max_of_one(const uint4 &v)
+    {
+        const uint32_t m = hmax4(v);
+        return fmaxf(bf16lo(m), bf16hi(m));
+    }
     template <int U> __device__ static float max_of(const uint4 (&v)[U])
     {
         uint32_t m = hmax4(v[0]);
@@ -157,18 +162,41 @@ template <> struct Logits<__nv_bfloat16> {
         const uint32_t w = word(v, j >> 1);
         return j & 1 ? bf16hi(w) : bf16lo(w);
     }
+    // Which of vector u's logits reach `low` (bf16, or NaN: none): bit 4 u + word, upper halves 16 bits up.
+    __device__ static uint32_t reach(const uint4 &v, float low, int u)
+    {
+        const __nv_bfloat162 l = __float2bfloat162_rn(low);
+        uint32_t hits = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const uint32_t w = word(v, j);
+            hits |= __hge2_mask(*reinterpret_cast<const __nv_bfloat162 *>(&w), l) & (0x00010001u << (4 * u + j));
+        }
+        return hits;
+    }
+    __device__ static int vector_of(int p) { return (p & 15) >> 2; }
+    __device__ static int place_of(int p) { return (p & 3) * 2 + (p >> 4); }
+    __device__ static float at_run_time(const uint4 &v, int j)
+    {
+        const uint32_t w = j < 4 ? (j < 2 ? v.x : v.y) : (j < 6 ? v.z : v.w);
+        return j & 1 ? bf16hi(w) : bf16lo(w);
+    }
     __device__ static uint32_t without(uint32_t w, int j) { return j & 1 ? (w & 0xffffu) | 0xff800000u : (w & 0xffff0000u) | 0xff80u; }
     __device__ static int word_of(int j) { return j >> 1; }
 };
 template <> struct Logits<float> {
     static constexpr int N = 4;
     static constexpr uint32_t kHole = 0xff800000u;
+    __device__ static float max_of_one(const uint4 &v)
+    {
+        return fmaxf(fmaxf(at(v, 0), at(v, 1)), fmaxf(at(v, 2), at(v, 3)));
+    }
     template <int U> __device__ static float max_of(const uint4 (&v)[U])
     {
-        float m = -INFINITY;
+        float m = max_of_one(v[0]);
 #pragma unroll
-        for (int u = 0; u < U; ++u)
-            m = fmaxf(m, fmaxf(fmaxf(at(v[u], 0), at(v[u], 1)), fmaxf(at(v[u], 2), at(v[u], 3))));
+        for (int u = 1; u < U; ++u)
+            m = fmaxf(m, max_of_one(v[u]));
         return m;
     }
     __device__ static void fold(const uint4 &v, float2 minus_m, float2 &S, float2 &A)
@@ -178,144 +206,192 @@ template <> struct Logits<float> {
             fold2(make_float2(max_nan(at(v, j), kClamp), max_nan(at(v, j + 1), kClamp)), minus_m, S, A);
     }
     __device__ static float at(const uint4 &v, int j) { return __uint_as_float(word(v, j)); }
+    __device__ static uint32_t reach(const uint4 &v, float low, int u)
+    {
+        uint32_t hits = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            hits |= at(v, j) >= low ? 1u << (4 * u + j) : 0u;
+        return hits;
+    }
+    __device__ static int vector_of(int p) { return p >> 2; }
+    __device__ static int place_of(int p) { return p & 3; }
+    __device__ static float at_run_time(const uint4 &v, int j)
+    {
+        return __uint_as_float(j < 2 ? (j < 1 ? v.x : v.y) : (j < 3 ? v.z : v.w));
+    }
     __device__ static uint32_t without(uint32_t, int) { return kHole; }
     __device__ static int word_of(int j) { return j; }
 };
 
 // ---------------------------------------------------------------- alternatives
 //
-// The n best of a row in one pass.  Each chunk of the row is in the threads' registers.  On the first chunk the n-th
-// best of the threads' own best logits is a bound that n logits reach, and since fewer than n threads have a better
-// one, at most 31 threads' logits (32 each) lie above it: those go to a list in shared memory, and its n-th best is the
-// bound from then on.  Later logits have higher ids, so only those strictly above the bound can matter.  The list
-// is cut back to n, and the bound raised, when it has grown; a chunk with more logits above the bound than the list
-// holds is taken like a first chunk.  Keys are unique, so the outcome does not depend on the order of the list.
+// The n best of a row in one pass.  Each chunk of the row is in the threads' registers.  The first chunk sets a bound:
+// the threads of one lane index are a group, and the n-th best of the 32 groups' best logits is reached by n logits at
+// least and, in a row in no particular order, by few more.  Those are added to a list in shared memory, the list is cut
+// back to its n best, and its n-th best is the bound from then on.  Later logits have higher ids, so only those strictly
+// above the bound can matter; they are added without a barrier, and after 2, 4, 8, ... chunks the list is cut and the
+// bound raised, so that about n logits are added from one cut to the next.  A row that adds more than the list holds
+// (one that ascends, or whose first chunk is forbidden) is read again with each chunk taken like a first one, and if
+// even that adds too many, n times.  Keys are unique, so the outcome does not depend on the order of the list.
 
 constexpr int kU = 4;                             // vectors per thread and chunk
 constexpr int kChunk = kU * kThreads;
 #ifndef LP_PERSM
 #define LP_PERSM 3
 #endif
-constexpr int kPerSm = LP_PERSM;
-constexpr int kListCap = 1088;                    // 32 kept + 31 threads' 32 logits + 1, and the row's ends
-constexpr int kListCut = 160;                     // cut the list back from here
+#ifndef LP_PERSM0
+#define LP_PERSM0 4
+#endif
+template <bool TOP> constexpr int kPerSm = TOP ? LP_PERSM : LP_PERSM0;  // CTAs per SM
+constexpr int kListCap = 1024;
 constexpr int kTopMax = TURNOPD_TOP_ALTERNATIVES_MAX;
+constexpr int kMaxCtas = 8;                       // of a cluster
 
-struct TopShared {
-    uint64_t list[kListCap];
-    uint64_t runs[kThreads];      // kWarps runs of 32 keys in descending order
+struct alignas(16) TopShared {
+    uint64_t list[kListCap + 2];
+    uint64_t lanes[kThreads];                     // the threads' best keys
+    uint64_t groups[kWarps][32];                  // each warp's copy of the groups' best
     uint64_t sorted[kTopMax];
-    uint64_t bound;
+    uint64_t merge[kMaxCtas * kTopMax];           // CTA 0: every CTA's n best
     int count;
+    bool lost;                                    // the list was full
 };
 
-// Place of a key, entry `at` of run `own`, among all of kWarps runs of 32 keys in descending order.  Keys differ, but
-// for empty entries (0), which have no place.
-__device__ __forceinline__ int place_among(uint64_t key, int own, int at, const uint64_t *runs)
+// The lowest value above b.
+__device__ __forceinline__ float next_above(float b, __nv_bfloat16)
 {
-    int place = at;
-#pragma unroll
-    for (int w = 1; w < kWarps; ++w) {
-        const int o = (own + w) & (kWarps - 1);
-        const uint64_t *run = runs + 32 * o;
-        int lo = 0;
-#pragma unroll
-        for (int h = 16; h > 0; h >>= 1)
-            lo += run[lo + h - 1] > key ? h : 0;
-        place += lo + (lo == 31 && run[31] > key);
-    }
-    return place;
+    const uint32_t u = __float_as_uint(b) & 0xffff0000u;
+    return __uint_as_float((u << 1) == 0 ? 0x00010000u : (u & 0x80000000u) ? u - 0x10000u : u + 0x10000u);
+}
+__device__ __forceinline__ float next_above(float b, float)
+{
+    const uint32_t u = __float_as_uint(b);
+    return __uint_as_float((u << 1) == 0 ? 1u : (u & 0x80000000u) ? u - 1u : u + 1u);
 }
 
-// n-th largest of kThreads keys, one per thread (0: none), in every thread; 0 if there are fewer.
-__device__ __forceinline__ uint64_t block_nth(uint64_t key, int n, TopShared &t)
+// Cuts the list to its n best, in order.
+__device__ __forceinline__ void cut_list(int n, TopShared &t)
 {
-    const int lane = threadIdx.x & 31;
-#pragma unroll
-    for (int k = 2; k <= 32; k <<= 1) {
-#pragma unroll
-        for (int j = k >> 1; j > 0; j >>= 1) {
-            const uint64_t o = __shfl_xor_sync(~0u, (unsigned long long)key, j);
-            const bool up = (lane & k) != 0 && k < 32;  // this run ascends
-            const bool low = (lane & j) == 0;
-            key = (low != up) == (key > o) ? key : o;
+    __syncthreads();
+    const int m = min(t.count, kListCap), tid = threadIdx.x;
+    // blocks of kThreads entries, each but the first beginning with the 32 best of those before
+    for (int start = 0;; start += kThreads - kTopMax) {
+        const int len = min(m - start, kThreads);
+        const uint64_t *block = t.list + start;
+        const uint64_t key = tid < len ? block[tid] : 0;
+        if (tid < kTopMax)
+            t.sorted[tid] = 0;
+        if (tid == len)
+            t.list[start + len] = 0;  // read below where len is odd; the next block's first entries are 0 or rewritten
+        __syncthreads();
+        if (key != 0) {
+            int place = 0;
+#pragma unroll 4
+            for (int j = 0; j < len; j += 2) {
+                const ulonglong2 o = *reinterpret_cast<const ulonglong2 *>(block + j);
+                place += (o.x > key) + (o.y > key);
+            }
+            if (place < kTopMax)
+                t.sorted[place] = key;
         }
+        __syncthreads();
+        const bool done = start + kThreads >= m;
+        if (tid < kTopMax)
+            t.list[done ? tid : start + kThreads - kTopMax + tid] = t.sorted[tid];
+        if (done)
+            break;
+        __syncthreads();
     }
-    if (threadIdx.x == 0)
-        t.bound = 0;
-    t.runs[threadIdx.x] = key;
-    __syncthreads();
-    if (key && place_among(key, threadIdx.x >> 5, lane, t.runs) == n - 1)
-        t.bound = key;
-    __syncthreads();
-    return t.bound;
-}
-
-// Cuts the list to its n best, in order; the n-th best is the bound.  Entries of ids from `from` on are dropped.
-__device__ __forceinline__ void cut_list(int n, TopShared &t, int64_t from = INT64_MAX)
-{
-    __syncthreads();
-    const int m = min(t.count, kListCap);
-    if (threadIdx.x < kTopMax)
-        t.sorted[threadIdx.x] = 0;
-    if (from != INT64_MAX)
-        for (int i = threadIdx.x; i < m; i += kThreads)
-            if (key_id(t.list[i]) >= from)
-                t.list[i] = 0;
-    __syncthreads();
-    for (int i = threadIdx.x; i < m; i += kThreads) {
-        const uint64_t key = t.list[i];
-        int place = 0;
-        for (int j = 0; j < m; ++j)
-            place += t.list[j] > key;
-        if (place < n)
-            t.sorted[place] = key;
-    }
-    __syncthreads();
-    if (threadIdx.x < n)
-        t.list[threadIdx.x] = t.sorted[threadIdx.x];
-    if (threadIdx.x == 0) {
+    if (tid == 0) {
+        if (t.count > kListCap)
+            t.lost = true;
         t.count = n;
-        t.bound = t.sorted[n - 1];
     }
     __syncthreads();
 }
 
-__device__ __forceinline__ int list_add(uint64_t key, TopShared &t)
+__device__ __forceinline__ void list_add(uint64_t key, TopShared &t)
 {
     const int at = atomicAdd(&t.count, 1);
     if (at < kListCap)
         t.list[at] = key;
-    return at;
 }
 
-// A first chunk: vector u of the thread holds ids id0 + u stride + 0..N-1 (none where u >= held).
+__device__ __forceinline__ uint4 pick(const uint4 (&v)[kU], int u)
+{
+    uint4 w = v[0];
+#pragma unroll
+    for (int k = 1; k < kU; ++k)
+        if (u == k)
+            w = v[k];
+    return w;
+}
+
+// One chunk: vector u of the thread holds ids id0 + u stride + 0..N-1 (none where u >= held), vm is their maximum.
+// `bound` is the n-th best logit so far; `first`: the chunk sets its own.
 template <typename TIn>
-__device__ __noinline__ void top_chunk(const uint4 (&v)[kU], int held, int64_t id0, int64_t stride, int n, TopShared &t)
+__device__ __forceinline__ void top_chunk(const uint4 (&v)[kU], float vm, int held, uint32_t id0, bool first, int n,
+                                          TopShared &t, float &bound)
 {
     using X = Logits<TIn>;
-    uint64_t best = 0;
+    constexpr uint32_t stride = kThreads * X::N;
+    float above = next_above(bound, TIn());  // what a logit has to reach
+    uint64_t least = 0;                      // a first chunk: the key it has to reach,
+    uint32_t tie_id = ~0u;                   // and so the last id that may equal `above`
+    if (first) {
+        // the thread's best: its logit, and an id not below its own (the last of its vector)
+        int u0 = kU - 1;
 #pragma unroll
-    for (int u = 0; u < kU; ++u)
+        for (int u = kU - 2; u >= 0; --u)
+            u0 = X::max_of_one(v[u]) == vm ? u : u0;
+        const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+        t.lanes[threadIdx.x] = held > 0 && vm == vm ? top_key(vm, id0 + u0 * stride + X::N - 1) : 0;
+        __syncthreads();
+        uint64_t best = 0;
 #pragma unroll
-        for (int j = 0; j < X::N; ++j)
-            if (u < held)
-                best = max(best, top_key(X::at(v[u], j), id0 + u * stride + j));
-    const uint64_t kept = t.bound;  // of the chunks before, 0 at the row's start
-    __syncthreads();
-    const uint64_t bound = max(block_nth(best, n, t), kept);
-    if (best >= bound && best != 0) {
+        for (int w = 0; w < kWarps; ++w)
+            best = max(best, t.lanes[32 * w + lane]);
+        t.groups[warp][lane] = best;
+        __syncwarp();
+        int place = 0;
 #pragma unroll
-        for (int u = 0; u < kU; ++u)
-#pragma unroll
-            for (int j = 0; j < X::N; ++j)
-                if (u < held) {
-                    const uint64_t key = top_key(X::at(v[u], j), id0 + u * stride + j);
-                    if (key >= bound)
-                        list_add(key, t);
-                }
+        for (int j = 0; j < 32; j += 2) {
+            const ulonglong2 o = *reinterpret_cast<const ulonglong2 *>(&t.groups[warp][j]);
+            place += (o.x > best) + (o.y > best);
+        }
+        const unsigned who = __ballot_sync(~0u, best != 0 && place == n - 1);
+        if (who)
+            least = __shfl_sync(~0u, (unsigned long long)best, __ffs(who) - 1);
+        const float own = least ? key_logit(least) : -INFINITY;  // 0: fewer than n groups, all of them are added
+        if (bound == -INFINITY || own >= above) {
+            above = own;
+            tie_id = least ? key_id(least) : ~0u;
+        } else {
+            least = 0;
+        }
     }
-    cut_list(n, t);
+    if (vm >= above) {
+        // bit p: element of word p % 16, upper half from bit 16 on (bf16); element p (fp32)
+        uint32_t hits = 0;
+#pragma unroll
+        for (int u = 0; u < kU; ++u) {
+            const float low = u >= held ? NAN : id0 + u * stride <= tie_id ? above : next_above(above, TIn());
+            hits |= X::reach(v[u], low, u);
+        }
+        while (hits) {
+            const int p = __ffs(hits) - 1;
+            hits &= hits - 1;
+            const int u = X::vector_of(p), j = X::place_of(p);
+            const uint64_t key = top_key(X::at_run_time(pick(v, u), j), id0 + u * stride + j);
+            if (key >= least)
+                list_add(key, t);
+        }
+    }
+    if (first) {
+        cut_list(n, t);
+        bound = t.sorted[n - 1] ? key_logit(t.sorted[n - 1]) : -INFINITY;
+    }
 }
 
 // ---------------------------------------------------------------- forward kernel
@@ -325,15 +401,12 @@ __device__ __noinline__ void top_chunk(const uint4 (&v)[kU], int held, int64_t i
 struct Share {
     const char *row;
     int32_t head, nvec, q0, len, chunks, token, y;
-    float zy;
     bool ok;
 };
 
-template <typename TIn>
-__device__ __forceinline__ Share get_share(const LogprobCall &c, const int4 *rows, int64_t k, int rank, int ctas)
+template <typename TIn> __device__ __forceinline__ Share get_share(const LogprobCall &c, Row r, int rank, int ctas)
 {
     constexpr int N = Logits<TIn>::N;
-    const Row r = get_row(c, rows, k);
     Share s;
     s.token = r.token;
     s.y = r.y;
@@ -347,7 +420,6 @@ __device__ __forceinline__ Share get_share(const LogprobCall &c, const int4 *row
     s.q0 = min(s.nvec, rank * per);
     s.len = min(s.nvec, s.q0 + per) - s.q0;
     s.chunks = (s.len + kChunk - 1) / kChunk;
-    s.zy = r.ok && r.y >= 0 ? to_float(z[r.y]) : -INFINITY;
     return s;
 }
 
@@ -364,13 +436,65 @@ __device__ __forceinline__ void load_chunk(const Share &s, int chunk, uint4 (&v)
     }
 }
 
+// The alternatives of a row whose list was full: every chunk like a first one, and if that fails too, the best logit
+// below the last one, n times.
+template <typename TIn>
+__device__ __noinline__ void top_again(const Share &s, bool has_end, float end_z, int end_id, int n, TopShared &t)
+{
+    constexpr int N = Logits<TIn>::N;
+    const uint64_t end_key = has_end ? top_key(end_z, end_id) : 0;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        t.count = 0;
+        t.lost = false;
+    }
+    __syncthreads();
+    float bound = -INFINITY;
+    for (int chunk = 0; chunk < s.chunks; ++chunk) {
+        uint4 v[kU];
+        load_chunk<TIn>(s, chunk, v);
+        const int q = chunk * kChunk + threadIdx.x;
+        const int held = q >= s.len ? 0 : min(kU, (s.len - q + kThreads - 1) / kThreads);
+        top_chunk<TIn>(v, Logits<TIn>::max_of(v), held, s.head + (uint32_t)(s.q0 + q) * N, true, n, t, bound);
+    }
+    if (end_key != 0)
+        list_add(end_key, t);
+    cut_list(n, t);
+    if (!t.lost)
+        return;
+    const TIn *z = reinterpret_cast<const TIn *>(s.row) + s.head + (int64_t)s.q0 * N;
+    uint64_t below = ~0ull;
+    for (int k = 0; k < n; ++k) {
+        uint64_t best = end_key < below ? end_key : 0;
+        for (int i = threadIdx.x; i < s.len * N; i += kThreads) {
+            const uint64_t key = top_key(to_float(z[i]), s.head + s.q0 * N + i);
+            best = key < below ? max(best, key) : best;
+        }
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1)
+            best = max(best, (uint64_t)__shfl_xor_sync(~0u, (unsigned long long)best, o));
+        if ((threadIdx.x & 31) == 0)
+            t.lanes[threadIdx.x >> 5] = best;
+        __syncthreads();
+        for (int w = 0; w < kWarps; ++w)
+            best = max(best, t.lanes[w]);
+        below = best;
+        if (threadIdx.x == 0)
+            t.sorted[k] = best;
+        __syncthreads();
+    }
+    if ((int)threadIdx.x >= n && threadIdx.x < kTopMax)
+        t.sorted[threadIdx.x] = 0;
+    __syncthreads();
+}
+
 template <typename TIn, bool TOP>
-__global__ void __launch_bounds__(kThreads, kPerSm) k_logprobs(LogprobCall c, const int4 *__restrict__ rows,
+__global__ void __launch_bounds__(kThreads, kPerSm<TOP>) k_logprobs(LogprobCall c, const int4 *__restrict__ rows,
                                                           const int32_t *__restrict__ nvalid)
 {
     using X = Logits<TIn>;
     __shared__ Part parts[kWarps];
-    __shared__ Part whole;      // this CTA's part of the row
+    __shared__ Part whole[kMaxCtas];  // CTA 0: the parts of the row
     __shared__ float norm[3];   // m, log S of the row, 1 if it is fine
     __shared__ TopShared top;
     __shared__ Share shares[2][kWarps];  // each warp its own: no barrier between a row's share and the next one's
@@ -382,18 +506,34 @@ __global__ void __launch_bounds__(kThreads, kPerSm) k_logprobs(LogprobCall c, co
     const int64_t first = blockIdx.x / ctas, step = gridDim.x / ctas;
     uint4 ahead[kU];
     int slot = 0;
+    if (ctas > 1)
+        asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
+    // lane 0 reads a row's indexes two rows ahead, so that nothing waits for them
+    Row coming{};
     if (first < n) {
-        if (lane == 0)
-            shares[0][warp] = get_share<TIn>(c, rows, first, rank, ctas);
+        if (lane == 0) {
+            shares[0][warp] = get_share<TIn>(c, get_row(c, rows, first), rank, ctas);
+            if (first + step < n)
+                coming = get_row(c, rows, first + step);
+        }
         __syncwarp();
         load_chunk<TIn>(shares[0][warp], 0, ahead);
     }
     for (int64_t k = first; k < n; k += step, slot ^= 1) {
         const bool more = k + step < n;
         const Share &s = shares[slot][warp], &next = shares[slot ^ 1][warp];
-        if (more && lane == 0)
-            shares[slot ^ 1][warp] = get_share<TIn>(c, rows, k + step, rank, ctas);
+        if (more && lane == 0) {
+            shares[slot ^ 1][warp] = get_share<TIn>(c, coming, rank, ctas);
+            if (k + 2 * step < n)
+                coming = get_row(c, rows, k + 2 * step);
+        }
         __syncwarp();
+        // the row's ends, before its first and after its last whole vector, and y's logit: needed last, asked for first
+        const TIn *z = reinterpret_cast<const TIn *>(s.row);
+        const int ends = rank == 0 && s.ok ? (int)c.vocab - s.nvec * X::N : 0;
+        const int end_id = (int)threadIdx.x < s.head ? threadIdx.x : s.nvec * X::N + threadIdx.x;
+        const float end_z = (int)threadIdx.x < ends ? to_float(z[end_id]) : 0.f;
+        const float zy = warp == 0 && s.ok && s.y >= 0 ? to_float(z[s.y]) : -INFINITY;
         // where y lies: in this thread's vector uy of chunk cy, or nowhere
         int cy = -1, uy = 0;
         if (s.y >= s.head) {
@@ -406,7 +546,7 @@ __global__ void __launch_bounds__(kThreads, kPerSm) k_logprobs(LogprobCall c, co
         const int chunks = s.chunks;
         if (TOP && threadIdx.x == 0) {
             top.count = 0;
-            top.bound = 0;
+            top.lost = false;
         }
         float m = kMaskedBelow;
         float2 S = splat(0.f), A = splat(0.f);
@@ -422,32 +562,12 @@ __global__ void __launch_bounds__(kThreads, kPerSm) k_logprobs(LogprobCall c, co
             const float vm = X::max_of(v);
             if (TOP) {
                 const int q = chunk * kChunk + threadIdx.x;
-                const int64_t id0 = s.head + (int64_t)(s.q0 + q) * X::N;
-                constexpr int stride = kThreads * X::N;
                 const int held = q >= s.len ? 0 : min(kU, (s.len - q + kThreads - 1) / kThreads);
-                bool grown = chunk == 0;
-                if (vm > bound && chunk > 0) {
-#pragma unroll
-                    for (int u = 0; u < kU; ++u)
-#pragma unroll
-                        for (int j = 0; j < X::N; ++j) {
-                            const float x = X::at(v[u], j);
-                            if (x > bound)
-                                grown |= list_add(top_key(x, id0 + u * stride + j), top) >= kListCut;
-                        }
+                if (chunk > 1 && (chunk & (chunk - 1)) == 0) {
+                    cut_list(c.n_top, top);
+                    bound = key_logit(top.sorted[c.n_top - 1]);
                 }
-                if (__syncthreads_or(grown)) {
-                    if (chunk == 0) {
-                        top_chunk<TIn>(v, held, id0, stride, c.n_top, top);
-                    } else if (top.count <= kListCap) {
-                        cut_list(c.n_top, top);
-                    } else {
-                        // more than the list holds: without this chunk's, then the chunk as a first one
-                        cut_list(c.n_top, top, s.head + (int64_t)(s.q0 + chunk * kChunk) * X::N);
-                        top_chunk<TIn>(v, held, id0, stride, c.n_top, top);
-                    }
-                    bound = top.bound ? key_logit(top.bound) : -INFINITY;
-                }
+                top_chunk<TIn>(v, vm, held, s.head + (uint32_t)(s.q0 + q) * X::N, chunk == 0, c.n_top, top, bound);
             }
             if (chunk == cy) {
                 const int j = (s.y - s.head) & (X::N - 1);
@@ -477,20 +597,13 @@ __global__ void __launch_bounds__(kThreads, kPerSm) k_logprobs(LogprobCall c, co
         if (chunks == 0 && more)
             load_chunk<TIn>(next, 0, ahead);
         Part p{m, S.x + S.y, A.x + A.y};
-        // the row's ends, before its first and after its last whole vector
-        const int tail = s.ok ? (int)c.vocab - s.head - s.nvec * X::N : 0;
         if (TOP)
             __syncthreads();
-        if (rank == 0 && (int)threadIdx.x < s.head + tail) {
-            const int v = (int)threadIdx.x < s.head ? threadIdx.x : s.nvec * X::N + threadIdx.x;
-            const float x = to_float(reinterpret_cast<const TIn *>(s.row)[v]);
-            if (TOP) {
-                const uint64_t key = top_key(x, v);
-                if (key > top.bound)
-                    list_add(key, top);
-            }
-            if (v != s.y) {
-                const float zc = max_nan(x, kClamp);
+        if ((int)threadIdx.x < ends) {
+            if (TOP && end_z >= bound)
+                list_add(top_key(end_z, end_id), top);
+            if (end_id != s.y) {
+                const float zc = max_nan(end_z, kClamp);
                 if (zc > p.m)
                     p = part_about(p, zc);
                 const float t = (zc - p.m) * kLog2e, e = ex2(t);
@@ -502,31 +615,36 @@ __global__ void __launch_bounds__(kThreads, kPerSm) k_logprobs(LogprobCall c, co
         if (lane == 0)
             parts[warp] = p;
         __syncthreads();
+        if (TOP && (top.count > c.n_top || chunks == 0))
+            cut_list(c.n_top, top);
+        if (TOP && top.lost)
+            top_again<TIn>(s, (int)threadIdx.x < ends, end_z, end_id, c.n_top, top);
+        // what CTA 0 needs of this one goes into its shared memory, once it runs
+        if (ctas > 1 && k == first)
+            asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
         if (warp == 0) {
             p = part_warp(lane < kWarps ? parts[lane] : part_empty());
             if (lane == 0)
-                whole = p;
+                *cluster.map_shared_rank(&whole[rank], 0) = p;
         }
-        if (TOP && (top.count > c.n_top || chunks == 0))
-            cut_list(c.n_top, top);
+        if (TOP && ctas > 1 && (int)threadIdx.x < kTopMax)
+            cluster.map_shared_rank(top.merge, 0)[kTopMax * rank + threadIdx.x] = top.sorted[threadIdx.x];
         if (ctas > 1)
             cluster.sync();
         else
             __syncthreads();
         if (rank == 0) {
             if (warp == 0) {
-                p = whole;
-                if (ctas > 1)
-                    p = part_warp(lane < ctas ? *cluster.map_shared_rank(&whole, lane) : part_empty());
+                p = part_warp(lane < ctas ? whole[lane] : part_empty());
                 // y's own term at the end
-                const float M = fmaxf(p.m, s.zy), zc = fmaxf(s.zy, kClamp);
+                const float M = fmaxf(p.m, zy), zc = fmaxf(zy, kClamp);
                 p = part_about(p, M);
                 const float ty = (zc - M) * kLog2e, ey = s.y >= 0 ? ex2(ty) : 0.f;
                 const float total = p.s + ey;
                 const float logs = ey == 1.f ? log1pf(p.s) : logf(total);
                 const float H = logs - kLn2 * (fmaf(ey, ty, p.a) / total);
                 const bool fine = s.ok && M > kMaskedBelow && M < -kMaskedBelow && isfinite(logs) && isfinite(H) &&
-                                  s.zy == s.zy;
+                                  zy == zy;
                 if (lane == 0) {
                     norm[0] = M;
                     norm[1] = logs;
@@ -534,7 +652,7 @@ __global__ void __launch_bounds__(kThreads, kPerSm) k_logprobs(LogprobCall c, co
                     const int64_t i = s.token;
                     if (fine) {
                         if (c.logprob)
-                            c.logprob[i] = (s.zy - M) - logs;
+                            c.logprob[i] = (zy - M) - logs;
                         if (c.entropy)
                             c.entropy[i] = H;
                         if (c.stats) {
@@ -549,25 +667,44 @@ __global__ void __launch_bounds__(kThreads, kPerSm) k_logprobs(LogprobCall c, co
                 }
             }
             if (TOP) {
+                // the CTAs' lists, each in order: a key's place among all is the number of keys above it
+                int place[kMaxCtas * kTopMax / kThreads];
+                uint64_t key[kMaxCtas * kTopMax / kThreads];
+#pragma unroll
+                for (int i = 0; i < kMaxCtas * kTopMax / kThreads; ++i) {
+                    const int e = threadIdx.x + i * kThreads, own = e / kTopMax;
+                    place[i] = e % kTopMax;
+                    key[i] = own >= ctas ? 0 : ctas == 1 ? top.sorted[place[i]] : top.merge[e];
+                    if (key[i] == 0)
+                        continue;
+                    for (int w = 0; w < ctas; ++w) {
+                        const uint64_t *run = top.merge + kTopMax * w;
+                        if (w == own || run[0] < key[i])
+                            continue;
+                        int lo = 0;
+#pragma unroll
+                        for (int h = 16; h > 0; h >>= 1)
+                            lo += run[lo + h - 1] > key[i] ? h : 0;
+                        place[i] += lo + (lo == 31 && run[31] > key[i]);
+                    }
+                }
                 __syncthreads();
-                // the CTAs' n best, each list in order: merged by the places of their keys
-                static_assert(kWarps * 32 == kThreads && kTopMax == 32, "one list to a run");
-                top.runs[threadIdx.x] = warp < ctas ? cluster.map_shared_rank(top.sorted, warp)[lane] : 0;
-                __syncthreads();
-                const uint64_t key = top.runs[threadIdx.x];
-                if (key != 0 && norm[2] != 0.f) {
-                    const int place = ctas > 1 ? place_among(key, warp, lane, top.runs) : lane;
-                    if (place < c.n_top) {
-                        c.top_ids[(int64_t)s.token * c.n_top + place] = (int32_t)key_id(key);
-                        c.top_logprob[(int64_t)s.token * c.n_top + place] = (key_logit(key) - norm[0]) - norm[1];
+#pragma unroll
+                for (int i = 0; i < kMaxCtas * kTopMax / kThreads; ++i) {
+                    if (key[i] != 0 && place[i] < c.n_top && norm[2] != 0.f) {
+                        c.top_ids[(int64_t)s.token * c.n_top + place[i]] = (int32_t)key_id(key[i]);
+                        c.top_logprob[(int64_t)s.token * c.n_top + place[i]] = (key_logit(key[i]) - norm[0]) - norm[1];
                     }
                 }
             }
         }
-        if (ctas > 1)
-            cluster.sync();
-        else
-            __syncthreads();
+        // CTA 0's memory is written again for the next row
+        if (more) {
+            if (ctas > 1)
+                cluster.sync();
+            else
+                __syncthreads();
+        }
     }
     // tokens that are not in the row list
     if (rows) {
@@ -646,9 +783,9 @@ cudaError_t launch_fwd(const LogprobCall &c, const int4 *rows, const int32_t *nv
     const int sms = device_sm_count();
     const int64_t vecs = c.vocab / Logits<TIn>::N;
     int ctas = 1;
-    while (ctas < 8 && c.T * ctas * 2 <= 2 * sms && vecs >= ctas * 2 * kThreads)
+    while (ctas < kMaxCtas && c.T * ctas * 2 <= 2 * sms && vecs >= ctas * 2 * kThreads)
         ctas *= 2;
-    const int64_t want = c.T * ctas, most = (int64_t)sms * kPerSm / ctas * ctas;
+    const int64_t want = c.T * ctas, most = (int64_t)sms * (c.n_top > 0 ? kPerSm<true> : kPerSm<false>) / ctas * ctas;
     cudaLaunchConfig_t cfg = {};
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
