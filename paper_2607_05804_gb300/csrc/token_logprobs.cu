@@ -721,30 +721,163 @@ __global__ void __launch_bounds__(kThreads, kPerSm<TOP>) k_logprobs(LogprobCall 
     }
 }
 
-template <typename TIn, typename TOut>
-__global__ void __launch_bounds__(kThreads) k_logprobs_bwd(LogprobGradCall c, const int4 *__restrict__ rows,
-                                                           const int32_t *__restrict__ nvalid)
+// ---------------------------------------------------------------- gradient kernel
+//
+// One read and one write per logit: the row's statistics are given.  CTAs take chunks of rows in turn, so few long rows
+// and many short ones fill the device alike; the row's numbers are read one chunk ahead.  No __restrict__ and no
+// read-only loads: the gradient may be written over the logits, each vector by the thread that read it.
+
+struct GradRow {
+    Row row;
+    float m, logs, gl, gh, H, lp;
+};
+
+__device__ __forceinline__ GradRow get_grad_row(const LogprobGradCall &c, const int4 *rows, int64_t k)
 {
+    GradRow g{};
+    g.row = get_row(c, rows, k);
+    const int64_t i = g.row.token;
+    g.m = c.stats[2 * i];
+    g.logs = c.stats[2 * i + 1];
+    if (c.d_logprob) {
+        g.gl = c.d_logprob[i];
+        g.lp = c.logprob[i];
+    }
+    if (c.d_entropy) {
+        g.gh = c.d_entropy[i];
+        g.H = c.entropy[i];
+    }
+    return g;
+}
+
+// -p (gl + gh (log p + H)) of two logits.
+template <bool ENT> __device__ __forceinline__ float2 grad2(float2 z, const GradRow &g)
+{
+    float2 lp = fadd2(fadd2(z, splat(-g.m)), splat(-g.logs));
+    if (ENT) {  // p = 0: keeps 0 times log p finite
+        lp.x = max_nan(lp.x, -1e4f);
+        lp.y = max_nan(lp.y, -1e4f);
+    }
+    const float2 p = ex2x2(fmul2(lp, splat(kLog2e)));
+    const float2 f = ENT ? ffma2(splat(-g.gh), fadd2(lp, splat(g.H)), splat(-g.gl)) : splat(-g.gl);
+    return fmul2(p, f);
+}
+// y's own: gl (1 - p) - gh p (log p + H), with 1 - p = -expm1(log p)
+__device__ __forceinline__ float grad_y(float z, const GradRow &g)
+{
+    const float lp = fmaxf((z - g.m) - g.logs, -1e4f), p = expf(lp);
+    return fmaf(-g.gl, expm1f(g.lp), -p * (g.gh * (lp + g.H)));
+}
+
+constexpr int kGradU = 4;
+constexpr int kGradChunk = kGradU * kThreads;  // vectors
+
+__device__ __forceinline__ uint4 ld_once(const uint4 *p)
+{
+    uint4 v;
+    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+                 : "l"(p)
+                 : "memory");
+    return v;
+}
+
+template <int N> __device__ __forceinline__ void st_once(float *p, const float (&g)[N])
+{
+#pragma unroll
+    for (int j = 0; j < N; j += 4)
+        __stcs(reinterpret_cast<float4 *>(p + j), make_float4(g[j], g[j + 1], g[j + 2], g[j + 3]));
+}
+template <int N> __device__ __forceinline__ void st_once(__nv_bfloat16 *p, const float (&g)[N])
+{
+    if constexpr (N == 8)
+        __stcs(reinterpret_cast<uint4 *>(p), make_uint4(pack_bf16x2(g[0], g[1]), pack_bf16x2(g[2], g[3]),
+                                                        pack_bf16x2(g[4], g[5]), pack_bf16x2(g[6], g[7])));
+    else
+        __stcs(reinterpret_cast<uint2 *>(p), make_uint2(pack_bf16x2(g[0], g[1]), pack_bf16x2(g[2], g[3])));
+}
+
+template <typename TIn, typename TOut, bool ENT>
+__global__ void __launch_bounds__(kThreads, 4) k_logprobs_bwd(LogprobGradCall c, const int4 *__restrict__ rows,
+                                                              const int32_t *__restrict__ nvalid)
+{
+    using X = Logits<TIn>;
+    constexpr int N = X::N;
+    constexpr int kOutAlign = sizeof(TOut) * N < 16 ? sizeof(TOut) * N : 16;
     const int64_t n = rows ? *nvalid : c.T;
-    for (int64_t k = blockIdx.x; k < n; k += gridDim.x) {
-        const Row row = get_row(c, rows, k);
-        if (!row.ok)
-            continue;
-        // no __restrict__: the gradient may be written over the logits
-        const TIn *z = static_cast<const TIn *>(c.logits) + (int64_t)row.r * c.ld;
-        TOut *g = static_cast<TOut *>(c.grad) + (int64_t)row.r * c.ld;
-        const int64_t i = row.token;
-        const float m = c.stats[2 * i], logs = c.stats[2 * i + 1];
-        const bool fine = m > -INFINITY;
-        const float gl = c.d_logprob ? c.d_logprob[i] : 0.f;
-        const float gh = c.d_entropy ? c.d_entropy[i] : 0.f, H = c.d_entropy ? c.entropy[i] : 0.f;
-        for (int64_t v = threadIdx.x; v < c.vocab; v += kThreads) {
-            const float lp = fmaxf((to_float(z[v]) - m) - logs, -1e4f);
-            const float p = expf(lp);
-            float o = -p * fmaf(gh, lp + H, gl);
-            if (v == row.y && c.d_logprob)
-                o = fmaf(-gl, expm1f(c.logprob[i]), -p * (gh * (lp + H)));
-            g[v] = from_float<TOut>(fine ? o : 0.f);
+    const int V = (int)c.vocab;
+    const int chunks = (V / N + kGradChunk - 1) / kGradChunk + (V < N);  // of the longest row
+    int64_t k = blockIdx.x / chunks;
+    int chunk = blockIdx.x % chunks;
+    const int64_t dk = gridDim.x / chunks;
+    const int dc = gridDim.x % chunks;
+    GradRow next{};
+    if (k < n)
+        next = get_grad_row(c, rows, k);
+    while (k < n) {
+        const GradRow g = next;
+        const int here = chunk;
+        k += dk;
+        chunk += dc;
+        if (chunk >= chunks) {
+            chunk -= chunks;
+            ++k;
+        }
+        const TIn *z = static_cast<const TIn *>(c.logits) + (g.row.ok ? (int64_t)g.row.r * c.ld : 0);
+        TOut *out = static_cast<TOut *>(c.grad) + (g.row.ok ? (int64_t)g.row.r * c.ld : 0);
+        const int len = g.row.ok ? V : 0;
+        const int head = min((int)((16 - (reinterpret_cast<uintptr_t>(z) & 15)) & 15) / (int)sizeof(TIn), len);
+        const int nvec = (len - head) / N;
+        const bool aligned = ((reinterpret_cast<uintptr_t>(out + head)) & (kOutAlign - 1)) == 0;
+        const int q = here * kGradChunk + threadIdx.x;
+        const uint4 *p = reinterpret_cast<const uint4 *>(z + head) + q;
+        uint4 v[kGradU];
+#pragma unroll
+        for (int u = 0; u < kGradU; ++u)
+            if (q + u * kThreads < nvec)
+                v[u] = ld_once(p + u * kThreads);
+        if (k < n)
+            next = get_grad_row(c, rows, k);
+        const bool fine = g.m > -INFINITY;
+        const int y = c.d_logprob ? g.row.y : -1;
+        // the row's ends
+        const int ends = here == 0 ? len - nvec * N : 0;
+        if ((int)threadIdx.x < ends) {
+            const int e = (int)threadIdx.x < head ? threadIdx.x : nvec * N + threadIdx.x;
+            const float x = to_float(z[e]);
+            const float o = e == y ? grad_y(x, g) : grad2<ENT>(splat(x), g).x;
+            out[e] = from_float<TOut>(fine ? o : 0.f);
+        }
+#pragma unroll
+        for (int u = 0; u < kGradU; ++u) {
+            if (q + u * kThreads >= nvec)
+                break;
+            const int id0 = head + (q + u * kThreads) * N;
+            float o[N];
+#pragma unroll
+            for (int j = 0; j < N; j += 2) {
+                const float2 w = grad2<ENT>(make_float2(X::at(v[u], j), X::at(v[u], j + 1)), g);
+                o[j] = w.x;
+                o[j + 1] = w.y;
+            }
+            if ((unsigned)(y - id0) < (unsigned)N) {
+#pragma unroll
+                for (int j = 0; j < N; ++j)
+                    if (id0 + j == y)
+                        o[j] = grad_y(X::at(v[u], j), g);
+            }
+            if (!fine) {
+#pragma unroll
+                for (int j = 0; j < N; ++j)
+                    o[j] = 0.f;
+            }
+            if (aligned) {
+                st_once(out + id0, o);
+            } else {
+#pragma unroll
+                for (int j = 0; j < N; ++j)
+                    out[id0 + j] = from_float<TOut>(o[j]);
+            }
         }
     }
 }
@@ -800,6 +933,17 @@ cudaError_t launch_fwd(const LogprobCall &c, const int4 *rows, const int32_t *nv
                        : cudaLaunchKernelEx(&cfg, k_logprobs<TIn, false>, c, rows, nvalid);
 }
 
+template <typename TIn, typename TOut>
+void launch_grad(const LogprobGradCall &c, const int4 *rows, const int32_t *nvalid, cudaStream_t stream)
+{
+    const int64_t chunks = c.vocab / Logits<TIn>::N / kGradChunk + 1;
+    const int grid = (int)std::min<int64_t>(c.T * chunks, (int64_t)device_sm_count() * 4);
+    if (c.d_entropy)
+        k_logprobs_bwd<TIn, TOut, true><<<grid, kThreads, 0, stream>>>(c, rows, nvalid);
+    else
+        k_logprobs_bwd<TIn, TOut, false><<<grid, kThreads, 0, stream>>>(c, rows, nvalid);
+}
+
 }  // namespace
 
 size_t logprob_workspace_bytes(int64_t T)
@@ -826,16 +970,15 @@ cudaError_t launch_token_logprobs_bwd(const LogprobGradCall &c, cudaStream_t str
         return e;
     if (c.mask && (c.flags & TURNOPD_ZERO_MASKED_GRAD))
         launch_zero_masked_grad(c.mask, c.row_of_token, c.T, c.num_rows, c.ld, c.vocab, c.grad, c.grad_dtype, stream);
-    const int grid = (int)std::min<int64_t>(c.T, (int64_t)device_sm_count() * 8);
     const bool in16 = c.in_dtype == TURNOPD_BF16, out16 = c.grad_dtype == TURNOPD_BF16;
     if (in16 && out16)
-        k_logprobs_bwd<__nv_bfloat16, __nv_bfloat16><<<grid, kThreads, 0, stream>>>(c, l.rows, l.nvalid);
+        launch_grad<__nv_bfloat16, __nv_bfloat16>(c, l.rows, l.nvalid, stream);
     else if (in16)
-        k_logprobs_bwd<__nv_bfloat16, float><<<grid, kThreads, 0, stream>>>(c, l.rows, l.nvalid);
+        launch_grad<__nv_bfloat16, float>(c, l.rows, l.nvalid, stream);
     else if (out16)
-        k_logprobs_bwd<float, __nv_bfloat16><<<grid, kThreads, 0, stream>>>(c, l.rows, l.nvalid);
+        launch_grad<float, __nv_bfloat16>(c, l.rows, l.nvalid, stream);
     else
-        k_logprobs_bwd<float, float><<<grid, kThreads, 0, stream>>>(c, l.rows, l.nvalid);
+        launch_grad<float, float>(c, l.rows, l.nvalid, stream);
     return cudaGetLastError();
 }
 
