@@ -10,6 +10,7 @@
 
 #include "common.cuh"
 #include "kernels.h"
+#include "packed.cuh"
 
 namespace turnopd {
 namespace {
@@ -17,8 +18,7 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
 constexpr int kE = 16;  // columns of a row that one thread holds
-constexpr int kMaxFwd = 1024 * kE;  // longest rows of the register kernels
-constexpr int kMaxBwd = 512 * kE;
+constexpr int kMaxBwd = 512 * kE;  // longest rows of the one-pass backward kernel
 
 __device__ __forceinline__ float param(const void *p, int32_t dtype, int64_t j)
 {
@@ -72,19 +72,6 @@ __device__ __forceinline__ void load_params8(const void *p, int32_t dtype, int64
         load8(static_cast<const float *>(p) + j, v);
 }
 
-// The columns of thread t among n that share a row: in pieces of eight, a piece of each thread in turn (rows on
-// 16-byte boundaries, d a multiple of 8), or one by one (any rows).  f(column, first of the thread's kE values).
-template <bool VEC, typename F> __device__ __forceinline__ void each_piece(int t, int n, int64_t d, F &&f)
-{
-    constexpr int W = VEC ? 8 : 1;
-#pragma unroll
-    for (int k = 0; k < kE / W; ++k) {
-        const int j = (k * n + t) * W;
-        if (j < d)
-            f(j, k * W);
-    }
-}
-
 // Sum over the `warps` warps of a row's group, the same value in every thread; red: one entry per warp of the block.
 // Every thread of the block calls it where a row has more than one warp.
 __device__ __forceinline__ float group_sum(float v, float *red, int first, int warps)
@@ -101,49 +88,87 @@ __device__ __forceinline__ float group_sum(float v, float *red, int first, int w
     return s;
 }
 
-// One row per group of n threads (a multiple of 32), kE columns to a thread, one read of x.
-template <typename TX, typename TY, bool VEC>
-__global__ void __launch_bounds__(1024) k_norm_fwd(NormCall c, int n)
+// The columns of one thread: P pieces, a piece of each of the row's n threads in turn.  A piece is 16 bytes of a row on
+// 16-byte boundaries with d a multiple of 8, kept as they are, or one column of any row.
+template <typename T, bool VEC> struct RowPiece {
+    static constexpr int W = VEC ? 16 / sizeof(T) : 1;
+    uint4 raw;
+    __device__ void load(const T *p) { raw = __ldcs(reinterpret_cast<const uint4 *>(p)); }
+    __device__ float at(int e) const
+    {
+        if constexpr (sizeof(T) == 4)
+            return __uint_as_float(word(raw, e));
+        else
+            return e & 1 ? bf16hi(word(raw, e >> 1)) : bf16lo(word(raw, e >> 1));
+    }
+};
+template <typename T> struct RowPiece<T, false> {
+    static constexpr int W = 1;
+    float raw;
+    __device__ void load(const T *p) { raw = to_float(*p); }
+    __device__ float at(int) const { return raw; }
+};
+
+template <int W> __device__ __forceinline__ void load_params(const void *p, int32_t dtype, int j, float (&v)[W])
 {
-    __shared__ float red[2][32];
-    const int t = threadIdx.x % n, group = threadIdx.x / n, warps = n / 32;
+    if constexpr (W == 1) {
+        v[0] = param(p, dtype, j);
+    } else if (dtype == TURNOPD_BF16) {
+#pragma unroll
+        for (int e = 0; e < W; e += 4) {
+            const uint2 u = *reinterpret_cast<const uint2 *>(static_cast<const __nv_bfloat16 *>(p) + j + e);
+            v[e] = bf16lo(u.x), v[e + 1] = bf16hi(u.x), v[e + 2] = bf16lo(u.y), v[e + 3] = bf16hi(u.y);
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < W; e += 4) {
+            const float4 u = *reinterpret_cast<const float4 *>(static_cast<const float *>(p) + j + e);
+            v[e] = u.x, v[e + 1] = u.y, v[e + 2] = u.z, v[e + 3] = u.w;
+        }
+    }
+}
+
+// One row per group of n threads (a multiple of 32), one read of x, all of it asked for at once.
+template <typename TX, typename TY, bool VEC, int P, int THREADS>
+__global__ void __launch_bounds__(THREADS) k_norm_fwd(NormCall c, int n)
+{
+    using X = RowPiece<TX, VEC>;
+    constexpr int W = X::W;
+    __shared__ float red[2][THREADS / 32];
+    const int t = threadIdx.x % n, group = threadIdx.x / n, warps = n / 32, d = (int)c.d;
     const int64_t i = (int64_t)blockIdx.x * (blockDim.x / n) + group;
     const bool layer = c.kind == TURNOPD_LAYER_NORM;
     const bool on = i < c.T && (!c.mask || c.mask[i]);
     const TX *x = static_cast<const TX *>(c.x) + i * c.ldx;
-    const float inv_d = 1.f / (float)c.d;
-    float v[kE], g[kE];
+    const float inv_d = 1.f / (float)d;
+    X v[P];
     if (on) {
-        each_piece<VEC>(t, n, c.d, [&](int j, int k) {
-            if constexpr (VEC)
-                load8(x + j, v + k);
-            else
-                v[k] = to_float(x[j]);
-        });
-        each_piece<VEC>(t, n, c.d, [&](int j, int k) {
-            if constexpr (VEC)
-                load_params8(c.gamma, c.param_dtype, j, g + k);
-            else
-                g[k] = param(c.gamma, c.param_dtype, j);
-        });
+#pragma unroll
+        for (int k = 0; k < P; ++k)
+            if ((k * n + t) * W < d)
+                v[k].load(x + (k * n + t) * W);
     }
     float mu = 0.f, q = 0.f;
     if (layer) {
         float s = 0.f;
-        if (on)
-            each_piece<VEC>(t, n, c.d, [&](int, int k) {
+        if (on) {
 #pragma unroll
-                for (int e = 0; e < (VEC ? 8 : 1); ++e)
-                    s += v[k + e];
-            });
+            for (int k = 0; k < P; ++k)
+                if ((k * n + t) * W < d)
+#pragma unroll
+                    for (int e = 0; e < W; ++e)
+                        s += v[k].at(e);
+        }
         mu = group_sum(s, red[0], group * warps, warps) * inv_d;
     }
-    if (on)
-        each_piece<VEC>(t, n, c.d, [&](int, int k) {
+    if (on) {
 #pragma unroll
-            for (int e = 0; e < (VEC ? 8 : 1); ++e)
-                q = fmaf(v[k + e] - mu, v[k + e] - mu, q);
-        });
+        for (int k = 0; k < P; ++k)
+            if ((k * n + t) * W < d)
+#pragma unroll
+                for (int e = 0; e < W; ++e)
+                    q = fmaf(v[k].at(e) - mu, v[k].at(e) - mu, q);
+    }
     q = group_sum(q, red[1], group * warps, warps);
     if (i >= c.T)
         return;
@@ -159,26 +184,32 @@ __global__ void __launch_bounds__(1024) k_norm_fwd(NormCall c, int n)
     if (r == 0.f)
         mu = 0.f;
     TY *y = static_cast<TY *>(c.y) + i * c.ldy;
-    each_piece<VEC>(t, n, c.d, [&](int j, int k) {
-        constexpr int W = VEC ? 8 : 1;
-        float o[W], b[W];
+#pragma unroll
+    for (int k = 0; k < P; ++k) {
+        const int j = (k * n + t) * W;
+        if (j >= d)
+            continue;
+        float o[W], g[W];
 #pragma unroll
         for (int e = 0; e < W; ++e)
-            b[e] = 0.f;
-        if (c.beta && r != 0.f) {
-            if constexpr (VEC)
-                load_params8(c.beta, c.param_dtype, j, b);
-            else
-                b[0] = param(c.beta, c.param_dtype, j);
+            o[e] = 0.f;
+        if (r != 0.f) {
+            load_params<W>(c.gamma, c.param_dtype, j, g);
+            if (c.beta)
+                load_params<W>(c.beta, c.param_dtype, j, o);
+#pragma unroll
+            for (int e = 0; e < W; ++e)
+                o[e] = fmaf((v[k].at(e) - mu) * r, g[e], o[e]);
         }
-#pragma unroll
-        for (int e = 0; e < W; ++e)
-            o[e] = r != 0.f ? fmaf((v[k + e] - mu) * r, g[k + e], b[e]) : 0.f;
-        if constexpr (VEC)
-            store8(y + j, o);
-        else
+        if constexpr (!VEC)
             y[j] = from_float<TY>(o[0]);
-    });
+        else if constexpr (W == 8)
+            store8(y + j, o);
+        else if constexpr (sizeof(TY) == 4)
+            __stcs(reinterpret_cast<float4 *>(y + j), make_float4(o[0], o[1], o[2], o[3]));
+        else
+            __stcs(reinterpret_cast<uint2 *>(y + j), make_uint2(pack_bf16x2(o[0], o[1]), pack_bf16x2(o[2], o[3])));
+    }
     if (t == 0) {
         if (c.mean)
             c.mean[i] = mu;
@@ -247,62 +278,100 @@ __device__ __forceinline__ void cp16(void *smem, const void *gmem)
                  : "memory");
 }
 
+constexpr int kBwdSingles = 8;  // columns of a thread where they are read one by one
 constexpr int kStages = 3;  // rows in flight per group: the one at hand and two ahead
+
+// Barrier of the n threads of one group (1 .. 8; 0 is the block's).
+__device__ __forceinline__ void group_barrier(int group, int n)
+{
+    asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "r"(n) : "memory");
+}
+
+__device__ __forceinline__ float2 sum2(float2 v)
+{
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1)
+        v = fadd2(v, make_float2(__shfl_xor_sync(~0u, v.x, o), __shfl_xor_sync(~0u, v.y, o)));
+    return v;
+}
 
 // One pass over x and dy: every thread keeps its columns of gamma, dgamma and dbeta in registers from row to row.
 // Group b of all takes rows b, b + groups, ... of the list of supervised tokens (of all tokens, without a list), so that
 // the sums are in a fixed order.  Aligned rows come through a ring in shared memory, in which each thread copies and
-// reads its own columns only: no barrier but the one of the row's two sums.
+// reads its own columns only: no barrier but the one of the row's two sums.  Columns from d on are zeros throughout.
 template <typename TX, typename TDY, typename TDX, bool VEC, bool WIDE>
-__global__ void __launch_bounds__(WIDE ? 512 : 320, WIDE ? 1 : 2) k_norm_bwd(NormGradCall c, const int4 *__restrict__ rows,
-                                                  const int32_t *__restrict__ nvalid, int n)
+__global__ void __launch_bounds__(VEC ? (WIDE ? 512 : 320) : (WIDE ? 1024 : 512), VEC && !WIDE ? 2 : 1)
+k_norm_bwd(NormGradCall c, const int4 *__restrict__ rows, const int32_t *__restrict__ nvalid, int n)
 {
+    constexpr int kE = VEC ? turnopd::kE : kBwdSingles;
     extern __shared__ __align__(16) char ring[];
-    __shared__ float2 red[2][16];
+    __shared__ __align__(16) float2 red[2][32];
+    constexpr int W = VEC ? 8 : 1, P = kE / W;  // columns to a piece, pieces to a thread
     const int t = threadIdx.x % n, group = threadIdx.x / n, warps = n / 32, per = blockDim.x / n;
-    const int64_t groups = (int64_t)gridDim.x * per, b = (int64_t)blockIdx.x * per + group;
-    const int64_t count = rows ? *nvalid : c.T, steps = (count + groups - 1) / groups;
+    const int groups = gridDim.x * per, b = blockIdx.x * per + group, d = (int)c.d;
+    const int count = rows ? *nvalid : (int)c.T;
     const bool layer = c.kind == TURNOPD_LAYER_NORM;
-    const float inv_d = 1.f / (float)c.d;
-    const size_t xbytes = sizeof(TX) * n * kE, stage = (sizeof(TX) + sizeof(TDY)) * n * kE;
+    const float inv_d = 1.f / (float)d;
+    const int xbytes = (int)sizeof(TX) * n * kE, stage = (int)(sizeof(TX) + sizeof(TDY)) * n * kE;
     char *own = ring + group * kStages * stage;
+    const auto column = [&](int k) { return (k * n + t) * W; };  // of piece k
 
-    float gamma[kE], dg[kE], db[kE];
+    float2 gamma[kE / 2], dg[kE / 2], db[kE / 2];
 #pragma unroll
-    for (int k = 0; k < kE; ++k)
-        gamma[k] = dg[k] = db[k] = 0.f;
-    each_piece<VEC>(t, n, c.d, [&](int j, int k) {
-        if constexpr (VEC)
-            load_params8(c.gamma, c.param_dtype, j, gamma + k);
-        else
-            gamma[k] = param(c.gamma, c.param_dtype, j);
-    });
+    for (int k = 0; k < kE / 2; ++k)
+        gamma[k] = dg[k] = db[k] = make_float2(0.f, 0.f);
+    float *gam = reinterpret_cast<float *>(gamma);
+#pragma unroll
+    for (int k = 0; k < P; ++k) {
+        const int j = column(k);
+        if (j < d) {
+            if constexpr (VEC)
+                load_params8(c.gamma, c.param_dtype, j, gam + k * W);
+            else
+                gam[k] = param(c.gamma, c.param_dtype, j);
+        }
+    }
+    if constexpr (VEC) {
+#pragma unroll
+        for (int k = 0; k < P; ++k)
+            if (column(k) >= d)
+                for (int s = 0; s < kStages; ++s) {
+                    for (int h = 0; h < (int)sizeof(TX) / 2; ++h)
+                        reinterpret_cast<uint4 *>(own + s * stage + column(k) * sizeof(TX))[h] = make_uint4(0, 0, 0, 0);
+                    for (int h = 0; h < (int)sizeof(TDY) / 2; ++h)
+                        reinterpret_cast<uint4 *>(own + s * stage + xbytes + column(k) * sizeof(TDY))[h] = make_uint4(0, 0, 0, 0);
+                }
+    }
 
     // the row of a step: -1 for none
-    const auto row_of = [&](int64_t m) -> int64_t {
+    const auto row_of = [&](int64_t m) -> int {
         const int64_t at = m * groups + b;
         if (at >= count)
             return -1;
-        return rows ? rows[at].x : at;
+        return rows ? rows[at].x : (int)at;
     };
-    const auto on = [&](int64_t i) { return i >= 0 && (rows || !c.mask || c.mask[i]); };
-    const auto copy = [&](int64_t i, int s) {
+    const auto on = [&](int i) { return i >= 0 && (rows || !c.mask || c.mask[i]); };
+    const auto copy = [&](int i, int s) {
         if (on(i)) {
-            const TX *x = static_cast<const TX *>(c.x) + i * c.ldx;
-            const TDY *dy = static_cast<const TDY *>(c.dy) + i * c.lddy;
+            const char *x = reinterpret_cast<const char *>(static_cast<const TX *>(c.x) + i * c.ldx);
+            const char *dy = reinterpret_cast<const char *>(static_cast<const TDY *>(c.dy) + i * c.lddy);
             char *to = own + s * stage;
-            each_piece<true>(t, n, c.d, [&](int j, int) {
+#pragma unroll
+            for (int k = 0; k < P; ++k) {
+                const int j = column(k);
+                if (j >= d)
+                    continue;
 #pragma unroll
                 for (int h = 0; h < (int)sizeof(TX) / 2; ++h)
-                    cp16(to + j * sizeof(TX) + 16 * h, reinterpret_cast<const char *>(x + j) + 16 * h);
+                    cp16(to + j * (int)sizeof(TX) + 16 * h, x + j * (int)sizeof(TX) + 16 * h);
 #pragma unroll
                 for (int h = 0; h < (int)sizeof(TDY) / 2; ++h)
-                    cp16(to + xbytes + j * sizeof(TDY) + 16 * h, reinterpret_cast<const char *>(dy + j) + 16 * h);
-            });
+                    cp16(to + xbytes + j * (int)sizeof(TDY) + 16 * h, dy + j * (int)sizeof(TDY) + 16 * h);
+            }
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
     };
-    int64_t i = row_of(0), i1 = row_of(1), i2 = row_of(2);
+    int i = row_of(0), i1 = row_of(1), i2 = row_of(2);
     if constexpr (VEC) {
         copy(i, 0);
         copy(i1, 1);
@@ -313,8 +382,8 @@ __global__ void __launch_bounds__(WIDE ? 512 : 320, WIDE ? 1 : 2) k_norm_bwd(Nor
         r = c.rstd[i];
     }
     int s = 0;
-    for (int64_t m = 0; m < steps; ++m) {
-        const int64_t i3 = row_of(m + 3);
+    for (int m = 0; i >= 0; ++m) {
+        const int i3 = row_of(m + 3);
         if constexpr (VEC)
             copy(i2, s >= 1 ? s - 1 : s + 2);
         float mu1 = 0.f, r1 = 0.f;
@@ -322,66 +391,79 @@ __global__ void __launch_bounds__(WIDE ? 512 : 320, WIDE ? 1 : 2) k_norm_bwd(Nor
             mu1 = layer ? c.mean[i1] : 0.f;
             r1 = c.rstd[i1];
         }
-        const bool part = r > 0.f;
-        float x[kE], dy[kE];
-        if constexpr (VEC) {
+        if constexpr (VEC)
             asm volatile("cp.async.wait_group 2;" ::: "memory");
-            if (part)
-                each_piece<true>(t, n, c.d, [&](int j, int k) {
-                    load8(reinterpret_cast<const TX *>(own + s * stage) + j, x + k);
-                    load8(reinterpret_cast<const TDY *>(own + s * stage + xbytes) + j, dy + k);
-                });
-        } else if (part) {
-            each_piece<false>(t, n, c.d, [&](int j, int k) {
-                x[k] = to_float(static_cast<const TX *>(c.x)[i * c.ldx + j]);
-                dy[k] = to_float(static_cast<const TDY *>(c.dy)[i * c.lddy + j]);
-            });
-        }
-        float sg = 0.f, sx = 0.f;
-        if (part)
-            each_piece<VEC>(t, n, c.d, [&](int, int k0) {
+        TDX *dx = static_cast<TDX *>(c.dx) + i * c.lddx;
+        if (r > 0.f) {
+            float2 sg = make_float2(0.f, 0.f), sx = sg;
+            float2 x[kE / 2], dy[kE / 2];  // xh and dy; aligned rows are read from the ring once more for dx instead
 #pragma unroll
-                for (int e = 0; e < (VEC ? 8 : 1); ++e) {
-                    const int k = k0 + e;
-                    x[k] = (x[k] - mu) * r;
-                    const float g = dy[k] * gamma[k];
-                    sg += g;
-                    sx = fmaf(g, x[k], sx);
-                    dg[k] = fmaf(dy[k], x[k], dg[k]);
-                    db[k] += dy[k];
-                }
-            });
-        if (c.dx) {
-            sg = warp_sum_f(sg);
-            sx = warp_sum_f(sx);
-            if (warps > 1) {
-                float2 *to = red[m & 1];
-                if ((threadIdx.x & 31) == 0)
-                    to[threadIdx.x >> 5] = make_float2(sg, sx);
-                __syncthreads();
-                const int first = group * warps;
-                sg = to[first].x;
-                sx = to[first].y;
-                for (int w = 1; w < warps; ++w) {
-                    sg += to[first + w].x;
-                    sx += to[first + w].y;
+            for (int k = 0; k < P; ++k) {
+                float2 *xk = x + k * W / 2, *dyk = dy + k * W / 2;
+                if constexpr (VEC) {
+                    load8(reinterpret_cast<const TX *>(own + s * stage) + column(k), reinterpret_cast<float *>(xk));
+                    load8(reinterpret_cast<const TDY *>(own + s * stage + xbytes) + column(k), reinterpret_cast<float *>(dyk));
+                } else {
+                    const int j = column(k);
+                    reinterpret_cast<float *>(x)[k] = j < d ? to_float(static_cast<const TX *>(c.x)[i * c.ldx + j]) : 0.f;
+                    reinterpret_cast<float *>(dy)[k] = j < d ? to_float(static_cast<const TDY *>(c.dy)[i * c.lddy + j]) : 0.f;
                 }
             }
-            sg = layer ? sg * inv_d : 0.f;
-            sx *= inv_d;
-            if (i >= 0) {
-                TDX *dx = static_cast<TDX *>(c.dx) + i * c.lddx;
-                each_piece<VEC>(t, n, c.d, [&](int j, int k) {
-                    constexpr int W = VEC ? 8 : 1;
-                    float o[W];
 #pragma unroll
-                    for (int e = 0; e < W; ++e)
-                        o[e] = part ? r * (fmaf(dy[k + e], gamma[k + e], -sg) - x[k + e] * sx) : 0.f;
+            for (int k = 0; k < kE / 2; ++k) {
+                x[k] = fmul2(fadd2(x[k], splat(-mu)), splat(r));
+                const float2 g = fmul2(dy[k], gamma[k]);
+                sg = fadd2(sg, g);
+                sx = ffma2(g, x[k], sx);
+                dg[k] = ffma2(dy[k], x[k], dg[k]);
+                db[k] = fadd2(db[k], dy[k]);
+            }
+            if (c.dx) {
+                float2 v = sum2(make_float2(sg.x + sg.y, sx.x + sx.y));
+                if (warps > 1) {
+                    float2 *to = red[m & 1];
+                    const int first = group * warps;
+                    if ((threadIdx.x & 31) == 0)
+                        to[threadIdx.x >> 5] = v;
+                    group_barrier(group, n);
+                    v = to[first];
+#pragma unroll 2
+                    for (int w = 1; w < warps; ++w)
+                        v = fadd2(v, to[first + w]);
+                }
+                // dx = r g + xh (-r mean(g xh)) - r mean g
+                const float2 c0 = splat(layer ? -r * (v.x * inv_d) : 0.f), c1 = splat(-r * (v.y * inv_d));
+#pragma unroll
+                for (int k = 0; k < P; ++k) {
+                    const int j = column(k);
+                    if constexpr (VEC) {
+                        float2 xk[4], dyk[4];
+                        load8(reinterpret_cast<const TX *>(own + s * stage) + j, reinterpret_cast<float *>(xk));
+                        load8(reinterpret_cast<const TDY *>(own + s * stage + xbytes) + j, reinterpret_cast<float *>(dyk));
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const float2 xh = fmul2(fadd2(xk[e], splat(-mu)), splat(r));
+                            xk[e] = ffma2(fmul2(dyk[e], gamma[4 * k + e]), splat(r), ffma2(xh, c1, c0));
+                        }
+                        if (j < d)
+                            store8(dx + j, reinterpret_cast<const float *>(xk));
+                    } else if (j < d) {
+                        const float g = reinterpret_cast<const float *>(dy)[k] * gam[k];
+                        dx[j] = from_float<TDX>(fmaf(g, r, fmaf(reinterpret_cast<const float *>(x)[k], c1.x, c0.x)));
+                    }
+                }
+            }
+        } else if (c.dx) {
+            const float zero[8] = {};
+#pragma unroll
+            for (int k = 0; k < P; ++k) {
+                const int j = column(k);
+                if (j < d) {
                     if constexpr (VEC)
-                        store8(dx + j, o);
+                        store8(dx + j, zero);
                     else
-                        dx[j] = from_float<TDX>(o[0]);
-                });
+                        dx[j] = from_float<TDX>(0.f);
+                }
             }
         }
         i = i1;
@@ -392,14 +474,25 @@ __global__ void __launch_bounds__(WIDE ? 512 : 320, WIDE ? 1 : 2) k_norm_bwd(Nor
         s = s == 2 ? 0 : s + 1;
     }
     if (c.dgamma || c.dbeta) {
-        float *part = static_cast<float *>(c.workspace) + b * 2 * c.d;
-        each_piece<VEC>(t, n, c.d, [&](int j, int k) {
+        float *part = static_cast<float *>(c.workspace) + (int64_t)b * 2 * d;
+        const float *dgs = reinterpret_cast<const float *>(dg), *dbs = reinterpret_cast<const float *>(db);
 #pragma unroll
-            for (int e = 0; e < (VEC ? 8 : 1); ++e) {
-                part[j + e] = dg[k + e];
-                part[c.d + j + e] = db[k + e];
+        for (int k = 0; k < P; ++k) {
+            const int j = column(k);
+            if (j < d) {
+                if constexpr (VEC) {
+#pragma unroll
+                    for (int h = 0; h < 8; h += 4) {
+                        const float *g = dgs + k * W + h, *e = dbs + k * W + h;
+                        *reinterpret_cast<float4 *>(part + j + h) = make_float4(g[0], g[1], g[2], g[3]);
+                        *reinterpret_cast<float4 *>(part + d + j + h) = make_float4(e[0], e[1], e[2], e[3]);
+                    }
+                } else {
+                    part[j] = dgs[k];
+                    part[d + j] = dbs[k];
+                }
             }
-        });
+        }
     }
     // rows of tokens that are not in the list
     if (rows && c.dx) {
@@ -414,10 +507,10 @@ __global__ void __launch_bounds__(WIDE ? 512 : 320, WIDE ? 1 : 2) k_norm_bwd(Nor
                 TDX *dx = static_cast<TDX *>(c.dx) + z * c.lddx;
                 if constexpr (VEC) {
                     const float zero[8] = {};
-                    for (int64_t j = lane * 8; j < c.d; j += 256)
+                    for (int j = lane * 8; j < d; j += 256)
                         store8(dx + j, zero);
                 } else {
-                    for (int64_t j = lane; j < c.d; j += 32)
+                    for (int j = lane; j < d; j += 32)
                         dx[j] = from_float<TDX>(0.f);
                 }
             }
@@ -522,8 +615,8 @@ constexpr int kMaxGrid = 320;         // CTAs of the backward pass, at most
 constexpr int kLongParts = 64;        // partial sums of the kernels for long rows
 constexpr int64_t kListFrom = 4096;   // tokens from which a loss mask is turned into a list of rows
 
-int row_threads(int64_t d) { return (int)((d + kE * 32 - 1) / (kE * 32)) * 32; }
-int rows_per_cta(int64_t d) { return std::max(1, kThreads / row_threads(d)); }
+int row_threads(int64_t d, int columns = kE) { return (int)((d + columns * 32 - 1) / (columns * 32)) * 32; }
+int rows_per_cta(int64_t d, int columns = kE) { return std::max(1, kThreads / row_threads(d, columns)); }
 
 int64_t partial_rows(int64_t T, int64_t d)
 {
@@ -538,16 +631,43 @@ bool on16(const void *p, int64_t ld, int32_t dtype)
     return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && ld * (dtype == TURNOPD_BF16 ? 2 : 4) % 16 == 0;
 }
 
+// Many rows: few threads to a row, each with up to 16 pieces (32 single columns), so that many rows are in flight and
+// most need no barrier.  Few rows: many threads to each, which answer sooner.
+template <typename X, typename Y, bool VEC, int P, int THREADS> void launch_fwd_pieces(const NormCall &c, cudaStream_t stream)
+{
+    constexpr int W = RowPiece<X, VEC>::W;
+    const int n = (int)((c.d + 32 * P * W - 1) / (32 * P * W)) * 32, per = std::max(1, 256 / n);
+    k_norm_fwd<X, Y, VEC, P, THREADS><<<(unsigned)((c.T + per - 1) / per), n * per, 0, stream>>>(c, n);
+}
+
+template <typename X, typename Y, bool VEC> void launch_fwd(const NormCall &c, cudaStream_t stream)
+{
+    constexpr int kMost = VEC ? 16 : 32, W = RowPiece<X, VEC>::W;
+    const int64_t pieces = (c.d + W - 1) / W;
+    if (pieces > 512 * kMost) {
+        const int grid = (int)std::min<int64_t>(c.T, (int64_t)device_sm_count() * 8);
+        k_norm_fwd_long<X, Y><<<grid, kThreads, 0, stream>>>(c);
+    } else if (c.T < 2 * device_sm_count() && pieces <= 1024 * 4) {
+        launch_fwd_pieces<X, Y, VEC, 4, 1024>(c, stream);
+    } else if (pieces <= 32 * 4) {
+        launch_fwd_pieces<X, Y, VEC, 4, 256>(c, stream);
+    } else if (pieces <= 32 * kMost / 2) {
+        launch_fwd_pieces<X, Y, VEC, kMost / 2, 256>(c, stream);
+    } else {
+        launch_fwd_pieces<X, Y, VEC, kMost, 512>(c, stream);
+    }
+}
+
 template <typename X, typename DY, typename DX>
 cudaError_t launch_bwd(const NormGradCall &c, bool vec, const int4 *rows, const int32_t *nvalid, int *parts,
                        cudaStream_t stream)
 {
-    const int n = row_threads(c.d), per = rows_per_cta(c.d);
-    const int64_t most = std::min<int64_t>(2 * device_sm_count(), kMaxGrid);
+    const int columns = vec ? kE : kBwdSingles, n = row_threads(c.d, columns), per = rows_per_cta(c.d, columns);
+    const bool wide = vec ? n * per > 320 : n * per > 512;  // one CTA per SM then, else two
+    const int64_t most = std::min<int64_t>((wide ? 1 : 2) * device_sm_count(), kMaxGrid);
     const int grid = (int)std::min<int64_t>((c.T + per - 1) / per, most);
     *parts = grid * per;
     const size_t smem = vec ? (sizeof(X) + sizeof(DY)) * n * per * kE * kStages : 0;
-    const bool wide = n * per > 320;  // one CTA per SM then, else two
     auto kernel = wide ? (vec ? k_norm_bwd<X, DY, DX, true, true> : k_norm_bwd<X, DY, DX, false, true>)
                        : (vec ? k_norm_bwd<X, DY, DX, true, false> : k_norm_bwd<X, DY, DX, false, false>);
     if (smem > 48 * 1024) {
@@ -573,19 +693,10 @@ cudaError_t launch_norm_fwd(const NormCall &c, cudaStream_t stream)
     const bool vec = c.d % 8 == 0 && on16(c.x, c.ldx, c.x_dtype) && on16(c.y, c.ldy, c.y_dtype) &&
                      on16(c.gamma, 8, c.param_dtype) && on16(c.beta, 8, c.param_dtype);
     with_types(c.x_dtype, c.y_dtype, [&](auto x, auto y) {
-        using X = decltype(x);
-        using Y = decltype(y);
-        if (c.d > kMaxFwd) {
-            const int grid = (int)std::min<int64_t>(c.T, (int64_t)device_sm_count() * 8);
-            k_norm_fwd_long<X, Y><<<grid, kThreads, 0, stream>>>(c);
-            return;
-        }
-        const int n = row_threads(c.d), per = rows_per_cta(c.d);
-        const unsigned grid = (unsigned)((c.T + per - 1) / per);
         if (vec)
-            k_norm_fwd<X, Y, true><<<grid, n * per, 0, stream>>>(c, n);
+            launch_fwd<decltype(x), decltype(y), true>(c, stream);
         else
-            k_norm_fwd<X, Y, false><<<grid, n * per, 0, stream>>>(c, n);
+            launch_fwd<decltype(x), decltype(y), false>(c, stream);
     });
     return cudaGetLastError();
 }
