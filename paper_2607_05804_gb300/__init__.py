@@ -453,14 +453,35 @@ def turnopd_vocab_shard_loss_grad(z_student, z_teacher, row_of_token, loss_mask,
 
 
 # ---------------------------------------------------------------- log probabilities of given tokens
+#
+# These calls are made once per decoding step too, where a few microseconds of marshalling count.
+
+def _arg(t, name, dtype=None, numel=0):
+    """The device pointer of a contiguous CUDA tensor (None stays None); _need says what is wrong with others."""
+    if t is None:
+        return None
+    if not t.is_cuda or (dtype is not None and t.dtype is not dtype) or t.numel() < numel or not t.is_contiguous():
+        _need(t, name, dtype, numel)
+    return t.data_ptr()
+
+
+def _handle(stream):
+    """The cudaStream_t of `stream`, or of the current stream (without the Stream object that current_stream() makes)."""
+    import torch
+
+    if stream is not None:
+        return stream.cuda_stream
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+
 
 def _rows_2d(t, name, like=None):
-    """(row stride) of a 2-D CUDA tensor with unit column stride."""
-    if not t.is_cuda or t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] > 1):
+    """The row stride of a 2-D CUDA tensor with unit column stride."""
+    shape, (ld, step) = t.shape, t.stride() if t.dim() == 2 else (0, 0)
+    if not t.is_cuda or ld == step == 0 or (step != 1 and shape[1] > 1):
         raise ValueError(f"{name} must be a 2-D CUDA tensor with unit column stride")
-    if like is not None and (t.shape != like.shape or t.stride(0) != like.stride(0)):
+    if like is not None and (shape != like.shape or ld != like.stride(0)):
         raise ValueError(f"{name} must match the logits in shape and row stride")
-    return max(t.stride(0), t.shape[1]) if t.shape[0] < 2 else t.stride(0)
+    return ld if shape[0] > 1 else max(ld, shape[1])
 
 
 def turnopd_token_logprobs_workspace_bytes(num_tokens: int) -> int:
@@ -485,25 +506,20 @@ def turnopd_token_logprobs(logits, vocab, row_of_token, token_ids, loss_mask, n_
     token; workspace may be None then); the outputs float32 [T] / [T, 2] / int32 and float32 [T, n_top], or None."""
     import torch
 
-    ld = _rows_2d(logits, "logits")
+    f32, i32 = torch.float32, torch.int32
+    ld, rows = _rows_2d(logits, "logits"), logits.shape[0]
     T = _num_tokens(logits, row_of_token, token_ids, loss_mask)
-    _need(row_of_token, "row_of_token", torch.int32, T)
-    _need(token_ids, "token_ids", torch.int32, T)
-    _need(loss_mask, "loss_mask", torch.uint8, T)
-    _need(logprob_out, "logprob_out", torch.float32, T)
-    _need(entropy_out, "entropy_out", torch.float32, T)
-    _need(stats_out, "stats_out", torch.float32, 2 * T)
-    _need(top_ids_out, "top_ids_out", torch.int32, T * int(n_top))
-    _need(top_logprob_out, "top_logprob_out", torch.float32, T * int(n_top))
-    _need(workspace, "workspace")
-    _need(dev_status, "dev_status", torch.int32, 1)
     if vocab > logits.shape[1]:
         raise ValueError("vocab is larger than the rows of logits")
-    _check(load().turnopd_token_logprobs(
-        _ptr(logits), _dtype_code(logits, "logits"), ld, int(vocab), logits.shape[0], _ptr(row_of_token),
-        _ptr(token_ids), _ptr(loss_mask), T, int(n_top), _ptr(logprob_out), _ptr(entropy_out), _ptr(stats_out),
-        _ptr(top_ids_out), _ptr(top_logprob_out), _ptr(workspace), _ws(workspace), _ptr(dev_status),
-        _stream(stream)), "turnopd_token_logprobs")
+    code = load().turnopd_token_logprobs(
+        logits.data_ptr(), _dtype_code(logits, "logits"), ld, int(vocab), rows, _arg(row_of_token, "row_of_token", i32, T),
+        _arg(token_ids, "token_ids", i32, T), _arg(loss_mask, "loss_mask", torch.uint8, T), T, int(n_top),
+        _arg(logprob_out, "logprob_out", f32, T), _arg(entropy_out, "entropy_out", f32, T),
+        _arg(stats_out, "stats_out", f32, 2 * T), _arg(top_ids_out, "top_ids_out", i32, T * n_top),
+        _arg(top_logprob_out, "top_logprob_out", f32, T * n_top), _arg(workspace, "workspace"), _ws(workspace),
+        _arg(dev_status, "dev_status", i32, 1), _handle(stream))
+    if code:
+        raise TurnopdError(code, "turnopd_token_logprobs")
 
 
 def turnopd_token_logprobs_bwd(logits, vocab, row_of_token, token_ids, loss_mask, stats, logprob, entropy, d_logprob,
@@ -513,57 +529,44 @@ def turnopd_token_logprobs_bwd(logits, vocab, row_of_token, token_ids, loss_mask
     the logits."""
     import torch
 
-    ld = _rows_2d(logits, "logits")
+    f32, i32 = torch.float32, torch.int32
+    ld, rows = _rows_2d(logits, "logits"), logits.shape[0]
     _rows_2d(grad_out, "grad_out", logits)
     T = _num_tokens(logits, row_of_token, token_ids, loss_mask)
-    _need(row_of_token, "row_of_token", torch.int32, T)
-    _need(token_ids, "token_ids", torch.int32, T)
-    _need(loss_mask, "loss_mask", torch.uint8, T)
-    _need(stats, "stats", torch.float32, 2 * T)
-    _need(logprob, "logprob", torch.float32, T)
-    _need(entropy, "entropy", torch.float32, T)
-    _need(d_logprob, "d_logprob", torch.float32, T)
-    _need(d_entropy, "d_entropy", torch.float32, T)
-    _need(workspace, "workspace")
-    _need(dev_status, "dev_status", torch.int32, 1)
     if vocab > logits.shape[1]:
         raise ValueError("vocab is larger than the rows of logits")
-    _check(load().turnopd_token_logprobs_bwd(
-        _ptr(logits), _dtype_code(logits, "logits"), ld, int(vocab), logits.shape[0], _ptr(row_of_token),
-        _ptr(token_ids), _ptr(loss_mask), T, _ptr(stats), _ptr(logprob), _ptr(entropy), _ptr(d_logprob),
-        _ptr(d_entropy), _ptr(grad_out), _dtype_code(grad_out, "grad_out"), int(flags), _ptr(workspace),
-        _ws(workspace), _ptr(dev_status), _stream(stream)), "turnopd_token_logprobs_bwd")
+    code = load().turnopd_token_logprobs_bwd(
+        logits.data_ptr(), _dtype_code(logits, "logits"), ld, int(vocab), rows, _arg(row_of_token, "row_of_token", i32, T),
+        _arg(token_ids, "token_ids", i32, T), _arg(loss_mask, "loss_mask", torch.uint8, T), T,
+        _arg(stats, "stats", f32, 2 * T), _arg(logprob, "logprob", f32, T), _arg(entropy, "entropy", f32, T),
+        _arg(d_logprob, "d_logprob", f32, T), _arg(d_entropy, "d_entropy", f32, T), grad_out.data_ptr(),
+        _dtype_code(grad_out, "grad_out"), int(flags), _arg(workspace, "workspace"), _ws(workspace),
+        _arg(dev_status, "dev_status", i32, 1), _handle(stream))
+    if code:
+        raise TurnopdError(code, "turnopd_token_logprobs_bwd")
 
 
 # ---------------------------------------------------------------- the norm before the LM head
-
-def _norm_checks(T, d, gamma, beta, loss_mask, mean, rstd):
-    import torch
-
-    _need(gamma, "gamma", None, d)
-    if beta is not None and beta.dtype != gamma.dtype:
-        raise ValueError("gamma and beta must have one dtype")
-    _need(beta, "beta", None, d)
-    _need(loss_mask, "loss_mask", torch.uint8, T)
-    _need(mean, "mean", torch.float32, T)
-    _need(rstd, "rstd", torch.float32, T)
-
 
 def turnopd_norm_fwd(x, gamma, beta, loss_mask, kind, eps, y_out, mean_out, rstd_out, dev_status, stream=None):
     """x [T, d] -> y_out [T, d] (rows any stride); gamma, beta [d] (beta or None); loss_mask uint8 [T] or None;
     mean_out, rstd_out float32 [T] or None; kind TURNOPD_LAYER_NORM or TURNOPD_RMS_NORM."""
     import torch
 
+    f32 = torch.float32
     ldx, ldy = _rows_2d(x, "x"), _rows_2d(y_out, "y_out")
     T, d = x.shape
     if y_out.shape != x.shape:
         raise ValueError("y_out must match x in shape")
-    _norm_checks(T, d, gamma, beta, loss_mask, mean_out, rstd_out)
-    _need(dev_status, "dev_status", torch.int32, 1)
-    _check(load().turnopd_norm_fwd(
-        _ptr(x), _dtype_code(x, "x"), ldx, _ptr(gamma), _ptr(beta), _dtype_code(gamma, "gamma"), _ptr(loss_mask), T, d,
-        int(kind), float(eps), _ptr(y_out), _dtype_code(y_out, "y_out"), ldy, _ptr(mean_out), _ptr(rstd_out),
-        _ptr(dev_status), _stream(stream)), "turnopd_norm_fwd")
+    if beta is not None and beta.dtype is not gamma.dtype:
+        raise ValueError("gamma and beta must have one dtype")
+    code = load().turnopd_norm_fwd(
+        x.data_ptr(), _dtype_code(x, "x"), ldx, _arg(gamma, "gamma", None, d), _arg(beta, "beta", None, d),
+        _dtype_code(gamma, "gamma"), _arg(loss_mask, "loss_mask", torch.uint8, T), T, d, int(kind), float(eps), y_out.data_ptr(),
+        _dtype_code(y_out, "y_out"), ldy, _arg(mean_out, "mean_out", f32, T), _arg(rstd_out, "rstd_out", f32, T),
+        _arg(dev_status, "dev_status", torch.int32, 1), _handle(stream))
+    if code:
+        raise TurnopdError(code, "turnopd_norm_fwd")
 
 
 def turnopd_norm_bwd_workspace_bytes(num_tokens: int, d: int) -> int:
@@ -575,20 +578,20 @@ def turnopd_norm_bwd(x, gamma, loss_mask, kind, mean, rstd, dy, dx_out, dgamma_o
     root-mean-square norm) and rstd are the forward call's."""
     import torch
 
+    f32 = torch.float32
     ldx, lddy = _rows_2d(x, "x"), _rows_2d(dy, "dy")
     T, d = x.shape
     if dy.shape != x.shape or (dx_out is not None and dx_out.shape != x.shape):
         raise ValueError("dy and dx_out must match x in shape")
     lddx = _rows_2d(dx_out, "dx_out") if dx_out is not None else d
-    _norm_checks(T, d, gamma, None, loss_mask, mean, rstd)
-    _need(dgamma_out, "dgamma_out", torch.float32, d)
-    _need(dbeta_out, "dbeta_out", torch.float32, d)
-    _need(workspace, "workspace")
-    _check(load().turnopd_norm_bwd(
-        _ptr(x), _dtype_code(x, "x"), ldx, _ptr(gamma), _dtype_code(gamma, "gamma"), _ptr(loss_mask), T, d, int(kind),
-        _ptr(mean), _ptr(rstd), _ptr(dy), _dtype_code(dy, "dy"), lddy, _ptr(dx_out),
-        TURNOPD_F32 if dx_out is None else _dtype_code(dx_out, "dx_out"), lddx, _ptr(dgamma_out), _ptr(dbeta_out),
-        _ptr(workspace), _ws(workspace), _stream(stream)), "turnopd_norm_bwd")
+    code = load().turnopd_norm_bwd(
+        x.data_ptr(), _dtype_code(x, "x"), ldx, _arg(gamma, "gamma", None, d), _dtype_code(gamma, "gamma"),
+        _arg(loss_mask, "loss_mask", torch.uint8, T), T, d, int(kind), _arg(mean, "mean", f32, T), _arg(rstd, "rstd", f32, T),
+        dy.data_ptr(), _dtype_code(dy, "dy"), lddy, None if dx_out is None else dx_out.data_ptr(),
+        TURNOPD_F32 if dx_out is None else _dtype_code(dx_out, "dx_out"), lddx, _arg(dgamma_out, "dgamma_out", f32, d),
+        _arg(dbeta_out, "dbeta_out", f32, d), _arg(workspace, "workspace"), _ws(workspace), _handle(stream))
+    if code:
+        raise TurnopdError(code, "turnopd_norm_bwd")
 
 
 # ---------------------------------------------------------------- rollout-depth controller (host)

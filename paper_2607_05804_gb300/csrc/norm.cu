@@ -109,21 +109,43 @@ template <typename T> struct RowPiece<T, false> {
     __device__ float at(int) const { return raw; }
 };
 
-template <int W> __device__ __forceinline__ void load_params(const void *p, int32_t dtype, int j, float (&v)[W])
+// Columns j + k step + 0..W-1 of gamma or beta, k < B, those below d; asked for together.
+template <int W, int B>
+__device__ __forceinline__ void load_params(const void *p, int32_t dtype, int j, int step, int d, float (&v)[B][W])
 {
-    if constexpr (W == 1) {
-        v[0] = param(p, dtype, j);
-    } else if (dtype == TURNOPD_BF16) {
+    if (dtype == TURNOPD_BF16) {
+        const __nv_bfloat16 *q = static_cast<const __nv_bfloat16 *>(p);
 #pragma unroll
-        for (int e = 0; e < W; e += 4) {
-            const uint2 u = *reinterpret_cast<const uint2 *>(static_cast<const __nv_bfloat16 *>(p) + j + e);
-            v[e] = bf16lo(u.x), v[e + 1] = bf16hi(u.x), v[e + 2] = bf16lo(u.y), v[e + 3] = bf16hi(u.y);
+        for (int k = 0; k < B; ++k) {
+            const int at = j + k * step;
+            if (at >= d)
+                break;
+            if constexpr (W == 1) {
+                v[k][0] = __bfloat162float(__ldg(q + at));
+            } else {
+#pragma unroll
+                for (int e = 0; e < W; e += 4) {
+                    const uint2 u = __ldg(reinterpret_cast<const uint2 *>(q + at + e));
+                    v[k][e] = bf16lo(u.x), v[k][e + 1] = bf16hi(u.x), v[k][e + 2] = bf16lo(u.y), v[k][e + 3] = bf16hi(u.y);
+                }
+            }
         }
     } else {
+        const float *q = static_cast<const float *>(p);
 #pragma unroll
-        for (int e = 0; e < W; e += 4) {
-            const float4 u = *reinterpret_cast<const float4 *>(static_cast<const float *>(p) + j + e);
-            v[e] = u.x, v[e + 1] = u.y, v[e + 2] = u.z, v[e + 3] = u.w;
+        for (int k = 0; k < B; ++k) {
+            const int at = j + k * step;
+            if (at >= d)
+                break;
+            if constexpr (W == 1) {
+                v[k][0] = __ldg(q + at);
+            } else {
+#pragma unroll
+                for (int e = 0; e < W; e += 4) {
+                    const float4 u = __ldg(reinterpret_cast<const float4 *>(q + at + e));
+                    v[k][e] = u.x, v[k][e + 1] = u.y, v[k][e + 2] = u.z, v[k][e + 3] = u.w;
+                }
+            }
         }
     }
 }
@@ -184,31 +206,43 @@ __global__ void __launch_bounds__(THREADS) k_norm_fwd(NormCall c, int n)
     if (r == 0.f)
         mu = 0.f;
     TY *y = static_cast<TY *>(c.y) + i * c.ldy;
+    constexpr int B = VEC ? (W == 8 ? 2 : 4) : P < 8 ? P : 8;  // pieces whose parameters are in flight together
+    static_assert(P % B == 0, "whole batches of pieces");
 #pragma unroll
-    for (int k = 0; k < P; ++k) {
-        const int j = (k * n + t) * W;
-        if (j >= d)
-            continue;
-        float o[W], g[W];
+    for (int k0 = 0; k0 < P; k0 += B) {
+        const int j0 = (k0 * n + t) * W;
+        if (j0 >= d)
+            break;
+        float g[B][W], o[B][W];
 #pragma unroll
-        for (int e = 0; e < W; ++e)
-            o[e] = 0.f;
-        if (r != 0.f) {
-            load_params<W>(c.gamma, c.param_dtype, j, g);
-            if (c.beta)
-                load_params<W>(c.beta, c.param_dtype, j, o);
+        for (int k = 0; k < B; ++k)
 #pragma unroll
             for (int e = 0; e < W; ++e)
-                o[e] = fmaf((v[k].at(e) - mu) * r, g[e], o[e]);
+                o[k][e] = 0.f;
+        if (r != 0.f) {
+            load_params<W, B>(c.gamma, c.param_dtype, j0, n * W, d, g);
+            if (c.beta)
+                load_params<W, B>(c.beta, c.param_dtype, j0, n * W, d, o);
         }
-        if constexpr (!VEC)
-            y[j] = from_float<TY>(o[0]);
-        else if constexpr (W == 8)
-            store8(y + j, o);
-        else if constexpr (sizeof(TY) == 4)
-            __stcs(reinterpret_cast<float4 *>(y + j), make_float4(o[0], o[1], o[2], o[3]));
-        else
-            __stcs(reinterpret_cast<uint2 *>(y + j), make_uint2(pack_bf16x2(o[0], o[1]), pack_bf16x2(o[2], o[3])));
+#pragma unroll
+        for (int k = 0; k < B; ++k) {
+            const int j = j0 + k * n * W;
+            if (j >= d)
+                break;
+            if (r != 0.f) {
+#pragma unroll
+                for (int e = 0; e < W; ++e)
+                    o[k][e] = fmaf((v[k0 + k].at(e) - mu) * r, g[k][e], o[k][e]);
+            }
+            if constexpr (!VEC)
+                y[j] = from_float<TY>(o[k][0]);
+            else if constexpr (W == 8)
+                store8(y + j, o[k]);
+            else if constexpr (sizeof(TY) == 4)
+                __stcs(reinterpret_cast<float4 *>(y + j), make_float4(o[k][0], o[k][1], o[k][2], o[k][3]));
+            else
+                __stcs(reinterpret_cast<uint2 *>(y + j), make_uint2(pack_bf16x2(o[k][0], o[k][1]), pack_bf16x2(o[k][2], o[k][3])));
+        }
     }
     if (t == 0) {
         if (c.mean)

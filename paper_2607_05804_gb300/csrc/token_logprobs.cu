@@ -29,22 +29,27 @@ constexpr float kMaskedBelow = -0x1p+126f;
 constexpr float kClamp = -0x1.8p+126f;
 constexpr uint32_t kClampBf16x2 = 0xfec0fec0u;
 
+enum RowState : int32_t { kRowBad = 0, kRowFine = 1, kRowMasked = 2 };
+
 struct Row {
-    int32_t token, r, y;
-    bool ok;
+    int32_t token, r, y, state;
 };
 
-// Item k of the row list; without one (no loss mask) token k itself, its indexes checked here.
+// Item k of the row list; without one token k itself, its mask and indexes checked here.
 template <typename Call> __device__ __forceinline__ Row get_row(const Call &c, const int4 *rows, int64_t k)
 {
     if (rows) {
         const int4 v = rows[k];
-        return Row{v.x, v.y, v.z, true};
+        return Row{v.x, v.y, v.z, kRowFine};
     }
-    Row o{(int32_t)k, c.row_of_token ? c.row_of_token[k] : (int32_t)k, c.token_ids ? c.token_ids[k] : -1, true};
-    o.ok = o.r >= 0 && o.r < c.num_rows && (!c.token_ids || (o.y >= 0 && o.y < c.vocab));
-    if (!o.ok && threadIdx.x == 0)
-        set_status(c.status, TURNOPD_ERR_TOKEN_RANGE);
+    if (c.mask && !c.mask[k])
+        return Row{(int32_t)k, 0, -1, kRowMasked};
+    Row o{(int32_t)k, c.row_of_token ? c.row_of_token[k] : (int32_t)k, c.token_ids ? c.token_ids[k] : -1, kRowFine};
+    if (!(o.r >= 0 && o.r < c.num_rows && (!c.token_ids || (o.y >= 0 && o.y < c.vocab)))) {
+        o.state = kRowBad;
+        if (threadIdx.x == 0)
+            set_status(c.status, TURNOPD_ERR_TOKEN_RANGE);
+    }
     return o;
 }
 
@@ -236,22 +241,14 @@ template <> struct Logits<float> {
 // even that adds too many, n times.  Keys are unique, so the outcome does not depend on the order of the list.
 
 constexpr int kU = 4;                             // vectors per thread and chunk
-constexpr int kChunk = kU * kThreads;
-#ifndef LP_PERSM
-#define LP_PERSM 3
-#endif
-#ifndef LP_PERSM0
-#define LP_PERSM0 4
-#endif
-template <bool TOP> constexpr int kPerSm = TOP ? LP_PERSM : LP_PERSM0;  // CTAs per SM
 constexpr int kListCap = 1024;
 constexpr int kTopMax = TURNOPD_TOP_ALTERNATIVES_MAX;
 constexpr int kMaxCtas = 8;                       // of a cluster
 
-struct alignas(16) TopShared {
+template <int NT> struct alignas(16) TopShared {
     uint64_t list[kListCap + 2];
-    uint64_t lanes[kThreads];                     // the threads' best keys
-    uint64_t groups[kWarps][32];                  // each warp's copy of the groups' best
+    uint64_t lanes[NT];                     // the threads' best keys
+    uint64_t groups[(NT / 32)][32];                  // each warp's copy of the groups' best
     uint64_t sorted[kTopMax];
     uint64_t merge[kMaxCtas * kTopMax];           // CTA 0: every CTA's n best
     int count;
@@ -271,13 +268,13 @@ __device__ __forceinline__ float next_above(float b, float)
 }
 
 // Cuts the list to its n best, in order.
-__device__ __forceinline__ void cut_list(int n, TopShared &t)
+template <int NT> __device__ __forceinline__ void cut_list(int n, TopShared<NT> &t)
 {
     __syncthreads();
     const int m = min(t.count, kListCap), tid = threadIdx.x;
-    // blocks of kThreads entries, each but the first beginning with the 32 best of those before
-    for (int start = 0;; start += kThreads - kTopMax) {
-        const int len = min(m - start, kThreads);
+    // blocks of NT entries, each but the first beginning with the 32 best of those before
+    for (int start = 0;; start += NT - kTopMax) {
+        const int len = min(m - start, NT);
         const uint64_t *block = t.list + start;
         const uint64_t key = tid < len ? block[tid] : 0;
         if (tid < kTopMax)
@@ -296,9 +293,9 @@ __device__ __forceinline__ void cut_list(int n, TopShared &t)
                 t.sorted[place] = key;
         }
         __syncthreads();
-        const bool done = start + kThreads >= m;
+        const bool done = start + NT >= m;
         if (tid < kTopMax)
-            t.list[done ? tid : start + kThreads - kTopMax + tid] = t.sorted[tid];
+            t.list[done ? tid : start + NT - kTopMax + tid] = t.sorted[tid];
         if (done)
             break;
         __syncthreads();
@@ -311,7 +308,7 @@ __device__ __forceinline__ void cut_list(int n, TopShared &t)
     __syncthreads();
 }
 
-__device__ __forceinline__ void list_add(uint64_t key, TopShared &t)
+template <int NT> __device__ __forceinline__ void list_add(uint64_t key, TopShared<NT> &t)
 {
     const int at = atomicAdd(&t.count, 1);
     if (at < kListCap)
@@ -328,118 +325,125 @@ __device__ __forceinline__ uint4 pick(const uint4 (&v)[kU], int u)
     return w;
 }
 
-// One chunk: vector u of the thread holds ids id0 + u stride + 0..N-1 (none where u >= held), vm is their maximum.
-// `bound` is the n-th best logit so far; `first`: the chunk sets its own.
-template <typename TIn>
-__device__ __forceinline__ void top_chunk(const uint4 (&v)[kU], float vm, int held, uint32_t id0, bool first, int n,
-                                          TopShared &t, float &bound)
+// Adds the logits of a chunk that reach `above` and, where equal to it, have ids up to tie_id, and whose keys reach
+// `least`.  Vector u of the thread holds ids id0 + u stride + 0..N-1 (none where u >= held).
+template <typename TIn, int NT>
+__device__ __forceinline__ void list_add_chunk(const uint4 (&v)[kU], int held, uint32_t id0, float above, uint32_t tie_id,
+                                               uint64_t least, TopShared<NT> &t)
 {
     using X = Logits<TIn>;
-    constexpr uint32_t stride = kThreads * X::N;
-    float above = next_above(bound, TIn());  // what a logit has to reach
-    uint64_t least = 0;                      // a first chunk: the key it has to reach,
-    uint32_t tie_id = ~0u;                   // and so the last id that may equal `above`
-    if (first) {
-        // the thread's best: its logit, and an id not below its own (the last of its vector)
-        int u0 = kU - 1;
+    constexpr uint32_t stride = NT * X::N;
+    // bit p: element of word p % 16, upper half from bit 16 on (bf16); element p (fp32)
+    uint32_t hits = 0;
 #pragma unroll
-        for (int u = kU - 2; u >= 0; --u)
-            u0 = X::max_of_one(v[u]) == vm ? u : u0;
-        const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-        t.lanes[threadIdx.x] = held > 0 && vm == vm ? top_key(vm, id0 + u0 * stride + X::N - 1) : 0;
-        __syncthreads();
-        uint64_t best = 0;
-#pragma unroll
-        for (int w = 0; w < kWarps; ++w)
-            best = max(best, t.lanes[32 * w + lane]);
-        t.groups[warp][lane] = best;
-        __syncwarp();
-        int place = 0;
-#pragma unroll
-        for (int j = 0; j < 32; j += 2) {
-            const ulonglong2 o = *reinterpret_cast<const ulonglong2 *>(&t.groups[warp][j]);
-            place += (o.x > best) + (o.y > best);
-        }
-        const unsigned who = __ballot_sync(~0u, best != 0 && place == n - 1);
-        if (who)
-            least = __shfl_sync(~0u, (unsigned long long)best, __ffs(who) - 1);
-        const float own = least ? key_logit(least) : -INFINITY;  // 0: fewer than n groups, all of them are added
-        if (bound == -INFINITY || own >= above) {
-            above = own;
-            tie_id = least ? key_id(least) : ~0u;
-        } else {
-            least = 0;
-        }
+    for (int u = 0; u < kU; ++u) {
+        const float low = u >= held ? NAN : id0 + u * stride <= tie_id ? above : next_above(above, TIn());
+        hits |= X::reach(v[u], low, u);
     }
-    if (vm >= above) {
-        // bit p: element of word p % 16, upper half from bit 16 on (bf16); element p (fp32)
-        uint32_t hits = 0;
-#pragma unroll
-        for (int u = 0; u < kU; ++u) {
-            const float low = u >= held ? NAN : id0 + u * stride <= tie_id ? above : next_above(above, TIn());
-            hits |= X::reach(v[u], low, u);
-        }
-        while (hits) {
-            const int p = __ffs(hits) - 1;
-            hits &= hits - 1;
-            const int u = X::vector_of(p), j = X::place_of(p);
-            const uint64_t key = top_key(X::at_run_time(pick(v, u), j), id0 + u * stride + j);
-            if (key >= least)
-                list_add(key, t);
-        }
-    }
-    if (first) {
-        cut_list(n, t);
-        bound = t.sorted[n - 1] ? key_logit(t.sorted[n - 1]) : -INFINITY;
+    while (hits) {
+        const int p = __ffs(hits) - 1;
+        hits &= hits - 1;
+        const int u = X::vector_of(p), j = X::place_of(p);
+        const uint64_t key = top_key(X::at_run_time(pick(v, u), j), id0 + u * stride + j);
+        if (key >= least)
+            list_add(key, t);
     }
 }
 
+// A chunk that sets its own bound; vm is the largest of the thread's logits, `bound` the n-th best so far.
+template <typename TIn, int NT>
+__device__ __forceinline__ void top_first_chunk(const uint4 (&v)[kU], float vm, int held, uint32_t id0, int n, TopShared<NT> &t,
+                                                float &bound)
+{
+    using X = Logits<TIn>;
+    constexpr uint32_t stride = NT * X::N;
+    // the thread's best: its logit, and an id not below its own (the last of its vector)
+    int u0 = kU - 1;
+#pragma unroll
+    for (int u = kU - 2; u >= 0; --u)
+        u0 = X::max_of_one(v[u]) == vm ? u : u0;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    t.lanes[threadIdx.x] = held > 0 && vm == vm ? top_key(vm, id0 + u0 * stride + X::N - 1) : 0;
+    __syncthreads();
+    uint64_t best = 0;
+#pragma unroll
+    for (int w = 0; w < (NT / 32); ++w)
+        best = max(best, t.lanes[32 * w + lane]);
+    t.groups[warp][lane] = best;
+    __syncwarp();
+    int place = 0;
+#pragma unroll
+    for (int j = 0; j < 32; j += 2) {
+        const ulonglong2 o = *reinterpret_cast<const ulonglong2 *>(&t.groups[warp][j]);
+        place += (o.x > best) + (o.y > best);
+    }
+    const unsigned who = __ballot_sync(~0u, best != 0 && place == n - 1);
+    uint64_t least = 0;  // 0: fewer than n groups, all of them are added
+    if (who)
+        least = __shfl_sync(~0u, (unsigned long long)best, __ffs(who) - 1);
+    const float own = least ? key_logit(least) : -INFINITY;
+    float above = next_above(bound, TIn());
+    uint32_t tie_id = ~0u;
+    if (bound == -INFINITY || own >= above) {
+        above = own;
+        tie_id = least ? key_id(least) : ~0u;
+    } else {
+        least = 0;
+    }
+    if (vm >= above)
+        list_add_chunk<TIn>(v, held, id0, above, tie_id, least, t);
+    cut_list(n, t);
+    bound = t.sorted[n - 1] ? key_logit(t.sorted[n - 1]) : -INFINITY;
+}
+
 // ---------------------------------------------------------------- forward kernel
+
+// CTAs of NT threads per SM: what the registers allow without spills.
+constexpr int per_sm(bool top, int nt) { return nt == 128 ? 7 : top ? 3 : 4; }
 
 // A row's share of one CTA: `len` of the row's whole 16-byte vectors, from the row's q0-th on; the first starts after
 // `head` logits.  CTA 0 of the cluster also takes the logits before and after the row's `nvec` vectors one by one.
 struct Share {
     const char *row;
-    int32_t head, nvec, q0, len, chunks, token, y;
-    bool ok;
+    int32_t head, nvec, q0, len, chunks, token, y, state;
 };
 
-template <typename TIn> __device__ __forceinline__ Share get_share(const LogprobCall &c, Row r, int rank, int ctas)
+template <typename TIn, int NT> __device__ __forceinline__ Share get_share(const LogprobCall &c, Row r, int rank, int ctas)
 {
     constexpr int N = Logits<TIn>::N;
     Share s;
     s.token = r.token;
     s.y = r.y;
-    s.ok = r.ok;
-    const TIn *z = static_cast<const TIn *>(c.logits) + (r.ok ? (int64_t)r.r * c.ld : 0);
+    s.state = r.state;
+    const TIn *z = static_cast<const TIn *>(c.logits) + (r.state == kRowFine ? (int64_t)r.r * c.ld : 0);
     s.row = reinterpret_cast<const char *>(z);
-    const int V = r.ok ? (int)c.vocab : 0;
+    const int V = r.state == kRowFine ? (int)c.vocab : 0;
     s.head = min((int)((16 - (reinterpret_cast<uintptr_t>(z) & 15)) & 15) / (int)sizeof(TIn), V);
     s.nvec = (V - s.head) / N;
     const int per = (s.nvec + ctas - 1) / ctas;
     s.q0 = min(s.nvec, rank * per);
     s.len = min(s.nvec, s.q0 + per) - s.q0;
-    s.chunks = (s.len + kChunk - 1) / kChunk;
+    s.chunks = (s.len + (kU * NT) - 1) / (kU * NT);
     return s;
 }
 
-template <typename TIn>
+template <typename TIn, int NT>
 __device__ __forceinline__ void load_chunk(const Share &s, int chunk, uint4 (&v)[kU])
 {
-    const int q = chunk * kChunk + threadIdx.x;
+    const int q = chunk * (kU * NT) + threadIdx.x;
     const uint4 *p = reinterpret_cast<const uint4 *>(s.row + s.head * sizeof(TIn)) + s.q0 + q;
     const int left = s.len - q;
 #pragma unroll
     for (int u = 0; u < kU; ++u) {
         constexpr uint32_t h = Logits<TIn>::kHole;
-        v[u] = u * kThreads < left ? ldg_stream(p + u * kThreads) : make_uint4(h, h, h, h);
+        v[u] = u * NT < left ? ldg_stream(p + u * NT) : make_uint4(h, h, h, h);
     }
 }
 
 // The alternatives of a row whose list was full: every chunk like a first one, and if that fails too, the best logit
 // below the last one, n times.
-template <typename TIn>
-__device__ __noinline__ void top_again(const Share &s, bool has_end, float end_z, int end_id, int n, TopShared &t)
+template <typename TIn, int NT>
+__device__ __noinline__ void top_again(const Share &s, bool has_end, float end_z, int end_id, int n, TopShared<NT> &t)
 {
     constexpr int N = Logits<TIn>::N;
     const uint64_t end_key = has_end ? top_key(end_z, end_id) : 0;
@@ -452,10 +456,10 @@ __device__ __noinline__ void top_again(const Share &s, bool has_end, float end_z
     float bound = -INFINITY;
     for (int chunk = 0; chunk < s.chunks; ++chunk) {
         uint4 v[kU];
-        load_chunk<TIn>(s, chunk, v);
-        const int q = chunk * kChunk + threadIdx.x;
-        const int held = q >= s.len ? 0 : min(kU, (s.len - q + kThreads - 1) / kThreads);
-        top_chunk<TIn>(v, Logits<TIn>::max_of(v), held, s.head + (uint32_t)(s.q0 + q) * N, true, n, t, bound);
+        load_chunk<TIn, NT>(s, chunk, v);
+        const int q = chunk * (kU * NT) + threadIdx.x;
+        const int held = q >= s.len ? 0 : min(kU, (s.len - q + NT - 1) / NT);
+        top_first_chunk<TIn>(v, Logits<TIn>::max_of(v), held, s.head + (uint32_t)(s.q0 + q) * N, n, t, bound);
     }
     if (end_key != 0)
         list_add(end_key, t);
@@ -466,7 +470,7 @@ __device__ __noinline__ void top_again(const Share &s, bool has_end, float end_z
     uint64_t below = ~0ull;
     for (int k = 0; k < n; ++k) {
         uint64_t best = end_key < below ? end_key : 0;
-        for (int i = threadIdx.x; i < s.len * N; i += kThreads) {
+        for (int i = threadIdx.x; i < s.len * N; i += NT) {
             const uint64_t key = top_key(to_float(z[i]), s.head + s.q0 * N + i);
             best = key < below ? max(best, key) : best;
         }
@@ -476,7 +480,7 @@ __device__ __noinline__ void top_again(const Share &s, bool has_end, float end_z
         if ((threadIdx.x & 31) == 0)
             t.lanes[threadIdx.x >> 5] = best;
         __syncthreads();
-        for (int w = 0; w < kWarps; ++w)
+        for (int w = 0; w < (NT / 32); ++w)
             best = max(best, t.lanes[w]);
         below = best;
         if (threadIdx.x == 0)
@@ -488,16 +492,16 @@ __device__ __noinline__ void top_again(const Share &s, bool has_end, float end_z
     __syncthreads();
 }
 
-template <typename TIn, bool TOP>
-__global__ void __launch_bounds__(kThreads, kPerSm<TOP>) k_logprobs(LogprobCall c, const int4 *__restrict__ rows,
+template <typename TIn, bool TOP, int NT>
+__global__ void __launch_bounds__(NT, per_sm(TOP, NT)) k_logprobs(LogprobCall c, const int4 *__restrict__ rows,
                                                           const int32_t *__restrict__ nvalid)
 {
     using X = Logits<TIn>;
-    __shared__ Part parts[kWarps];
+    __shared__ Part parts[(NT / 32)];
     __shared__ Part whole[kMaxCtas];  // CTA 0: the parts of the row
     __shared__ float norm[3];   // m, log S of the row, 1 if it is fine
-    __shared__ TopShared top;
-    __shared__ Share shares[2][kWarps];  // each warp its own: no barrier between a row's share and the next one's
+    __shared__ TopShared<NT> top;
+    __shared__ Share shares[2][(NT / 32)];  // each warp its own: no barrier between a row's share and the next one's
     namespace cg = cooperative_groups;
     cg::cluster_group cluster = cg::this_cluster();
     const int rank = (int)cluster.block_rank(), ctas = (int)cluster.num_blocks();
@@ -512,35 +516,35 @@ __global__ void __launch_bounds__(kThreads, kPerSm<TOP>) k_logprobs(LogprobCall 
     Row coming{};
     if (first < n) {
         if (lane == 0) {
-            shares[0][warp] = get_share<TIn>(c, get_row(c, rows, first), rank, ctas);
+            shares[0][warp] = get_share<TIn, NT>(c, get_row(c, rows, first), rank, ctas);
             if (first + step < n)
                 coming = get_row(c, rows, first + step);
         }
         __syncwarp();
-        load_chunk<TIn>(shares[0][warp], 0, ahead);
+        load_chunk<TIn, NT>(shares[0][warp], 0, ahead);
     }
     for (int64_t k = first; k < n; k += step, slot ^= 1) {
         const bool more = k + step < n;
         const Share &s = shares[slot][warp], &next = shares[slot ^ 1][warp];
         if (more && lane == 0) {
-            shares[slot ^ 1][warp] = get_share<TIn>(c, coming, rank, ctas);
+            shares[slot ^ 1][warp] = get_share<TIn, NT>(c, coming, rank, ctas);
             if (k + 2 * step < n)
                 coming = get_row(c, rows, k + 2 * step);
         }
         __syncwarp();
         // the row's ends, before its first and after its last whole vector, and y's logit: needed last, asked for first
         const TIn *z = reinterpret_cast<const TIn *>(s.row);
-        const int ends = rank == 0 && s.ok ? (int)c.vocab - s.nvec * X::N : 0;
+        const int ends = rank == 0 && s.state == kRowFine ? (int)c.vocab - s.nvec * X::N : 0;
         const int end_id = (int)threadIdx.x < s.head ? threadIdx.x : s.nvec * X::N + threadIdx.x;
         const float end_z = (int)threadIdx.x < ends ? to_float(z[end_id]) : 0.f;
-        const float zy = warp == 0 && s.ok && s.y >= 0 ? to_float(z[s.y]) : -INFINITY;
+        const float zy = warp == 0 && s.state == kRowFine && s.y >= 0 ? to_float(z[s.y]) : -INFINITY;
         // where y lies: in this thread's vector uy of chunk cy, or nowhere
         int cy = -1, uy = 0;
         if (s.y >= s.head) {
             const int f = (s.y - s.head) / X::N - s.q0;
-            if (f >= 0 && f < s.len && (f & (kThreads - 1)) == (int)threadIdx.x) {
-                cy = f / kChunk;
-                uy = f / kThreads & (kU - 1);
+            if (f >= 0 && f < s.len && (f & (NT - 1)) == (int)threadIdx.x) {
+                cy = f / (kU * NT);
+                uy = f / NT & (kU - 1);
             }
         }
         const int chunks = s.chunks;
@@ -558,16 +562,22 @@ __global__ void __launch_bounds__(kThreads, kPerSm<TOP>) k_logprobs(LogprobCall 
                 v[u] = ahead[u];
             const bool last = chunk + 1 == chunks;
             if (!last || more)
-                load_chunk<TIn>(last ? next : s, last ? 0 : chunk + 1, ahead);
+                load_chunk<TIn, NT>(last ? next : s, last ? 0 : chunk + 1, ahead);
             const float vm = X::max_of(v);
             if (TOP) {
-                const int q = chunk * kChunk + threadIdx.x;
-                const int held = q >= s.len ? 0 : min(kU, (s.len - q + kThreads - 1) / kThreads);
                 if (chunk > 1 && (chunk & (chunk - 1)) == 0) {
                     cut_list(c.n_top, top);
                     bound = key_logit(top.sorted[c.n_top - 1]);
                 }
-                top_chunk<TIn>(v, vm, held, s.head + (uint32_t)(s.q0 + q) * X::N, chunk == 0, c.n_top, top, bound);
+                if (chunk == 0 || vm > bound) {
+                    const int q = chunk * (kU * NT) + threadIdx.x;
+                    const int held = q >= s.len ? 0 : min(kU, (s.len - q + NT - 1) / NT);
+                    const uint32_t id0 = s.head + (uint32_t)(s.q0 + q) * X::N;
+                    if (chunk == 0)
+                        top_first_chunk<TIn>(v, vm, held, id0, c.n_top, top, bound);
+                    else
+                        list_add_chunk<TIn>(v, held, id0, next_above(bound, TIn()), ~0u, 0, top);
+                }
             }
             if (chunk == cy) {
                 const int j = (s.y - s.head) & (X::N - 1);
@@ -595,7 +605,7 @@ __global__ void __launch_bounds__(kThreads, kPerSm<TOP>) k_logprobs(LogprobCall 
                 X::fold(v[u], splat(-m), S, A);
         }
         if (chunks == 0 && more)
-            load_chunk<TIn>(next, 0, ahead);
+            load_chunk<TIn, NT>(next, 0, ahead);
         Part p{m, S.x + S.y, A.x + A.y};
         if (TOP)
             __syncthreads();
@@ -623,7 +633,7 @@ __global__ void __launch_bounds__(kThreads, kPerSm<TOP>) k_logprobs(LogprobCall 
         if (ctas > 1 && k == first)
             asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
         if (warp == 0) {
-            p = part_warp(lane < kWarps ? parts[lane] : part_empty());
+            p = part_warp(lane < (NT / 32) ? parts[lane] : part_empty());
             if (lane == 0)
                 *cluster.map_shared_rank(&whole[rank], 0) = p;
         }
@@ -643,7 +653,7 @@ __global__ void __launch_bounds__(kThreads, kPerSm<TOP>) k_logprobs(LogprobCall 
                 const float total = p.s + ey;
                 const float logs = ey == 1.f ? log1pf(p.s) : logf(total);
                 const float H = logs - kLn2 * (fmaf(ey, ty, p.a) / total);
-                const bool fine = s.ok && M > kMaskedBelow && M < -kMaskedBelow && isfinite(logs) && isfinite(H) &&
+                const bool fine = s.state == kRowFine && M > kMaskedBelow && M < -kMaskedBelow && isfinite(logs) && isfinite(H) &&
                                   zy == zy;
                 if (lane == 0) {
                     norm[0] = M;
@@ -660,19 +670,19 @@ __global__ void __launch_bounds__(kThreads, kPerSm<TOP>) k_logprobs(LogprobCall 
                             c.stats[2 * i + 1] = logs;
                         }
                     } else {
-                        if (s.ok)
+                        if (s.state == kRowFine)
                             set_status(c.status, TURNOPD_ERR_NONFINITE);
-                        write_nothing(c, i, -INFINITY);
+                        write_nothing(c, i, s.state == kRowMasked ? 0.f : -INFINITY);
                     }
                 }
             }
             if (TOP) {
                 // the CTAs' lists, each in order: a key's place among all is the number of keys above it
-                int place[kMaxCtas * kTopMax / kThreads];
-                uint64_t key[kMaxCtas * kTopMax / kThreads];
+                int place[kMaxCtas * kTopMax / NT];
+                uint64_t key[kMaxCtas * kTopMax / NT];
 #pragma unroll
-                for (int i = 0; i < kMaxCtas * kTopMax / kThreads; ++i) {
-                    const int e = threadIdx.x + i * kThreads, own = e / kTopMax;
+                for (int i = 0; i < kMaxCtas * kTopMax / NT; ++i) {
+                    const int e = threadIdx.x + i * NT, own = e / kTopMax;
                     place[i] = e % kTopMax;
                     key[i] = own >= ctas ? 0 : ctas == 1 ? top.sorted[place[i]] : top.merge[e];
                     if (key[i] == 0)
@@ -690,7 +700,7 @@ __global__ void __launch_bounds__(kThreads, kPerSm<TOP>) k_logprobs(LogprobCall 
                 }
                 __syncthreads();
 #pragma unroll
-                for (int i = 0; i < kMaxCtas * kTopMax / kThreads; ++i) {
+                for (int i = 0; i < kMaxCtas * kTopMax / NT; ++i) {
                     if (key[i] != 0 && place[i] < c.n_top && norm[2] != 0.f) {
                         c.top_ids[(int64_t)s.token * c.n_top + place[i]] = (int32_t)key_id(key[i]);
                         c.top_logprob[(int64_t)s.token * c.n_top + place[i]] = (key_logit(key[i]) - norm[0]) - norm[1];
@@ -708,7 +718,7 @@ __global__ void __launch_bounds__(kThreads, kPerSm<TOP>) k_logprobs(LogprobCall 
     }
     // tokens that are not in the row list
     if (rows) {
-        for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < c.T; i += (int64_t)gridDim.x * kThreads) {
+        for (int64_t i = (int64_t)blockIdx.x * NT + threadIdx.x; i < c.T; i += (int64_t)gridDim.x * NT) {
             const bool on = c.mask[i] != 0;
             bool listed = on;
             if (listed && c.row_of_token)
@@ -823,9 +833,10 @@ __global__ void __launch_bounds__(kThreads, 4) k_logprobs_bwd(LogprobGradCall c,
             chunk -= chunks;
             ++k;
         }
-        const TIn *z = static_cast<const TIn *>(c.logits) + (g.row.ok ? (int64_t)g.row.r * c.ld : 0);
-        TOut *out = static_cast<TOut *>(c.grad) + (g.row.ok ? (int64_t)g.row.r * c.ld : 0);
-        const int len = g.row.ok ? V : 0;
+        const bool listed = g.row.state == kRowFine;
+        const TIn *z = static_cast<const TIn *>(c.logits) + (listed ? (int64_t)g.row.r * c.ld : 0);
+        TOut *out = static_cast<TOut *>(c.grad) + (listed ? (int64_t)g.row.r * c.ld : 0);
+        const int len = listed ? V : 0;
         const int head = min((int)((16 - (reinterpret_cast<uintptr_t>(z) & 15)) & 15) / (int)sizeof(TIn), len);
         const int nvec = (len - head) / N;
         const bool aligned = ((reinterpret_cast<uintptr_t>(out + head)) & (kOutAlign - 1)) == 0;
@@ -880,14 +891,40 @@ __global__ void __launch_bounds__(kThreads, 4) k_logprobs_bwd(LogprobGradCall c,
             }
         }
     }
+    // masked tokens' rows in chunks, 32 of them looked up at a time (with a token -> row map, which may send a masked
+    // token to a supervised one's row, they are zeroed before this kernel)
+    if (c.mask && !c.row_of_token && (c.flags & TURNOPD_ZERO_MASKED_GRAD)) {
+        constexpr int M = 16 / sizeof(TOut), kPart = 4 * kThreads * M;  // columns
+        const int parts = (V + kPart - 1) / kPart;
+        const int64_t items = c.T * parts;
+        for (int64_t j0 = blockIdx.x; j0 < items; j0 += 32ll * gridDim.x) {
+            const int64_t mine = j0 + (int64_t)(threadIdx.x & 31) * gridDim.x;
+            unsigned off = __ballot_sync(~0u, mine < items && !c.mask[mine / parts]);
+            while (off) {
+                const int64_t item = j0 + (int64_t)(__ffs(off) - 1) * gridDim.x;
+                off &= off - 1;
+                const int64_t row = item / parts;
+                const int from = (int)(item - row * parts) * kPart, to = min(V, from + kPart);
+                TOut *out = static_cast<TOut *>(c.grad) + row * c.ld + from;
+                const int len = to - from;
+                const int head = min((int)((16 - (reinterpret_cast<uintptr_t>(out) & 15)) & 15) / (int)sizeof(TOut), len);
+                const int nvec = (len - head) / M, ends = len - nvec * M;
+                if ((int)threadIdx.x < ends)
+                    out[(int)threadIdx.x < head ? threadIdx.x : nvec * M + threadIdx.x] = from_float<TOut>(0.f);
+                for (int q = threadIdx.x; q < nvec; q += kThreads)
+                    __stcs(reinterpret_cast<uint4 *>(out + head) + q, make_uint4(0u, 0u, 0u, 0u));
+            }
+        }
+    }
 }
 
 template <typename Call> struct Lists {
     int4 *rows = nullptr;
     int32_t *nvalid = nullptr;
-    cudaError_t make(const Call &c, cudaStream_t stream)
+    // `direct`: a CTA to every token, which looks at the mask itself
+    cudaError_t make(const Call &c, bool direct, cudaStream_t stream)
     {
-        if (!c.mask)
+        if (!c.mask || direct)
             return cudaSuccess;
         const int64_t nblk = (c.T + kCompactBlock - 1) / kCompactBlock;
         char *p = static_cast<char *>(c.workspace);
@@ -909,16 +946,23 @@ template <typename Call> struct Lists {
     }
 };
 
-// Few rows: each is shared by a cluster of CTAs, so that the device's SMs all have some of it.
-template <typename TIn>
-cudaError_t launch_fwd(const LogprobCall &c, const int4 *rows, const int32_t *nvalid, cudaStream_t stream)
+// Few rows: each is shared by a cluster of CTAs, so that the device's SMs all have some of it.  The slices are two
+// chunks long at least: below that the exchange costs more than it saves (152 rows x 8,192: one CTA 4.2 us, two 5.0).
+int cluster_ctas(const LogprobCall &c)
 {
     const int sms = device_sm_count();
-    const int64_t vecs = c.vocab / Logits<TIn>::N;
+    const int64_t vecs = c.vocab / (c.in_dtype == TURNOPD_BF16 ? 8 : 4);
     int ctas = 1;
-    while (ctas < kMaxCtas && c.T * ctas * 2 <= 2 * sms && vecs >= ctas * 2 * kThreads)
+    while (ctas < kMaxCtas && c.T * ctas * 2 <= 2 * sms && vecs >= ctas * 2 * kU * 256)
         ctas *= 2;
-    const int64_t want = c.T * ctas, most = (int64_t)sms * (c.n_top > 0 ? kPerSm<true> : kPerSm<false>) / ctas * ctas;
+    return ctas;
+}
+
+template <typename TIn, int NT>
+cudaError_t launch_fwd(const LogprobCall &c, int ctas, const int4 *rows, const int32_t *nvalid, cudaStream_t stream)
+{
+    const int64_t want = c.T * ctas;
+    const int64_t most = (int64_t)device_sm_count() * per_sm(c.n_top > 0, NT) / ctas * ctas;
     cudaLaunchConfig_t cfg = {};
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -927,17 +971,27 @@ cudaError_t launch_fwd(const LogprobCall &c, const int4 *rows, const int32_t *nv
     cfg.attrs = attr;
     cfg.numAttrs = ctas > 1 ? 1 : 0;
     cfg.gridDim = dim3((unsigned)std::min(want, most));
-    cfg.blockDim = dim3(kThreads);
+    cfg.blockDim = dim3(NT);
     cfg.stream = stream;
-    return c.n_top > 0 ? cudaLaunchKernelEx(&cfg, k_logprobs<TIn, true>, c, rows, nvalid)
-                       : cudaLaunchKernelEx(&cfg, k_logprobs<TIn, false>, c, rows, nvalid);
+    return c.n_top > 0 ? cudaLaunchKernelEx(&cfg, k_logprobs<TIn, true, NT>, c, rows, nvalid)
+                       : cudaLaunchKernelEx(&cfg, k_logprobs<TIn, false, NT>, c, rows, nvalid);
 }
 
-template <typename TIn, typename TOut>
-void launch_grad(const LogprobGradCall &c, const int4 *rows, const int32_t *nvalid, cudaStream_t stream)
+// Rows enough for four CTAs on every SM: CTAs of 128 threads, of which one row's merge hides behind more of the others'
+// reads (5,000 rows x 8,192 bf16 with ten alternatives 46 us, with 256 threads 66; 2,458 x 50,304 67 and 88).
+template <typename TIn>
+cudaError_t launch_fwd(const LogprobCall &c, int ctas, const int4 *rows, const int32_t *nvalid, cudaStream_t stream)
 {
-    const int64_t chunks = c.vocab / Logits<TIn>::N / kGradChunk + 1;
-    const int grid = (int)std::min<int64_t>(c.T * chunks, (int64_t)device_sm_count() * 4);
+    return c.T >= 4 * device_sm_count() ? launch_fwd<TIn, 128>(c, ctas, rows, nvalid, stream)
+                                        : launch_fwd<TIn, 256>(c, ctas, rows, nvalid, stream);
+}
+
+constexpr int kGradPerSm = 4;
+
+template <typename TIn, typename TOut>
+void launch_grad(const LogprobGradCall &c, const int4 *rows, const int32_t *nvalid, int64_t items, cudaStream_t stream)
+{
+    const int grid = (int)std::min<int64_t>(items, (int64_t)device_sm_count() * kGradPerSm);
     if (c.d_entropy)
         k_logprobs_bwd<TIn, TOut, true><<<grid, kThreads, 0, stream>>>(c, rows, nvalid);
     else
@@ -954,31 +1008,33 @@ size_t logprob_workspace_bytes(int64_t T)
 
 cudaError_t launch_token_logprobs(const LogprobCall &c, cudaStream_t stream)
 {
+    const int ctas = cluster_ctas(c);
     Lists<LogprobCall> l;
-    const cudaError_t e = l.make(c, stream);
+    const cudaError_t e = l.make(c, c.T * ctas <= 2 * device_sm_count(), stream);
     if (e != cudaSuccess)
         return e;
-    return c.in_dtype == TURNOPD_BF16 ? launch_fwd<__nv_bfloat16>(c, l.rows, l.nvalid, stream)
-                                      : launch_fwd<float>(c, l.rows, l.nvalid, stream);
+    return c.in_dtype == TURNOPD_BF16 ? launch_fwd<__nv_bfloat16>(c, ctas, l.rows, l.nvalid, stream)
+                                      : launch_fwd<float>(c, ctas, l.rows, l.nvalid, stream);
 }
 
 cudaError_t launch_token_logprobs_bwd(const LogprobGradCall &c, cudaStream_t stream)
 {
+    const bool in16 = c.in_dtype == TURNOPD_BF16, out16 = c.grad_dtype == TURNOPD_BF16;
+    const int64_t items = c.T * (c.vocab / (in16 ? 8 : 4) / kGradChunk + 1);
     Lists<LogprobGradCall> l;
-    const cudaError_t e = l.make(c, stream);
+    const cudaError_t e = l.make(c, items <= (int64_t)device_sm_count() * kGradPerSm, stream);
     if (e != cudaSuccess)
         return e;
-    if (c.mask && (c.flags & TURNOPD_ZERO_MASKED_GRAD))
+    if (c.mask && c.row_of_token && (c.flags & TURNOPD_ZERO_MASKED_GRAD))
         launch_zero_masked_grad(c.mask, c.row_of_token, c.T, c.num_rows, c.ld, c.vocab, c.grad, c.grad_dtype, stream);
-    const bool in16 = c.in_dtype == TURNOPD_BF16, out16 = c.grad_dtype == TURNOPD_BF16;
     if (in16 && out16)
-        launch_grad<__nv_bfloat16, __nv_bfloat16>(c, l.rows, l.nvalid, stream);
+        launch_grad<__nv_bfloat16, __nv_bfloat16>(c, l.rows, l.nvalid, items, stream);
     else if (in16)
-        launch_grad<__nv_bfloat16, float>(c, l.rows, l.nvalid, stream);
+        launch_grad<__nv_bfloat16, float>(c, l.rows, l.nvalid, items, stream);
     else if (out16)
-        launch_grad<float, __nv_bfloat16>(c, l.rows, l.nvalid, stream);
+        launch_grad<float, __nv_bfloat16>(c, l.rows, l.nvalid, items, stream);
     else
-        launch_grad<float, float>(c, l.rows, l.nvalid, stream);
+        launch_grad<float, float>(c, l.rows, l.nvalid, items, stream);
     return cudaGetLastError();
 }
 

@@ -333,6 +333,27 @@ def test_gradient_masks_and_skipped_tokens():
     check_grad(out[8:], zc[8:], V, y[on[8:]], gl[on[8:]], gh[on[8:]])
 
 
+@pytest.mark.parametrize("T", [60, 3000])
+def test_masked_tokens_that_point_at_supervised_rows(T):
+    """A token -> row map with 0 for masked tokens: row 0 keeps its supervised token's gradient."""
+    V = 3000
+    g = torch.Generator(device="cuda").manual_seed(T)
+    mask = (torch.rand(T, generator=g, device="cuda") < 0.5).to(torch.uint8)
+    on = mask.nonzero()[:, 0]
+    z, y_row = make(on.numel(), V, F, seed=T)
+    rows = torch.zeros(T, dtype=torch.int32, device="cuda")
+    rows[on] = torch.arange(on.numel(), device="cuda").int()
+    y = torch.zeros(T, dtype=torch.int32, device="cuda")
+    y[on] = y_row
+    o = forward(z, V, y, rows=rows, mask=mask)
+    gl = torch.randn(T, generator=g, device="cuda")
+    ws = torch.empty(P.turnopd_token_logprobs_workspace_bytes(T), dtype=torch.uint8, device="cuda")
+    out = torch.full_like(z, 3.0)
+    P.turnopd_token_logprobs_bwd(z, V, rows, y, mask, o["stats"], o["lp"], o["H"], gl, None, out, P.TURNOPD_ZERO_MASKED_GRAD,
+                                 ws, o["status"])
+    check_grad(out, z, V, y[on], gl[on], torch.zeros_like(gl[on]))
+
+
 def test_gradient_against_differences():
     """Along random directions, against central differences of the float64 objective."""
     V, n = 777, 8
