@@ -18,7 +18,7 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
 constexpr int kE = 16;  // columns of a row that one thread holds
-constexpr int kMaxBwd = 512 * kE;  // longest rows of the one-pass backward kernel
+constexpr int kMaxRow = 512 * kE;  // longest rows that a block holds
 
 __device__ __forceinline__ float param(const void *p, int32_t dtype, int64_t j)
 {
@@ -72,183 +72,164 @@ __device__ __forceinline__ void load_params8(const void *p, int32_t dtype, int64
         load8(static_cast<const float *>(p) + j, v);
 }
 
-// Sum over the `warps` warps of a row's group, the same value in every thread; red: one entry per warp of the block.
-// Every thread of the block calls it where a row has more than one warp.
-__device__ __forceinline__ float group_sum(float v, float *red, int first, int warps)
+__device__ __forceinline__ void cp16(void *smem, const void *gmem)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(smem)), "l"(gmem)
+                 : "memory");
+}
+
+// Barrier of the n threads of one group (barriers 1 .. 8; 0 is the block's).
+__device__ __forceinline__ void group_barrier(int group, int n)
+{
+    asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "r"(n) : "memory");
+}
+
+// ---------------------------------------------------------------- forward
+
+// 16 bytes of a row: W elements as pairs of floats.
+template <typename T> struct Piece {
+    static constexpr int W = 16 / (int)sizeof(T);
+    static __device__ float2 pair(const uint4 &u, int j)
+    {
+        if constexpr (sizeof(T) == 2)
+            return unpack2(word(u, j));
+        else
+            return make_float2(__uint_as_float(word(u, 2 * j)), __uint_as_float(word(u, 2 * j + 1)));
+    }
+};
+
+template <int W, typename TY> __device__ __forceinline__ void store_piece(TY *p, const float2 (&o)[W / 2])
+{
+    if constexpr (W == 8) {
+        store8(p, reinterpret_cast<const float *>(o));
+    } else if constexpr (sizeof(TY) == 4) {
+        __stcs(reinterpret_cast<float4 *>(p), make_float4(o[0].x, o[0].y, o[1].x, o[1].y));
+    } else {
+        __stcs(reinterpret_cast<uint2 *>(p), make_uint2(pack_bf16x2(o[0].x, o[0].y), pack_bf16x2(o[1].x, o[1].y)));
+    }
+}
+
+// gamma and beta are kept in shared memory as fp32 pairs, in W planes of every W-th column: the pieces of a row that
+// starts off a 16-byte boundary begin at any column, and in this layout neighbouring threads' columns lie next to each
+// other wherever they begin.
+template <int W> __host__ __device__ constexpr int plane_size(int d) { return d / W + 2; }
+
+// Sum over a row's warps, the same value in every one of its N threads; red: an entry per warp of the block.
+template <int N> __device__ __forceinline__ float group_sum(float v, float *red, int group)
 {
     v = warp_sum_f(v);
-    if (warps == 1)
+    if (N == 32)
         return v;
     if ((threadIdx.x & 31) == 0)
         red[threadIdx.x >> 5] = v;
-    __syncthreads();
-    float s = red[first];
-    for (int w = 1; w < warps; ++w)
-        s += red[first + w];
+    group_barrier(group, N);
+    float s = red[group * (N / 32)];
+#pragma unroll
+    for (int w = 1; w < N / 32; ++w)
+        s += red[group * (N / 32) + w];
     return s;
 }
 
-// The columns of one thread: P pieces, a piece of each of the row's n threads in turn.  A piece is 16 bytes of a row on
-// 16-byte boundaries with d a multiple of 8, kept as they are, or one column of any row.
-template <typename T, bool VEC> struct RowPiece {
-    static constexpr int W = VEC ? 16 / sizeof(T) : 1;
-    uint4 raw;
-    __device__ void load(const T *p) { raw = __ldcs(reinterpret_cast<const uint4 *>(p)); }
-    __device__ float at(int e) const
-    {
-        if constexpr (sizeof(T) == 4)
-            return __uint_as_float(word(raw, e));
-        else
-            return e & 1 ? bf16hi(word(raw, e >> 1)) : bf16lo(word(raw, e >> 1));
-    }
-};
-template <typename T> struct RowPiece<T, false> {
-    static constexpr int W = 1;
-    float raw;
-    __device__ void load(const T *p) { raw = to_float(*p); }
-    __device__ float at(int) const { return raw; }
-};
-
-// Columns j + k step + 0..W-1 of gamma or beta, k < B, those below d; asked for together.
-template <int W, int B>
-__device__ __forceinline__ void load_params(const void *p, int32_t dtype, int j, int step, int d, float (&v)[B][W])
+// N threads take a row, P of its whole 16-byte pieces to a thread, kept as they were read: one read of x, all of it
+// asked for at once, and with N = 32 no barrier.  The elements before and after the whole pieces go to the row's first
+// lanes, one to each.  A group takes `reps` rows in turn.
+template <typename TX, typename TY, int N, int P>
+__global__ void __launch_bounds__(256, P == 16 ? 2 : P == 8 ? 3 : 4) k_norm_fwd(NormCall c, int reps)
 {
-    if (dtype == TURNOPD_BF16) {
-        const __nv_bfloat16 *q = static_cast<const __nv_bfloat16 *>(p);
-#pragma unroll
-        for (int k = 0; k < B; ++k) {
-            const int at = j + k * step;
-            if (at >= d)
-                break;
-            if constexpr (W == 1) {
-                v[k][0] = __bfloat162float(__ldg(q + at));
-            } else {
-#pragma unroll
-                for (int e = 0; e < W; e += 4) {
-                    const uint2 u = __ldg(reinterpret_cast<const uint2 *>(q + at + e));
-                    v[k][e] = bf16lo(u.x), v[k][e + 1] = bf16hi(u.x), v[k][e + 2] = bf16lo(u.y), v[k][e + 3] = bf16hi(u.y);
-                }
-            }
-        }
-    } else {
-        const float *q = static_cast<const float *>(p);
-#pragma unroll
-        for (int k = 0; k < B; ++k) {
-            const int at = j + k * step;
-            if (at >= d)
-                break;
-            if constexpr (W == 1) {
-                v[k][0] = __ldg(q + at);
-            } else {
-#pragma unroll
-                for (int e = 0; e < W; e += 4) {
-                    const float4 u = __ldg(reinterpret_cast<const float4 *>(q + at + e));
-                    v[k][e] = u.x, v[k][e + 1] = u.y, v[k][e + 2] = u.z, v[k][e + 3] = u.w;
-                }
-            }
-        }
-    }
-}
-
-// One row per group of n threads (a multiple of 32), one read of x, all of it asked for at once.
-template <typename TX, typename TY, bool VEC, int P, int THREADS>
-__global__ void __launch_bounds__(THREADS) k_norm_fwd(NormCall c, int n)
-{
-    using X = RowPiece<TX, VEC>;
-    constexpr int W = X::W;
-    __shared__ float red[2][THREADS / 32];
-    const int t = threadIdx.x % n, group = threadIdx.x / n, warps = n / 32, d = (int)c.d;
-    const int64_t i = (int64_t)blockIdx.x * (blockDim.x / n) + group;
+    using X = Piece<TX>;
+    constexpr int W = X::W, kPer = 256 / N;
+    extern __shared__ __align__(16) float2 planes[];
+    __shared__ float red[4][8];
+    const int t = threadIdx.x % N, group = threadIdx.x / N, d = (int)c.d, S = plane_size<W>(d);
     const bool layer = c.kind == TURNOPD_LAYER_NORM;
-    const bool on = i < c.T && (!c.mask || c.mask[i]);
-    const TX *x = static_cast<const TX *>(c.x) + i * c.ldx;
     const float inv_d = 1.f / (float)d;
-    X v[P];
-    if (on) {
-#pragma unroll
-        for (int k = 0; k < P; ++k)
-            if ((k * n + t) * W < d)
-                v[k].load(x + (k * n + t) * W);
-    }
-    float mu = 0.f, q = 0.f;
-    if (layer) {
-        float s = 0.f;
+    for (int j = threadIdx.x; j < d; j += 256)
+        planes[(j & (W - 1)) * S + j / W] =
+            make_float2(param(c.gamma, c.param_dtype, j), c.beta ? param(c.beta, c.param_dtype, j) : 0.f);
+    __syncthreads();
+    int sums = 0;  // taken so far: the next one's place in `red`, which is free again two sums later
+    for (int rep = 0; rep < reps; ++rep) {
+        const int64_t i = ((int64_t)blockIdx.x * reps + rep) * kPer + group;
+        if (i >= c.T)
+            break;
+        const bool on = !c.mask || c.mask[i];
+        const TX *x = static_cast<const TX *>(c.x) + i * c.ldx;
+        TY *y = static_cast<TY *>(c.y) + i * c.ldy;
+        const int head = min((int)((16 - (reinterpret_cast<uintptr_t>(x) & 15)) & 15) / (int)sizeof(TX), d);
+        const int whole = (d - head) / W, ends = d - whole * W;
+        const int end = t < head ? t : whole * W + t;  // the column of this lane's single element
+        float mu = 0.f, r = 0.f, z = 0.f;
+        uint4 v[P];
         if (on) {
+            const uint4 *p = reinterpret_cast<const uint4 *>(x + head) + t;
 #pragma unroll
             for (int k = 0; k < P; ++k)
-                if ((k * n + t) * W < d)
+                v[k] = k * N + t < whole ? __ldcs(p + k * N) : make_uint4(0u, 0u, 0u, 0u);
+            if (t < ends)
+                z = to_float(x[end]);
+            if (layer) {
+                float2 s = make_float2(z, 0.f);
 #pragma unroll
-                    for (int e = 0; e < W; ++e)
-                        s += v[k].at(e);
-        }
-        mu = group_sum(s, red[0], group * warps, warps) * inv_d;
-    }
-    if (on) {
+                for (int k = 0; k < P; ++k)
 #pragma unroll
-        for (int k = 0; k < P; ++k)
-            if ((k * n + t) * W < d)
-#pragma unroll
-                for (int e = 0; e < W; ++e)
-                    q = fmaf(v[k].at(e) - mu, v[k].at(e) - mu, q);
-    }
-    q = group_sum(q, red[1], group * warps, warps);
-    if (i >= c.T)
-        return;
-    float r = 0.f;
-    if (on) {
-        r = 1.f / sqrtf(q * inv_d + c.eps);
-        if (!(isfinite(mu) && isfinite(r) && r > 0.f)) {
-            r = 0.f;
-            if (t == 0)
-                set_status(c.status, TURNOPD_ERR_NONFINITE);
-        }
-    }
-    if (r == 0.f)
-        mu = 0.f;
-    TY *y = static_cast<TY *>(c.y) + i * c.ldy;
-    constexpr int B = VEC ? (W == 8 ? 2 : 4) : P < 8 ? P : 8;  // pieces whose parameters are in flight together
-    static_assert(P % B == 0, "whole batches of pieces");
-#pragma unroll
-    for (int k0 = 0; k0 < P; k0 += B) {
-        const int j0 = (k0 * n + t) * W;
-        if (j0 >= d)
-            break;
-        float g[B][W], o[B][W];
-#pragma unroll
-        for (int k = 0; k < B; ++k)
-#pragma unroll
-            for (int e = 0; e < W; ++e)
-                o[k][e] = 0.f;
-        if (r != 0.f) {
-            load_params<W, B>(c.gamma, c.param_dtype, j0, n * W, d, g);
-            if (c.beta)
-                load_params<W, B>(c.beta, c.param_dtype, j0, n * W, d, o);
-        }
-#pragma unroll
-        for (int k = 0; k < B; ++k) {
-            const int j = j0 + k * n * W;
-            if (j >= d)
-                break;
-            if (r != 0.f) {
-#pragma unroll
-                for (int e = 0; e < W; ++e)
-                    o[k][e] = fmaf((v[k0 + k].at(e) - mu) * r, g[k][e], o[k][e]);
+                    for (int j = 0; j < W / 2; ++j)
+                        s = fadd2(s, X::pair(v[k], j));
+                mu = group_sum<N>(s.x + s.y, red[sums++ & 3], group) * inv_d;
             }
-            if constexpr (!VEC)
-                y[j] = from_float<TY>(o[k][0]);
-            else if constexpr (W == 8)
-                store8(y + j, o[k]);
-            else if constexpr (sizeof(TY) == 4)
-                __stcs(reinterpret_cast<float4 *>(y + j), make_float4(o[k][0], o[k][1], o[k][2], o[k][3]));
-            else
-                __stcs(reinterpret_cast<uint2 *>(y + j), make_uint2(pack_bf16x2(o[k][0], o[k][1]), pack_bf16x2(o[k][2], o[k][3])));
+            float2 q = make_float2(t < ends ? (z - mu) * (z - mu) : 0.f, 0.f);
+#pragma unroll
+            for (int k = 0; k < P; ++k)
+                if (k * N + t < whole)
+#pragma unroll
+                    for (int j = 0; j < W / 2; ++j) {
+                        const float2 u = fadd2(X::pair(v[k], j), splat(-mu));
+                        q = ffma2(u, u, q);
+                    }
+            r = 1.f / sqrtf(group_sum<N>(q.x + q.y, red[sums++ & 3], group) * inv_d + c.eps);
+            if (!(isfinite(mu) && isfinite(r) && r > 0.f)) {
+                mu = r = 0.f;
+                if (t == 0)
+                    set_status(c.status, TURNOPD_ERR_NONFINITE);
+            }
         }
-    }
-    if (t == 0) {
-        if (c.mean)
-            c.mean[i] = mu;
-        if (c.rstd)
-            c.rstd[i] = r;
+        constexpr int kOut = (int)sizeof(TY) * W < 16 ? (int)sizeof(TY) * W : 16;  // a piece's store is aligned to this
+        const bool vector_out = (reinterpret_cast<uintptr_t>(y + head) & (kOut - 1)) == 0;
+        const float2 *at[W];  // gamma and beta of the h-th columns of this thread's pieces
+#pragma unroll
+        for (int h = 0; h < W; ++h)
+            at[h] = planes + ((head + h) & (W - 1)) * S + (head + h) / W + t;
+#pragma unroll
+        for (int k = 0; k < P; ++k) {
+            if (k * N + t >= whole)
+                break;
+            float2 o[W / 2];
+#pragma unroll
+            for (int j = 0; j < W / 2; ++j) {
+                const float2 a = at[2 * j][k * N], b = at[2 * j + 1][k * N];
+                const float2 xh = fmul2(fadd2(X::pair(v[k], j), splat(-mu)), splat(r));
+                o[j] = ffma2(xh, make_float2(a.x, b.x), make_float2(a.y, b.y));
+                if (r == 0.f)
+                    o[j] = make_float2(0.f, 0.f);
+            }
+            TY *to = y + head + (k * N + t) * W;
+            if (vector_out) {
+                store_piece<W>(to, o);
+            } else {
+#pragma unroll
+                for (int h = 0; h < W; ++h)
+                    to[h] = from_float<TY>(h & 1 ? o[h / 2].y : o[h / 2].x);
+            }
+        }
+        if (t < ends) {
+            const float2 a = planes[(end & (W - 1)) * S + end / W];
+            y[end] = from_float<TY>(r != 0.f ? fmaf((z - mu) * r, a.x, a.y) : 0.f);
+        }
+        if (t == 0) {
+            if (c.mean)
+                c.mean[i] = mu;
+            if (c.rstd)
+                c.rstd[i] = r;
+        }
     }
 }
 
@@ -306,20 +287,8 @@ __device__ __forceinline__ bool takes_part(const NormGradCall &c, int64_t i)
     return (!c.mask || c.mask[i]) && c.rstd[i] > 0.f;
 }
 
-__device__ __forceinline__ void cp16(void *smem, const void *gmem)
-{
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(smem)), "l"(gmem)
-                 : "memory");
-}
-
 constexpr int kBwdSingles = 8;  // columns of a thread where they are read one by one
 constexpr int kStages = 3;  // rows in flight per group: the one at hand and two ahead
-
-// Barrier of the n threads of one group (1 .. 8; 0 is the block's).
-__device__ __forceinline__ void group_barrier(int group, int n)
-{
-    asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "r"(n) : "memory");
-}
 
 __device__ __forceinline__ float2 sum2(float2 v)
 {
@@ -579,7 +548,7 @@ __global__ void __launch_bounds__(1024) k_norm_bwd_sum(NormGradCall c, int n)
     }
 }
 
-// Rows longer than kMaxBwd.
+// Rows longer than kMaxRow.
 template <typename TX, typename TDY, typename TDX>
 __global__ void __launch_bounds__(kThreads) k_norm_dx(NormGradCall c)
 {
@@ -654,7 +623,7 @@ int rows_per_cta(int64_t d, int columns = kE) { return std::max(1, kThreads / ro
 
 int64_t partial_rows(int64_t T, int64_t d)
 {
-    if (d > kMaxBwd)
+    if (d > kMaxRow)
         return std::min<int64_t>(std::max<int64_t>(T, 1), kLongParts);
     const int64_t per = rows_per_cta(d);
     return std::min<int64_t>((T + per - 1) / per, kMaxGrid) * per;
@@ -665,31 +634,48 @@ bool on16(const void *p, int64_t ld, int32_t dtype)
     return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && ld * (dtype == TURNOPD_BF16 ? 2 : 4) % 16 == 0;
 }
 
-// Many rows: few threads to a row, each with up to 16 pieces (32 single columns), so that many rows are in flight and
-// most need no barrier.  Few rows: many threads to each, which answer sooner.
-template <typename X, typename Y, bool VEC, int P, int THREADS> void launch_fwd_pieces(const NormCall &c, cudaStream_t stream)
+template <typename X, typename Y, int N, int P> cudaError_t launch_fwd_rows(const NormCall &c, cudaStream_t stream)
 {
-    constexpr int W = RowPiece<X, VEC>::W;
-    const int n = (int)((c.d + 32 * P * W - 1) / (32 * P * W)) * 32, per = std::max(1, 256 / n);
-    k_norm_fwd<X, Y, VEC, P, THREADS><<<(unsigned)((c.T + per - 1) / per), n * per, 0, stream>>>(c, n);
+    constexpr int W = Piece<X>::W, kPer = 256 / N;
+    const int64_t ctas = (c.T + kPer - 1) / kPer;
+    // every CTA lays gamma and beta out first: for several rows where there are many, but in eight rounds of CTAs or
+    // so, so that those with more masked rows do not leave the device idle at the end
+    const int reps = (int)std::min<int64_t>(8, std::max<int64_t>(1, ctas / (16 * device_sm_count())));
+    const size_t smem = sizeof(float2) * W * plane_size<W>((int)c.d);
+    auto kernel = k_norm_fwd<X, Y, N, P>;
+    if (smem > 40 * 1024) {
+        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        if (e != cudaSuccess)
+            return e;
+    }
+    kernel<<<(unsigned)((ctas + reps - 1) / reps), 256, smem, stream>>>(c, reps);
+    return cudaGetLastError();
 }
 
-template <typename X, typename Y, bool VEC> void launch_fwd(const NormCall &c, cudaStream_t stream)
+// Many rows: as few threads to a row as hold it, so that many rows are in flight and most need no barrier.  Few rows:
+// many threads to each, which answer sooner.
+template <typename X, typename Y> cudaError_t launch_fwd(const NormCall &c, cudaStream_t stream)
 {
-    constexpr int kMost = VEC ? 16 : 32, W = RowPiece<X, VEC>::W;
-    const int64_t pieces = (c.d + W - 1) / W;
-    if (pieces > 512 * kMost) {
+    const int64_t pieces = c.d / Piece<X>::W;
+    const bool few = c.T * ((pieces + 511) / 512) < 8 * device_sm_count();
+    if (c.d > kMaxRow) {
         const int grid = (int)std::min<int64_t>(c.T, (int64_t)device_sm_count() * 8);
         k_norm_fwd_long<X, Y><<<grid, kThreads, 0, stream>>>(c);
-    } else if (c.T < 2 * device_sm_count() && pieces <= 1024 * 4) {
-        launch_fwd_pieces<X, Y, VEC, 4, 1024>(c, stream);
-    } else if (pieces <= 32 * 4) {
-        launch_fwd_pieces<X, Y, VEC, 4, 256>(c, stream);
-    } else if (pieces <= 32 * kMost / 2) {
-        launch_fwd_pieces<X, Y, VEC, kMost / 2, 256>(c, stream);
-    } else {
-        launch_fwd_pieces<X, Y, VEC, kMost, 512>(c, stream);
+        return cudaGetLastError();
     }
+    if (pieces <= 32 * 4)
+        return launch_fwd_rows<X, Y, 32, 4>(c, stream);
+    if (few && pieces <= 128 * 4)
+        return launch_fwd_rows<X, Y, 128, 4>(c, stream);
+    if (few && pieces <= 256 * 4)
+        return launch_fwd_rows<X, Y, 256, 4>(c, stream);
+    if (pieces <= 32 * 8)
+        return launch_fwd_rows<X, Y, 32, 8>(c, stream);
+    if (pieces <= 32 * 16)
+        return launch_fwd_rows<X, Y, 32, 16>(c, stream);
+    if (pieces <= 64 * 16)
+        return launch_fwd_rows<X, Y, 64, 16>(c, stream);
+    return launch_fwd_rows<X, Y, 128, 16>(c, stream);
 }
 
 template <typename X, typename DY, typename DX>
@@ -704,7 +690,7 @@ cudaError_t launch_bwd(const NormGradCall &c, bool vec, const int4 *rows, const 
     const size_t smem = vec ? (sizeof(X) + sizeof(DY)) * n * per * kE * kStages : 0;
     auto kernel = wide ? (vec ? k_norm_bwd<X, DY, DX, true, true> : k_norm_bwd<X, DY, DX, false, true>)
                        : (vec ? k_norm_bwd<X, DY, DX, true, false> : k_norm_bwd<X, DY, DX, false, false>);
-    if (smem > 48 * 1024) {
+    if (smem > 40 * 1024) {  // with the kernel's static shared memory it may pass the default limit of 48 KB
         const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
         if (e != cudaSuccess)
             return e;
@@ -724,15 +710,9 @@ size_t norm_bwd_workspace_bytes(int64_t T, int64_t d)
 
 cudaError_t launch_norm_fwd(const NormCall &c, cudaStream_t stream)
 {
-    const bool vec = c.d % 8 == 0 && on16(c.x, c.ldx, c.x_dtype) && on16(c.y, c.ldy, c.y_dtype) &&
-                     on16(c.gamma, 8, c.param_dtype) && on16(c.beta, 8, c.param_dtype);
-    with_types(c.x_dtype, c.y_dtype, [&](auto x, auto y) {
-        if (vec)
-            launch_fwd<decltype(x), decltype(y), true>(c, stream);
-        else
-            launch_fwd<decltype(x), decltype(y), false>(c, stream);
-    });
-    return cudaGetLastError();
+    cudaError_t e = cudaSuccess;
+    with_types(c.x_dtype, c.y_dtype, [&](auto x, auto y) { e = launch_fwd<decltype(x), decltype(y)>(c, stream); });
+    return e;
 }
 
 cudaError_t launch_norm_bwd(const NormGradCall &c, cudaStream_t stream)
@@ -740,7 +720,7 @@ cudaError_t launch_norm_bwd(const NormGradCall &c, cudaStream_t stream)
     cudaError_t e = cudaSuccess;
     int parts = 0;
     const bool sums = c.dgamma || c.dbeta;
-    if (c.d > kMaxBwd) {
+    if (c.d > kMaxRow) {
         with_types(c.x_dtype, c.dy_dtype, [&](auto x, auto dy) {
             using X = decltype(x);
             using DY = decltype(dy);

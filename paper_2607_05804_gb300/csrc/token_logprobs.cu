@@ -20,7 +20,6 @@ namespace turnopd {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kWarps = kThreads / 32;
 
 // Logits at or below this are masked values: they have probability 0, and a row with nothing else has no distribution.
 // It is where the running maximum starts.  Lower logits (-inf, the type's lowest value) are raised to kClamp for the
@@ -43,7 +42,7 @@ template <typename Call> __device__ __forceinline__ Row get_row(const Call &c, c
         return Row{v.x, v.y, v.z, kRowFine};
     }
     if (c.mask && !c.mask[k])
-        return Row{(int32_t)k, 0, -1, kRowMasked};
+        return Row{(int32_t)k, (int32_t)k, -1, kRowMasked};
     Row o{(int32_t)k, c.row_of_token ? c.row_of_token[k] : (int32_t)k, c.token_ids ? c.token_ids[k] : -1, kRowFine};
     if (!(o.r >= 0 && o.r < c.num_rows && (!c.token_ids || (o.y >= 0 && o.y < c.vocab)))) {
         o.state = kRowBad;
@@ -833,7 +832,10 @@ __global__ void __launch_bounds__(kThreads, 4) k_logprobs_bwd(LogprobGradCall c,
             chunk -= chunks;
             ++k;
         }
-        const bool listed = g.row.state == kRowFine;
+        // without a list a masked token's row may be zeroed here (one that a token -> row map names is zeroed before,
+        // since the map may send a masked token to a supervised one's row)
+        const bool zeros = g.row.state == kRowMasked && !c.row_of_token && (c.flags & TURNOPD_ZERO_MASKED_GRAD);
+        const bool listed = g.row.state == kRowFine || zeros;
         const TIn *z = static_cast<const TIn *>(c.logits) + (listed ? (int64_t)g.row.r * c.ld : 0);
         TOut *out = static_cast<TOut *>(c.grad) + (listed ? (int64_t)g.row.r * c.ld : 0);
         const int len = listed ? V : 0;
@@ -849,7 +851,7 @@ __global__ void __launch_bounds__(kThreads, 4) k_logprobs_bwd(LogprobGradCall c,
                 v[u] = ld_once(p + u * kThreads);
         if (k < n)
             next = get_grad_row(c, rows, k);
-        const bool fine = g.m > -INFINITY;
+        const bool fine = !zeros && g.m > -INFINITY;
         const int y = c.d_logprob ? g.row.y : -1;
         // the row's ends
         const int ends = here == 0 ? len - nvec * N : 0;
@@ -888,31 +890,6 @@ __global__ void __launch_bounds__(kThreads, 4) k_logprobs_bwd(LogprobGradCall c,
 #pragma unroll
                 for (int j = 0; j < N; ++j)
                     out[id0 + j] = from_float<TOut>(o[j]);
-            }
-        }
-    }
-    // masked tokens' rows in chunks, 32 of them looked up at a time (with a token -> row map, which may send a masked
-    // token to a supervised one's row, they are zeroed before this kernel)
-    if (c.mask && !c.row_of_token && (c.flags & TURNOPD_ZERO_MASKED_GRAD)) {
-        constexpr int M = 16 / sizeof(TOut), kPart = 4 * kThreads * M;  // columns
-        const int parts = (V + kPart - 1) / kPart;
-        const int64_t items = c.T * parts;
-        for (int64_t j0 = blockIdx.x; j0 < items; j0 += 32ll * gridDim.x) {
-            const int64_t mine = j0 + (int64_t)(threadIdx.x & 31) * gridDim.x;
-            unsigned off = __ballot_sync(~0u, mine < items && !c.mask[mine / parts]);
-            while (off) {
-                const int64_t item = j0 + (int64_t)(__ffs(off) - 1) * gridDim.x;
-                off &= off - 1;
-                const int64_t row = item / parts;
-                const int from = (int)(item - row * parts) * kPart, to = min(V, from + kPart);
-                TOut *out = static_cast<TOut *>(c.grad) + row * c.ld + from;
-                const int len = to - from;
-                const int head = min((int)((16 - (reinterpret_cast<uintptr_t>(out) & 15)) & 15) / (int)sizeof(TOut), len);
-                const int nvec = (len - head) / M, ends = len - nvec * M;
-                if ((int)threadIdx.x < ends)
-                    out[(int)threadIdx.x < head ? threadIdx.x : nvec * M + threadIdx.x] = from_float<TOut>(0.f);
-                for (int q = threadIdx.x; q < nvec; q += kThreads)
-                    __stcs(reinterpret_cast<uint4 *>(out + head) + q, make_uint4(0u, 0u, 0u, 0u));
             }
         }
     }
@@ -1022,10 +999,11 @@ cudaError_t launch_token_logprobs_bwd(const LogprobGradCall &c, cudaStream_t str
     const bool in16 = c.in_dtype == TURNOPD_BF16, out16 = c.grad_dtype == TURNOPD_BF16;
     const int64_t items = c.T * (c.vocab / (in16 ? 8 : 4) / kGradChunk + 1);
     Lists<LogprobGradCall> l;
-    const cudaError_t e = l.make(c, items <= (int64_t)device_sm_count() * kGradPerSm, stream);
+    const bool direct = items <= (int64_t)device_sm_count() * kGradPerSm;
+    const cudaError_t e = l.make(c, direct, stream);
     if (e != cudaSuccess)
         return e;
-    if (c.mask && c.row_of_token && (c.flags & TURNOPD_ZERO_MASKED_GRAD))
+    if (c.mask && (c.row_of_token || !direct) && (c.flags & TURNOPD_ZERO_MASKED_GRAD))
         launch_zero_masked_grad(c.mask, c.row_of_token, c.T, c.num_rows, c.ld, c.vocab, c.grad, c.grad_dtype, stream);
     if (in16 && out16)
         launch_grad<__nv_bfloat16, __nv_bfloat16>(c, l.rows, l.nvalid, items, stream);

@@ -166,7 +166,7 @@ def check_backward(dx, dg, db, x, gamma, kind, dy, eps=1e-6):
 @pytest.mark.parametrize("T,d", SHAPES + [(2000, 64), (700, 1001), (1500, 4096)])
 def test_backward(T, d, kind):
     for xdt, dydt, dxdt, pdt, ld, off in ((BF, F, BF, BF, d, 0), (F, F, F, F, d, 0), (BF, BF, BF, F, d + 3, 1),
-                                          (F, BF, F, BF, d + 8, 0), (BF, F, F, F, d + 8, 8)):
+                                          (F, BF, F, BF, d + 8, 0), (BF, F, F, F, d + 8, 8), (BF, BF, BF, BF, d, 0)):
         x, gamma, _, g = make(T, d, xdt, seed=d + T, ld=ld, offset=off)
         gamma = gamma.to(pdt)
         dy = strided(T, d, ld, off, dydt)
