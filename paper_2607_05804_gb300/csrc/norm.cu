@@ -114,11 +114,15 @@ template <int W, typename TY> __device__ __forceinline__ void store_piece(TY *p,
 // other wherever they begin.
 template <int W> __host__ __device__ constexpr int plane_size(int d) { return d / W + 2; }
 
-// Sum over a row's warps, the same value in every one of its N threads; red: an entry per warp of the block.
+// Sum over a row, the same value in every one of its N threads; red: an entry per warp of the block.
 template <int N> __device__ __forceinline__ float group_sum(float v, float *red, int group)
 {
-    v = warp_sum_f(v);
-    if (N == 32)
+    constexpr int kLanes = N < 32 ? N : 32;
+    const unsigned lanes = N < 32 ? ((1u << (N & 31)) - 1u) << (threadIdx.x & 31 & ~(N - 1)) : ~0u;
+#pragma unroll
+    for (int o = kLanes / 2; o > 0; o >>= 1)
+        v += __shfl_xor_sync(lanes, v, o);
+    if (N <= 32)
         return v;
     if ((threadIdx.x & 31) == 0)
         red[threadIdx.x >> 5] = v;
@@ -131,13 +135,14 @@ template <int N> __device__ __forceinline__ float group_sum(float v, float *red,
 }
 
 // N threads take a row, P of its whole 16-byte pieces to a thread, kept as they were read: one read of x, all of it
-// asked for at once, and with N = 32 no barrier.  The elements before and after the whole pieces go to the row's first
-// lanes, one to each.  A group takes `reps` rows in turn.
+// asked for at once, and with N <= 32 no barrier.  The elements before and after the whole pieces go to the row's first
+// threads, one to each.  A group takes `reps` rows in turn.
 template <typename TX, typename TY, int N, int P>
 __global__ void __launch_bounds__(256, P == 16 ? 2 : P == 8 ? 3 : 4) k_norm_fwd(NormCall c, int reps)
 {
     using X = Piece<TX>;
     constexpr int W = X::W, kPer = 256 / N;
+    static_assert(N >= 2 * (W - 1), "a thread to each end");
     extern __shared__ __align__(16) float2 planes[];
     __shared__ float red[4][8];
     const int t = threadIdx.x % N, group = threadIdx.x / N, d = (int)c.d, S = plane_size<W>(d);
@@ -152,15 +157,26 @@ __global__ void __launch_bounds__(256, P == 16 ? 2 : P == 8 ? 3 : 4) k_norm_fwd(
         const int64_t i = ((int64_t)blockIdx.x * reps + rep) * kPer + group;
         if (i >= c.T)
             break;
-        const bool on = !c.mask || c.mask[i];
         const TX *x = static_cast<const TX *>(c.x) + i * c.ldx;
         TY *y = static_cast<TY *>(c.y) + i * c.ldy;
         const int head = min((int)((16 - (reinterpret_cast<uintptr_t>(x) & 15)) & 15) / (int)sizeof(TX), d);
         const int whole = (d - head) / W, ends = d - whole * W;
-        const int end = t < head ? t : whole * W + t;  // the column of this lane's single element
+        const int end = t < head ? t : whole * W + t;  // the column of this thread's single element
+        constexpr int kOut = (int)sizeof(TY) * W < 16 ? (int)sizeof(TY) * W : 16;  // a piece's store is aligned to this
+        const bool vector_out = (reinterpret_cast<uintptr_t>(y + head) & (kOut - 1)) == 0;
+        const auto put = [&](int k, const float2(&o)[W / 2]) {
+            TY *to = y + head + (k * N + t) * W;
+            if (vector_out) {
+                store_piece<W>(to, o);
+            } else {
+#pragma unroll
+                for (int h = 0; h < W; ++h)
+                    to[h] = from_float<TY>(h & 1 ? o[h / 2].y : o[h / 2].x);
+            }
+        };
         float mu = 0.f, r = 0.f, z = 0.f;
         uint4 v[P];
-        if (on) {
+        if (!c.mask || c.mask[i]) {
             const uint4 *p = reinterpret_cast<const uint4 *>(x + head) + t;
 #pragma unroll
             for (int k = 0; k < P; ++k)
@@ -176,6 +192,7 @@ __global__ void __launch_bounds__(256, P == 16 ? 2 : P == 8 ? 3 : 4) k_norm_fwd(
                         s = fadd2(s, X::pair(v[k], j));
                 mu = group_sum<N>(s.x + s.y, red[sums++ & 3], group) * inv_d;
             }
+            // in a block of its own: in one with the loop above the compiler keeps the unpacked pieces, and spills
             float2 q = make_float2(t < ends ? (z - mu) * (z - mu) : 0.f, 0.f);
 #pragma unroll
             for (int k = 0; k < P; ++k)
@@ -192,37 +209,37 @@ __global__ void __launch_bounds__(256, P == 16 ? 2 : P == 8 ? 3 : 4) k_norm_fwd(
                     set_status(c.status, TURNOPD_ERR_NONFINITE);
             }
         }
-        constexpr int kOut = (int)sizeof(TY) * W < 16 ? (int)sizeof(TY) * W : 16;  // a piece's store is aligned to this
-        const bool vector_out = (reinterpret_cast<uintptr_t>(y + head) & (kOut - 1)) == 0;
-        const float2 *at[W];  // gamma and beta of the h-th columns of this thread's pieces
+        if (r != 0.f) {
+            // xh = x r - mu r, off by half a unit of mu r at most, as mu itself is
+            const float m = -mu * r;
+            int at[W];  // gamma and beta of the h-th columns of this thread's pieces
 #pragma unroll
-        for (int h = 0; h < W; ++h)
-            at[h] = planes + ((head + h) & (W - 1)) * S + (head + h) / W + t;
+            for (int h = 0; h < W; ++h)
+                at[h] = ((head + h) & (W - 1)) * S + (head + h) / W + t;
 #pragma unroll
-        for (int k = 0; k < P; ++k) {
-            if (k * N + t >= whole)
-                break;
-            float2 o[W / 2];
+            for (int k = 0; k < P; ++k) {
+                if (k * N + t >= whole)
+                    break;
+                float2 o[W / 2];
 #pragma unroll
-            for (int j = 0; j < W / 2; ++j) {
-                const float2 a = at[2 * j][k * N], b = at[2 * j + 1][k * N];
-                const float2 xh = fmul2(fadd2(X::pair(v[k], j), splat(-mu)), splat(r));
-                o[j] = ffma2(xh, make_float2(a.x, b.x), make_float2(a.y, b.y));
-                if (r == 0.f)
-                    o[j] = make_float2(0.f, 0.f);
+                for (int j = 0; j < W / 2; ++j) {
+                    const float2 a = planes[at[2 * j] + k * N], b = planes[at[2 * j + 1] + k * N];
+                    const float2 xh = ffma2(X::pair(v[k], j), splat(r), splat(m));
+                    o[j].x = fmaf(xh.x, a.x, a.y);
+                    o[j].y = fmaf(xh.y, b.x, b.y);
+                }
+                put(k, o);
             }
-            TY *to = y + head + (k * N + t) * W;
-            if (vector_out) {
-                store_piece<W>(to, o);
-            } else {
-#pragma unroll
-                for (int h = 0; h < W; ++h)
-                    to[h] = from_float<TY>(h & 1 ? o[h / 2].y : o[h / 2].x);
+            if (t < ends) {
+                const float2 a = planes[(end & (W - 1)) * S + end / W];
+                y[end] = from_float<TY>(fmaf((z - mu) * r, a.x, a.y));
             }
-        }
-        if (t < ends) {
-            const float2 a = planes[(end & (W - 1)) * S + end / W];
-            y[end] = from_float<TY>(r != 0.f ? fmaf((z - mu) * r, a.x, a.y) : 0.f);
+        } else {
+            const float2 zero[W / 2] = {};
+            for (int k = 0; k * N + t < whole; ++k)
+                put(k, zero);
+            if (t < ends)
+                y[end] = from_float<TY>(0.f);
         }
         if (t == 0) {
             if (c.mean)
@@ -638,9 +655,10 @@ template <typename X, typename Y, int N, int P> cudaError_t launch_fwd_rows(cons
 {
     constexpr int W = Piece<X>::W, kPer = 256 / N;
     const int64_t ctas = (c.T + kPer - 1) / kPer;
-    // every CTA lays gamma and beta out first: for several rows where there are many, but in eight rounds of CTAs or
-    // so, so that those with more masked rows do not leave the device idle at the end
-    const int reps = (int)std::min<int64_t>(8, std::max<int64_t>(1, ctas / (16 * device_sm_count())));
+    // every CTA lays gamma and beta out first: for several rows where there are many, but in several rounds of CTAs, so
+    // that those with more masked rows do not leave the device idle at the end
+    const int64_t round = device_sm_count() * (P == 16 ? 2 : P == 8 ? 3 : 4);
+    const int reps = (int)std::min<int64_t>(16, std::max<int64_t>(1, ctas / (4 * round)));
     const size_t smem = sizeof(float2) * W * plane_size<W>((int)c.d);
     auto kernel = k_norm_fwd<X, Y, N, P>;
     if (smem > 40 * 1024) {
@@ -663,6 +681,8 @@ template <typename X, typename Y> cudaError_t launch_fwd(const NormCall &c, cuda
         k_norm_fwd_long<X, Y><<<grid, kThreads, 0, stream>>>(c);
         return cudaGetLastError();
     }
+    if (pieces <= 16 * 4)
+        return launch_fwd_rows<X, Y, 16, 4>(c, stream);
     if (pieces <= 32 * 4)
         return launch_fwd_rows<X, Y, 32, 4>(c, stream);
     if (few && pieces <= 128 * 4)
