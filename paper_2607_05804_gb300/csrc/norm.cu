@@ -64,14 +64,6 @@ __device__ __forceinline__ void store8(float *p, const float *v)
     __stcs(reinterpret_cast<float4 *>(p), make_float4(v[0], v[1], v[2], v[3]));
     __stcs(reinterpret_cast<float4 *>(p) + 1, make_float4(v[4], v[5], v[6], v[7]));
 }
-__device__ __forceinline__ void load_params8(const void *p, int32_t dtype, int64_t j, float *v)
-{
-    if (dtype == TURNOPD_BF16)
-        load8(static_cast<const __nv_bfloat16 *>(p) + j, v);
-    else
-        load8(static_cast<const float *>(p) + j, v);
-}
-
 __device__ __forceinline__ void cp16(void *smem, const void *gmem)
 {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(smem)), "l"(gmem)
@@ -174,26 +166,33 @@ __global__ void __launch_bounds__(256, P == 16 ? 2 : P == 8 ? 3 : 4) k_norm_fwd(
                     to[h] = from_float<TY>(h & 1 ? o[h / 2].y : o[h / 2].x);
             }
         };
+        // The sums are taken for masked rows too (of nothing): no barrier stands under a condition that every thread
+        // reads from the caller's memory for itself.
+        const bool on = !c.mask || c.mask[i];
         float mu = 0.f, r = 0.f, z = 0.f;
         uint4 v[P];
-        if (!c.mask || c.mask[i]) {
+        if (on) {
             const uint4 *p = reinterpret_cast<const uint4 *>(x + head) + t;
 #pragma unroll
             for (int k = 0; k < P; ++k)
                 v[k] = k * N + t < whole ? __ldcs(p + k * N) : make_uint4(0u, 0u, 0u, 0u);
             if (t < ends)
                 z = to_float(x[end]);
-            if (layer) {
-                float2 s = make_float2(z, 0.f);
+        }
+        if (layer) {
+            float2 s = make_float2(z, 0.f);
+            if (on) {
 #pragma unroll
                 for (int k = 0; k < P; ++k)
 #pragma unroll
                     for (int j = 0; j < W / 2; ++j)
                         s = fadd2(s, X::pair(v[k], j));
-                mu = group_sum<N>(s.x + s.y, red[sums++ & 3], group) * inv_d;
             }
-            // in a block of its own: in one with the loop above the compiler keeps the unpacked pieces, and spills
-            float2 q = make_float2(t < ends ? (z - mu) * (z - mu) : 0.f, 0.f);
+            mu = group_sum<N>(s.x + s.y, red[sums++ & 3], group) * inv_d;
+        }
+        // in a block of its own: in one with the loop above the compiler keeps the unpacked pieces, and spills
+        float2 q = make_float2(t < ends ? (z - mu) * (z - mu) : 0.f, 0.f);
+        if (on) {
 #pragma unroll
             for (int k = 0; k < P; ++k)
                 if (k * N + t < whole)
@@ -202,13 +201,18 @@ __global__ void __launch_bounds__(256, P == 16 ? 2 : P == 8 ? 3 : 4) k_norm_fwd(
                         const float2 u = fadd2(X::pair(v[k], j), splat(-mu));
                         q = ffma2(u, u, q);
                     }
-            r = 1.f / sqrtf(group_sum<N>(q.x + q.y, red[sums++ & 3], group) * inv_d + c.eps);
+        }
+        const float squares = group_sum<N>(q.x + q.y, red[sums++ & 3], group) * inv_d;
+        if (on) {
+            r = 1.f / sqrtf(squares + c.eps);
             if (!(isfinite(mu) && isfinite(r) && r > 0.f)) {
-                mu = r = 0.f;
+                r = 0.f;
                 if (t == 0)
                     set_status(c.status, TURNOPD_ERR_NONFINITE);
             }
         }
+        if (r == 0.f)
+            mu = 0.f;
         if (r != 0.f) {
             // xh = x r - mu r, off by half a unit of mu r at most, as mu itself is
             const float m = -mu * r;
@@ -259,7 +263,8 @@ template <typename TX, typename TY> __global__ void __launch_bounds__(kThreads) 
         const TX *x = static_cast<const TX *>(c.x) + i * c.ldx;
         TY *y = static_cast<TY *>(c.y) + i * c.ldy;
         float mu = 0.f, r = 0.f;
-        bool fine = !c.mask || c.mask[i];
+        // one thread looks, and all go by what it saw: the sums below are the block's
+        bool fine = __syncthreads_or(threadIdx.x == 0 && (!c.mask || c.mask[i]));
         if (fine) {
             if (layer) {
                 float s = 0.f;
@@ -317,12 +322,25 @@ __device__ __forceinline__ float2 sum2(float2 v)
 
 // One pass over x and dy: every thread keeps its columns of gamma, dgamma and dbeta in registers from row to row.
 // Group b of all takes rows b, b + groups, ... of the list of supervised tokens (of all tokens, without a list), so that
-// the sums are in a fixed order.  Aligned rows come through a ring in shared memory, in which each thread copies and
-// reads its own columns only: no barrier but the one of the row's two sums.  Columns from d on are zeros throughout.
-template <typename TX, typename TDY, typename TDX, bool VEC, bool WIDE>
-__global__ void __launch_bounds__(VEC ? (WIDE ? 512 : 320) : (WIDE ? 1024 : 512), VEC && !WIDE ? 2 : 1)
+// the sums are in a fixed order.
+//
+// kPieces: the three arrays' rows begin at the same element of a group of eight.  The groups' number is a multiple of eight,
+// so all rows of one group begin there too, and a thread keeps the same columns from row to row wherever the rows begin:
+// pieces of eight from the row's first boundary on, and the first threads one of the elements before and after the whole
+// pieces each.  (With a list of rows, only where every row begins at a boundary.)  The pieces come through a ring in
+// shared memory, in which each thread copies and reads its own only: no barrier but the one of the row's two sums.
+// kWhole is the same without ends, and kSingles reads column by column.  Missing columns are zeros throughout.
+enum BwdForm {
+    kSingles,  // any rows, column by column
+    kPieces,   // rows that begin anywhere, but in all three arrays alike
+    kWhole,    // rows that begin at boundaries, d a multiple of eight: no ends
+};
+
+template <typename TX, typename TDY, typename TDX, BwdForm FORM, bool WIDE>
+__global__ void __launch_bounds__(FORM ? (WIDE ? 512 : 320) : (WIDE ? 1024 : 512), FORM && !WIDE ? 2 : 1)
 k_norm_bwd(NormGradCall c, const int4 *__restrict__ rows, const int32_t *__restrict__ nvalid, int n)
 {
+    constexpr bool VEC = FORM != kSingles, ENDS = FORM == kPieces;
     constexpr int kE = VEC ? turnopd::kE : kBwdSingles;
     extern __shared__ __align__(16) char ring[];
     __shared__ __align__(16) float2 red[2][32];
@@ -334,32 +352,47 @@ k_norm_bwd(NormGradCall c, const int4 *__restrict__ rows, const int32_t *__restr
     const float inv_d = 1.f / (float)d;
     const int xbytes = (int)sizeof(TX) * n * kE, stage = (int)(sizeof(TX) + sizeof(TDY)) * n * kE;
     char *own = ring + group * kStages * stage;
-    const auto column = [&](int k) { return (k * n + t) * W; };  // of piece k
+    const int head = ENDS ? min((int)(-(reinterpret_cast<intptr_t>(static_cast<const TX *>(c.x) + b * c.ldx) / (int)sizeof(TX)) & 7), d) : 0;
+    const int whole = VEC ? (d - head) / 8 : d, ends = ENDS ? d - whole * 8 : 0;
+    const int end = t < head ? t : whole * 8 + t;  // the single column of this thread, where t < ends
+    const auto column = [&](int k) { return head + (k * n + t) * W; };  // of piece k
+    const auto there = [&](int k) { return k * n + t < whole; };
 
     float2 gamma[kE / 2], dg[kE / 2], db[kE / 2];
 #pragma unroll
     for (int k = 0; k < kE / 2; ++k)
         gamma[k] = dg[k] = db[k] = make_float2(0.f, 0.f);
     float *gam = reinterpret_cast<float *>(gamma);
+    const auto load_gamma = [&](const auto *g) {
 #pragma unroll
-    for (int k = 0; k < P; ++k) {
-        const int j = column(k);
-        if (j < d) {
-            if constexpr (VEC)
-                load_params8(c.gamma, c.param_dtype, j, gam + k * W);
-            else
-                gam[k] = param(c.gamma, c.param_dtype, j);
-        }
-    }
+        for (int k = 0; k < P; ++k)
+            if (there(k)) {
+                if (FORM == kWhole && (reinterpret_cast<uintptr_t>(g) & 15) == 0) {
+                    if constexpr (FORM == kWhole)
+                        load8(g + column(k), gam + k * W);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < W; ++e)
+                        gam[k * W + e] = to_float(__ldg(g + column(k) + e));
+                }
+            }
+    };
+    if (c.param_dtype == TURNOPD_BF16)
+        load_gamma(static_cast<const __nv_bfloat16 *>(c.gamma));
+    else
+        load_gamma(static_cast<const float *>(c.gamma));
+    const float gamma_end = ENDS && t < ends ? param(c.gamma, c.param_dtype, end) : 0.f;
+    float dg_end = 0.f, db_end = 0.f;
     if constexpr (VEC) {
 #pragma unroll
         for (int k = 0; k < P; ++k)
-            if (column(k) >= d)
+            if (!there(k))
                 for (int s = 0; s < kStages; ++s) {
+                    const int at = (k * n + t) * 8;
                     for (int h = 0; h < (int)sizeof(TX) / 2; ++h)
-                        reinterpret_cast<uint4 *>(own + s * stage + column(k) * sizeof(TX))[h] = make_uint4(0, 0, 0, 0);
+                        reinterpret_cast<uint4 *>(own + s * stage + at * sizeof(TX))[h] = make_uint4(0, 0, 0, 0);
                     for (int h = 0; h < (int)sizeof(TDY) / 2; ++h)
-                        reinterpret_cast<uint4 *>(own + s * stage + xbytes + column(k) * sizeof(TDY))[h] = make_uint4(0, 0, 0, 0);
+                        reinterpret_cast<uint4 *>(own + s * stage + xbytes + at * sizeof(TDY))[h] = make_uint4(0, 0, 0, 0);
                 }
     }
 
@@ -373,20 +406,20 @@ k_norm_bwd(NormGradCall c, const int4 *__restrict__ rows, const int32_t *__restr
     const auto on = [&](int i) { return i >= 0 && (rows || !c.mask || c.mask[i]); };
     const auto copy = [&](int i, int s) {
         if (on(i)) {
-            const char *x = reinterpret_cast<const char *>(static_cast<const TX *>(c.x) + i * c.ldx);
-            const char *dy = reinterpret_cast<const char *>(static_cast<const TDY *>(c.dy) + i * c.lddy);
+            const TX *x = static_cast<const TX *>(c.x) + i * c.ldx;
+            const TDY *dy = static_cast<const TDY *>(c.dy) + i * c.lddy;
             char *to = own + s * stage;
 #pragma unroll
             for (int k = 0; k < P; ++k) {
-                const int j = column(k);
-                if (j >= d)
+                if (!there(k))
                     continue;
+                const int j = column(k), at = (k * n + t) * 8;
 #pragma unroll
-                for (int h = 0; h < (int)sizeof(TX) / 2; ++h)
-                    cp16(to + j * (int)sizeof(TX) + 16 * h, x + j * (int)sizeof(TX) + 16 * h);
+                for (int h = 0; h < 8; h += 16 / (int)sizeof(TX))
+                    cp16(to + (at + h) * (int)sizeof(TX), x + j + h);
 #pragma unroll
-                for (int h = 0; h < (int)sizeof(TDY) / 2; ++h)
-                    cp16(to + xbytes + j * (int)sizeof(TDY) + 16 * h, dy + j * (int)sizeof(TDY) + 16 * h);
+                for (int h = 0; h < 8; h += 16 / (int)sizeof(TDY))
+                    cp16(to + xbytes + (at + h) * (int)sizeof(TDY), dy + j + h);
             }
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
@@ -396,33 +429,40 @@ k_norm_bwd(NormGradCall c, const int4 *__restrict__ rows, const int32_t *__restr
         copy(i, 0);
         copy(i1, 1);
     }
-    float mu = 0.f, r = 0.f;
-    if (on(i)) {
-        mu = layer ? c.mean[i] : 0.f;
-        r = c.rstd[i];
-    }
+    // a row's numbers and this thread's single column are read a row ahead
+    float mu = 0.f, r = 0.f, xe = 0.f, dye = 0.f;
+    const auto numbers = [&](int i, float &mu, float &r, float &xe, float &dye) {
+        mu = r = xe = dye = 0.f;
+        if (on(i)) {
+            mu = layer ? c.mean[i] : 0.f;
+            r = c.rstd[i];
+            if (ENDS && t < ends) {
+                xe = to_float(static_cast<const TX *>(c.x)[i * c.ldx + end]);
+                dye = to_float(static_cast<const TDY *>(c.dy)[i * c.lddy + end]);
+            }
+        }
+    };
+    numbers(i, mu, r, xe, dye);
     int s = 0;
     for (int m = 0; i >= 0; ++m) {
         const int i3 = row_of(m + 3);
         if constexpr (VEC)
             copy(i2, s >= 1 ? s - 1 : s + 2);
-        float mu1 = 0.f, r1 = 0.f;
-        if (on(i1)) {
-            mu1 = layer ? c.mean[i1] : 0.f;
-            r1 = c.rstd[i1];
-        }
+        float mu1, r1, xe1, dye1;
+        numbers(i1, mu1, r1, xe1, dye1);
         if constexpr (VEC)
             asm volatile("cp.async.wait_group 2;" ::: "memory");
         TDX *dx = static_cast<TDX *>(c.dx) + i * c.lddx;
+        // (as in the forward pass, the sums are taken whatever rstd says)
+        float2 sg = make_float2(0.f, 0.f), sx = sg;
+        float2 x[kE / 2], dy[kE / 2];  // xh and dy; pieces are read from the ring once more for dx instead
         if (r > 0.f) {
-            float2 sg = make_float2(0.f, 0.f), sx = sg;
-            float2 x[kE / 2], dy[kE / 2];  // xh and dy; aligned rows are read from the ring once more for dx instead
 #pragma unroll
             for (int k = 0; k < P; ++k) {
-                float2 *xk = x + k * W / 2, *dyk = dy + k * W / 2;
                 if constexpr (VEC) {
-                    load8(reinterpret_cast<const TX *>(own + s * stage) + column(k), reinterpret_cast<float *>(xk));
-                    load8(reinterpret_cast<const TDY *>(own + s * stage + xbytes) + column(k), reinterpret_cast<float *>(dyk));
+                    float2 *xk = x + k * W / 2, *dyk = dy + k * W / 2;
+                    load8(reinterpret_cast<const TX *>(own + s * stage) + (k * n + t) * 8, reinterpret_cast<float *>(xk));
+                    load8(reinterpret_cast<const TDY *>(own + s * stage + xbytes) + (k * n + t) * 8, reinterpret_cast<float *>(dyk));
                 } else {
                     const int j = column(k);
                     reinterpret_cast<float *>(x)[k] = j < d ? to_float(static_cast<const TX *>(c.x)[i * c.ldx + j]) : 0.f;
@@ -438,19 +478,29 @@ k_norm_bwd(NormGradCall c, const int4 *__restrict__ rows, const int32_t *__restr
                 dg[k] = ffma2(dy[k], x[k], dg[k]);
                 db[k] = fadd2(db[k], dy[k]);
             }
-            if (c.dx) {
-                float2 v = sum2(make_float2(sg.x + sg.y, sx.x + sx.y));
-                if (warps > 1) {
-                    float2 *to = red[m & 1];
-                    const int first = group * warps;
-                    if ((threadIdx.x & 31) == 0)
-                        to[threadIdx.x >> 5] = v;
-                    group_barrier(group, n);
-                    v = to[first];
+            if (ENDS) {
+                xe = t < ends ? (xe - mu) * r : 0.f;
+                const float g = dye * gamma_end;
+                sg.x += g;
+                sx.x = fmaf(g, xe, sx.x);
+                dg_end = fmaf(dye, xe, dg_end);
+                db_end += dye;
+            }
+        }
+        if (c.dx) {
+            float2 v = sum2(make_float2(sg.x + sg.y, sx.x + sx.y));
+            if (warps > 1) {
+                float2 *to = red[m & 1];
+                const int first = group * warps;
+                if ((threadIdx.x & 31) == 0)
+                    to[threadIdx.x >> 5] = v;
+                group_barrier(group, n);
+                v = to[first];
 #pragma unroll 2
-                    for (int w = 1; w < warps; ++w)
-                        v = fadd2(v, to[first + w]);
-                }
+                for (int w = 1; w < warps; ++w)
+                    v = fadd2(v, to[first + w]);
+            }
+            if (r > 0.f) {
                 // dx = r g + xh (-r mean(g xh)) - r mean g
                 const float2 c0 = splat(layer ? -r * (v.x * inv_d) : 0.f), c1 = splat(-r * (v.y * inv_d));
 #pragma unroll
@@ -458,32 +508,35 @@ k_norm_bwd(NormGradCall c, const int4 *__restrict__ rows, const int32_t *__restr
                     const int j = column(k);
                     if constexpr (VEC) {
                         float2 xk[4], dyk[4];
-                        load8(reinterpret_cast<const TX *>(own + s * stage) + j, reinterpret_cast<float *>(xk));
-                        load8(reinterpret_cast<const TDY *>(own + s * stage + xbytes) + j, reinterpret_cast<float *>(dyk));
+                        load8(reinterpret_cast<const TX *>(own + s * stage) + (k * n + t) * 8, reinterpret_cast<float *>(xk));
+                        load8(reinterpret_cast<const TDY *>(own + s * stage + xbytes) + (k * n + t) * 8, reinterpret_cast<float *>(dyk));
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
                             const float2 xh = fmul2(fadd2(xk[e], splat(-mu)), splat(r));
                             xk[e] = ffma2(fmul2(dyk[e], gamma[4 * k + e]), splat(r), ffma2(xh, c1, c0));
                         }
-                        if (j < d)
+                        if (there(k))
                             store8(dx + j, reinterpret_cast<const float *>(xk));
                     } else if (j < d) {
                         const float g = reinterpret_cast<const float *>(dy)[k] * gam[k];
                         dx[j] = from_float<TDX>(fmaf(g, r, fmaf(reinterpret_cast<const float *>(x)[k], c1.x, c0.x)));
                     }
                 }
-            }
-        } else if (c.dx) {
-            const float zero[8] = {};
+                if (ENDS && t < ends)
+                    dx[end] = from_float<TDX>(fmaf(dye * gamma_end, r, fmaf(xe, c1.x, c0.x)));
+            } else {
+                const float zero[8] = {};
 #pragma unroll
-            for (int k = 0; k < P; ++k) {
-                const int j = column(k);
-                if (j < d) {
-                    if constexpr (VEC)
-                        store8(dx + j, zero);
-                    else
-                        dx[j] = from_float<TDX>(0.f);
+                for (int k = 0; k < P; ++k) {
+                    if (there(k)) {
+                        if constexpr (VEC)
+                            store8(dx + column(k), zero);
+                        else
+                            dx[column(k)] = from_float<TDX>(0.f);
+                    }
                 }
+                if (ENDS && t < ends)
+                    dx[end] = from_float<TDX>(0.f);
             }
         }
         i = i1;
@@ -491,26 +544,53 @@ k_norm_bwd(NormGradCall c, const int4 *__restrict__ rows, const int32_t *__restr
         i2 = i3;
         mu = mu1;
         r = r1;
+        xe = xe1;
+        dye = dye1;
         s = s == 2 ? 0 : s + 1;
     }
     if (c.dgamma || c.dbeta) {
-        float *part = static_cast<float *>(c.workspace) + (int64_t)b * 2 * d;
+        // the block's groups are added up first, in shared memory, in their order: one row of partial sums per block
+        // (rows that begin anywhere go there too, to be written out in order)
+        const bool one = per == 1 && FORM != kPieces;
+        float *part = one ? static_cast<float *>(c.workspace) + (int64_t)blockIdx.x * 2 * d
+                          : reinterpret_cast<float *>(ring) + group * 2 * d;
+        if (!one) {
+            if constexpr (VEC)
+                asm volatile("cp.async.wait_all;" ::: "memory");
+            __syncthreads();
+        }
         const float *dgs = reinterpret_cast<const float *>(dg), *dbs = reinterpret_cast<const float *>(db);
 #pragma unroll
-        for (int k = 0; k < P; ++k) {
-            const int j = column(k);
-            if (j < d) {
-                if constexpr (VEC) {
+        for (int k = 0; k < P; ++k)
+            if (there(k)) {
+                float *g = part + column(k), *e = g + d;
+                if constexpr (FORM == kWhole) {
 #pragma unroll
                     for (int h = 0; h < 8; h += 4) {
-                        const float *g = dgs + k * W + h, *e = dbs + k * W + h;
-                        *reinterpret_cast<float4 *>(part + j + h) = make_float4(g[0], g[1], g[2], g[3]);
-                        *reinterpret_cast<float4 *>(part + d + j + h) = make_float4(e[0], e[1], e[2], e[3]);
+                        const float *a = dgs + k * W + h, *z = dbs + k * W + h;
+                        *reinterpret_cast<float4 *>(g + h) = make_float4(a[0], a[1], a[2], a[3]);
+                        *reinterpret_cast<float4 *>(e + h) = make_float4(z[0], z[1], z[2], z[3]);
                     }
                 } else {
-                    part[j] = dgs[k];
-                    part[d + j] = dbs[k];
+#pragma unroll
+                    for (int h = 0; h < W; ++h) {
+                        g[h] = dgs[k * W + h];
+                        e[h] = dbs[k * W + h];
+                    }
                 }
+            }
+        if (ENDS && t < ends) {
+            part[end] = dg_end;
+            part[d + end] = db_end;
+        }
+        if (!one) {
+            __syncthreads();
+            const float *all = reinterpret_cast<const float *>(ring);
+            for (int j = threadIdx.x; j < 2 * d; j += blockDim.x) {
+                float sum = all[j];
+                for (int g = 1; g < per; ++g)
+                    sum += all[g * 2 * d + j];
+                static_cast<float *>(c.workspace)[(int64_t)blockIdx.x * 2 * d + j] = sum;
             }
         }
     }
@@ -527,8 +607,10 @@ k_norm_bwd(NormGradCall c, const int4 *__restrict__ rows, const int32_t *__restr
                 TDX *dx = static_cast<TDX *>(c.dx) + z * c.lddx;
                 if constexpr (VEC) {
                     const float zero[8] = {};
-                    for (int j = lane * 8; j < d; j += 256)
+                    for (int j = lane * 8; j + 8 <= d; j += 256)
                         store8(dx + j, zero);
+                    if (lane < (d & 7))
+                        dx[(d & ~7) + lane] = from_float<TDX>(0.f);
                 } else {
                     for (int j = lane; j < d; j += 32)
                         dx[j] = from_float<TDX>(0.f);
@@ -542,6 +624,7 @@ k_norm_bwd(NormGradCall c, const int4 *__restrict__ rows, const int32_t *__restr
 __global__ void __launch_bounds__(1024) k_norm_bwd_sum(NormGradCall c, int n)
 {
     __shared__ float part[32][33];
+    pdl_begin();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int64_t j = (int64_t)blockIdx.x * 32 + lane;
     const float *p = static_cast<const float *>(c.workspace) + j;
@@ -575,7 +658,7 @@ __global__ void __launch_bounds__(kThreads) k_norm_dx(NormGradCall c)
         const TX *x = static_cast<const TX *>(c.x) + i * c.ldx;
         const TDY *dy = static_cast<const TDY *>(c.dy) + i * c.lddy;
         TDX *dx = static_cast<TDX *>(c.dx) + i * c.lddx;
-        if (!takes_part(c, i)) {
+        if (!__syncthreads_or(threadIdx.x == 0 && takes_part(c, i))) {
             for (int64_t j = threadIdx.x; j < c.d; j += kThreads)
                 dx[j] = from_float<TDX>(0.f);
             continue;
@@ -640,16 +723,19 @@ int rows_per_cta(int64_t d, int columns = kE) { return std::max(1, kThreads / ro
 
 int64_t partial_rows(int64_t T, int64_t d)
 {
-    if (d > kMaxRow)
-        return std::min<int64_t>(std::max<int64_t>(T, 1), kLongParts);
-    const int64_t per = rows_per_cta(d);
-    return std::min<int64_t>((T + per - 1) / per, kMaxGrid) * per;
+    return d > kMaxRow ? std::min<int64_t>(std::max<int64_t>(T, 1), kLongParts) : std::min<int64_t>(T + 8, kMaxGrid);
 }
 
-bool on16(const void *p, int64_t ld, int32_t dtype)
-{
-    return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && ld * (dtype == TURNOPD_BF16 ? 2 : 4) % 16 == 0;
-}
+// The element of a group of eight at which row 0 of an array begins, and by how many the next row begins later.
+struct Start {
+    int at, step;
+    Start(const void *p, int64_t ld, int32_t dtype)
+        : at((int)(reinterpret_cast<uintptr_t>(p) / (dtype == TURNOPD_BF16 ? 2 : 4) & 7)), step((int)(ld & 7))
+    {
+    }
+    bool operator==(const Start &o) const { return at == o.at && step == o.step; }
+    bool boundary() const { return at == 0 && step == 0; }
+};
 
 template <typename X, typename Y, int N, int P> cudaError_t launch_fwd_rows(const NormCall &c, cudaStream_t stream)
 {
@@ -699,17 +785,25 @@ template <typename X, typename Y> cudaError_t launch_fwd(const NormCall &c, cuda
 }
 
 template <typename X, typename DY, typename DX>
-cudaError_t launch_bwd(const NormGradCall &c, bool vec, const int4 *rows, const int32_t *nvalid, int *parts,
+cudaError_t launch_bwd(const NormGradCall &c, BwdForm form, const int4 *rows, const int32_t *nvalid, int *parts,
                        cudaStream_t stream)
 {
+    const bool vec = form != kSingles;
     const int columns = vec ? kE : kBwdSingles, n = row_threads(c.d, columns), per = rows_per_cta(c.d, columns);
     const bool wide = vec ? n * per > 320 : n * per > 512;  // one CTA per SM then, else two
     const int64_t most = std::min<int64_t>((wide ? 1 : 2) * device_sm_count(), kMaxGrid);
-    const int grid = (int)std::min<int64_t>((c.T + per - 1) / per, most);
-    *parts = grid * per;
-    const size_t smem = vec ? (sizeof(X) + sizeof(DY)) * n * per * kE * kStages : 0;
-    auto kernel = wide ? (vec ? k_norm_bwd<X, DY, DX, true, true> : k_norm_bwd<X, DY, DX, false, true>)
-                       : (vec ? k_norm_bwd<X, DY, DX, true, false> : k_norm_bwd<X, DY, DX, false, false>);
+    // two rows to a group at least, once there is one for every SM: each block's partial sums are written and read again
+    // (512 rows x 4,096: one row 11.6 us, two 10.7, eight 14.5)
+    const int64_t blocks = (c.T + per - 1) / per;
+    int grid = (int)std::min<int64_t>(blocks > device_sm_count() ? (blocks + 1) / 2 : blocks, most);
+    if (form == kPieces)
+        grid = std::min((grid * per + 7) / 8 * 8 / per, kMaxGrid);  // a multiple of eight groups
+    *parts = grid;
+    const size_t row = (sizeof(X) + sizeof(DY)) * n * columns;
+    const size_t smem = per * std::max<size_t>(vec ? kStages * row : 0, per > 1 ? sizeof(float) * 2 * (size_t)c.d : 0);
+    auto kernel = form == kWhole    ? (wide ? k_norm_bwd<X, DY, DX, kWhole, true> : k_norm_bwd<X, DY, DX, kWhole, false>)
+                  : form == kPieces ? (wide ? k_norm_bwd<X, DY, DX, kPieces, true> : k_norm_bwd<X, DY, DX, kPieces, false>)
+                                    : (wide ? k_norm_bwd<X, DY, DX, kSingles, true> : k_norm_bwd<X, DY, DX, kSingles, false>);
     if (smem > 40 * 1024) {  // with the kernel's static shared memory it may pass the default limit of 48 KB
         const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
         if (e != cudaSuccess)
@@ -759,7 +853,10 @@ cudaError_t launch_norm_bwd(const NormGradCall &c, cudaStream_t stream)
         int32_t *nvalid = nullptr;
         // Many rows: the supervised ones are listed first, so that every CTA has as many of them.  (Without sums there
         // may be no workspace.)
-        if (c.mask && c.T >= kListFrom && sums) {
+        const Start x0(c.x, c.ldx, c.x_dtype);
+        const bool vec = x0 == Start(c.dy, c.lddy, c.dy_dtype) && (!c.dx || x0 == Start(c.dx, c.lddx, c.dx_dtype));
+        const BwdForm form = !vec ? kSingles : x0.boundary() && c.d % 8 == 0 ? kWhole : kPieces;
+        if (c.mask && c.T >= kListFrom && sums && (!vec || x0.boundary())) {
             const int64_t nblk = (c.T + kCompactBlock - 1) / kCompactBlock;
             char *p = static_cast<char *>(c.workspace) + align256(sizeof(float) * 2 * (size_t)c.d * (size_t)partial_rows(c.T, c.d));
             rows = reinterpret_cast<int4 *>(p);
@@ -776,18 +873,15 @@ cudaError_t launch_norm_bwd(const NormGradCall &c, cudaStream_t stream)
             if (e != cudaSuccess)
                 return e;
         }
-        const bool vec = c.d % 8 == 0 && on16(c.x, c.ldx, c.x_dtype) && on16(c.dy, c.lddy, c.dy_dtype) &&
-                         (!c.dx || on16(c.dx, c.lddx, c.dx_dtype)) && on16(c.gamma, 8, c.param_dtype);
         with_types(c.x_dtype, c.dy_dtype, [&](auto x, auto dy) {
             using X = decltype(x);
             using DY = decltype(dy);
-            e = c.dx_dtype == TURNOPD_BF16 ? launch_bwd<X, DY, __nv_bfloat16>(c, vec, rows, nvalid, &parts, stream)
-                                           : launch_bwd<X, DY, float>(c, vec, rows, nvalid, &parts, stream);
+            e = c.dx_dtype == TURNOPD_BF16 ? launch_bwd<X, DY, __nv_bfloat16>(c, form, rows, nvalid, &parts, stream)
+                                           : launch_bwd<X, DY, float>(c, form, rows, nvalid, &parts, stream);
         });
     }
     if (e == cudaSuccess && sums) {
-        k_norm_bwd_sum<<<(unsigned)((2 * c.d + 31) / 32), 1024, 0, stream>>>(c, parts);
-        e = cudaGetLastError();
+        e = launch_dependent(k_norm_bwd_sum, dim3((unsigned)((2 * c.d + 31) / 32)), dim3(1024), 0, stream, c, parts);
     }
     return e;
 }

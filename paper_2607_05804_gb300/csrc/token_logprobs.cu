@@ -500,7 +500,9 @@ __global__ void __launch_bounds__(NT, per_sm(TOP, NT)) k_logprobs(LogprobCall c,
     __shared__ Part whole[kMaxCtas];  // CTA 0: the parts of the row
     __shared__ float norm[3];   // m, log S of the row, 1 if it is fine
     __shared__ TopShared<NT> top;
-    __shared__ Share shares[2][(NT / 32)];  // each warp its own: no barrier between a row's share and the next one's
+    // Thread 0 reads a row's indexes and all go by what it read.  The share of the row after next is laid out while a row
+    // is worked on; the barrier at the row's end publishes it.
+    __shared__ Share shares[3];
     namespace cg = cooperative_groups;
     cg::cluster_group cluster = cg::this_cluster();
     const int rank = (int)cluster.block_rank(), ctas = (int)cluster.num_blocks();
@@ -511,26 +513,26 @@ __global__ void __launch_bounds__(NT, per_sm(TOP, NT)) k_logprobs(LogprobCall c,
     int slot = 0;
     if (ctas > 1)
         asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
-    // lane 0 reads a row's indexes two rows ahead, so that nothing waits for them
-    Row coming{};
+    Row coming{};  // thread 0: the row whose share is laid out next
     if (first < n) {
-        if (lane == 0) {
-            shares[0][warp] = get_share<TIn, NT>(c, get_row(c, rows, first), rank, ctas);
+        if (threadIdx.x == 0) {
+            shares[0] = get_share<TIn, NT>(c, get_row(c, rows, first), rank, ctas);
             if (first + step < n)
-                coming = get_row(c, rows, first + step);
+                shares[1] = get_share<TIn, NT>(c, get_row(c, rows, first + step), rank, ctas);
+            if (first + 2 * step < n)
+                coming = get_row(c, rows, first + 2 * step);
         }
-        __syncwarp();
-        load_chunk<TIn, NT>(shares[0][warp], 0, ahead);
+        __syncthreads();
+        load_chunk<TIn, NT>(shares[0], 0, ahead);
     }
-    for (int64_t k = first; k < n; k += step, slot ^= 1) {
+    for (int64_t k = first; k < n; k += step, slot = slot == 2 ? 0 : slot + 1) {
         const bool more = k + step < n;
-        const Share &s = shares[slot][warp], &next = shares[slot ^ 1][warp];
-        if (more && lane == 0) {
-            shares[slot ^ 1][warp] = get_share<TIn, NT>(c, coming, rank, ctas);
-            if (k + 2 * step < n)
-                coming = get_row(c, rows, k + 2 * step);
+        const Share &s = shares[slot], &next = shares[slot == 2 ? 0 : slot + 1];
+        if (threadIdx.x == 0 && k + 2 * step < n) {
+            shares[slot == 0 ? 2 : slot - 1] = get_share<TIn, NT>(c, coming, rank, ctas);
+            if (k + 3 * step < n)
+                coming = get_row(c, rows, k + 3 * step);
         }
-        __syncwarp();
         // the row's ends, before its first and after its last whole vector, and y's logit: needed last, asked for first
         const TIn *z = reinterpret_cast<const TIn *>(s.row);
         const int ends = rank == 0 && s.state == kRowFine ? (int)c.vocab - s.nvec * X::N : 0;

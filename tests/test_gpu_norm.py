@@ -176,6 +176,26 @@ def test_backward(T, d, kind):
         check_backward(dx, dg, db, x, gamma, kind, dy)
 
 
+@pytest.mark.parametrize("d,pads", [(1001, (0, 0, 0)), (1001, (3, 0, 5)), (2048, (0, 3, 0)), (4100, (1, 1, 1)), (7000, (0, 2, 0)),
+                                    (320, (8, 0, 16)), (1024, (0, 0, 0))])
+@pytest.mark.parametrize("kind", [LAYER, RMS])
+def test_many_masked_rows(d, pads, kind):
+    """Rows enough for a list of the supervised ones, where the three arrays' rows begin alike and where they do not."""
+    T = 5000
+    x, gamma, _, g = make(T, d, BF, seed=d, ld=d + pads[0])
+    dy = strided(T, d, d + pads[1], 0, F)
+    dy.copy_(torch.randn((T, d), generator=g, device="cuda"))
+    mask = (torch.rand(T, generator=g, device="cuda") < 0.4).to(torch.uint8)
+    on, off = mask.nonzero()[:, 0], (mask == 0).nonzero()[:, 0]
+    x[off], dy[off] = float("nan"), float("nan")
+    y, mean, rstd, st = forward(x, gamma, None, kind, BF, mask=mask)
+    assert st.item() == 0 and not y[off].any()
+    check_forward(y[on], mean[on], rstd[on], x[on], gamma, None, kind)
+    dx, dg, db = backward(x, gamma, kind, mean, rstd, dy, BF, mask=mask, ldx=d + pads[2])
+    assert not dx[off].any()
+    check_backward(dx[on], dg, db, x[on], gamma, kind, dy[on])
+
+
 def test_single_outputs_and_same_bits():
     T, d = 900, 2048
     x, gamma, _, g = make(T, d, BF, seed=6)
