@@ -808,7 +808,8 @@ template <int N> __device__ __forceinline__ void st_once(__nv_bfloat16 *p, const
         __stcs(reinterpret_cast<uint2 *>(p), make_uint2(pack_bf16x2(g[0], g[1]), pack_bf16x2(g[2], g[3])));
 }
 
-template <typename TIn, typename TOut, bool ENT>
+// DIRECT: a loss mask without a list, looked at here.
+template <typename TIn, typename TOut, bool ENT, bool DIRECT>
 __global__ void __launch_bounds__(kThreads, 4) k_logprobs_bwd(LogprobGradCall c, const int4 *__restrict__ rows,
                                                               const int32_t *__restrict__ nvalid)
 {
@@ -836,7 +837,7 @@ __global__ void __launch_bounds__(kThreads, 4) k_logprobs_bwd(LogprobGradCall c,
         }
         // without a list a masked token's row may be zeroed here (one that a token -> row map names is zeroed before,
         // since the map may send a masked token to a supervised one's row)
-        const bool zeros = g.row.state == kRowMasked && !c.row_of_token && (c.flags & TURNOPD_ZERO_MASKED_GRAD);
+        const bool zeros = DIRECT && g.row.state == kRowMasked && !c.row_of_token && (c.flags & TURNOPD_ZERO_MASKED_GRAD);
         const bool listed = g.row.state == kRowFine || zeros;
         const TIn *z = static_cast<const TIn *>(c.logits) + (listed ? (int64_t)g.row.r * c.ld : 0);
         TOut *out = static_cast<TOut *>(c.grad) + (listed ? (int64_t)g.row.r * c.ld : 0);
@@ -971,10 +972,10 @@ template <typename TIn, typename TOut>
 void launch_grad(const LogprobGradCall &c, const int4 *rows, const int32_t *nvalid, int64_t items, cudaStream_t stream)
 {
     const int grid = (int)std::min<int64_t>(items, (int64_t)device_sm_count() * kGradPerSm);
-    if (c.d_entropy)
-        k_logprobs_bwd<TIn, TOut, true><<<grid, kThreads, 0, stream>>>(c, rows, nvalid);
-    else
-        k_logprobs_bwd<TIn, TOut, false><<<grid, kThreads, 0, stream>>>(c, rows, nvalid);
+    const bool direct = c.mask && !rows;
+    auto kernel = c.d_entropy ? (direct ? k_logprobs_bwd<TIn, TOut, true, true> : k_logprobs_bwd<TIn, TOut, true, false>)
+                              : (direct ? k_logprobs_bwd<TIn, TOut, false, true> : k_logprobs_bwd<TIn, TOut, false, false>);
+    kernel<<<grid, kThreads, 0, stream>>>(c, rows, nvalid);
 }
 
 }  // namespace
