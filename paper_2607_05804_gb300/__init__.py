@@ -465,13 +465,14 @@ def _arg(t, name, dtype=None, numel=0):
     return t.data_ptr()
 
 
-def _handle(stream):
-    """The cudaStream_t of `stream`, or of the current stream (without the Stream object that current_stream() makes)."""
-    import torch
-
+def _handle(stream, t):
+    """The cudaStream_t of `stream`, or of the current stream of t's device (without the Stream object that
+    torch.cuda.current_stream() makes)."""
     if stream is not None:
         return stream.cuda_stream
-    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+    import torch
+
+    return torch._C._cuda_getCurrentRawStream(t.get_device())
 
 
 def _rows_2d(t, name, like=None):
@@ -517,7 +518,7 @@ def turnopd_token_logprobs(logits, vocab, row_of_token, token_ids, loss_mask, n_
         _arg(logprob_out, "logprob_out", f32, T), _arg(entropy_out, "entropy_out", f32, T),
         _arg(stats_out, "stats_out", f32, 2 * T), _arg(top_ids_out, "top_ids_out", i32, T * n_top),
         _arg(top_logprob_out, "top_logprob_out", f32, T * n_top), _arg(workspace, "workspace"), _ws(workspace),
-        _arg(dev_status, "dev_status", i32, 1), _handle(stream))
+        _arg(dev_status, "dev_status", i32, 1), _handle(stream, logits))
     if code:
         raise TurnopdError(code, "turnopd_token_logprobs")
 
@@ -541,7 +542,7 @@ def turnopd_token_logprobs_bwd(logits, vocab, row_of_token, token_ids, loss_mask
         _arg(stats, "stats", f32, 2 * T), _arg(logprob, "logprob", f32, T), _arg(entropy, "entropy", f32, T),
         _arg(d_logprob, "d_logprob", f32, T), _arg(d_entropy, "d_entropy", f32, T), grad_out.data_ptr(),
         _dtype_code(grad_out, "grad_out"), int(flags), _arg(workspace, "workspace"), _ws(workspace),
-        _arg(dev_status, "dev_status", i32, 1), _handle(stream))
+        _arg(dev_status, "dev_status", i32, 1), _handle(stream, logits))
     if code:
         raise TurnopdError(code, "turnopd_token_logprobs_bwd")
 
@@ -564,7 +565,7 @@ def turnopd_norm_fwd(x, gamma, beta, loss_mask, kind, eps, y_out, mean_out, rstd
         x.data_ptr(), _dtype_code(x, "x"), ldx, _arg(gamma, "gamma", None, d), _arg(beta, "beta", None, d),
         _dtype_code(gamma, "gamma"), _arg(loss_mask, "loss_mask", torch.uint8, T), T, d, int(kind), float(eps), y_out.data_ptr(),
         _dtype_code(y_out, "y_out"), ldy, _arg(mean_out, "mean_out", f32, T), _arg(rstd_out, "rstd_out", f32, T),
-        _arg(dev_status, "dev_status", torch.int32, 1), _handle(stream))
+        _arg(dev_status, "dev_status", torch.int32, 1), _handle(stream, x))
     if code:
         raise TurnopdError(code, "turnopd_norm_fwd")
 
@@ -589,7 +590,7 @@ def turnopd_norm_bwd(x, gamma, loss_mask, kind, mean, rstd, dy, dx_out, dgamma_o
         _arg(loss_mask, "loss_mask", torch.uint8, T), T, d, int(kind), _arg(mean, "mean", f32, T), _arg(rstd, "rstd", f32, T),
         dy.data_ptr(), _dtype_code(dy, "dy"), lddy, None if dx_out is None else dx_out.data_ptr(),
         TURNOPD_F32 if dx_out is None else _dtype_code(dx_out, "dx_out"), lddx, _arg(dgamma_out, "dgamma_out", f32, d),
-        _arg(dbeta_out, "dbeta_out", f32, d), _arg(workspace, "workspace"), _ws(workspace), _handle(stream))
+        _arg(dbeta_out, "dbeta_out", f32, d), _arg(workspace, "workspace"), _ws(workspace), _handle(stream, x))
     if code:
         raise TurnopdError(code, "turnopd_norm_bwd")
 

@@ -232,10 +232,10 @@ template <> struct Logits<float> {
 //
 // The n best of a row in one pass.  Each chunk of the row is in the threads' registers.  The first chunk sets a bound:
 // the threads of one lane index are a group, and the n-th best of the 32 groups' best logits is reached by n logits at
-// least and, in a row in no particular order, by few more.  Those are added to a list in shared memory, the list is cut
-// back to its n best, and its n-th best is the bound from then on.  Later logits have higher ids, so only those strictly
-// above the bound can matter; they are added without a barrier, and after 2, 4, 8, ... chunks the list is cut and the
-// bound raised, so that about n logits are added from one cut to the next.  A row that adds more than the list holds
+// least and, in a row in no particular order, by few more.  Those are added to a list in shared memory.  Later logits have
+// higher ids, so only those strictly above the bound can matter; they are added without a barrier, and after 2, 4, 8, ...
+// chunks (with many alternatives after the first too) the list is cut back to its n best and the bound raised to the n-th, so that about n logits are added from one
+// cut to the next.  A row that adds more than the list holds
 // (one that ascends, or whose first chunk is forbidden) is read again with each chunk taken like a first one, and if
 // even that adds too many, n times.  Keys are unique, so the outcome does not depend on the order of the list.
 
@@ -248,7 +248,6 @@ template <int NT> struct alignas(16) TopShared {
     uint64_t list[kListCap + 2];
     uint64_t lanes[NT];                     // the threads' best keys
     uint64_t groups[(NT / 32)][32];                  // each warp's copy of the groups' best
-    uint64_t sorted[kTopMax];
     uint64_t merge[kMaxCtas * kTopMax];           // CTA 0: every CTA's n best
     int count;
     bool lost;                                    // the list was full
@@ -266,35 +265,34 @@ __device__ __forceinline__ float next_above(float b, float)
     return __uint_as_float((u << 1) == 0 ? 1u : (u & 0x80000000u) ? u - 1u : u + 1u);
 }
 
-// Cuts the list to its n best, in order.
+// Cuts the list to its n best, in order (the 32 best, rather, with zeros after the last; the list's count is n).
 template <int NT> __device__ __forceinline__ void cut_list(int n, TopShared<NT> &t)
 {
     __syncthreads();
     const int m = min(t.count, kListCap), tid = threadIdx.x;
     // blocks of NT entries, each but the first beginning with the 32 best of those before
     for (int start = 0;; start += NT - kTopMax) {
+        uint64_t *block = t.list + start;
         const int len = min(m - start, NT);
-        const uint64_t *block = t.list + start;
-        const uint64_t key = tid < len ? block[tid] : 0;
-        if (tid < kTopMax)
-            t.sorted[tid] = 0;
-        if (tid == len)
-            t.list[start + len] = 0;  // read below where len is odd; the next block's first entries are 0 or rewritten
-        __syncthreads();
-        if (key != 0) {
-            int place = 0;
+        // a key's place is the number of keys above it, counted by `lanes` neighbouring threads
+        const int bits = len > 1 ? 32 - __clz(len - 1) : 0, lanes = min(NT >> bits, 32);
+        const int at = tid / lanes, lane = tid & (lanes - 1);
+        const uint64_t key = at < len ? block[at] : 0;
+        int place = 0;
 #pragma unroll 4
-            for (int j = 0; j < len; j += 2) {
-                const ulonglong2 o = *reinterpret_cast<const ulonglong2 *>(block + j);
-                place += (o.x > key) + (o.y > key);
-            }
-            if (place < kTopMax)
-                t.sorted[place] = key;
+        for (int j = 2 * lane; j < len; j += 2 * lanes) {
+            const ulonglong2 o = *reinterpret_cast<const ulonglong2 *>(block + j);
+            place += (o.x > key) + (o.y > key && j + 1 < len);
         }
+        for (int o = lanes >> 1; o > 0; o >>= 1)
+            place += __shfl_xor_sync(~0u, place, o);
         __syncthreads();
         const bool done = start + NT >= m;
-        if (tid < kTopMax)
-            t.list[done ? tid : start + NT - kTopMax + tid] = t.sorted[tid];
+        uint64_t *to = done ? t.list : block + NT - kTopMax;
+        if (lane == 0 && key != 0 && place < kTopMax)
+            to[place] = key;
+        if (done && tid >= len && tid < kTopMax)
+            to[tid] = 0;
         if (done)
             break;
         __syncthreads();
@@ -391,8 +389,8 @@ __device__ __forceinline__ void top_first_chunk(const uint4 (&v)[kU], float vm, 
     }
     if (vm >= above)
         list_add_chunk<TIn>(v, held, id0, above, tie_id, least, t);
-    cut_list(n, t);
-    bound = t.sorted[n - 1] ? key_logit(t.sorted[n - 1]) : -INFINITY;
+    if (least != 0)
+        bound = own;  // n logits of this chunk reach it, with lower ids than any later one
 }
 
 // ---------------------------------------------------------------- forward kernel
@@ -459,6 +457,8 @@ __device__ __noinline__ void top_again(const Share &s, bool has_end, float end_z
         const int q = chunk * (kU * NT) + threadIdx.x;
         const int held = q >= s.len ? 0 : min(kU, (s.len - q + NT - 1) / NT);
         top_first_chunk<TIn>(v, Logits<TIn>::max_of(v), held, s.head + (uint32_t)(s.q0 + q) * N, n, t, bound);
+        cut_list(n, t);
+        bound = t.list[n - 1] ? key_logit(t.list[n - 1]) : -INFINITY;
     }
     if (end_key != 0)
         list_add(end_key, t);
@@ -483,15 +483,15 @@ __device__ __noinline__ void top_again(const Share &s, bool has_end, float end_z
             best = max(best, t.lanes[w]);
         below = best;
         if (threadIdx.x == 0)
-            t.sorted[k] = best;
+            t.list[k] = best;
         __syncthreads();
     }
     if ((int)threadIdx.x >= n && threadIdx.x < kTopMax)
-        t.sorted[threadIdx.x] = 0;
+        t.list[threadIdx.x] = 0;
     __syncthreads();
 }
 
-template <typename TIn, bool TOP, int NT>
+template <typename TIn, bool TOP, int NT, bool CLUSTER>
 __global__ void __launch_bounds__(NT, per_sm(TOP, NT)) k_logprobs(LogprobCall c, const int4 *__restrict__ rows,
                                                           const int32_t *__restrict__ nvalid)
 {
@@ -505,13 +505,14 @@ __global__ void __launch_bounds__(NT, per_sm(TOP, NT)) k_logprobs(LogprobCall c,
     __shared__ Share shares[3];
     namespace cg = cooperative_groups;
     cg::cluster_group cluster = cg::this_cluster();
-    const int rank = (int)cluster.block_rank(), ctas = (int)cluster.num_blocks();
+    const int rank = CLUSTER ? (int)cluster.block_rank() : 0, ctas = CLUSTER ? (int)cluster.num_blocks() : 1;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int64_t n = rows ? *nvalid : c.T;
     const int64_t first = blockIdx.x / ctas, step = gridDim.x / ctas;
     uint4 ahead[kU];
     int slot = 0;
-    if (ctas > 1)
+    const int first_cut = c.n_top > 16 ? 1 : 2;  // the worst of 32 groups' best is a loose bound
+    if (CLUSTER)
         asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
     Row coming{};  // thread 0: the row whose share is laid out next
     if (first < n) {
@@ -566,9 +567,9 @@ __global__ void __launch_bounds__(NT, per_sm(TOP, NT)) k_logprobs(LogprobCall c,
                 load_chunk<TIn, NT>(last ? next : s, last ? 0 : chunk + 1, ahead);
             const float vm = X::max_of(v);
             if (TOP) {
-                if (chunk > 1 && (chunk & (chunk - 1)) == 0) {
+                if (chunk >= first_cut && (chunk & (chunk - 1)) == 0) {
                     cut_list(c.n_top, top);
-                    bound = key_logit(top.sorted[c.n_top - 1]);
+                    bound = key_logit(top.list[c.n_top - 1]);
                 }
                 if (chunk == 0 || vm > bound) {
                     const int q = chunk * (kU * NT) + threadIdx.x;
@@ -626,21 +627,21 @@ __global__ void __launch_bounds__(NT, per_sm(TOP, NT)) k_logprobs(LogprobCall c,
         if (lane == 0)
             parts[warp] = p;
         __syncthreads();
-        if (TOP && (top.count > c.n_top || chunks == 0))
+        if (TOP && (top.count > c.n_top || chunks <= first_cut))  // else it is as the last cut left it
             cut_list(c.n_top, top);
         if (TOP && top.lost)
             top_again<TIn>(s, (int)threadIdx.x < ends, end_z, end_id, c.n_top, top);
         // what CTA 0 needs of this one goes into its shared memory, once it runs
-        if (ctas > 1 && k == first)
+        if (CLUSTER && k == first)
             asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
         if (warp == 0) {
             p = part_warp(lane < (NT / 32) ? parts[lane] : part_empty());
             if (lane == 0)
-                *cluster.map_shared_rank(&whole[rank], 0) = p;
+                *(CLUSTER ? cluster.map_shared_rank(&whole[rank], 0) : &whole[0]) = p;
         }
-        if (TOP && ctas > 1 && (int)threadIdx.x < kTopMax)
-            cluster.map_shared_rank(top.merge, 0)[kTopMax * rank + threadIdx.x] = top.sorted[threadIdx.x];
-        if (ctas > 1)
+        if (TOP && CLUSTER && (int)threadIdx.x < kTopMax)
+            cluster.map_shared_rank(top.merge, 0)[kTopMax * rank + threadIdx.x] = top.list[threadIdx.x];
+        if (CLUSTER)
             cluster.sync();
         else
             __syncthreads();
@@ -678,40 +679,40 @@ __global__ void __launch_bounds__(NT, per_sm(TOP, NT)) k_logprobs(LogprobCall c,
                 }
             }
             if (TOP) {
-                // the CTAs' lists, each in order: a key's place among all is the number of keys above it
-                int place[kMaxCtas * kTopMax / NT];
-                uint64_t key[kMaxCtas * kTopMax / NT];
-#pragma unroll
-                for (int i = 0; i < kMaxCtas * kTopMax / NT; ++i) {
-                    const int e = threadIdx.x + i * NT, own = e / kTopMax;
-                    place[i] = e % kTopMax;
-                    key[i] = own >= ctas ? 0 : ctas == 1 ? top.sorted[place[i]] : top.merge[e];
-                    if (key[i] == 0)
-                        continue;
-                    for (int w = 0; w < ctas; ++w) {
-                        const uint64_t *run = top.merge + kTopMax * w;
-                        if (w == own || run[0] < key[i])
-                            continue;
-                        int lo = 0;
+                // the CTAs' lists, each in order: a key's place among all is the number of keys above it, which every
+                // other list is searched for (side by side: one search alone waits for shared memory at each step)
+                int place = threadIdx.x % kTopMax;
+                uint64_t key = 0;
+                if constexpr (CLUSTER) {
+                    static_assert(!CLUSTER || kMaxCtas * kTopMax == NT, "a thread to every key");
+                    const int own = threadIdx.x / kTopMax;
+                    key = own < ctas ? top.merge[threadIdx.x] : 0;
+                    if (key != 0) {
+                        int lo[kMaxCtas] = {};
 #pragma unroll
                         for (int h = 16; h > 0; h >>= 1)
-                            lo += run[lo + h - 1] > key[i] ? h : 0;
-                        place[i] += lo + (lo == 31 && run[31] > key[i]);
+#pragma unroll
+                            for (int w = 0; w < kMaxCtas; ++w)
+                                if (w < ctas)
+                                    lo[w] += top.merge[kTopMax * w + lo[w] + h - 1] > key ? h : 0;
+#pragma unroll
+                        for (int w = 0; w < kMaxCtas; ++w)
+                            if (w < ctas && w != own)
+                                place += lo[w] + (lo[w] == 31 && top.merge[kTopMax * w + 31] > key);
                     }
+                } else if (threadIdx.x < kTopMax) {
+                    key = top.list[threadIdx.x];
                 }
                 __syncthreads();
-#pragma unroll
-                for (int i = 0; i < kMaxCtas * kTopMax / NT; ++i) {
-                    if (key[i] != 0 && place[i] < c.n_top && norm[2] != 0.f) {
-                        c.top_ids[(int64_t)s.token * c.n_top + place[i]] = (int32_t)key_id(key[i]);
-                        c.top_logprob[(int64_t)s.token * c.n_top + place[i]] = (key_logit(key[i]) - norm[0]) - norm[1];
-                    }
+                if (key != 0 && place < c.n_top && norm[2] != 0.f) {
+                    c.top_ids[(int64_t)s.token * c.n_top + place] = (int32_t)key_id(key);
+                    c.top_logprob[(int64_t)s.token * c.n_top + place] = (key_logit(key) - norm[0]) - norm[1];
                 }
             }
         }
         // CTA 0's memory is written again for the next row
         if (more) {
-            if (ctas > 1)
+            if (CLUSTER)
                 cluster.sync();
             else
                 __syncthreads();
@@ -926,19 +927,20 @@ template <typename Call> struct Lists {
     }
 };
 
-// Few rows: each is shared by a cluster of CTAs, so that the device's SMs all have some of it.  The slices are two
-// chunks long at least: below that the exchange costs more than it saves (152 rows x 8,192: one CTA 4.2 us, two 5.0).
+// Few rows: each is shared by a cluster of CTAs, so that the device's SMs all have some of it, up to 8 CTAs for 3 SMs.
+// Powers of two: 64 fp32 rows x 151,936 with 20 alternatives take 19 us with 4 CTAs to a row, 26 with 7; 200 bf16 rows 26
+// with 2, 29 with one.  The slices are two chunks long at least: below that the exchange costs more than it saves
+// (152 rows x 8,192: one CTA 4.2 us, two 5.0).
 int cluster_ctas(const LogprobCall &c)
 {
-    const int sms = device_sm_count();
     const int64_t vecs = c.vocab / (c.in_dtype == TURNOPD_BF16 ? 8 : 4);
     int ctas = 1;
-    while (ctas < kMaxCtas && c.T * ctas * 2 <= 2 * sms && vecs >= ctas * 2 * kU * 256)
+    while (ctas < kMaxCtas && 3 * c.T * ctas * 2 <= 8 * device_sm_count() && vecs >= ctas * 2 * kU * 256)
         ctas *= 2;
     return ctas;
 }
 
-template <typename TIn, int NT>
+template <typename TIn, int NT, bool CLUSTER>
 cudaError_t launch_fwd(const LogprobCall &c, int ctas, const int4 *rows, const int32_t *nvalid, cudaStream_t stream)
 {
     const int64_t want = c.T * ctas;
@@ -949,12 +951,12 @@ cudaError_t launch_fwd(const LogprobCall &c, int ctas, const int4 *rows, const i
     attr[0].val.clusterDim.x = ctas;
     attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = ctas > 1 ? 1 : 0;
+    cfg.numAttrs = CLUSTER ? 1 : 0;
     cfg.gridDim = dim3((unsigned)std::min(want, most));
     cfg.blockDim = dim3(NT);
     cfg.stream = stream;
-    return c.n_top > 0 ? cudaLaunchKernelEx(&cfg, k_logprobs<TIn, true, NT>, c, rows, nvalid)
-                       : cudaLaunchKernelEx(&cfg, k_logprobs<TIn, false, NT>, c, rows, nvalid);
+    return c.n_top > 0 ? cudaLaunchKernelEx(&cfg, k_logprobs<TIn, true, NT, CLUSTER>, c, rows, nvalid)
+                       : cudaLaunchKernelEx(&cfg, k_logprobs<TIn, false, NT, CLUSTER>, c, rows, nvalid);
 }
 
 // Rows enough for four CTAs on every SM: CTAs of 128 threads, of which one row's merge hides behind more of the others'
@@ -962,8 +964,10 @@ cudaError_t launch_fwd(const LogprobCall &c, int ctas, const int4 *rows, const i
 template <typename TIn>
 cudaError_t launch_fwd(const LogprobCall &c, int ctas, const int4 *rows, const int32_t *nvalid, cudaStream_t stream)
 {
-    return c.T >= 4 * device_sm_count() ? launch_fwd<TIn, 128>(c, ctas, rows, nvalid, stream)
-                                        : launch_fwd<TIn, 256>(c, ctas, rows, nvalid, stream);
+    if (ctas > 1)
+        return launch_fwd<TIn, 256, true>(c, ctas, rows, nvalid, stream);
+    return c.T >= 4 * device_sm_count() ? launch_fwd<TIn, 128, false>(c, ctas, rows, nvalid, stream)
+                                        : launch_fwd<TIn, 256, false>(c, ctas, rows, nvalid, stream);
 }
 
 constexpr int kGradPerSm = 4;
@@ -990,7 +994,7 @@ cudaError_t launch_token_logprobs(const LogprobCall &c, cudaStream_t stream)
 {
     const int ctas = cluster_ctas(c);
     Lists<LogprobCall> l;
-    const cudaError_t e = l.make(c, c.T * ctas <= 2 * device_sm_count(), stream);
+    const cudaError_t e = l.make(c, c.T * ctas <= (int64_t)device_sm_count() * per_sm(c.n_top > 0, 256), stream);
     if (e != cudaSuccess)
         return e;
     return c.in_dtype == TURNOPD_BF16 ? launch_fwd<__nv_bfloat16>(c, ctas, l.rows, l.nvalid, stream)
