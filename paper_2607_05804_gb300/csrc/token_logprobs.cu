@@ -234,8 +234,8 @@ template <> struct Logits<float> {
 // the threads of one lane index are a group, and the n-th best of the 32 groups' best logits is reached by n logits at
 // least and, in a row in no particular order, by few more.  Those are added to a list in shared memory.  Later logits have
 // higher ids, so only those strictly above the bound can matter; they are added without a barrier, and after 2, 4, 8, ...
-// chunks (with many alternatives after the first too) the list is cut back to its n best and the bound raised to the n-th, so that about n logits are added from one
-// cut to the next.  A row that adds more than the list holds
+// chunks or 4, 16, ... the list is cut back to its n best and the bound raised to the n-th: n or 3 n logits, about, are
+// added from one cut to the next.  A row that adds more than the list holds
 // (one that ascends, or whose first chunk is forbidden) is read again with each chunk taken like a first one, and if
 // even that adds too many, n times.  Keys are unique, so the outcome does not depend on the order of the list.
 
@@ -511,7 +511,11 @@ __global__ void __launch_bounds__(NT, per_sm(TOP, NT)) k_logprobs(LogprobCall c,
     const int64_t first = blockIdx.x / ctas, step = gridDim.x / ctas;
     uint4 ahead[kU];
     int slot = 0;
-    const int first_cut = c.n_top > 16 ? 1 : 2;  // the worst of 32 groups' best is a loose bound
+    // Chunks before which the list is cut: powers of four where few rows are shared out and a cut's barriers count (64 fp32
+    // rows with 20 alternatives: 18.5 us, with powers of two 19.4), of two where many rows keep the SMs busy (2,458 rows x
+    // 50,304 with 32: 102 us and 109).  With many alternatives after the first too: its bound is a loose one.
+    constexpr int kCuts = NT == 256 ? 0x55555555 : -1;
+    const int first_cut = c.n_top > 16 ? 1 : NT == 256 ? 4 : 2;
     if (CLUSTER)
         asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
     Row coming{};  // thread 0: the row whose share is laid out next
@@ -567,7 +571,7 @@ __global__ void __launch_bounds__(NT, per_sm(TOP, NT)) k_logprobs(LogprobCall c,
                 load_chunk<TIn, NT>(last ? next : s, last ? 0 : chunk + 1, ahead);
             const float vm = X::max_of(v);
             if (TOP) {
-                if (chunk >= first_cut && (chunk & (chunk - 1)) == 0) {
+                if (chunk >= first_cut && (chunk & (chunk - 1)) == 0 && (chunk & kCuts)) {
                     cut_list(c.n_top, top);
                     bound = key_logit(top.list[c.n_top - 1]);
                 }
