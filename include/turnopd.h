@@ -411,7 +411,8 @@ turnopd_status turnopd_vocab_shard_loss_grad(const void *z_student, const void *
  *   aligned; NULL and 0 will do when loss_mask is NULL.
  * Device errors (the token's outputs are those of a masked one, its stats (-inf, 0)):
  *   TURNOPD_ERR_TOKEN_RANGE (row or token id), TURNOPD_ERR_NONFINITE (a row that holds
- *   NaN or +inf, or no logit above -1.2e38).
+ *   NaN or a logit of 2^126 or more, such as +inf, or no logit above -2^126: below
+ *   that logits count as forbidden).
  * Precision: fp32 arithmetic on exact inputs.  The sums leave y out and add its
  *   term at the end, so that logprob_out and entropy_out keep their relative
  *   precision where y is all but certain.
@@ -441,7 +442,9 @@ size_t turnopd_token_logprobs_workspace_bytes(int64_t num_tokens);
  *   columns [vocab, ld) and other rows are not written unless
  *   TURNOPD_ZERO_MASKED_GRAD, which zero-fills columns [0, vocab) of masked tokens'
  *   rows.  grad_out may be the logits themselves (grad_dtype = in_dtype), else it
- *   may not overlap them.  A row belongs to one supervised token at most.
+ *   may not overlap them.  A row belongs to one supervised token at most, and in
+ *   place with TURNOPD_ZERO_MASKED_GRAD to no masked token besides (it would be
+ *   zeroed before it is read; give masked tokens row -1 there).
  * Flags: TURNOPD_ZERO_MASKED_GRAD only.  Workspace as in the forward call.
  * Device errors: TURNOPD_ERR_TOKEN_RANGE (row or token id; token skipped).
  * Precision: 1 - p_y is -expm1(logprob[i]), so it keeps its relative precision.

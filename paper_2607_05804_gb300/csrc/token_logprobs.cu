@@ -491,6 +491,12 @@ __device__ __noinline__ void top_again(const Share &s, bool has_end, float end_z
     __syncthreads();
 }
 
+// One pass over each row: chunks of kU 16-byte vectors to a thread, the next one's loads out while one is summed.  A CTA or
+// a cluster takes rows in turn; a cluster's CTAs push their parts to CTA 0, which writes the row's outputs.
+//
+// Bound: HBM with many rows, 9,830 x 151,936 bf16 in 469 us (6,370 GB/s, 0.94 of a copy).  With alternatives the issue
+// rate: 2,458 x 50,304 bf16 take 49 us without, 68 with 10, 103 with 32 (14 instructions to a logit, not 8).  With few rows
+// latency: one row of 151,936 takes 5.4 us, 9 with five alternatives, of which the exchange and cold code are most.
 template <typename TIn, bool TOP, int NT, bool CLUSTER>
 __global__ void __launch_bounds__(NT, per_sm(TOP, NT)) k_logprobs(LogprobCall c, const int4 *__restrict__ rows,
                                                           const int32_t *__restrict__ nvalid)
@@ -813,7 +819,11 @@ template <int N> __device__ __forceinline__ void st_once(__nv_bfloat16 *p, const
         __stcs(reinterpret_cast<uint2 *>(p), make_uint2(pack_bf16x2(g[0], g[1]), pack_bf16x2(g[2], g[3])));
 }
 
+// Items of one chunk of one row, taken in turn, so that long and short rows load every SM alike; an item's statistics come
+// with its first loads, one item ahead.  Each logit is read before its place is written: grad may be the logits.
 // DIRECT: a loss mask without a list, looked at here.
+//
+// Bound: HBM.  4,915 x 151,936 bf16 in place, with the entropy's term: 444 us, 6,730 GB/s (0.99 of a copy).
 template <typename TIn, typename TOut, bool ENT, bool DIRECT>
 __global__ void __launch_bounds__(kThreads, 4) k_logprobs_bwd(LogprobGradCall c, const int4 *__restrict__ rows,
                                                               const int32_t *__restrict__ nvalid)
