@@ -494,7 +494,7 @@ __device__ __noinline__ void top_again(const Share &s, bool has_end, float end_z
 // One pass over each row: chunks of kU 16-byte vectors to a thread, the next one's loads out while one is summed.  A CTA or
 // a cluster takes rows in turn; a cluster's CTAs push their parts to CTA 0, which writes the row's outputs.
 //
-// Bound: HBM with many rows, 9,830 x 151,936 bf16 in 469 us (6,370 GB/s, 0.94 of a copy).  With alternatives the issue
+// Bound: HBM with many rows, 9,830 x 151,936 bf16 in 463 us (6,450 GB/s, 0.95 of a copy).  With alternatives the issue
 // rate: 2,458 x 50,304 bf16 take 49 us without, 68 with 10, 103 with 32 (14 instructions to a logit, not 8).  With few rows
 // latency: one row of 151,936 takes 5.4 us, 9 with five alternatives, of which the exchange and cold code are most.
 template <typename TIn, bool TOP, int NT, bool CLUSTER>
