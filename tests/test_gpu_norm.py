@@ -81,6 +81,22 @@ def test_forward(T, d, kind):
         check_forward(y2, None, None, x, gamma, None, kind)
 
 
+@pytest.mark.parametrize("kind", [LAYER, RMS])
+@pytest.mark.parametrize("d", [63, 511, 1001, 1537, 2047, 2601, 4100, 5119, 7003, 8191])
+def test_forward_many_rows(d, kind):
+    """Rows enough that as few threads as hold a row take it: every such split, with rows of any alignment and a mask."""
+    T = 1300
+    for xdt, ydt, ld, off in ((BF, BF, d, 0), (BF, F, d + 8 - d % 8, 0), (F, BF, d + 1, 1), (F, F, d, 0)):
+        x, gamma, beta, g = make(T, d, xdt, seed=d, ld=ld, offset=off)
+        mask = (torch.rand(T, generator=g, device="cuda") < 0.6).to(torch.uint8)
+        x[mask == 0] = float("nan")  # masked rows are not read
+        y, mean, rstd, st = forward(x, gamma, beta, kind, ydt, mask=mask, ldy=ld, offset=off)
+        assert st.item() == 0
+        on = mask.bool()
+        check_forward(y[on], mean[on], rstd[on], x[on], gamma, beta, kind)
+        assert not y[~on].any() and not mean[~on].any() and not rstd[~on].any()
+
+
 def test_parameters_of_any_alignment():
     T, d = 20, 1024
     x, gamma, beta, _ = make(T, d, BF, seed=1)
