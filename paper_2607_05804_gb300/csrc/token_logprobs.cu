@@ -916,7 +916,8 @@ __global__ void __launch_bounds__(kThreads, 4) k_logprobs_bwd(LogprobGradCall c,
 template <typename Call> struct Lists {
     int4 *rows = nullptr;
     int32_t *nvalid = nullptr;
-    // `direct`: a CTA to every token, which looks at the mask itself
+    // `direct`: a CTA to every token, which looks at the mask itself (64 bf16 rows x 151,936, 0.6 of them supervised: 8.2 us,
+    // with a list 12.0; the gradient of 64 x 1,024 fp32 3.0 and 6.7)
     cudaError_t make(const Call &c, bool direct, cudaStream_t stream)
     {
         if (!c.mask || direct)

@@ -230,6 +230,27 @@ def test_single_outputs_and_same_bits():
     assert all(torch.equal(a, b) for a, b in zip(full, again))
 
 
+@pytest.mark.parametrize("T,d,pad", [(4400, 4096, 0), (4400, 4096, 8), (4300, 4100, 4), (2200, 8192, 0), (70_000, 256, 0),
+                                     (4000, 4096, 0)])
+@pytest.mark.parametrize("kind", [LAYER, RMS])
+def test_listed_rows_at_boundaries(T, d, pad, kind):
+    """Elements enough for a list of the supervised rows, whose rows begin at 16-byte boundaries; the last has too few."""
+    x, gamma, _, g = make(T, d, BF, seed=d, ld=d + pad)
+    dy = strided(T, d, d + pad, 0, F)
+    dy.copy_(torch.randn((T, d), generator=g, device="cuda"))
+    mask = (torch.rand(T, generator=g, device="cuda") < 0.3).to(torch.uint8)
+    on = mask.bool()
+    x[~on] = float("nan")
+    dy[~on] = float("nan")
+    x[7], mask[7] = float("inf"), 1  # a row that the forward call reports, treated as masked
+    on[7] = False
+    _, mean, rstd, st = forward(x, gamma, None, kind, F, mask=mask)
+    assert st.item() == 9
+    dx, dg, db = backward(x, gamma, kind, mean, rstd, dy, BF, mask=mask, ldx=d + pad)
+    assert not dx[~on].any()
+    check_backward(dx[on], dg, db, x[on], gamma, kind, dy[on])
+
+
 @pytest.mark.parametrize("kind", [LAYER, RMS])
 def test_gradient_against_differences(kind):
     """Along random directions of x, gamma and beta, against central differences of the float64 objective."""
