@@ -59,10 +59,14 @@ struct Part {
 
 __device__ __forceinline__ Part part_empty() { return Part{kMaskedBelow, 0.f, 0.f}; }
 
+// A change of reference by d (in powers of two).  2^-1000 is 0: bounded there, d times a sum stays finite, and a sum about a
+// reference far below the new one (-1e37, as forbidden tokens are filled with) becomes 0 and not -inf times 0.
+__device__ __forceinline__ float shift(float from, float to) { return fmaxf((from - to) * kLog2e, -1000.f); }
+
 // The part's sums about another reference m.
 __device__ __forceinline__ Part part_about(Part p, float m)
 {
-    const float d = (p.m - m) * kLog2e, f = ex2(d);
+    const float d = shift(p.m, m), f = ex2(d);
     return Part{m, p.s * f, fmaf(d, p.s, p.a) * f};
 }
 
@@ -606,7 +610,7 @@ __global__ void __launch_bounds__(NT, per_sm(TOP, NT)) k_logprobs(LogprobCall c,
             }
             const float tm = chunk == cy ? X::max_of(v) : vm;
             if (tm > m) {
-                const float d = (m - tm) * kLog2e;
+                const float d = shift(m, tm);
                 const float2 f = splat(ex2(d));
                 A = fmul2(ffma2(splat(d), S, A), f);
                 S = fmul2(S, f);

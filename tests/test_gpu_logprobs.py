@@ -152,6 +152,43 @@ def test_forbidden_vocabulary(dtype, gone):
     assert o["lp"][0].item() == 0.0 and abs(o["H"][0].item()) == 0.0
 
 
+@pytest.mark.parametrize("dtype", [BF, F])
+@pytest.mark.parametrize("fill", [-1e33, -1e35, -1e37, -8e37])
+@pytest.mark.parametrize("n,V", [(6, 20_000), (6, 151_936), (310, 20_000), (620, 20_000), (620, 151_936)])
+def test_forbidden_vocabulary_of_any_fill(dtype, fill, n, V):
+    """Forbidden tokens as any large negative number, with one CTA and with several to a row."""
+    z, y = make(n, V, dtype, seed=n)
+    for r in range(n):
+        kept = torch.randperm(V, device="cuda")[:(1, 2, 3, 19, 200, V - 1)[r % 6]]
+        kept[0] = y[r]
+        row = torch.full((V,), fill, device="cuda", dtype=dtype)
+        row[kept] = z[r, kept]
+        z[r] = row
+    y2 = y.clone()
+    y2[2] = int((z[2] == z[2].min()).nonzero()[0])  # a forbidden one was given
+    for yy in (y, y2):
+        o = forward(z, V, yy, n_top=20)
+        assert o["status"].item() == 0
+        check_forward(o, z, V, yy, 20)
+    gl, gh = torch.linspace(-1, 1, n, device="cuda"), torch.linspace(1, 2, n, device="cuda")
+    out = torch.empty_like(z)
+    P.turnopd_token_logprobs_bwd(z, V, None, y2, None, o["stats"], o["lp"], o["H"], gl, gh, out, 0, None, o["status"])
+    check_grad(out, z, V, y2, gl, gh)
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
+@pytest.mark.parametrize("n", [3, 310, 620])
+def test_one_logit_far_above_the_rest(dtype, n):
+    V = 20_000
+    for at in (0, 7, 9000, V - 1):
+        z, y = make(n, V, dtype, seed=at + 1)
+        z[:, at] = 1e37
+        y[::2] = at
+        o = forward(z, V, y, n_top=5)
+        assert o["status"].item() == 0
+        check_forward(o, z, V, y, 5)
+
+
 def test_masks_rows_and_skipped_tokens():
     V, T = 5003, 300
     z, _ = make(40, V, BF, seed=1, ld=5008)
