@@ -398,7 +398,8 @@ turnopd_status turnopd_vocab_shard_loss_grad(const void *z_student, const void *
  *   logits       [num_rows, ld] row-major, in_dtype (F32 or BF16), any element
  *                 alignment; columns [vocab, ld) are not read.
  *   row_of_token  int32[num_tokens] or NULL (then num_rows >= num_tokens);
- *                 several tokens may name one row.
+ *                 several tokens may name one row.  With it and num_rows 0 (no
+ *                 token is supervised) logits may be NULL.
  *   token_ids     int32[num_tokens], or NULL (then logprob_out is NULL too).
  *   loss_mask     uint8[num_tokens] or NULL.
  *   n_top         0 (no alternatives) to min(vocab, TURNOPD_TOP_ALTERNATIVES_MAX).
@@ -437,6 +438,7 @@ size_t turnopd_token_logprobs_workspace_bytes(int64_t num_tokens);
  *   logprob and entropy are its outputs (logprob and token_ids are needed if
  *   d_logprob is given, entropy if d_entropy is); d_logprob, d_entropy
  *   float32[num_tokens], either nullable.
+ *   With row_of_token and num_rows 0 logits and grad_out may be NULL.
  * Output: grad_out [num_rows, ld] of grad_dtype (F32 or BF16).  Rows of supervised
  *   tokens get the gradient (zeros where the forward call found no distribution),
  *   columns [vocab, ld) and other rows are not written unless

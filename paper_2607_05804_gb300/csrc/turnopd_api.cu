@@ -444,6 +444,10 @@ size_t turnopd_token_logprobs_workspace_bytes(int64_t num_tokens)
 static bool is_dtype(int32_t t) { return t == TURNOPD_F32 || t == TURNOPD_BF16; }
 static size_t dtype_size(int32_t t) { return t == TURNOPD_BF16 ? 2 : 4; }
 
+// A token -> row map over no rows at all (a batch without a supervised token) leaves nothing to read or write:
+// the logits of such a call may be NULL, as an empty array's pointer is.
+static bool no_rows(int64_t num_rows, const int32_t *row_of_token) { return row_of_token && num_rows == 0; }
+
 static bool bad_logit_shape(const void *logits, int32_t in_dtype, int64_t ld, int64_t vocab, int64_t num_rows,
                             const int32_t *row_of_token, int64_t num_tokens)
 {
@@ -459,7 +463,7 @@ turnopd_status turnopd_token_logprobs(const void *logits, int32_t in_dtype, int6
                                       size_t workspace_bytes, int32_t *dev_status, turnopd_stream_t stream)
 {
     NvtxRange nvtx("turnopd_token_logprobs");
-    if (!dev_status || (num_tokens > 0 && !logits))
+    if (!dev_status || (num_tokens > 0 && !logits && !no_rows(num_rows, row_of_token)))
         return TURNOPD_ERR_NULL;
     if (num_tokens > 0 && ((!logprob_out && !entropy_out && !stats_out && n_top == 0) || (logprob_out && !token_ids) ||
                            (n_top > 0 && (!top_ids_out || !top_logprob_out))))
@@ -490,7 +494,7 @@ turnopd_status turnopd_token_logprobs_bwd(const void *logits, int32_t in_dtype, 
                                           int32_t *dev_status, turnopd_stream_t stream)
 {
     NvtxRange nvtx("turnopd_token_logprobs_bwd");
-    if (!dev_status || (num_tokens > 0 && (!logits || !grad_out || !stats)))
+    if (!dev_status || (num_tokens > 0 && (!stats || ((!logits || !grad_out) && !no_rows(num_rows, row_of_token)))))
         return TURNOPD_ERR_NULL;
     if (num_tokens > 0 &&
         ((!d_logprob && !d_entropy) || (d_logprob && (!logprob || !token_ids)) || (d_entropy && !entropy)))

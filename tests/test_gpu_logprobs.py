@@ -414,6 +414,34 @@ def test_gradient_against_differences():
         assert abs(diff - got) <= 1e-4 * size + 1e-6
 
 
+@pytest.mark.parametrize("T", [5, 3000])
+def test_compact_layout_without_rows(T):
+    """No token is supervised, so no row of logits is there: every output is a masked token's.  A token that is supervised
+    all the same has no row to name."""
+    V = 1000
+    z, grad = torch.empty((0, V), device="cuda"), torch.empty((0, V), device="cuda")
+    rows, y = torch.full((T,), -1, dtype=torch.int32, device="cuda"), torch.zeros(T, dtype=torch.int32, device="cuda")
+    ws = torch.empty(P.turnopd_token_logprobs_workspace_bytes(T), dtype=torch.uint8, device="cuda")
+    gl = torch.ones(T, device="cuda")
+    for on in (None, 3):
+        mask = torch.zeros(T, dtype=torch.uint8, device="cuda")
+        if on is not None:
+            mask[on], rows[on] = 1, 0
+        o = forward(z, V, y, rows=rows, mask=mask, n_top=4)
+        assert o["status"].item() == (0 if on is None else 5)
+        assert not o["lp"].any() and not o["H"].any() and (o["ids"] == -1).all() and not o["tlp"].any()
+        want = torch.zeros((T, 2), device="cuda")
+        if on is not None:
+            want[on, 0] = -float("inf")
+        assert torch.equal(o["stats"], want)
+        for flags in (0, P.TURNOPD_ZERO_MASKED_GRAD):
+            o["status"].zero_()
+            P.turnopd_token_logprobs_bwd(z, V, rows, y, mask, o["stats"], o["lp"], o["H"], gl, gl, grad, flags, ws, o["status"])
+            assert o["status"].item() == (0 if on is None else 5)
+    with pytest.raises(P.TurnopdError):  # a row to each token: none may be missing
+        forward(z, V, y, n_top=4)
+
+
 def test_nothing_to_do():
     z = torch.zeros((0, 64), device="cuda")
     o = forward(z, 64)

@@ -67,6 +67,21 @@ def test_policy_head(kind, d, V):
         assert abs(got[t] - want) <= 1e-9 + 1e-9 * want
 
 
+def test_batch_without_a_supervised_token():
+    """All zeros, as a rank of a data-parallel step may meet it."""
+    b, x, gamma, beta, head, mask, y, rand = setup(P.TURNOPD_LAYER_NORM, 264, 1000)
+    mask = torch.zeros_like(mask)
+    ph = PolicyHead(gamma, head, mask, y, beta=beta, kind=P.TURNOPD_LAYER_NORM, n_top=5)
+    lp, H = ph.forward(x)
+    assert not lp.any() and not H.any() and (ph.top_ids == -1).all() and not ph.top_logprob.any()
+    grads = ph.backward(rand(mask.numel()), rand(mask.numel()))
+    for got, shape in zip(grads, (x.shape, gamma.shape, beta.shape, head.shape)):
+        assert got.shape == shape and not got.any()
+    tid, off = torch.from_numpy(b.turn_id).cuda(), torch.from_numpy(b.traj_offsets).cuda()
+    assert not ph.turn_entropy(tid, off, b.max_turns).any()
+    assert ph.status() == 0
+
+
 def test_norm_in_front_of_the_fused_head():
     """The distillation step from the last block's output: norm, both LM heads in the loss, and back through the norm."""
     d, d_t, V = 256, 320, 2000
