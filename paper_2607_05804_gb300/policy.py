@@ -17,7 +17,8 @@ from . import (TURNOPD_RMS_NORM, turnopd_norm_bwd, turnopd_norm_bwd_workspace_by
 class PolicyHead:
     """gamma, beta [d] (beta or None) and head [vocab, d] are the model's; loss_mask uint8 [T], token_ids int32 [T] the
     batch's.  forward(x) fills logprob, entropy [T] and, for n_top > 0, top_ids, top_logprob [T, n_top]; backward() takes
-    dL/dlogprob and dL/dentropy and returns (dx [T, d], dgamma, dbeta, dhead)."""
+    dL/dlogprob and dL/dentropy and returns (dx [T, d], dgamma, dbeta, dhead).  Parameters and x may require gradients;
+    autograd records nothing of either call."""
 
     def __init__(self, gamma, head, loss_mask, token_ids, *, beta=None, kind=TURNOPD_RMS_NORM, eps=1e-6, n_top=0):
         self.gamma, self.beta, self.head, self.kind, self.eps, self.n_top = gamma, beta, head, int(kind), float(eps), int(n_top)
@@ -40,6 +41,7 @@ class PolicyHead:
         self.ws_n = torch.empty(max(turnopd_norm_bwd_workspace_bytes(T, d), 256), dtype=torch.uint8, device=dev)
         self.dev_status = torch.zeros(1, dtype=torch.int32, device=dev)
 
+    @torch.no_grad()
     def forward(self, x):
         self.x = x
         turnopd_norm_fwd(x, self.gamma, self.beta, self.loss_mask, self.kind, self.eps, self.h, self.mean, self.rstd,
@@ -51,6 +53,7 @@ class PolicyHead:
                                self.dev_status)
         return self.logprob, self.entropy
 
+    @torch.no_grad()
     def backward(self, d_logprob, d_entropy=None):
         """After it the logits hold their gradient."""
         g = self.logits

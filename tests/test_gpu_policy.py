@@ -82,6 +82,21 @@ def test_batch_without_a_supervised_token():
     assert ph.status() == 0
 
 
+def test_parameters_that_require_gradients():
+    """A model's own parameters and hidden states: the same numbers, and nothing recorded for autograd."""
+    b, x, gamma, beta, head, mask, y, rand = setup(P.TURNOPD_LAYER_NORM, 264, 1000)
+    gl, gh = rand(mask.numel()), rand(mask.numel())
+    outs = []
+    for wrap in (lambda t: t, lambda t: torch.nn.Parameter(t.clone())):
+        ph = PolicyHead(wrap(gamma), wrap(head), mask, y, beta=wrap(beta), kind=P.TURNOPD_LAYER_NORM)
+        xx = wrap(x)
+        lp, H = ph.forward(xx)
+        out = [t.clone() for t in (lp, H)] + [t.clone() for t in ph.backward(gl, gh)]
+        assert ph.status() == 0 and not any(t.requires_grad for t in out)
+        outs.append(out)
+    assert all(torch.equal(a, b) for a, b in zip(*outs))
+
+
 def test_norm_in_front_of_the_fused_head():
     """The distillation step from the last block's output: norm, both LM heads in the loss, and back through the norm."""
     d, d_t, V = 256, 320, 2000
