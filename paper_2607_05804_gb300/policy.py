@@ -40,10 +40,11 @@ class PolicyHead:
         self.ws_l = torch.empty(max(turnopd_token_logprobs_workspace_bytes(T), 256), dtype=torch.uint8, device=dev)
         self.ws_n = torch.empty(max(turnopd_norm_bwd_workspace_bytes(T, d), 256), dtype=torch.uint8, device=dev)
         self.dev_status = torch.zeros(1, dtype=torch.int32, device=dev)
+        self.ready = False  # the logits are a forward pass's, not yet written over by their gradient
 
     @torch.no_grad()
     def forward(self, x):
-        self.x = x
+        self.x, self.ready = x, False
         turnopd_norm_fwd(x, self.gamma, self.beta, self.loss_mask, self.kind, self.eps, self.h, self.mean, self.rstd,
                          self.dev_status)
         self.hs = self.h[self.at]
@@ -51,14 +52,18 @@ class PolicyHead:
         turnopd_token_logprobs(self.logits, self.logits.shape[1], self.rows, self.token_ids, self.loss_mask, self.n_top,
                                self.logprob, self.entropy, self.stats, self.top_ids, self.top_logprob, self.ws_l,
                                self.dev_status)
+        self.ready = True
         return self.logprob, self.entropy
 
     @torch.no_grad()
     def backward(self, d_logprob, d_entropy=None):
-        """After it the logits hold their gradient."""
+        """Once after each forward pass, with x as it was: after it the logits hold their gradient."""
+        if not self.ready:
+            raise RuntimeError("PolicyHead.backward needs a forward pass of its own: the logits hold the last one's gradient")
         g = self.logits
         turnopd_token_logprobs_bwd(g, g.shape[1], self.rows, self.token_ids, self.loss_mask, self.stats, self.logprob,
                                    self.entropy, d_logprob, d_entropy, g, 0, self.ws_l, self.dev_status)
+        self.ready = False
         dhead = torch.mm(g.t(), self.hs)
         self.dh[self.at] = torch.mm(g, self.head)
         dx = torch.empty_like(self.x)

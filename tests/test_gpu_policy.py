@@ -97,6 +97,22 @@ def test_parameters_that_require_gradients():
     assert all(torch.equal(a, b) for a, b in zip(*outs))
 
 
+def test_a_backward_pass_to_each_forward_pass():
+    """The logits hold their gradient after a backward pass: a second one has nothing to start from and is refused."""
+    b, x, gamma, beta, head, mask, y, rand = setup(P.TURNOPD_RMS_NORM, 256, 1000)
+    ph = PolicyHead(gamma, head, mask, y)
+    gl = rand(mask.numel())
+    with pytest.raises(RuntimeError):
+        ph.backward(gl)
+    ph.forward(x)
+    first = [t.clone() for t in ph.backward(gl) if t is not None]
+    with pytest.raises(RuntimeError):
+        ph.backward(gl)
+    ph.forward(x)
+    again = [t for t in ph.backward(gl) if t is not None]
+    assert ph.status() == 0 and all(torch.equal(a, b) for a, b in zip(first, again))
+
+
 def test_norm_in_front_of_the_fused_head():
     """The distillation step from the last block's output: norm, both LM heads in the loss, and back through the norm."""
     d, d_t, V = 256, 320, 2000
