@@ -753,6 +753,14 @@ struct Start {
     bool boundary() const { return at == 0 && step == 0; }
 };
 
+// Dynamic shared memory of a kernel up to `most`, the largest amount that any call of this kernel asks for: every call sets
+// the same limit, since another host thread's call may come between one that sets it and its launch.  (From 40 KB: with the
+// kernel's static shared memory it may pass the default limit of 48 KB.)
+template <typename K> cudaError_t allow_shared(K kernel, size_t most)
+{
+    return most > 40 * 1024 ? cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)most) : cudaSuccess;
+}
+
 template <typename X, typename Y, int N, int P> cudaError_t launch_fwd_rows(const NormCall &c, cudaStream_t stream)
 {
     constexpr int W = Piece<X>::W, kPer = 256 / N;
@@ -763,11 +771,9 @@ template <typename X, typename Y, int N, int P> cudaError_t launch_fwd_rows(cons
     const int reps = (int)std::min<int64_t>(16, std::max<int64_t>(1, ctas / (4 * round)));
     const size_t smem = sizeof(float2) * W * plane_size<W>((int)c.d);
     auto kernel = k_norm_fwd<X, Y, N, P>;
-    if (smem > 40 * 1024) {
-        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-        if (e != cudaSuccess)
-            return e;
-    }
+    const cudaError_t e = allow_shared(kernel, sizeof(float2) * W * plane_size<W>(N * P * W));  // d / W <= N P pieces
+    if (e != cudaSuccess)
+        return e;
     kernel<<<(unsigned)((ctas + reps - 1) / reps), 256, smem, stream>>>(c, reps);
     return cudaGetLastError();
 }
@@ -825,11 +831,12 @@ cudaError_t launch_bwd(const NormGradCall &c, BwdForm form, const int4 *rows, co
     auto kernel = form == kWhole    ? (wide ? k_norm_bwd<X, DY, DX, kWhole, true> : k_norm_bwd<X, DY, DX, kWhole, false>)
                   : form == kPieces ? (wide ? k_norm_bwd<X, DY, DX, kPieces, true> : k_norm_bwd<X, DY, DX, kPieces, false>)
                                     : (wide ? k_norm_bwd<X, DY, DX, kSingles, true> : k_norm_bwd<X, DY, DX, kSingles, false>);
-    if (smem > 40 * 1024) {  // with the kernel's static shared memory it may pass the default limit of 48 KB
-        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-        if (e != cudaSuccess)
-            return e;
-    }
+    // pieces: the ring of a whole block, and no less than a group's 8 d bytes of sums with n * 16 >= d; single columns: the
+    // sums of the groups of 256 threads
+    const cudaError_t e = allow_shared(kernel, vec ? kStages * (sizeof(X) + sizeof(DY)) * (wide ? 512 : 320) * kE
+                                                   : sizeof(float) * 2 * kThreads * kBwdSingles);
+    if (e != cudaSuccess)
+        return e;
     kernel<<<grid, n * per, smem, stream>>>(c, rows, nvalid, n);
     return cudaGetLastError();
 }

@@ -291,6 +291,42 @@ def test_offsets_beyond_32_bits():
     check_backward(y, dg, db, x, gamma, LAYER, dy)
 
 
+def test_host_threads_with_rows_of_different_lengths():
+    """Two host threads on streams of their own, with rows of lengths that one kernel takes with different amounts of
+    shared memory: each call gets what it asks for."""
+    import threading
+
+    failed = []
+
+    def work(d, stream, calls):
+        x, gamma, beta, g = make(40, d, BF, seed=d)
+        dy = torch.randn((40, d), generator=g, device="cuda")
+        y, dx = torch.empty_like(x), torch.empty_like(x)
+        mean, rstd = torch.empty(40, device="cuda"), torch.empty(40, device="cuda")
+        dg, db, st = torch.empty(d, device="cuda"), torch.empty(d, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+        ws = torch.empty(P.turnopd_norm_bwd_workspace_bytes(40, d), dtype=torch.uint8, device="cuda")
+        torch.cuda.synchronize()
+        start.wait()
+        try:
+            for _ in range(calls):
+                P.turnopd_norm_fwd(x, gamma, beta, None, LAYER, 1e-6, y, mean, rstd, st, stream)
+                P.turnopd_norm_bwd(x, gamma, None, LAYER, mean, rstd, dy, dx, dg, db, ws, stream)
+            stream.synchronize()
+            check_forward(y, mean, rstd, x, gamma, beta, LAYER)
+            check_backward(dx, dg, db, x, gamma, LAYER, dy)
+        except Exception as e:  # noqa: BLE001
+            failed.append((d, repr(e)))
+
+    for lengths in ((8192, 6400), (5120, 4608)):
+        start = threading.Barrier(len(lengths))
+        threads = [threading.Thread(target=work, args=(d, torch.cuda.Stream(), 4000)) for d in lengths]
+        for t in threads:
+            t.start()
+        for t in threads:
+            t.join()
+    assert not failed, failed
+
+
 def test_nothing_to_do():
     x = torch.zeros((0, 64), device="cuda")
     gamma = torch.ones(64, device="cuda")
