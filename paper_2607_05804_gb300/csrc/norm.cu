@@ -4,7 +4,8 @@
 // xh = (x - mu) r, y = xh gamma + beta.  With g = dy gamma:
 //   dx = r (g - mean g - xh mean(g xh))   (root-mean-square form: without mean g),
 //   dgamma = sum_i dy_i xh_i, dbeta = sum_i dy_i over the rows.
-// The variance is a second pass over x - mu, so a mean much larger than the deviation costs no digits.
+// The variance and xh are taken from x - mu in a second pass, so a mean much larger than the deviation costs no digits but
+// those of mu's own rounding.
 
 #include <algorithm>
 
@@ -197,7 +198,8 @@ __global__ void __launch_bounds__(256, fwd_per_sm(P)) k_norm_fwd(NormCall c, int
                     for (int j = 0; j < W / 2; ++j)
                         s = fadd2(s, X::pair(v[k], j));
             }
-            mu = group_sum<N>(s.x + s.y, red[sums++ & 3], group) * inv_d;
+            // divided, not times 1/d: a sum that is exact (a row of equal numbers) has its exact mean
+            mu = group_sum<N>(s.x + s.y, red[sums++ & 3], group) / (float)d;
         }
         // in a block of its own: in one with the loop above the compiler keeps the unpacked pieces, and spills
         float2 q = make_float2(t < ends ? (z - mu) * (z - mu) : 0.f, 0.f);
@@ -223,8 +225,7 @@ __global__ void __launch_bounds__(256, fwd_per_sm(P)) k_norm_fwd(NormCall c, int
         if (r == 0.f)
             mu = 0.f;
         if (r != 0.f) {
-            // xh = x r - mu r, off by half a unit of mu r at most, as mu itself is
-            const float m = -mu * r;
+            // xh = (x - mu) r, as the backward pass takes it: x r - mu r would be off by half a unit of mu r
             int at[W];  // gamma and beta of the h-th columns of this thread's pieces
 #pragma unroll
             for (int h = 0; h < W; ++h)
@@ -237,7 +238,7 @@ __global__ void __launch_bounds__(256, fwd_per_sm(P)) k_norm_fwd(NormCall c, int
 #pragma unroll
                 for (int j = 0; j < W / 2; ++j) {
                     const float2 a = planes[at[2 * j] + k * N], b = planes[at[2 * j + 1] + k * N];
-                    const float2 xh = ffma2(X::pair(v[k], j), splat(r), splat(m));
+                    const float2 xh = fmul2(fadd2(X::pair(v[k], j), splat(-mu)), splat(r));
                     o[j].x = fmaf(xh.x, a.x, a.y);
                     o[j].y = fmaf(xh.y, b.x, b.y);
                 }

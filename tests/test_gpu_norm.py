@@ -122,6 +122,19 @@ def test_large_means_and_constant_rows():
     assert st.item() == 9 and not y.any() and not rstd.any()
 
 
+@pytest.mark.parametrize("d", [8, 100, 1000, 1001, 1024, 2049, 4095, 4096, 5120, 6400, 8191, 9000])
+@pytest.mark.parametrize("T", [3, 1300])
+def test_constant_rows_are_beta(T, d):
+    """The sum of a row of equal whole numbers is exact below 2^24, and so is its d-th part: nothing is left of such a row,
+    in any column, but beta."""
+    for xdt, ld, off in ((BF, d, 0), (F, d, 0), (BF, d + 3, 1), (F, d + 1, 1)):
+        x, gamma, beta, _ = make(T, d, xdt, seed=d, ld=ld, offset=off)
+        value = torch.tensor([700.0, 1296.0, -1016.0], device="cuda").repeat(T // 3 + 1)[:T]
+        x.copy_(value[:, None].expand(T, d))
+        y, mean, rstd, st = forward(x, gamma, beta, LAYER, F, eps=1e-6)
+        assert st.item() == 0 and torch.equal(mean, value) and torch.equal(y, beta.expand(T, d))
+
+
 @pytest.mark.parametrize("kind", [LAYER, RMS])
 def test_masks_and_non_finite_rows(kind):
     T, d = 150, 1000
