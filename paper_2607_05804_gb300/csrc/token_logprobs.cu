@@ -517,8 +517,16 @@ __global__ void __launch_bounds__(NT, per_sm(TOP, NT)) k_logprobs(LogprobCall c,
     cg::cluster_group cluster = cg::this_cluster();
     const int rank = CLUSTER ? (int)cluster.block_rank() : 0, ctas = CLUSTER ? (int)cluster.num_blocks() : 1;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int64_t n = rows ? *nvalid : c.T;
-    const int64_t first = blockIdx.x / ctas, step = gridDim.x / ctas;
+    // One thread reads the list's length too: it says how many barriers there are.  (A cluster has no list.)
+    __shared__ int list_length;
+    if (!CLUSTER && rows) {
+        if (threadIdx.x == 0)
+            list_length = *nvalid;
+        __syncthreads();
+    }
+    // (32 bits hold three steps beyond 2^31 - 1; 64 cost registers: 2,458 x 50,304 with 10 alternatives 67.6 us and 68.4)
+    const uint32_t n = !CLUSTER && rows ? list_length : (int)c.T;
+    const uint32_t first = blockIdx.x / ctas, step = gridDim.x / ctas;
     uint4 ahead[kU];
     int slot = 0;
     // Chunks before which the list is cut: powers of four where few rows are shared out and a cut's barriers count (64 fp32
@@ -540,7 +548,7 @@ __global__ void __launch_bounds__(NT, per_sm(TOP, NT)) k_logprobs(LogprobCall c,
         __syncthreads();
         load_chunk<TIn, NT>(shares[0], 0, ahead);
     }
-    for (int64_t k = first; k < n; k += step, slot = slot == 2 ? 0 : slot + 1) {
+    for (uint32_t k = first; k < n; k += step, slot = slot == 2 ? 0 : slot + 1) {
         const bool more = k + step < n;
         const Share &s = shares[slot], &next = shares[slot == 2 ? 0 : slot + 1];
         if (threadIdx.x == 0 && k + 2 * step < n) {
@@ -1013,7 +1021,9 @@ cudaError_t launch_token_logprobs(const LogprobCall &c, cudaStream_t stream)
 {
     const int ctas = cluster_ctas(c);
     Lists<LogprobCall> l;
-    const cudaError_t e = l.make(c, c.T * ctas <= (int64_t)device_sm_count() * per_sm(c.n_top > 0, 256), stream);
+    // (clusters are for fewer tokens than that)
+    const bool direct = ctas > 1 || c.T <= (int64_t)device_sm_count() * per_sm(c.n_top > 0, 256);
+    const cudaError_t e = l.make(c, direct, stream);
     if (e != cudaSuccess)
         return e;
     return c.in_dtype == TURNOPD_BF16 ? launch_fwd<__nv_bfloat16>(c, ctas, l.rows, l.nvalid, stream)

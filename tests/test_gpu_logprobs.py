@@ -442,6 +442,34 @@ def test_compact_layout_without_rows(T):
         forward(z, V, y, n_top=4)
 
 
+@pytest.mark.parametrize("dtype", [BF, F])
+@pytest.mark.parametrize("n_top", [0, 7])
+@pytest.mark.parametrize("on", [0, 1, 2, 700, 1063, 1064, 1065, 2999, 3000])
+def test_lists_of_few_and_of_many_rows(on, n_top, dtype):
+    """Tokens enough for a list of the supervised ones, with none, few, as many as CTAs and all of them on it."""
+    V, T = 1003, 3000
+    z, y = make(T, V, dtype, seed=on, ld=1008)
+    mask = torch.zeros(T, dtype=torch.uint8, device="cuda")
+    mask[torch.randperm(T, device="cuda", generator=torch.Generator(device="cuda").manual_seed(on))[:on]] = 1
+    at, off = mask.nonzero()[:, 0], (mask == 0).nonzero()[:, 0]
+    z[off] = float("nan")
+    o = forward(z, V, y, mask=mask, n_top=n_top)
+    assert o["status"].item() == 0
+    if on:
+        check_forward(o, z[at], V, y[at], n_top, at=at)
+    assert not o["lp"][off].any() and not o["H"][off].any() and not o["stats"][off].any()
+    if n_top:
+        assert (o["ids"][off] == -1).all() and not o["tlp"][off].any()
+    gl = torch.linspace(-1, 1, T, device="cuda")
+    ws = torch.empty(P.turnopd_token_logprobs_workspace_bytes(T), dtype=torch.uint8, device="cuda")
+    for flags, left in ((0, 3.0), (P.TURNOPD_ZERO_MASKED_GRAD, 0.0)):
+        out = torch.full_like(z, 3.0)
+        P.turnopd_token_logprobs_bwd(z, V, None, y, mask, o["stats"], o["lp"], o["H"], gl, gl, out, flags, ws, o["status"])
+        assert o["status"].item() == 0 and (out[off, :V] == left).all() and (out[:, V:] == 3.0).all()
+        if on:
+            check_grad(out[at], z[at], V, y[at], gl[at], gl[at])
+
+
 def test_nothing_to_do():
     z = torch.zeros((0, 64), device="cuda")
     o = forward(z, 64)

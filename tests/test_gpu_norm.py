@@ -264,6 +264,28 @@ def test_listed_rows_at_boundaries(T, d, pad, kind):
     check_backward(dx[on], dg, db, x[on], gamma, kind, dy[on])
 
 
+@pytest.mark.parametrize("xdt,dydt", [(BF, F), (F, F), (F, BF), (BF, BF)])
+@pytest.mark.parametrize("T,d", [(4400, 4096), (4300, 4100), (70_000, 256)])
+@pytest.mark.parametrize("on", [0, 1, 303, 304, 305, 2433, -1])
+def test_lists_of_few_and_of_many_rows(T, d, on, xdt, dydt):
+    """Elements enough for a list of the supervised rows, with none, few, as many as blocks or groups and all of them on it."""
+    x, gamma, _, g = make(T, d, xdt, seed=on + 2, ld=d + -d % 8)
+    dy = strided(T, d, d + -d % 8, 0, dydt)
+    dy.copy_(torch.randn((T, d), generator=g, device="cuda"))
+    mask = torch.zeros(T, dtype=torch.uint8, device="cuda")
+    mask[torch.randperm(T, generator=g, device="cuda")[:on if on >= 0 else T]] = 1
+    on_, off = mask.nonzero()[:, 0], mask == 0
+    x[off], dy[off] = float("nan"), float("nan")
+    _, mean, rstd, st = forward(x, gamma, None, LAYER, F, mask=mask)
+    assert st.item() == 0
+    dx, dg, db = backward(x, gamma, LAYER, mean, rstd, dy, xdt, mask=mask, ldx=d + -d % 8)
+    assert not dx[off].any()
+    if on_.numel():
+        check_backward(dx[on_], dg, db, x[on_], gamma, LAYER, dy[on_])
+    else:
+        assert not dg.any() and not db.any()
+
+
 @pytest.mark.parametrize("kind", [LAYER, RMS])
 def test_gradient_against_differences(kind):
     """Along random directions of x, gamma and beta, against central differences of the float64 objective."""
