@@ -473,8 +473,9 @@ __device__ __noinline__ void top_again(const Share &s, bool has_end, float end_z
     uint64_t below = ~0ull;
     for (int k = 0; k < n; ++k) {
         uint64_t best = end_key < below ? end_key : 0;
-        for (int i = threadIdx.x; i < s.len * N; i += NT) {
-            const uint64_t key = top_key(to_float(z[i]), s.head + s.q0 * N + i);
+        // (unsigned: the step after the last may pass 2^31 - 1)
+        for (uint32_t i = threadIdx.x; i < (uint32_t)s.len * N; i += NT) {
+            const uint64_t key = top_key(to_float(z[i]), (uint32_t)(s.head + s.q0 * N) + i);
             best = key < below ? max(best, key) : best;
         }
 #pragma unroll

@@ -269,6 +269,20 @@ def test_offsets_beyond_32_bits():
     assert not z[:-3].any() and o["status"].item() == 0
 
 
+def test_longest_row_read_once_for_each_alternative():
+    """A row of 2^31 - 1 logits whose first chunk qualifies too many: five lanes' vectors of every 32 hold 4, the others 0,
+    so the sixth best of the groups is a 0.  203 tokens: one CTA takes the row."""
+    V, T = 2 ** 31 - 1, 203
+    z = torch.zeros(2 ** 31, dtype=BF, device="cuda")
+    z.view(-1, 32, 8)[:, :5] = 4.0
+    rows, mask = torch.zeros(T, dtype=torch.int32, device="cuda"), torch.zeros(T, dtype=torch.uint8, device="cuda")
+    mask[7] = 1
+    o = forward(z[:V].view(1, V), V, None, rows=rows, mask=mask, n_top=6)
+    assert o["status"].item() == 0
+    assert o["ids"][7].tolist() == [0, 1, 2, 3, 4, 5] and (o["ids"][mask == 0] == -1).all()
+    assert o["stats"][7, 0] == 4.0
+
+
 def test_same_bits_on_every_run_and_stream():
     V = 30_000
     z, y = make(333, V, BF, seed=12)
