@@ -484,6 +484,94 @@ def test_lists_of_few_and_of_many_rows(on, n_top, dtype):
             check_grad(out[at], z[at], V, y[at], gl[at], gl[at])
 
 
+@pytest.mark.parametrize("T", [300, 3000])
+@pytest.mark.parametrize("dtype", [BF, F])
+def test_tokens_that_are_not_on_the_list(T, dtype):
+    """Masked tokens and indexes out of range where the kernels look at the mask themselves (300 tokens) and where the
+    supervised ones are listed (3,000): every output of such a token, and its gradient left alone."""
+    V, R = 2003, 50
+    z, _ = make(R, V, dtype, seed=T, ld=2008)
+    g = torch.Generator(device="cuda").manual_seed(T)
+    mask = (torch.rand(T, generator=g, device="cuda") < 0.5).to(torch.uint8)
+    rows, y = (torch.randint(n, (T,), generator=g, device="cuda").int() for n in (R, V))
+    off, on = (mask == 0).nonzero()[:, 0], mask.nonzero()[:, 0]
+    rows[off], y[off] = -7, V + 9
+    bad = on[[0, 1, 2, 3, -1]]
+    rows[bad[0]], rows[bad[1]], y[bad[2]], y[bad[3]], rows[bad[4]] = R, -1, V, -2, 2 ** 31 - 1
+    o = forward(z, V, y, rows=rows, mask=mask, n_top=4)
+    assert o["status"].item() == 5
+    good = on[4:-1]
+    check_forward(o, z[rows[good].long()], V, y[good], 4, at=good)
+    for at, m in ((off, 0.0), (bad, -float("inf"))):
+        assert not o["lp"][at].any() and not o["H"][at].any() and (o["ids"][at] == -1).all() and not o["tlp"][at].any()
+        assert (o["stats"][at, 0] == m).all() and (o["stats"][at, 1] == 0).all()
+    # a row to each supervised token; one token has no row, one an id out of range, and their rows are left alone
+    rows = torch.full((T,), -1, dtype=torch.int32, device="cuda")
+    rows[on] = torch.arange(on.numel(), device="cuda").int()
+    zc, yc = make(on.numel(), V, dtype, seed=T + 1, ld=2008)
+    y[on] = yc
+    rows[bad[1]], y[bad[4]] = on.numel(), V
+    rest = torch.ones(on.numel(), dtype=torch.bool, device="cuda")
+    rest[[1, -1]] = False
+    o = forward(zc, V, y, rows=rows, mask=mask)
+    assert o["status"].item() == 5
+    gl, gh = torch.randn(T, generator=g, device="cuda"), torch.randn(T, generator=g, device="cuda")
+    ws = torch.empty(P.turnopd_token_logprobs_workspace_bytes(T), dtype=torch.uint8, device="cuda")
+    for flags in (0, P.TURNOPD_ZERO_MASKED_GRAD):
+        out = torch.full_like(zc, 3.0)
+        o["status"].zero_()
+        P.turnopd_token_logprobs_bwd(zc, V, rows, y, mask, o["stats"], o["lp"], o["H"], gl, gh, out, flags, ws, o["status"])
+        assert o["status"].item() == 5 and (out[~rest] == 3.0).all() and (out[:, V:] == 3.0).all()
+        check_grad(out[rest], zc[rest], V, y[on[rest]], gl[on[rest]], gh[on[rest]])
+
+
+def test_ties_across_clusters_of_eight():
+    """70,000 bf16 columns and few rows: eight CTAs to a row, ties within and across their slices."""
+    V = 70_000
+    i = torch.arange(V, device="cuda")
+    rows = [torch.zeros(V, device="cuda"), (i % 2).float(), (i // 8750).float(), -(i // 8750).float(), (i % 8750 == 0).float(),
+            (i >= V - 20).float(), torch.where(i % 8192 == 8191, 1.0, -1.0), torch.linspace(-4, 4, V, device="cuda")]
+    z = torch.stack(rows).to(BF)
+    y = torch.arange(len(rows), device="cuda").int() * 9001
+    for n_top in (1, 9, 32):
+        check_forward(forward(z, V, y, n_top=n_top), z, V, y, n_top)
+
+
+@pytest.mark.parametrize("n,V,masked", [(3, 151_936, False), (700, 5003, False), (3000, 1003, True)])
+def test_in_a_cuda_graph(n, V, masked):
+    """Both calls captured and replayed on new logits give the bits of the calls outside."""
+    z, y = make(n, V, BF, seed=n)
+    z2, _ = make(n, V, BF, seed=n + 1)
+    mask = (torch.arange(n, device="cuda") % 3 != 0).to(torch.uint8) if masked else None
+    gl = torch.linspace(-1, 1, n, device="cuda")
+    new = lambda *s: torch.zeros(s, device="cuda")  # noqa: E731
+    lp, H, stats, tlp, out = new(n), new(n), new(n, 2), new(n, 5), torch.zeros_like(z)
+    ids, st = torch.zeros((n, 5), dtype=torch.int32, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+    ws = torch.empty(P.turnopd_token_logprobs_workspace_bytes(n), dtype=torch.uint8, device="cuda")
+
+    def both(stream=None):
+        P.turnopd_token_logprobs(z, V, None, y, mask, 5, lp, H, stats, ids, tlp, ws, st, stream)
+        P.turnopd_token_logprobs_bwd(z, V, None, y, mask, stats, lp, H, gl, gl, out, P.TURNOPD_ZERO_MASKED_GRAD if masked else 0,
+                                     ws, st, stream)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        both()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        both()
+    z.copy_(z2)
+    for _ in range(2):
+        graph.replay()
+    torch.cuda.synchronize()
+    got = [t.clone() for t in (lp, H, stats, ids, tlp, out)]
+    both()
+    assert st.item() == 0 and all(torch.equal(a, b) for a, b in zip(got, (lp, H, stats, ids, tlp, out)))
+    check_forward(forward(z, V, y, n_top=5), z, V, y, 5)
+
+
 def test_nothing_to_do():
     z = torch.zeros((0, 64), device="cuda")
     o = forward(z, 64)

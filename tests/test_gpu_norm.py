@@ -362,6 +362,55 @@ def test_host_threads_with_rows_of_different_lengths():
     assert not failed, failed
 
 
+@pytest.mark.parametrize("xdt,d", [(BF, 512), (BF, 1024), (BF, 2048), (BF, 4096), (BF, 6144), (BF, 8192), (F, 256), (F, 512),
+                                   (F, 1024), (F, 1536), (F, 2048), (F, 4096), (F, 8192)])
+@pytest.mark.parametrize("pad", [0, 1])
+def test_rows_that_fill_every_thread(xdt, d, pad):
+    """Widths whose pieces are exactly the threads' number of them, with rows few and many."""
+    for T in (5, 1300):
+        x, gamma, beta, _ = make(T, d, xdt, seed=d, ld=d + pad)
+        for kind in (LAYER, RMS):
+            y, mean, rstd, st = forward(x, gamma, beta, kind, BF, ldy=d + pad)
+            assert st.item() == 0
+            check_forward(y, mean, rstd, x, gamma, beta, kind)
+
+
+@pytest.mark.parametrize("T,d,masked", [(3, 4096, False), (600, 1001, True), (4400, 4096, True)])
+def test_in_a_cuda_graph(T, d, masked):
+    """Both calls captured and replayed on new hidden states give the bits of the calls outside."""
+    x, gamma, beta, g = make(T, d, BF, seed=T)
+    x2 = make(T, d, BF, seed=T + 1)[0]
+    dy = torch.randn((T, d), generator=g, device="cuda")
+    mask = (torch.arange(T, device="cuda") % 3 != 0).to(torch.uint8) if masked else None
+    y, dx = torch.zeros_like(x), torch.zeros_like(x)
+    mean, rstd, dg, db = (torch.zeros(n, device="cuda") for n in (T, T, d, d))
+    st = torch.zeros(1, dtype=torch.int32, device="cuda")
+    ws = torch.empty(P.turnopd_norm_bwd_workspace_bytes(T, d), dtype=torch.uint8, device="cuda")
+
+    def both():
+        P.turnopd_norm_fwd(x, gamma, beta, mask, LAYER, 1e-6, y, mean, rstd, st)
+        P.turnopd_norm_bwd(x, gamma, mask, LAYER, mean, rstd, dy, dx, dg, db, ws)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        both()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        both()
+    x.copy_(x2)
+    for _ in range(2):
+        graph.replay()
+    torch.cuda.synchronize()
+    got = [t.clone() for t in (y, mean, rstd, dx, dg, db)]
+    both()
+    assert st.item() == 0 and all(torch.equal(a, b) for a, b in zip(got, (y, mean, rstd, dx, dg, db)))
+    on = mask.bool() if masked else torch.ones(T, dtype=torch.bool, device="cuda")
+    check_forward(y[on], mean[on], rstd[on], x[on], gamma, beta, LAYER)
+    check_backward(dx[on], dg, db, x[on], gamma, LAYER, dy[on])
+
+
 def test_nothing_to_do():
     x = torch.zeros((0, 64), device="cuda")
     gamma = torch.ones(64, device="cuda")
