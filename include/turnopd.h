@@ -416,7 +416,9 @@ turnopd_status turnopd_vocab_shard_loss_grad(const void *z_student, const void *
  *   that logits count as forbidden).
  * Precision: fp32 arithmetic on exact inputs.  The sums leave y out and add its
  *   term at the end, so that logprob_out and entropy_out keep their relative
- *   precision where y is all but certain.
+ *   precision where y is all but certain.  Without token_ids, and where another
+ *   token than y is all but certain, log S and the entropy are good to the
+ *   absolute precision of fp32 sums of about 1 only.
  */
 #define TURNOPD_TOP_ALTERNATIVES_MAX 32
 turnopd_status turnopd_token_logprobs(const void *logits, int32_t in_dtype, int64_t ld, int64_t vocab,

@@ -127,16 +127,16 @@ template <int N> __device__ __forceinline__ float group_sum(float v, float *red,
     return s;
 }
 
-// CTAs of 256 threads per SM: what the registers allow, but for 60 bytes of spills with twelve pieces (32,768 x 5,120 bf16
-// layer norm: 125 us with three CTAs and twelve pieces, 130 with two and sixteen).
+// CTAs of 256 threads per SM: what the registers allow, but for up to 56 bytes of spills with twelve pieces (32,768 x
+// 5,120 bf16 layer norm: 124 us with three CTAs and twelve pieces, 130 with two and sixteen).
 constexpr int fwd_per_sm(int pieces) { return pieces > 12 ? 2 : pieces > 4 ? 3 : 4; }
 
 // N threads take a row, P of its whole 16-byte pieces to a thread, kept as they were read: one read of x, all of it
 // asked for at once, and with N <= 32 no barrier.  The elements before and after the whole pieces go to the row's first
 // threads, one to each.  A group takes `reps` rows in turn.
 //
-// Bound: HBM.  32,768 x 4,096 bf16 take 91 us (5,890 GB/s) as layer norm, 75 (5,700) as root-mean-square norm with 0.6 of
-// the rows supervised; 32,768 x 8,192 180 (5,980); with rows off 16-byte boundaries the 4,096 columns take 94.  Fewer
+// Bound: HBM.  32,768 x 4,096 bf16 take 92 us (5,850 GB/s) as layer norm, 76 (5,670) as root-mean-square norm with 0.6 of
+// the rows supervised; 32,768 x 8,192 184 (5,830); with rows off 16-byte boundaries the 4,096 columns take 96.  Fewer
 // warps (14 per SM) with all of a row's loads out beat many: the pieces stay packed, and converting them twice is cheaper
 // than the registers of their values (137 us at 4,096 with spills).
 template <typename TX, typename TY, int N, int P>
@@ -342,8 +342,8 @@ __device__ __forceinline__ float2 sum2(float2 v)
 // kWhole is the same without ends, and kSingles reads column by column.  Missing columns are zeros throughout.
 //
 // Bound: HBM, with the arithmetic of both dx and dgamma close behind (0.57 of the issue slots).  32,768 x 5,120, bf16 x and
-// dx, fp32 dy, 0.6 of the rows supervised: 160 us with the sum over blocks, 5,890 GB/s.  16,384 x 4,096 with rows off
-// boundaries: kPieces 139 us, kSingles 250.
+// dx, fp32 dy, 0.6 of the rows supervised: 159 us with the sum over blocks, 5,930 GB/s.  16,384 x 4,096 with rows off
+// boundaries: kPieces 140 us, kSingles 268.
 enum BwdForm {
     kSingles,  // any rows, column by column
     kPieces,   // rows that begin anywhere, but in all three arrays alike
@@ -737,9 +737,11 @@ template <typename F> void with_types(int32_t a, int32_t b, F &&f)
 
 constexpr int kMaxGrid = 320;         // CTAs of the backward pass, at most
 constexpr int kLongParts = 64;        // partial sums of the kernels for long rows
-// Elements from which a loss mask is turned into a list of rows, two launches that take 5 us (0.6 of the rows supervised,
-// without a list and with: 8,192 x 1,024 16.5 and 20.6 us, 2,048 x 5,120 23.6 and 25.4, 4,096 x 4,096 28.7 and 29.2, 4,096 x
-// 5,120 38 and 37, 16,384 x 5,120 111 and 88).
+// Elements from which a loss mask is turned into a list of rows, two launches that take 5 us.  bf16 x, fp32 dy, 0.6 of the
+// rows supervised, us without a list and with one.  Below the limit: 8,192 x 1,024 16.0 and 20.5, 1,024 x 8,192 21.3 and
+// 24.2, 2,048 x 5,120 23.2 and 25.1, but 2,048 x 6,000 30.2 and 27.1.  From it on: 32,768 x 640 37.5 and 35.2, 2,048 x 8,192
+// 33.2 and 31.4, 4,096 x 5,120 37.1 and 36.9, 8,192 x 2,560 41.4 and 36.5, 16,384 x 5,120 109 and 89, but 16,384 x 1,024 23.7
+// and 26.7, 4,096 x 4,096 29.1 and 29.5, 65,536 x 256 30.4 and 30.8.  These four exceptions cost 13 % at most.
 constexpr int64_t kListFrom = 1 << 24;
 
 int row_threads(int64_t d, int columns = kE) { return (int)((d + columns * 32 - 1) / (columns * 32)) * 32; }
@@ -787,8 +789,8 @@ template <typename X, typename Y, int N, int P> cudaError_t launch_fwd_rows(cons
 }
 
 // Many rows: as few threads to a row as hold it, so that many rows are in flight and most need no barrier.  Few rows:
-// many threads to each, which answer sooner (300 rows x 4,096 bf16: 5.0 us with 128 threads, 6.2 with 32; 2,000 rows: 9.9
-// and 8.4).
+// many threads to each, which answer sooner (300 rows x 4,096 bf16: 4.2 us with 128 threads, 5.4 with 32; 2,000 rows: 9.3
+// and 7.7).
 template <typename X, typename Y> cudaError_t launch_fwd(const NormCall &c, cudaStream_t stream)
 {
     const int64_t pieces = c.d / Piece<X>::W;
@@ -828,7 +830,7 @@ cudaError_t launch_bwd(const NormGradCall &c, BwdForm form, const int4 *rows, co
     const bool wide = vec ? n * per > 320 : n * per > 512;  // one CTA per SM then, else two
     const int64_t most = std::min<int64_t>((wide ? 1 : 2) * device_sm_count(), kMaxGrid);
     // two rows to a group at least, once there is one for every SM: each block's partial sums are written and read again
-    // (512 rows x 4,096: one row 11.6 us, two 10.7, eight 14.5)
+    // (512 rows x 4,096: one row 10.8 us, two 9.9, eight 13.6)
     const int64_t blocks = (c.T + per - 1) / per;
     int grid = (int)std::min<int64_t>(blocks > device_sm_count() ? (blocks + 1) / 2 : blocks, most);
     if (form == kPieces)

@@ -499,9 +499,9 @@ __device__ __noinline__ void top_again(const Share &s, bool has_end, float end_z
 // One pass over each row: chunks of kU 16-byte vectors to a thread, the next one's loads out while one is summed.  A CTA or
 // a cluster takes rows in turn; a cluster's CTAs push their parts to CTA 0, which writes the row's outputs.
 //
-// Bound: HBM with many rows, 9,830 x 151,936 bf16 in 463 us (6,450 GB/s, 0.95 of a copy).  With alternatives the issue
-// rate: 2,458 x 50,304 bf16 take 49 us without, 68 with 10, 103 with 32 (14 instructions to a logit, not 8).  With few rows
-// latency: one row of 151,936 takes 5.4 us, 9 with five alternatives, of which the exchange and cold code are most.
+// Bound: HBM with many rows, 9,830 x 151,936 bf16 in 455 us (6,570 GB/s, 0.97 of a copy).  With alternatives the issue
+// rate: 2,458 x 50,304 bf16 take 46 us without, 67 with 10, 100 with 32 (14 instructions to a logit, not 8).  With few rows
+// latency: one row of 151,936 takes 4.3 us, 7.9 with five alternatives, of which the exchange and cold code are most.
 template <typename TIn, bool TOP, int NT, bool CLUSTER>
 __global__ void __launch_bounds__(NT, per_sm(TOP, NT)) k_logprobs(LogprobCall c, const int4 *__restrict__ rows,
                                                           const int32_t *__restrict__ nvalid)
@@ -531,8 +531,8 @@ __global__ void __launch_bounds__(NT, per_sm(TOP, NT)) k_logprobs(LogprobCall c,
     uint4 ahead[kU];
     int slot = 0;
     // Chunks before which the list is cut: powers of four where few rows are shared out and a cut's barriers count (64 fp32
-    // rows with 20 alternatives: 18.5 us, with powers of two 19.4), of two where many rows keep the SMs busy (2,458 rows x
-    // 50,304 with 32: 102 us and 109).  With many alternatives after the first too: its bound is a loose one.
+    // rows with 20 alternatives: 18.1 us, with powers of two 18.3), of two where many rows keep the SMs busy (2,458 rows x
+    // 50,304 with 32: 100 us and 107).  With many alternatives after the first too: its bound is a loose one.
     constexpr int kCuts = NT == 256 ? 0x55555555 : -1;
     const int first_cut = c.n_top > 16 ? 1 : NT == 256 ? 4 : 2;
     if (CLUSTER)
@@ -836,7 +836,7 @@ template <int N> __device__ __forceinline__ void st_once(__nv_bfloat16 *p, const
 // with its first loads, one item ahead.  Each logit is read before its place is written: grad may be the logits.
 // DIRECT: a loss mask without a list, looked at here.
 //
-// Bound: HBM.  4,915 x 151,936 bf16 in place, with the entropy's term: 444 us, 6,730 GB/s (0.99 of a copy).
+// Bound: HBM.  4,915 x 151,936 bf16 with the entropy's term: 445 us (6,710 GB/s, 0.99 of a copy), in place 450.
 template <typename TIn, typename TOut, bool ENT, bool DIRECT>
 __global__ void __launch_bounds__(kThreads, 4) k_logprobs_bwd(LogprobGradCall c, const int4 *__restrict__ rows,
                                                               const int32_t *__restrict__ nvalid)
@@ -929,8 +929,8 @@ __global__ void __launch_bounds__(kThreads, 4) k_logprobs_bwd(LogprobGradCall c,
 template <typename Call> struct Lists {
     int4 *rows = nullptr;
     int32_t *nvalid = nullptr;
-    // `direct`: a CTA to every token, which looks at the mask itself (64 bf16 rows x 151,936, 0.6 of them supervised: 8.2 us,
-    // with a list 12.0; the gradient of 64 x 1,024 fp32 3.0 and 6.7)
+    // `direct`: a CTA to every token, which looks at the mask itself (300 bf16 rows x 8,192, 0.6 of them supervised: 3.8 us,
+    // with a list 8.5; the gradient of 64 x 1,024 fp32 2.3 and 6.7)
     cudaError_t make(const Call &c, bool direct, cudaStream_t stream)
     {
         if (!c.mask || direct)
@@ -956,9 +956,9 @@ template <typename Call> struct Lists {
 };
 
 // Few rows: each is shared by a cluster of CTAs, so that the device's SMs all have some of it, up to 8 CTAs for 3 SMs.
-// Powers of two: 64 fp32 rows x 151,936 with 20 alternatives take 19 us with 4 CTAs to a row, 26 with 7; 200 bf16 rows 26
-// with 2, 29 with one.  The slices are two chunks long at least: below that the exchange costs more than it saves
-// (152 rows x 8,192: one CTA 4.2 us, two 5.0).
+// Powers of two: 64 fp32 rows x 151,936 with 20 alternatives take 18.1 us with 4 CTAs to a row, 19.8 with 2, 24.9 with 8;
+// 200 bf16 rows with ten 22.3 with 2, 23.6 with one.  The slices are a chunk long at least: below that the exchange costs
+// more than it saves (152 rows x 8,192: one CTA 3.4 us, two 4.2).
 int cluster_ctas(const LogprobCall &c)
 {
     const int64_t vecs = c.vocab / (c.in_dtype == TURNOPD_BF16 ? 8 : 4);
@@ -988,7 +988,7 @@ cudaError_t launch_fwd(const LogprobCall &c, int ctas, const int4 *rows, const i
 }
 
 // Rows enough for four CTAs on every SM: CTAs of 128 threads, of which one row's merge hides behind more of the others'
-// reads (5,000 rows x 8,192 bf16 with ten alternatives 46 us, with 256 threads 66; 2,458 x 50,304 67 and 88).
+// reads (5,000 rows x 8,192 bf16 with ten alternatives 38 us, with 256 threads 59; 2,458 x 50,304 67 and 81).
 template <typename TIn>
 cudaError_t launch_fwd(const LogprobCall &c, int ctas, const int4 *rows, const int32_t *nvalid, cudaStream_t stream)
 {

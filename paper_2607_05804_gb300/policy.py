@@ -3,7 +3,10 @@ entropies and alternatives, and the way back -- dL/dlogits, the LM head's and th
 term or an entropy bonus beside the distillation loss.
 
 The norm and everything about the logits run in libturnopd's kernels; the LM head's three products are plain matrix
-products.  Buffers are made once per batch shape, the gradient is written over the logits.
+products, whose results have the head's type: dL/dh too is rounded to it before the norm's backward pass.  A head is made for
+one batch: its mask's supervised tokens are counted on the host, and the logits have a row to each.  The gradient is
+written over the logits; log probabilities, entropies, alternatives, dgamma and dbeta are the head's own buffers, which the
+next call overwrites.
 """
 from __future__ import annotations
 
