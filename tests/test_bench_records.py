@@ -40,6 +40,15 @@ def test_source_hash_covers_the_kernel_sources():
         assert os.path.exists(os.path.join(ROOT, rel)), rel
 
 
+def test_records_are_of_the_current_sources():
+    """An edit of a hashed source takes the traffic out of bench.py's line until the record is captured again."""
+    b = load_bench()
+    for name, sources in (("row_kernel_traffic.json", b.ROW_KERNEL_SOURCES), ("topk_traffic.json", b.TOPK_KERNEL_SOURCES)):
+        with open(os.path.join(ROOT, "profiles", name)) as fh:
+            assert json.load(fh)["source_hash"] == b.source_hash(sources), name
+    assert b.committed_traffic("packed") > 0 and b.committed_traffic("packed", 1000, "topk") > 0
+
+
 def test_peak_falls_back_without_the_measured_file(monkeypatch, tmp_path):
     b = load_bench()
     monkeypatch.setattr(b, "ROOT", str(tmp_path))
