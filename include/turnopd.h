@@ -68,10 +68,13 @@ typedef enum {
 
 enum { TURNOPD_FULL_VOCAB = 0, TURNOPD_SAMPLED_TOKEN = 1 };       /* loss mode     */
 enum { TURNOPD_F32 = 0, TURNOPD_BF16 = 1 };                       /* element type  */
+enum { TURNOPD_E4M3 = 2, TURNOPD_INT8 = 3 };                      /* 8-bit codes of kept activations */
 enum { TURNOPD_SCOPE_TRAJ = 0, TURNOPD_SCOPE_BATCH = 1 };         /* normalisation */
 
 /* Write zeros into the gradient rows of masked tokens that own a row. */
 #define TURNOPD_ZERO_MASKED_GRAD 0x1u
+/* Add the gradient to what the output holds. */
+#define TURNOPD_ACCUMULATE_GRAD 0x2u
 /* Diagnostic: force the portable one-CTA-per-row kernel instead of the
  * cluster-resident kernel (results agree within the documented tolerance). */
 #define TURNOPD_FORCE_PORTABLE 0x100u
@@ -514,6 +517,150 @@ turnopd_status turnopd_norm_bwd(const void *x, int32_t x_dtype, int64_t ldx, con
                                 void *workspace, size_t workspace_bytes, turnopd_stream_t stream);
 
 size_t turnopd_norm_bwd_workspace_bytes(int64_t num_tokens, int64_t d);
+
+/*
+ * ---- From the token ids to the norm before the LM head ----
+ *
+ * What stands outside a policy model's matrix products on the other side of its blocks:
+ * the embedding, and the norms, gate and residual connection between two blocks.  `mask`
+ * is uint8[num_tokens] or NULL (every token takes part): rows of tokens with mask 0 (the
+ * padding of a batch, say) are not read, and their rows of the outputs are zero.  Columns
+ * [d, ld) of an output are not written, and outputs may not overlap inputs unless the
+ * entry says so.
+ *
+ * turnopd_embedding_fwd -- rows of an embedding table, scaled:
+ *   out[i, j] = scale w[token_ids[i], j]
+ * Inputs: w [vocab, ldw] row-major, w_dtype (F32 or BF16); token_ids int32[num_tokens];
+ *   scale finite (in fp32).
+ * Output: out [num_tokens, ldo] of out_dtype.
+ * Device errors: TURNOPD_ERR_TOKEN_RANGE (id outside [0, vocab): its row is zero).
+ */
+turnopd_status turnopd_embedding_fwd(const void *w, int32_t w_dtype, int64_t ldw, int64_t vocab,
+                                     const int32_t *token_ids, const uint8_t *mask, int64_t num_tokens,
+                                     int64_t d, double scale, void *out, int32_t out_dtype, int64_t ldo,
+                                     int32_t *dev_status, turnopd_stream_t stream);
+
+/*
+ * turnopd_embedding_bwd -- the table's gradient:
+ *   dw[v, j] = scale sum_{i : token_ids[i] = v} dout[i, j]
+ * Inputs: dout [num_tokens, ldg] of dout_dtype; token_ids, mask, scale as above.
+ * Output: dw [vocab, ldw] of dw_dtype: the whole table, zero where an id does not occur.
+ *   With TURNOPD_ACCUMULATE_GRAD the sums are added to dw (in fp32, rounded once), and
+ *   rows of ids that do not occur are neither read nor written: a head tied to the
+ *   embedding has its own gradient there already.
+ * Flags: TURNOPD_ACCUMULATE_GRAD only.
+ * Workspace: turnopd_embedding_bwd_workspace_bytes(num_tokens, d, vocab), 256-byte aligned.
+ * Device errors: TURNOPD_ERR_TOKEN_RANGE (token ignored).
+ * Precision: fp32 sums in a fixed order.
+ */
+turnopd_status turnopd_embedding_bwd(const void *dout, int32_t dout_dtype, int64_t ldg,
+                                     const int32_t *token_ids, const uint8_t *mask, int64_t num_tokens,
+                                     int64_t d, double scale, void *dw, int32_t dw_dtype, int64_t ldw,
+                                     int64_t vocab, uint32_t flags, void *workspace, size_t workspace_bytes,
+                                     int32_t *dev_status, turnopd_stream_t stream);
+
+size_t turnopd_embedding_bwd_workspace_bytes(int64_t num_tokens, int64_t d, int64_t vocab);
+
+/*
+ * turnopd_block_norm_fwd -- between a block and the next one: the norm of the block's
+ * output, its gate and scale, the residual connection, and the norm of the result that
+ * the next block reads.  For row r of the residual stream and y of the block's output:
+ *   b  = N_post(y)                                  (y itself without gamma_post)
+ *   r' = resid_scale r + branch_scale gate b        (gate 1 without one)
+ *   h  = N_pre(r')                                  (not computed without gamma_pre)
+ *   N(x)_j = (x_j - mu) rho gamma_j + beta_j, with mu and rho = 1 / sqrt(... + eps) of
+ *   `kind` as in turnopd_norm_fwd.
+ * Inputs:
+ *   resid [num_tokens, ldr] of resid_dtype, y [num_tokens, ldy] of y_dtype (F32 or BF16)
+ *   gamma_post, beta_post, gamma_pre, beta_pre  [d] of param_dtype or NULL (a beta needs
+ *     its gamma)
+ *   gate  NULL; [d] of param_dtype with ldg = 0; or [num_tokens, ldg] of y_dtype, a value
+ *     for every element
+ *   resid_scale, branch_scale finite (in fp32); kind and eps are those of both norms.
+ * Outputs:
+ *   resid_out [num_tokens, ldro] of resid_dtype: r'; may be resid (with its stride)
+ *   h_out     [num_tokens, ldh] of y_dtype; NULL without gamma_pre.  It is taken from r'
+ *             before r' is rounded to resid_dtype.
+ *   stats_out float32[num_tokens, 4], 16-byte aligned, or NULL: (mu, rho) of N_post and of
+ *             N_pre, which turnopd_block_norm_bwd takes; 0 where there is no such norm.
+ * Device errors (the token is treated as masked): TURNOPD_ERR_NONFINITE (a mu or rho is
+ *   not finite).
+ * Precision: fp32; the variance is summed over x - mu.
+ */
+turnopd_status turnopd_block_norm_fwd(const void *resid, int32_t resid_dtype, int64_t ldr, const void *y,
+                                      int32_t y_dtype, int64_t ldy, const void *gamma_post,
+                                      const void *beta_post, const void *gate, int64_t ldg,
+                                      const void *gamma_pre, const void *beta_pre, int32_t param_dtype,
+                                      const uint8_t *mask, int64_t num_tokens, int64_t d, int32_t kind,
+                                      double eps, double resid_scale, double branch_scale, void *resid_out,
+                                      int64_t ldro, void *h_out, int64_t ldh, float *stats_out,
+                                      int32_t *dev_status, turnopd_stream_t stream);
+
+/*
+ * turnopd_block_norm_bwd -- its backward pass.  With D = dr' + J_pre^T dh (the gradient
+ * of r' from the stream and through N_pre) and E = branch_scale gate D:
+ *   d_resid = resid_scale D,  dy = J_post^T E,  dgate = branch_scale b D,
+ *   dgamma_post[j] = sum_i E xh_post, dbeta_post[j] = sum_i E,
+ *   dgamma_pre[j]  = sum_i dh xh_pre, dbeta_pre[j]  = sum_i dh
+ * over the tokens that take part and whose statistics were finite (rho > 0); J^T as in
+ * turnopd_norm_bwd.
+ * Inputs:
+ *   resid    r' as the forward call wrote it, of resid_dtype: F32, BF16, or TURNOPD_E4M3 /
+ *            TURNOPD_INT8 codes that turnopd_act8_store made of it, with their exponents
+ *            resid_exps.  Read only if there is a gamma_pre.
+ *   y        the block's output, the same way; read only with gamma_post or dgate_out.
+ *   gamma_post, beta_post, gate, gamma_pre, mask, kind and the scales as in the forward
+ *            call (beta_post is read for dgate_out only); stats its stats_out (NULL will
+ *            do without norms)
+ *   dh       [num_tokens, lddh] of grad_y_dtype, needed with gamma_pre
+ *   d_resid_out [num_tokens, lddro] of grad_r_dtype: dr'; or NULL (0), with gamma_pre only
+ * Outputs (each nullable, but not all):
+ *   d_resid  [num_tokens, lddr] of grad_r_dtype; may be d_resid_out (with its stride)
+ *   dy_out   [num_tokens, lddy] of grad_y_dtype
+ *   dgate_out  float32[d] for a gate per channel, else [num_tokens, lddg] of grad_y_dtype
+ *   dgamma_post_out, dbeta_post_out, dgamma_pre_out, dbeta_pre_out  float32[d], only with
+ *            the norm they belong to (overwritten; fixed-order sums)
+ * A gate for every element is of grad_y_dtype here.
+ * Workspace: turnopd_block_norm_bwd_workspace_bytes(num_tokens, d), 256-byte aligned; NULL
+ *   and 0 will do where none of the float32[d] outputs is asked for.
+ */
+turnopd_status turnopd_block_norm_bwd(const void *resid, int32_t resid_dtype, int64_t ldr,
+                                      const uint8_t *resid_exps, const void *y, int32_t y_dtype, int64_t ldy,
+                                      const uint8_t *y_exps, const void *gamma_post, const void *beta_post,
+                                      const void *gate, int64_t ldg, const void *gamma_pre,
+                                      int32_t param_dtype, const uint8_t *mask, int64_t num_tokens, int64_t d,
+                                      int32_t kind, double resid_scale, double branch_scale,
+                                      const float *stats, int32_t grad_r_dtype, int32_t grad_y_dtype,
+                                      const void *dh, int64_t lddh, const void *d_resid_out, int64_t lddro,
+                                      void *d_resid, int64_t lddr, void *dy_out, int64_t lddy, void *dgate_out,
+                                      int64_t lddg, float *dgamma_post_out, float *dbeta_post_out,
+                                      float *dgamma_pre_out, float *dbeta_pre_out, void *workspace,
+                                      size_t workspace_bytes, turnopd_stream_t stream);
+
+size_t turnopd_block_norm_bwd_workspace_bytes(int64_t num_tokens, int64_t d);
+
+/*
+ * turnopd_act8_store -- puts activations away in 8 bits until the backward pass needs
+ * them.  32 columns of a row (the last group may have fewer) share an exponent k, the
+ * smallest integer of at least -126 with max |x| <= M 2^k (M = 448 for TURNOPD_E4M3, 127
+ * for TURNOPD_INT8); a code is x 2^-k rounded to the nearest one, ties to even.
+ * Inputs: x [num_tokens, ldx] of x_dtype (F32 or BF16).
+ * Outputs:
+ *   codes [num_tokens, ldc] bytes of code_dtype (TURNOPD_E4M3: one sign, four exponent,
+ *         three mantissa bits, no infinities; TURNOPD_INT8: two's complement)
+ *   exps  uint8[num_tokens, (d + 31) / 32], contiguous: k + 127; 0 for masked tokens.  A
+ *         group that holds NaN or inf gets 255 and codes of 0, and loads as NaN.
+ * Device errors: TURNOPD_ERR_NONFINITE (such a group).
+ *
+ * turnopd_act8_load -- takes them back: out[i, j] = code 2^k of out_dtype, exact in either
+ * type (what lies beyond the type's largest value becomes that value).
+ */
+turnopd_status turnopd_act8_store(const void *x, int32_t x_dtype, int64_t ldx, const uint8_t *mask,
+                                  int64_t num_tokens, int64_t d, void *codes, int32_t code_dtype, int64_t ldc,
+                                  uint8_t *exps, int32_t *dev_status, turnopd_stream_t stream);
+turnopd_status turnopd_act8_load(const void *codes, int32_t code_dtype, int64_t ldc, const uint8_t *exps,
+                                 int64_t num_tokens, int64_t d, void *out, int32_t out_dtype, int64_t ldo,
+                                 turnopd_stream_t stream);
 
 /*
  * ---- Adaptive rollout-depth controller and loss-allocation diagnostics ----

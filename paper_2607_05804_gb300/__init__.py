@@ -34,6 +34,10 @@ __all__ = [
     "TURNOPD_TOP_ALTERNATIVES_MAX", "TURNOPD_LAYER_NORM", "TURNOPD_RMS_NORM",
     "turnopd_token_logprobs", "turnopd_token_logprobs_bwd", "turnopd_token_logprobs_workspace_bytes",
     "turnopd_norm_fwd", "turnopd_norm_bwd", "turnopd_norm_bwd_workspace_bytes",
+    "TURNOPD_E4M3", "TURNOPD_INT8", "TURNOPD_ACCUMULATE_GRAD",
+    "turnopd_embedding_fwd", "turnopd_embedding_bwd", "turnopd_embedding_bwd_workspace_bytes",
+    "turnopd_block_norm_fwd", "turnopd_block_norm_bwd", "turnopd_block_norm_bwd_workspace_bytes",
+    "turnopd_act8_store", "turnopd_act8_load",
 ]
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -41,8 +45,10 @@ _LIB_PATH = os.path.join(_HERE, "libturnopd.so")
 
 TURNOPD_FULL_VOCAB, TURNOPD_SAMPLED_TOKEN = 0, 1
 TURNOPD_F32, TURNOPD_BF16 = 0, 1
+TURNOPD_E4M3, TURNOPD_INT8 = 2, 3
 TURNOPD_SCOPE_TRAJ, TURNOPD_SCOPE_BATCH = 0, 1
 TURNOPD_ZERO_MASKED_GRAD = 0x1
+TURNOPD_ACCUMULATE_GRAD = 0x2
 TURNOPD_FORCE_PORTABLE = 0x100
 TURNOPD_MAX_TURNS = 4096
 TURNOPD_STATIC_MAX_TOKENS = 65536
@@ -117,6 +123,14 @@ def load():
         "turnopd_norm_fwd": [P, i32, i64, P, P, i32, P, i64, i64, i32, f64, P, i32, i64, P, P, P, P],
         "turnopd_norm_bwd": [P, i32, i64, P, i32, P, i64, i64, i32, P, P, P, i32, i64, P, i32, i64, P, P, P, sz,
                              P],
+        "turnopd_embedding_fwd": [P, i32, i64, i64, P, P, i64, i64, f64, P, i32, i64, P, P],
+        "turnopd_embedding_bwd": [P, i32, i64, P, P, i64, i64, f64, P, i32, i64, i64, u32, P, sz, P, P],
+        "turnopd_block_norm_fwd": [P, i32, i64, P, i32, i64, P, P, P, i64, P, P, i32, P, i64, i64, i32, f64, f64, f64,
+                                   P, i64, P, i64, P, P, P],
+        "turnopd_block_norm_bwd": [P, i32, i64, P, P, i32, i64, P, P, P, P, i64, P, i32, P, i64, i64, i32, f64, f64, P,
+                                   i32, i32, P, i64, P, i64, P, i64, P, i64, P, i64, P, P, P, P, P, sz, P],
+        "turnopd_act8_store": [P, i32, i64, P, i64, i64, P, i32, i64, P, P, P],
+        "turnopd_act8_load": [P, i32, i64, P, i64, i64, P, i32, i64, P],
     })
     for name, args in sig.items():
         fn = getattr(lib, name)
@@ -139,6 +153,10 @@ def load():
     lib.turnopd_token_logprobs_workspace_bytes.restype = sz
     lib.turnopd_norm_bwd_workspace_bytes.argtypes = [i64, i64]
     lib.turnopd_norm_bwd_workspace_bytes.restype = sz
+    lib.turnopd_embedding_bwd_workspace_bytes.argtypes = [i64, i64, i64]
+    lib.turnopd_embedding_bwd_workspace_bytes.restype = sz
+    lib.turnopd_block_norm_bwd_workspace_bytes.argtypes = [i64, i64]
+    lib.turnopd_block_norm_bwd_workspace_bytes.restype = sz
     lib.turnopd_vocab_stats_bytes.argtypes = [i64]
     lib.turnopd_vocab_stats_bytes.restype = sz
     lib.turnopd_status_string.argtypes = [ctypes.c_int]
@@ -593,6 +611,207 @@ def turnopd_norm_bwd(x, gamma, loss_mask, kind, mean, rstd, dy, dx_out, dgamma_o
         _arg(dbeta_out, "dbeta_out", f32, d), _arg(workspace, "workspace"), _ws(workspace), _handle(stream, x))
     if code:
         raise TurnopdError(code, "turnopd_norm_bwd")
+
+
+# ---------------------------------------------------------------- from the token ids to the norm before the LM head
+
+def _rows_like(t, name, shape, dtype=None):
+    """Pointer and row stride of a 2-D CUDA tensor of a given shape and type (None stays None)."""
+    if t is None:
+        return None, shape[1]
+    ld = _rows_2d(t, name)
+    if t.shape != shape:
+        raise ValueError(f"{name} must have shape {tuple(shape)}, has {tuple(t.shape)}")
+    if dtype is not None and t.dtype is not dtype:
+        raise ValueError(f"{name} must have dtype {dtype}, got {t.dtype}")
+    return t.data_ptr(), ld
+
+
+def turnopd_embedding_fwd(w, token_ids, mask, scale, out, dev_status, stream=None):
+    """out[i] = scale w[token_ids[i]]: w [vocab, d], token_ids int32 [T], mask uint8 [T] or None (every token),
+    out [T, d]; rows of masked tokens are zero."""
+    import torch
+
+    T, (V, d) = token_ids.numel(), w.shape
+    ldw = _rows_2d(w, "w")
+    po, ldo = _rows_like(out, "out", (T, d))
+    code = load().turnopd_embedding_fwd(
+        w.data_ptr(), _dtype_code(w, "w"), ldw, V, _arg(token_ids, "token_ids", torch.int32, T),
+        _arg(mask, "mask", torch.uint8, T), T, d, float(scale), po, _dtype_code(out, "out"), ldo,
+        _arg(dev_status, "dev_status", torch.int32, 1), _handle(stream, w))
+    if code:
+        raise TurnopdError(code, "turnopd_embedding_fwd")
+
+
+def turnopd_embedding_bwd_workspace_bytes(num_tokens: int, d: int, vocab: int) -> int:
+    return int(load().turnopd_embedding_bwd_workspace_bytes(int(num_tokens), int(d), int(vocab)))
+
+
+def turnopd_embedding_bwd(dout, token_ids, mask, scale, dw, flags, workspace, dev_status, stream=None):
+    """dw [vocab, d] from dout [T, d]: the whole table, zeros included, or with TURNOPD_ACCUMULATE_GRAD added to the rows of
+    the ids that occur."""
+    import torch
+
+    T, (V, d) = token_ids.numel(), dw.shape
+    ldw = _rows_2d(dw, "dw")
+    pg, ldg = _rows_like(dout, "dout", (T, d))
+    code = load().turnopd_embedding_bwd(
+        pg, _dtype_code(dout, "dout"), ldg, _arg(token_ids, "token_ids", torch.int32, T), _arg(mask, "mask", torch.uint8, T),
+        T, d, float(scale), dw.data_ptr(), _dtype_code(dw, "dw"), ldw, V, int(flags), _arg(workspace, "workspace"),
+        _ws(workspace), _arg(dev_status, "dev_status", torch.int32, 1), _handle(stream, dw))
+    if code:
+        raise TurnopdError(code, "turnopd_embedding_bwd")
+
+
+def _gate_arg(gate, T, d, dtype, param_dtype, name="gate"):
+    """Pointer and stride of a gate: [d] (stride 0) or [T, d]."""
+    if gate is None:
+        return None, 0
+    if gate.dim() == 1:
+        return _arg(gate, name, param_dtype, d), 0
+    return _rows_like(gate, name, (T, d), dtype)
+
+
+def _param_dtype(*params):
+    """The dtype of the parameters that are given, which have to share one."""
+    import torch
+
+    types = {p.dtype for p in params if p is not None}
+    if len(types) > 1:
+        raise ValueError("the norms' parameters and a gate per channel must have one dtype")
+    t = types.pop() if types else torch.float32
+    if t is not torch.float32 and t is not torch.bfloat16:
+        raise ValueError("the norms' parameters and a gate per channel must be float32 or bfloat16")
+    return t
+
+
+def _code_of(dtype):
+    import torch
+
+    return TURNOPD_BF16 if dtype is torch.bfloat16 else TURNOPD_F32
+
+
+def turnopd_block_norm_fwd(resid, y, gamma_post, beta_post, gate, gamma_pre, beta_pre, mask, kind, eps, resid_scale,
+                           branch_scale, resid_out, h_out, stats_out, dev_status, stream=None):
+    """resid_out = resid_scale resid + branch_scale gate N_post(y) and h_out = N_pre(resid_out), all [T, d].  resid_out
+    has resid's type and may be resid, h_out has y's.  Vectors [d] or None: without gamma_post y is taken as it is, without
+    gamma_pre there is no h_out.  gate [d], [T, d] (of y's type) or None; mask uint8 [T] or None; stats_out float32 [T, 4]
+    or None."""
+    import torch
+
+    ldr, ldy = _rows_2d(resid, "resid"), _rows_2d(y, "y")
+    T, d = resid.shape
+    if y.shape != resid.shape:
+        raise ValueError("y must match resid in shape")
+    pt = _param_dtype(gamma_post, beta_post, gamma_pre, beta_pre, gate if gate is not None and gate.dim() == 1 else None)
+    pg, ldg = _gate_arg(gate, T, d, y.dtype, pt)
+    po, ldro = _rows_like(resid_out, "resid_out", resid.shape, resid.dtype)
+    ph, ldh = _rows_like(h_out, "h_out", resid.shape, y.dtype)
+    code = load().turnopd_block_norm_fwd(
+        resid.data_ptr(), _dtype_code(resid, "resid"), ldr, y.data_ptr(), _dtype_code(y, "y"), ldy,
+        _arg(gamma_post, "gamma_post", pt, d), _arg(beta_post, "beta_post", pt, d), pg, ldg,
+        _arg(gamma_pre, "gamma_pre", pt, d), _arg(beta_pre, "beta_pre", pt, d), _code_of(pt),
+        _arg(mask, "mask", torch.uint8, T), T, d, int(kind), float(eps), float(resid_scale), float(branch_scale), po, ldro,
+        ph, ldh, _arg(stats_out, "stats_out", torch.float32, 4 * T), _arg(dev_status, "dev_status", torch.int32, 1),
+        _handle(stream, resid))
+    if code:
+        raise TurnopdError(code, "turnopd_block_norm_fwd")
+
+
+def turnopd_block_norm_bwd_workspace_bytes(num_tokens: int, d: int) -> int:
+    return int(load().turnopd_block_norm_bwd_workspace_bytes(int(num_tokens), int(d)))
+
+
+def _kept(x, name, shape):
+    """Pointer, type code, row stride and exponents of an activation: a tensor, (codes, exponents), or None."""
+    import torch
+
+    if x is None:
+        return None, TURNOPD_F32, shape[1], None
+    if isinstance(x, (tuple, list)):
+        codes, exps = x
+        p, ld = _rows_like(codes, name, shape)
+        return p, _act8_code(codes, name), ld, _arg(exps, f"{name}'s exponents", torch.uint8, shape[0] * ((shape[1] + 31) // 32))
+    p, ld = _rows_like(x, name, shape)
+    return p, _dtype_code(x, name), ld, None
+
+
+def turnopd_block_norm_bwd(resid, y, gamma_post, beta_post, gate, gamma_pre, mask, kind, resid_scale, branch_scale, stats, dh,
+                           d_resid_out, d_resid, dy, dgate, dgamma_post, dbeta_post, dgamma_pre, dbeta_pre, workspace,
+                           stream=None):
+    """Gradients from dh and d_resid_out (either None where the forward call makes no h, or nothing comes back through the
+    residual stream).  resid (what the forward call wrote) and y are tensors [T, d] or the (codes, exponents) of
+    turnopd_act8_store, and None where nothing needs them.  d_resid [T, d] of d_resid_out's type (it may be d_resid_out), dy
+    and a gate's gradient for every element [T, d] of dh's; dgate [d] and the norms' gradients float32 [d]; each output
+    may be None."""
+    import torch
+
+    f32 = torch.float32
+    first = dh if dh is not None else d_resid_out
+    if first is None or first.dim() != 2:
+        raise ValueError("dh or d_resid_out must be a 2-D CUDA tensor")
+    T, d = shape = first.shape
+    channel = gate is not None and gate.dim() == 1
+    gy = next((t.dtype for t in (dh, dy, dgate if not channel else None, None if channel else gate) if t is not None), f32)
+    gr = next((t.dtype for t in (d_resid_out, d_resid) if t is not None), f32)
+    pt = _param_dtype(gamma_post, beta_post, gamma_pre, gate if channel else None)
+    pr, rcode, ldr, rexps = _kept(resid, "resid", shape)
+    py, ycode, ldy, yexps = _kept(y, "y", shape)
+    pg, ldg = _gate_arg(gate, T, d, gy, pt)
+    ph, lddh = _rows_like(dh, "dh", shape, gy)
+    pro, lddro = _rows_like(d_resid_out, "d_resid_out", shape, gr)
+    pdr, lddr = _rows_like(d_resid, "d_resid", shape, gr)
+    pdy, lddy = _rows_like(dy, "dy", shape, gy)
+    pdg, lddg = (_arg(dgate, "dgate", f32, d), 0) if channel else _rows_like(dgate, "dgate", shape, gy)
+    if not (gy in (f32, torch.bfloat16) and gr in (f32, torch.bfloat16)):
+        raise ValueError("gradients must be float32 or bfloat16")
+    code = load().turnopd_block_norm_bwd(
+        pr, rcode, ldr, rexps, py, ycode, ldy, yexps, _arg(gamma_post, "gamma_post", pt, d),
+        _arg(beta_post, "beta_post", pt, d), pg, ldg, _arg(gamma_pre, "gamma_pre", pt, d), _code_of(pt),
+        _arg(mask, "mask", torch.uint8, T), T, d, int(kind), float(resid_scale), float(branch_scale),
+        _arg(stats, "stats", f32, 4 * T), _code_of(gr), _code_of(gy), ph, lddh, pro, lddro, pdr, lddr, pdy, lddy, pdg, lddg,
+        _arg(dgamma_post, "dgamma_post", f32, d), _arg(dbeta_post, "dbeta_post", f32, d),
+        _arg(dgamma_pre, "dgamma_pre", f32, d), _arg(dbeta_pre, "dbeta_pre", f32, d), _arg(workspace, "workspace"),
+        _ws(workspace), _handle(stream, first))
+    if code:
+        raise TurnopdError(code, "turnopd_block_norm_bwd")
+
+
+def _act8_code(codes, name):
+    import torch
+
+    if codes.dtype is torch.float8_e4m3fn:
+        return TURNOPD_E4M3
+    if codes.dtype is torch.int8:
+        return TURNOPD_INT8
+    raise ValueError(f"{name}: codes must be float8_e4m3fn or int8")
+
+
+def turnopd_act8_store(x, mask, codes, exps, dev_status, stream=None):
+    """x [T, d] -> codes [T, d] (float8_e4m3fn or int8) and exps uint8 [T, ceil(d / 32)]: x is about codes 2^(exps - 127)."""
+    import torch
+
+    ldx, (T, d) = _rows_2d(x, "x"), x.shape
+    pc, ldc = _rows_like(codes, "codes", x.shape)
+    code = load().turnopd_act8_store(
+        x.data_ptr(), _dtype_code(x, "x"), ldx, _arg(mask, "mask", torch.uint8, T), T, d, pc, _act8_code(codes, "codes"), ldc,
+        _arg(exps, "exps", torch.uint8, T * ((d + 31) // 32)), _arg(dev_status, "dev_status", torch.int32, 1),
+        _handle(stream, x))
+    if code:
+        raise TurnopdError(code, "turnopd_act8_store")
+
+
+def turnopd_act8_load(codes, exps, out, stream=None):
+    """What codes and exps stand for, into out [T, d] (float32 or bfloat16)."""
+    import torch
+
+    ldc, (T, d) = _rows_2d(codes, "codes"), codes.shape
+    po, ldo = _rows_like(out, "out", codes.shape)
+    code = load().turnopd_act8_load(codes.data_ptr(), _act8_code(codes, "codes"), ldc,
+                                    _arg(exps, "exps", torch.uint8, T * ((d + 31) // 32)), T, d, po, _dtype_code(out, "out"),
+                                    ldo, _handle(stream, out))
+    if code:
+        raise TurnopdError(code, "turnopd_act8_load")
 
 
 # ---------------------------------------------------------------- rollout-depth controller (host)

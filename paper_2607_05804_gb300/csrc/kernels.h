@@ -268,4 +268,118 @@ size_t norm_bwd_workspace_bytes(int64_t T, int64_t d);
 cudaError_t launch_norm_fwd(const NormCall &c, cudaStream_t stream);
 cudaError_t launch_norm_bwd(const NormGradCall &c, cudaStream_t stream);
 
+// Norms around a block with its gate and residual connection (ldg 0: a gate per channel), and their backward pass.
+struct BlockCall {
+    const void *resid;
+    int32_t resid_dtype;
+    int64_t ldr;
+    const void *y;
+    int32_t y_dtype;
+    int64_t ldy;
+    const void *gamma_post, *beta_post, *gate;
+    int64_t ldg;
+    const void *gamma_pre, *beta_pre;
+    int32_t param_dtype;
+    const uint8_t *mask;
+    int64_t T, d;
+    int32_t kind;
+    float eps, resid_scale, branch_scale;
+    void *resid_out;
+    int64_t ldro;
+    void *h;
+    int64_t ldh;
+    float *stats;
+    int32_t *status;
+};
+
+struct BlockGradCall {
+    const void *resid;  // r', or its codes
+    int32_t resid_dtype;
+    int64_t ldr;
+    const uint8_t *resid_exps;
+    const void *y;  // or its codes
+    int32_t y_dtype;
+    int64_t ldy;
+    const uint8_t *y_exps;
+    const void *gamma_post, *beta_post, *gate;
+    int64_t ldg;
+    const void *gamma_pre;
+    int32_t param_dtype;
+    const uint8_t *mask;
+    int64_t T, d;
+    int32_t kind;
+    float resid_scale, branch_scale;
+    const float *stats;
+    int32_t grad_r_dtype, grad_y_dtype;  // of dr' and dr; of dh, dy, and a gate of its own for each token with its gradient
+    const void *dh;
+    int64_t lddh;
+    const void *d_resid_out;
+    int64_t lddro;
+    void *d_resid;
+    int64_t lddr;
+    void *dy;
+    int64_t lddy;
+    void *dgate;
+    int64_t lddg;
+    float *dgamma_post, *dbeta_post, *dgamma_pre, *dbeta_pre;
+    void *workspace;
+};
+
+size_t block_bwd_workspace_bytes(int64_t T, int64_t d);
+cudaError_t launch_block_fwd(const BlockCall &c, cudaStream_t stream);
+cudaError_t launch_block_bwd(const BlockGradCall &c, cudaStream_t stream);
+
+// Embedding lookup with scaling, and its gradient.
+struct EmbedCall {
+    const void *w;
+    int32_t w_dtype;
+    int64_t ldw, vocab;
+    const int32_t *ids;
+    const uint8_t *mask;
+    int64_t T, d;
+    float scale;
+    void *out;
+    int32_t out_dtype;
+    int64_t ldo;
+    int32_t *status;
+};
+
+struct EmbedGradCall {
+    const void *dout;
+    int32_t dout_dtype;
+    int64_t ldg;
+    const int32_t *ids;
+    const uint8_t *mask;
+    int64_t T, d;
+    float scale;
+    void *dw;
+    int32_t dw_dtype;
+    int64_t ldw, vocab;
+    bool accumulate;
+    void *workspace;
+    int32_t *status;
+};
+
+size_t embed_bwd_workspace_bytes(int64_t T, int64_t d, int64_t vocab);
+cudaError_t launch_embed(const EmbedCall &c, cudaStream_t stream);
+cudaError_t launch_embed_bwd(const EmbedGradCall &c, cudaStream_t stream);
+
+// Activations in 8 bits (x: stored from, out: loaded to).
+struct Act8Call {
+    const void *x;
+    void *out;
+    int32_t x_dtype;
+    int64_t ldx;
+    const uint8_t *mask;
+    int64_t T, d;
+    void *codes;
+    int32_t code_dtype;
+    int64_t ldc;
+    uint8_t *exps;
+    int32_t *status;
+};
+
+cudaError_t launch_act8_store(const Act8Call &c, cudaStream_t stream);
+cudaError_t launch_act8_load(const Act8Call &c, cudaStream_t stream);
+
 }  // namespace turnopd

@@ -9,6 +9,7 @@
 
 #include <algorithm>
 
+#include "columns.cuh"
 #include "common.cuh"
 #include "kernels.h"
 #include "packed.cuh"
@@ -20,12 +21,6 @@ constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
 constexpr int kE = 16;  // columns of a row that one thread holds
 constexpr int kMaxRow = 512 * kE;  // longest rows that a block holds
-
-__device__ __forceinline__ float param(const void *p, int32_t dtype, int64_t j)
-{
-    return dtype == TURNOPD_BF16 ? __bfloat162float(static_cast<const __nv_bfloat16 *>(p)[j])
-                                 : static_cast<const float *>(p)[j];
-}
 
 // Sum over the block in a fixed order, the same value in every thread.
 __device__ __forceinline__ float block_sum(float v, float *red)
@@ -40,41 +35,6 @@ __device__ __forceinline__ float block_sum(float v, float *red)
     for (int w = 1; w < kWarps; ++w)
         s += red[w];
     return s;
-}
-
-// Eight columns from or to 16-byte aligned memory.
-__device__ __forceinline__ void load8(const __nv_bfloat16 *p, float *v)
-{
-    const uint4 u = *reinterpret_cast<const uint4 *>(p);
-    v[0] = bf16lo(u.x), v[1] = bf16hi(u.x), v[2] = bf16lo(u.y), v[3] = bf16hi(u.y);
-    v[4] = bf16lo(u.z), v[5] = bf16hi(u.z), v[6] = bf16lo(u.w), v[7] = bf16hi(u.w);
-}
-__device__ __forceinline__ void load8(const float *p, float *v)
-{
-    const float4 a = reinterpret_cast<const float4 *>(p)[0], b = reinterpret_cast<const float4 *>(p)[1];
-    v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w;
-    v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
-}
-__device__ __forceinline__ void store8(__nv_bfloat16 *p, const float *v)
-{
-    __stcs(reinterpret_cast<uint4 *>(p), make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]),
-                                                    pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])));
-}
-__device__ __forceinline__ void store8(float *p, const float *v)
-{
-    __stcs(reinterpret_cast<float4 *>(p), make_float4(v[0], v[1], v[2], v[3]));
-    __stcs(reinterpret_cast<float4 *>(p) + 1, make_float4(v[4], v[5], v[6], v[7]));
-}
-__device__ __forceinline__ void cp16(void *smem, const void *gmem)
-{
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(smem)), "l"(gmem)
-                 : "memory");
-}
-
-// Barrier of the n threads of one group (barriers 1 .. 8; 0 is the block's).
-__device__ __forceinline__ void group_barrier(int group, int n)
-{
-    asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "r"(n) : "memory");
 }
 
 // ---------------------------------------------------------------- forward
@@ -722,19 +682,6 @@ template <typename TX, typename TDY> __global__ void __launch_bounds__(kThreads)
     }
 }
 
-// f(x type, second type) with values of the element types that two dtype codes name
-template <typename F> void with_types(int32_t a, int32_t b, F &&f)
-{
-    if (a == TURNOPD_BF16 && b == TURNOPD_BF16)
-        f(__nv_bfloat16(), __nv_bfloat16());
-    else if (a == TURNOPD_BF16)
-        f(__nv_bfloat16(), float());
-    else if (b == TURNOPD_BF16)
-        f(float(), __nv_bfloat16());
-    else
-        f(float(), float());
-}
-
 constexpr int kMaxGrid = 320;         // CTAs of the backward pass, at most
 constexpr int kLongParts = 64;        // partial sums of the kernels for long rows
 // Elements from which a loss mask is turned into a list of rows, two launches that take 5 us.  bf16 x, fp32 dy, 0.6 of the
@@ -762,14 +709,6 @@ struct Start {
     bool operator==(const Start &o) const { return at == o.at && step == o.step; }
     bool boundary() const { return at == 0 && step == 0; }
 };
-
-// Dynamic shared memory of a kernel up to `most`, the largest amount that any call of this kernel asks for: every call sets
-// the same limit, since another host thread's call may come between one that sets it and its launch.  (From 40 KB: with the
-// kernel's static shared memory it may pass the default limit of 48 KB.)
-template <typename K> cudaError_t allow_shared(K kernel, size_t most)
-{
-    return most > 40 * 1024 ? cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)most) : cudaSuccess;
-}
 
 template <typename X, typename Y, int N, int P> cudaError_t launch_fwd_rows(const NormCall &c, cudaStream_t stream)
 {

@@ -578,6 +578,183 @@ turnopd_status turnopd_norm_bwd(const void *x, int32_t x_dtype, int64_t ldx, con
     return cuda_status(launch_norm_bwd(c, s));
 }
 
+// Rows [T, ld] of d elements of an array that a call takes.
+static bool bad_rows(const void *p, size_t esz, int64_t ld, int64_t d) { return ld < d || misaligned(p, esz); }
+static bool bad_count(int64_t T, int64_t d) { return T < 0 || T > INT32_MAX || d < 1 || d > INT32_MAX; }
+static bool finite_f32(double x) { return std::isfinite((float)x); }
+static bool is_code(int32_t t) { return t == TURNOPD_E4M3 || t == TURNOPD_INT8; }
+static size_t stored_size(int32_t t) { return is_code(t) ? 1 : dtype_size(t); }
+
+turnopd_status turnopd_embedding_fwd(const void *w, int32_t w_dtype, int64_t ldw, int64_t vocab, const int32_t *token_ids,
+                                     const uint8_t *mask, int64_t num_tokens, int64_t d, double scale, void *out,
+                                     int32_t out_dtype, int64_t ldo, int32_t *dev_status, turnopd_stream_t stream)
+{
+    NvtxRange nvtx("turnopd_embedding_fwd");
+    if (!dev_status || (num_tokens > 0 && (!w || !token_ids || !out)))
+        return TURNOPD_ERR_NULL;
+    if (!is_dtype(w_dtype) || !is_dtype(out_dtype))
+        return TURNOPD_ERR_UNSUPPORTED;
+    if (bad_count(num_tokens, d) || vocab < 1 || vocab > INT32_MAX || bad_rows(w, dtype_size(w_dtype), ldw, d) ||
+        bad_rows(out, dtype_size(out_dtype), ldo, d) || misaligned(token_ids, 4) || !finite_f32(scale))
+        return TURNOPD_ERR_SHAPE;
+    if (num_tokens == 0)
+        return TURNOPD_OK;
+    EmbedCall c{w, w_dtype, ldw, vocab, token_ids, mask, num_tokens, d, (float)scale, out, out_dtype, ldo, dev_status};
+    return cuda_status(launch_embed(c, (cudaStream_t)stream));
+}
+
+size_t turnopd_embedding_bwd_workspace_bytes(int64_t num_tokens, int64_t d, int64_t vocab)
+{
+    if (bad_count(num_tokens, d) || vocab < 1 || vocab > INT32_MAX)
+        return 0;
+    return embed_bwd_workspace_bytes(num_tokens, d, vocab);
+}
+
+turnopd_status turnopd_embedding_bwd(const void *dout, int32_t dout_dtype, int64_t ldg, const int32_t *token_ids,
+                                     const uint8_t *mask, int64_t num_tokens, int64_t d, double scale, void *dw,
+                                     int32_t dw_dtype, int64_t ldw, int64_t vocab, uint32_t flags, void *workspace,
+                                     size_t workspace_bytes, int32_t *dev_status, turnopd_stream_t stream)
+{
+    NvtxRange nvtx("turnopd_embedding_bwd");
+    if (!dev_status || !dw || (num_tokens > 0 && (!dout || !token_ids)))
+        return TURNOPD_ERR_NULL;
+    if (!is_dtype(dout_dtype) || !is_dtype(dw_dtype) || (flags & ~(uint32_t)TURNOPD_ACCUMULATE_GRAD))
+        return TURNOPD_ERR_UNSUPPORTED;
+    if (bad_count(num_tokens, d) || vocab < 1 || vocab > INT32_MAX || bad_rows(dout, dtype_size(dout_dtype), ldg, d) ||
+        bad_rows(dw, dtype_size(dw_dtype), ldw, d) || misaligned(token_ids, 4) || !finite_f32(scale))
+        return TURNOPD_ERR_SHAPE;
+    if (!workspace || misaligned(workspace, 256) || workspace_bytes < embed_bwd_workspace_bytes(num_tokens, d, vocab))
+        return TURNOPD_ERR_WORKSPACE;
+    const bool accumulate = (flags & TURNOPD_ACCUMULATE_GRAD) != 0;
+    if (num_tokens == 0 && accumulate)
+        return TURNOPD_OK;
+    EmbedGradCall c{dout, dout_dtype, ldg, token_ids, mask, num_tokens, d, (float)scale, dw, dw_dtype, ldw, vocab, accumulate,
+                    workspace, dev_status};
+    return cuda_status(launch_embed_bwd(c, (cudaStream_t)stream));
+}
+
+turnopd_status turnopd_block_norm_fwd(const void *resid, int32_t resid_dtype, int64_t ldr, const void *y, int32_t y_dtype,
+                                      int64_t ldy, const void *gamma_post, const void *beta_post, const void *gate,
+                                      int64_t ldg, const void *gamma_pre, const void *beta_pre, int32_t param_dtype,
+                                      const uint8_t *mask, int64_t num_tokens, int64_t d, int32_t kind, double eps,
+                                      double resid_scale, double branch_scale, void *resid_out, int64_t ldro, void *h_out,
+                                      int64_t ldh, float *stats_out, int32_t *dev_status, turnopd_stream_t stream)
+{
+    NvtxRange nvtx("turnopd_block_norm_fwd");
+    if (!dev_status || (num_tokens > 0 && (!resid || !y || !resid_out || (gamma_pre && !h_out))))
+        return TURNOPD_ERR_NULL;
+    if (!is_dtype(resid_dtype) || !is_dtype(y_dtype) || !is_dtype(param_dtype) ||
+        (kind != TURNOPD_LAYER_NORM && kind != TURNOPD_RMS_NORM) || (beta_post && !gamma_post) || (beta_pre && !gamma_pre) ||
+        (h_out && !gamma_pre) || (resid_out == resid && resid && ldro != ldr))
+        return TURNOPD_ERR_UNSUPPORTED;
+    const size_t rs = dtype_size(resid_dtype), ys = dtype_size(y_dtype), ps = dtype_size(param_dtype);
+    if (bad_count(num_tokens, d) || bad_rows(resid, rs, ldr, d) || bad_rows(y, ys, ldy, d) || bad_rows(resid_out, rs, ldro, d) ||
+        (gamma_pre && bad_rows(h_out, ys, ldh, d)) || (gate && (ldg ? bad_rows(gate, ys, ldg, d) : misaligned(gate, ps))) ||
+        misaligned(gamma_post, ps) || misaligned(beta_post, ps) || misaligned(gamma_pre, ps) || misaligned(beta_pre, ps) ||
+        misaligned(stats_out, 16) || !(eps >= 0.0 && eps <= 3e38) || !finite_f32(resid_scale) || !finite_f32(branch_scale))
+        return TURNOPD_ERR_SHAPE;
+    if (num_tokens == 0)
+        return TURNOPD_OK;
+    BlockCall c{resid, resid_dtype, ldr, y, y_dtype, ldy, gamma_post, beta_post, gate, gate ? ldg : 0, gamma_pre, beta_pre,
+                param_dtype, mask, num_tokens, d, kind, (float)eps, (float)resid_scale, (float)branch_scale, resid_out, ldro,
+                h_out, ldh, stats_out, dev_status};
+    return cuda_status(launch_block_fwd(c, (cudaStream_t)stream));
+}
+
+size_t turnopd_block_norm_bwd_workspace_bytes(int64_t num_tokens, int64_t d)
+{
+    return bad_count(num_tokens, d) ? 0 : block_bwd_workspace_bytes(num_tokens, d);
+}
+
+turnopd_status turnopd_block_norm_bwd(const void *resid, int32_t resid_dtype, int64_t ldr, const uint8_t *resid_exps,
+                                      const void *y, int32_t y_dtype, int64_t ldy, const uint8_t *y_exps,
+                                      const void *gamma_post, const void *beta_post, const void *gate, int64_t ldg,
+                                      const void *gamma_pre, int32_t param_dtype, const uint8_t *mask, int64_t num_tokens,
+                                      int64_t d, int32_t kind, double resid_scale, double branch_scale, const float *stats,
+                                      int32_t grad_r_dtype, int32_t grad_y_dtype, const void *dh, int64_t lddh,
+                                      const void *d_resid_out, int64_t lddro, void *d_resid, int64_t lddr, void *dy_out,
+                                      int64_t lddy, void *dgate_out, int64_t lddg, float *dgamma_post_out,
+                                      float *dbeta_post_out, float *dgamma_pre_out, float *dbeta_pre_out, void *workspace,
+                                      size_t workspace_bytes, turnopd_stream_t stream)
+{
+    NvtxRange nvtx("turnopd_block_norm_bwd");
+    const bool channel = gate && ldg == 0;
+    const bool sums = dgamma_post_out || dbeta_post_out || dgamma_pre_out || dbeta_pre_out || (dgate_out && channel);
+    const bool needs_y = gamma_post || dgate_out;
+    if (!d_resid && !dy_out && !dgate_out && !sums)
+        return TURNOPD_ERR_NULL;
+    if (num_tokens > 0 &&
+        ((gamma_pre && (!resid || !dh || (is_code(resid_dtype) && !resid_exps))) || (!gamma_pre && !d_resid_out) ||
+         (needs_y && (!y || (is_code(y_dtype) && !y_exps))) || ((gamma_pre || gamma_post) && !stats)))
+        return TURNOPD_ERR_NULL;
+    if ((!is_dtype(resid_dtype) && !is_code(resid_dtype)) || (!is_dtype(y_dtype) && !is_code(y_dtype)) ||
+        !is_dtype(param_dtype) || !is_dtype(grad_r_dtype) || !is_dtype(grad_y_dtype) ||
+        (kind != TURNOPD_LAYER_NORM && kind != TURNOPD_RMS_NORM) || (beta_post && !gamma_post) || (dgate_out && !gate) ||
+        ((dgamma_post_out || dbeta_post_out) && !gamma_post) || ((dgamma_pre_out || dbeta_pre_out) && !gamma_pre) ||
+        (dh && !gamma_pre) || (d_resid == d_resid_out && d_resid && lddr != lddro))
+        return TURNOPD_ERR_UNSUPPORTED;
+    const size_t gr = dtype_size(grad_r_dtype), gy = dtype_size(grad_y_dtype), ps = dtype_size(param_dtype);
+    if (bad_count(num_tokens, d) || (gamma_pre && bad_rows(resid, stored_size(resid_dtype), ldr, d)) ||
+        (needs_y && bad_rows(y, stored_size(y_dtype), ldy, d)) || (gamma_pre && bad_rows(dh, gy, lddh, d)) ||
+        (d_resid_out && bad_rows(d_resid_out, gr, lddro, d)) || (d_resid && bad_rows(d_resid, gr, lddr, d)) ||
+        (dy_out && bad_rows(dy_out, gy, lddy, d)) || (gate && (channel ? misaligned(gate, ps) : bad_rows(gate, gy, ldg, d))) ||
+        (dgate_out && (channel ? misaligned(dgate_out, 4) : bad_rows(dgate_out, gy, lddg, d))) ||
+        misaligned(gamma_post, ps) || misaligned(beta_post, ps) || misaligned(gamma_pre, ps) || misaligned(stats, 16) ||
+        misaligned(dgamma_post_out, 4) || misaligned(dbeta_post_out, 4) || misaligned(dgamma_pre_out, 4) ||
+        misaligned(dbeta_pre_out, 4) || !finite_f32(resid_scale) || !finite_f32(branch_scale))
+        return TURNOPD_ERR_SHAPE;
+    if (sums && (!workspace || misaligned(workspace, 256) || workspace_bytes < block_bwd_workspace_bytes(num_tokens, d)))
+        return TURNOPD_ERR_WORKSPACE;
+    cudaStream_t s = (cudaStream_t)stream;
+    if (num_tokens == 0) {
+        cudaError_t e = cudaSuccess;
+        for (void *p : {(void *)dgamma_post_out, (void *)dbeta_post_out, (void *)dgamma_pre_out, (void *)dbeta_pre_out,
+                        channel ? dgate_out : nullptr})
+            if (p && e == cudaSuccess)
+                e = cudaMemsetAsync(p, 0, sizeof(float) * (size_t)d, s);
+        return cuda_status(e);
+    }
+    BlockGradCall c{resid, resid_dtype, ldr, resid_exps, y, y_dtype, ldy, y_exps, gamma_post, beta_post, gate, gate ? ldg : 0,
+                    gamma_pre, param_dtype, mask, num_tokens, d, kind, (float)resid_scale, (float)branch_scale, stats,
+                    grad_r_dtype, grad_y_dtype, dh, lddh, d_resid_out, lddro, d_resid, lddr, dy_out, lddy, dgate_out, lddg,
+                    dgamma_post_out, dbeta_post_out, dgamma_pre_out, dbeta_pre_out, workspace};
+    return cuda_status(launch_block_bwd(c, s));
+}
+
+turnopd_status turnopd_act8_store(const void *x, int32_t x_dtype, int64_t ldx, const uint8_t *mask, int64_t num_tokens,
+                                  int64_t d, void *codes, int32_t code_dtype, int64_t ldc, uint8_t *exps,
+                                  int32_t *dev_status, turnopd_stream_t stream)
+{
+    NvtxRange nvtx("turnopd_act8_store");
+    if (!dev_status || (num_tokens > 0 && (!x || !codes || !exps)))
+        return TURNOPD_ERR_NULL;
+    if (!is_dtype(x_dtype) || !is_code(code_dtype))
+        return TURNOPD_ERR_UNSUPPORTED;
+    if (bad_count(num_tokens, d) || bad_rows(x, dtype_size(x_dtype), ldx, d) || ldc < d)
+        return TURNOPD_ERR_SHAPE;
+    if (num_tokens == 0)
+        return TURNOPD_OK;
+    Act8Call c{x, nullptr, x_dtype, ldx, mask, num_tokens, d, codes, code_dtype, ldc, exps, dev_status};
+    return cuda_status(launch_act8_store(c, (cudaStream_t)stream));
+}
+
+turnopd_status turnopd_act8_load(const void *codes, int32_t code_dtype, int64_t ldc, const uint8_t *exps, int64_t num_tokens,
+                                 int64_t d, void *out, int32_t out_dtype, int64_t ldo, turnopd_stream_t stream)
+{
+    NvtxRange nvtx("turnopd_act8_load");
+    if (num_tokens > 0 && (!codes || !exps || !out))
+        return TURNOPD_ERR_NULL;
+    if (!is_dtype(out_dtype) || !is_code(code_dtype))
+        return TURNOPD_ERR_UNSUPPORTED;
+    if (bad_count(num_tokens, d) || bad_rows(out, dtype_size(out_dtype), ldo, d) || ldc < d)
+        return TURNOPD_ERR_SHAPE;
+    if (num_tokens == 0)
+        return TURNOPD_OK;
+    Act8Call c{nullptr, out, out_dtype, ldo, nullptr, num_tokens, d, const_cast<void *>(codes), code_dtype, ldc,
+               const_cast<uint8_t *>(exps), nullptr};
+    return cuda_status(launch_act8_load(c, (cudaStream_t)stream));
+}
+
 turnopd_status turnopd_turn_stats(const float *token_loss, const int32_t *turn_id,
                                   const uint8_t *loss_mask, const int64_t *traj_offsets,
                                   int32_t num_traj, int64_t num_tokens, int32_t max_turns,
