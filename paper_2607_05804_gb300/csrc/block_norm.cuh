@@ -1,0 +1,106 @@
+// What the kernels of the norms around a block share.
+#pragma once
+
+#include <initializer_list>
+
+#include "columns.cuh"
+#include "common.cuh"
+#include "kernels.h"
+#include "packed.cuh"
+
+namespace turnopd {
+
+constexpr int kBlockMaxRow = 8192;   // longest rows that a block of threads holds
+constexpr int kBlockMaxParts = 320;  // CTAs of the backward pass, at most
+
+__device__ __forceinline__ float2 warp_sum2(float2 v)
+{
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1)
+        v = fadd2(v, make_float2(__shfl_xor_sync(~0u, v.x, o), __shfl_xor_sync(~0u, v.y, o)));
+    return v;
+}
+
+// Sum over the `warps` warps of a group, the same values in every thread; red: an entry per warp of the block, free again
+// two sums later.
+__device__ __forceinline__ float2 group_sum2(float2 v, float2 *red, int group, int warps)
+{
+    v = warp_sum2(v);
+    if (warps == 1)
+        return v;
+    const int first = group * warps;
+    if ((threadIdx.x & 31) == 0)
+        red[threadIdx.x >> 5] = v;
+    group_barrier(group, warps * 32);
+    v = red[first];
+    for (int w = 1; w < warps; ++w)
+        v = fadd2(v, red[first + w]);
+    return v;
+}
+
+// Column j of row i of an array of any type; 8-bit codes with their exponents.
+__device__ __forceinline__ float element(const void *p, int32_t dtype, int64_t ld, const uint8_t *exps, int64_t d, int64_t i, int64_t j)
+{
+    if (dtype == TURNOPD_BF16 || dtype == TURNOPD_F32)
+        return param(p, dtype, i * ld + j);
+    const uint8_t b = static_cast<const uint8_t *>(p)[i * ld + j];
+    const float s = act_scale(exps[i * ((d + kActGroup - 1) / kActGroup) + j / kActGroup]);
+    return (dtype == TURNOPD_E4M3 ? decode_e4m3(b) : (float)(int8_t)b) * s;
+}
+
+__device__ __forceinline__ void put(void *p, int32_t dtype, int64_t at, float v)
+{
+    if (dtype == TURNOPD_BF16)
+        static_cast<__nv_bfloat16 *>(p)[at] = __float2bfloat16_rn(v);
+    else
+        static_cast<float *>(p)[at] = v;
+}
+
+// Whether row i takes part: supervised, and its statistics were finite.
+__device__ __forceinline__ bool takes_part(const BlockGradCall &c, int64_t i, float4 &stats)
+{
+    if (c.mask && !c.mask[i])
+        return false;
+    stats = c.stats ? reinterpret_cast<const float4 *>(c.stats)[i] : make_float4(0.f, 0.f, 0.f, 0.f);
+    return (!c.gamma_post || stats.y > 0.f) && (!c.gamma_pre || stats.w > 0.f);
+}
+
+inline int stored_bytes(int32_t dtype) { return dtype == TURNOPD_F32 ? 4 : dtype == TURNOPD_BF16 ? 2 : 1; }
+
+// The element of a group of eight at which row 0 of an array begins, and by how many the next row begins later.  Where they
+// are 0 each row begins at a boundary that eight columns can be copied from (16 bytes, 8 for codes).
+struct Phase {
+    bool given;
+    int at, step;
+    Phase(const void *p, int64_t ld, int32_t dtype)
+        : given(p), at((int)(reinterpret_cast<uintptr_t>(p) / stored_bytes(dtype) & 7)), step((int)(ld & 7))
+    {
+    }
+};
+
+// The phase that all arrays of a call share, if they do.
+struct Phases {
+    bool alike = true;
+    int at = 0, step = 0;
+    Phases(std::initializer_list<Phase> all)
+    {
+        bool first = true;
+        for (const Phase &p : all) {
+            if (!p.given)
+                continue;
+            if (first)
+                at = p.at, step = p.step;
+            alike = alike && p.at == at && p.step == step;
+            first = false;
+        }
+    }
+};
+
+// The row kernels of the backward pass, by the types of dr' and of dh; *parts: rows of partial sums that they leave in the
+// workspace, 4 d floats each (dh xh_pre, dh, X xh_post, X; the second and fourth only where block_bwd_bias says).  *taken:
+// whether they take such rows.
+bool block_bwd_bias(const BlockGradCall &c);
+template <typename TR, typename TY>
+cudaError_t launch_block_rows_bwd(const BlockGradCall &c, int *parts, bool *taken, cudaStream_t stream);
+
+}  // namespace turnopd

@@ -263,6 +263,19 @@ def test_many_rows_masks_and_in_place(d):
             assert o[name] is None or torch.equal(o[name], p[name]), name
 
 
+@pytest.mark.parametrize("d", [64, 1001, 4096])
+def test_arrays_of_different_strides(d):
+    """Rows that begin at different elements in different arrays: the results are the same numbers."""
+    for gate, kind in (("channel", RMS), ("token", LAYER)):
+        c = case(150, d, (BF, BF, F, 0, 0), gate=gate, kind=kind, masked=0.2)
+        c.y = strided(150, d, d + 3, 1, BF).copy_(c.y)
+        out = c.forward()
+        c.check_forward(*out)
+        c.dh = strided(150, d, d + 5, 0, BF).copy_(c.dh)
+        o = c.backward(out[0], c.y, out[2])
+        c.check_backward(o, out[0], c.y, out[2])
+
+
 @pytest.mark.parametrize("code", [E4M3, INT8])
 @pytest.mark.parametrize("T,d,pad", [(1, 32, 0), (5, 33, 0), (40, 1001, 0), (300, 4096, 0), (300, 4096, 16), (200, 5120, 0), (7, 8192, 0),
                                      (3, 9000, 0), (64, 520, 0), (64, 520, 3)])
