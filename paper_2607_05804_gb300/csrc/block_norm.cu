@@ -99,236 +99,6 @@ __global__ void __launch_bounds__(kThreads) k_block_fwd_long(BlockCall c)
     }
 }
 
-// ---------------------------------------------------------------- forward, rows that a block's threads hold
-
-// Eight columns of a row as they are stored.
-template <typename T> struct Raw8 {
-    static constexpr int kWords = sizeof(T) / 2;  // of 16 bytes
-    uint4 w[kWords];
-    __device__ void load(const T *p)
-    {
-#pragma unroll
-        for (int k = 0; k < kWords; ++k)
-            w[k] = __ldcs(reinterpret_cast<const uint4 *>(p) + k);
-    }
-    __device__ void clear()
-    {
-#pragma unroll
-        for (int k = 0; k < kWords; ++k)
-            w[k] = make_uint4(0u, 0u, 0u, 0u);
-    }
-    __device__ float2 pair(int e) const
-    {
-        if constexpr (sizeof(T) == 2)
-            return unpack2(word(w[0], e));
-        else
-            return make_float2(__uint_as_float(word(w[e / 2], 2 * (e & 1))), __uint_as_float(word(w[e / 2], 2 * (e & 1) + 1)));
-    }
-};
-
-// n threads take a row, P pieces of eight columns to a thread, kept as they were read until r' is there; then the loads of
-// the group's next row go out, and that row's bytes arrive while this one's second norm is taken and its results are written.
-// ENDS: the rows begin anywhere, but in all arrays at the same element of a group of eight: pieces from the row's first
-// boundary on, and the first threads one of the elements before and after them each.  The parameters come from the L1 cache.
-template <typename TR, typename TY, int P, bool GATE, bool ENDS, int MOST, int PER_SM>
-__global__ void __launch_bounds__(MOST, PER_SM) k_block_fwd(BlockCall c, int n, bool vector_params, int phase, int phase_step)
-{
-    __shared__ float2 red[4][32];
-    const int t = threadIdx.x % n, group = threadIdx.x / n, warps = n / 32, per = blockDim.x / n, d = (int)c.d;
-    const int64_t groups = (int64_t)gridDim.x * per;
-    const bool layer = c.kind == TURNOPD_LAYER_NORM, pre = c.gamma_pre, post = c.gamma_post;
-    const float inv_d = 1.f / (float)d;
-    int sums = 0;  // taken so far: the next one's place in `red`, which is free again two sums later
-    Raw8<TR> r[P];
-    Raw8<TY> y[P], g[GATE ? P : 1];
-    float re = 0.f, ye = 0.f, ge = 0.f;
-    bool on = false;
-    struct Place {
-        int head, whole, ends, end;
-    };
-    const auto place = [&](int64_t i) {
-        Place p;
-        p.head = ENDS ? min((8 - (int)((phase + i * phase_step) & 7)) & 7, d) : 0;
-        p.whole = (d - p.head) / 8;
-        p.ends = ENDS ? d - p.whole * 8 : 0;
-        p.end = t < p.head ? t : p.whole * 8 + t;  // the single column of this thread, where t < ends
-        return p;
-    };
-    const auto load = [&](int64_t i, const Place &at) {
-        on = i < c.T && (!c.mask || c.mask[i]);
-        const TR *rr = static_cast<const TR *>(c.resid) + i * c.ldr;
-        const TY *yy = static_cast<const TY *>(c.y) + i * c.ldy, *gg = static_cast<const TY *>(c.gate) + i * c.ldg;
-#pragma unroll
-        for (int k = 0; k < P; ++k) {
-            const int j = at.head + (k * n + t) * 8;
-            if (on && k * n + t < at.whole) {
-                y[k].load(yy + j);
-                r[k].load(rr + j);
-                if (GATE)
-                    g[GATE ? k : 0].load(gg + j);
-            } else {
-                r[k].clear();
-                y[k].clear();
-                if (GATE)
-                    g[GATE ? k : 0].clear();
-            }
-        }
-        if (ENDS) {
-            const bool there = on && t < at.ends;
-            re = there ? to_float(rr[at.end]) : 0.f;
-            ye = there ? to_float(yy[at.end]) : 0.f;
-            ge = GATE && there ? to_float(gg[at.end]) : 0.f;
-        }
-    };
-    int64_t i = (int64_t)blockIdx.x * per + group;
-    Place at = place(i);
-    load(i, at);
-    for (; i < c.T; i += groups) {
-        const auto there = [&](int k) { return k * n + t < at.whole; };
-        const auto column = [&](int k) { return at.head + (k * n + t) * 8; };
-        const bool at_end = ENDS && t < at.ends;
-        // columns of piece k of a parameter
-        const auto parameter = [&](const void *p, int k, float2 *v) {
-            float *f = reinterpret_cast<float *>(v);
-            if (!there(k)) {
-                v[0] = v[1] = v[2] = v[3] = make_float2(0.f, 0.f);
-            } else if (!ENDS && vector_params) {
-                if (c.param_dtype == TURNOPD_BF16)
-                    load8(static_cast<const __nv_bfloat16 *>(p) + column(k), f);
-                else
-                    load8(static_cast<const float *>(p) + column(k), f);
-            } else {
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    f[e] = param(p, c.param_dtype, column(k) + e);
-            }
-        };
-        // mu and rho of the columns that x(k, e) gives in pairs, and of a single one; missing columns are zeros.  The sums are
-        // taken for rows that do not take part too: no barrier stands under a condition that every thread reads from the
-        // caller's memory for itself.
-        const auto statistics = [&](const auto &x, float xe, float &mu, float &rho) {
-            mu = 0.f;
-            if (layer) {
-                float2 s = make_float2(xe, 0.f);
-#pragma unroll
-                for (int k = 0; k < P; ++k)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        s = fadd2(s, x(k, e));
-                // divided, not times 1/d: a sum that is exact (a row of equal numbers) has its exact mean
-                mu = group_sum2(make_float2(s.x + s.y, 0.f), red[sums++ & 3], group, warps).x / (float)d;
-            }
-            float2 q = make_float2(at_end ? (xe - mu) * (xe - mu) : 0.f, 0.f);
-#pragma unroll
-            for (int k = 0; k < P; ++k)
-                if (there(k))
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const float2 v = fadd2(x(k, e), splat(-mu));
-                        q = ffma2(v, v, q);
-                    }
-            rho = 1.f / sqrtf(group_sum2(make_float2(q.x + q.y, 0.f), red[sums++ & 3], group, warps).x * inv_d + c.eps);
-            return isfinite(mu) && isfinite(rho) && rho > 0.f;
-        };
-        bool fine = on;
-        float mu0 = 0.f, rho0 = 0.f, mu1 = 0.f, rho1 = 0.f;
-        if (post)
-            fine = statistics([&](int k, int e) { return y[k].pair(e); }, ye, mu0, rho0) && fine;
-        float2 v[P][4];
-#pragma unroll
-        for (int k = 0; k < P; ++k) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                v[k][e] = y[k].pair(e);
-            float2 a[4];
-            if (post) {
-                parameter(c.gamma_post, k, a);
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    v[k][e] = fmul2(fmul2(fadd2(v[k][e], splat(-mu0)), splat(rho0)), a[e]);
-                if (c.beta_post) {
-                    parameter(c.beta_post, k, a);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        v[k][e] = fadd2(v[k][e], a[e]);
-                }
-            }
-            if (GATE) {
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    v[k][e] = fmul2(v[k][e], g[GATE ? k : 0].pair(e));
-            } else if (c.gate) {
-                parameter(c.gate, k, a);
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    v[k][e] = fmul2(v[k][e], a[e]);
-            }
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                v[k][e] = ffma2(v[k][e], splat(c.branch_scale), fmul2(r[k].pair(e), splat(c.resid_scale)));
-        }
-        float ve = 0.f;
-        if (at_end) {
-            ve = ye;
-            if (post)
-                ve = fmaf((ve - mu0) * rho0, param(c.gamma_post, c.param_dtype, at.end),
-                          c.beta_post ? param(c.beta_post, c.param_dtype, at.end) : 0.f);
-            if (GATE)
-                ve *= ge;
-            else if (c.gate)
-                ve *= param(c.gate, c.param_dtype, at.end);
-            ve = fmaf(ve, c.branch_scale, re * c.resid_scale);
-        }
-        const bool took_part = on;
-        const Place next = ENDS ? place(i + groups) : at;
-        load(i + groups, next);
-        if (pre) {
-            const bool finite = statistics([&](int k, int e) { return v[k][e]; }, ve, mu1, rho1);
-            fine = finite && fine;
-        }
-        if (took_part && !fine && t == 0)
-            set_status(c.status, TURNOPD_ERR_NONFINITE);
-        TR *out = static_cast<TR *>(c.resid_out) + i * c.ldro;
-        TY *h = static_cast<TY *>(c.h) + i * c.ldh;
-#pragma unroll
-        for (int k = 0; k < P; ++k) {
-            if (!there(k))
-                continue;
-            float2 o[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                o[e] = fine ? v[k][e] : make_float2(0.f, 0.f);
-            store8(out + column(k), reinterpret_cast<const float *>(o));
-            if (pre) {
-                if (fine) {
-                    float2 a[4];
-                    parameter(c.gamma_pre, k, a);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        o[e] = fmul2(fmul2(fadd2(o[e], splat(-mu1)), splat(rho1)), a[e]);
-                    if (c.beta_pre) {
-                        parameter(c.beta_pre, k, a);
-#pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            o[e] = fadd2(o[e], a[e]);
-                    }
-                }
-                store8(h + column(k), reinterpret_cast<const float *>(o));
-            }
-        }
-        if (at_end) {
-            out[at.end] = from_float<TR>(fine ? ve : 0.f);
-            if (pre)
-                h[at.end] = from_float<TY>(fine ? fmaf((ve - mu1) * rho1, param(c.gamma_pre, c.param_dtype, at.end),
-                                                       c.beta_pre ? param(c.beta_pre, c.param_dtype, at.end) : 0.f)
-                                                : 0.f);
-        }
-        if (c.stats && t == 0)
-            reinterpret_cast<float4 *>(c.stats)[i] = fine ? make_float4(mu0, rho0, mu1, rho1) : make_float4(0.f, 0.f, 0.f, 0.f);
-        at = next;
-    }
-}
-
 // ---------------------------------------------------------------- backward, rows of any length
 
 // What the backward pass needs of one column of a row.
@@ -511,34 +281,6 @@ int64_t partial_rows(int64_t T, int64_t d)
     return d > kBlockMaxRow ? std::min<int64_t>(std::max<int64_t>(T, 1), kLongParts) : std::min<int64_t>(T + 8, kBlockMaxParts);
 }
 
-template <typename TR, typename TY, int P, int MOST, int PER_SM>
-cudaError_t launch_fwd_rows(const BlockCall &c, const Phases &phases, cudaStream_t stream)
-{
-    bool vector_params = true;
-    for (const void *p : {c.gamma_post, c.beta_post, c.gamma_pre, c.ldg ? nullptr : c.gate, c.beta_pre})
-        vector_params = vector_params && reinterpret_cast<uintptr_t>(p) % 16 == 0;
-    const int n = (int)((c.d + P * 256 - 1) / (P * 256)) * 32, per = std::max(1, std::min(256, MOST) / n);
-    const int64_t blocks = (c.T + per - 1) / per;
-    const auto go = [&](auto kernel) {
-        const int resident = std::max(PER_SM * MOST / (n * per), 1);
-        const unsigned grid = (unsigned)std::min<int64_t>(blocks, (int64_t)device_sm_count() * resident);
-        kernel<<<grid, n * per, 0, stream>>>(c, n, vector_params, phases.at, phases.step);
-        return cudaGetLastError();
-    };
-    const bool gate = c.gate && c.ldg;
-    if (phases.at || phases.step || c.d % 8)
-        return gate ? go(k_block_fwd<TR, TY, P, true, true, MOST, PER_SM>) : go(k_block_fwd<TR, TY, P, false, true, MOST, PER_SM>);
-    return gate ? go(k_block_fwd<TR, TY, P, true, false, MOST, PER_SM>) : go(k_block_fwd<TR, TY, P, false, false, MOST, PER_SM>);
-}
-
-// Many rows: four pieces to a thread, so that many rows are in flight; few rows: one, so that each answers sooner.
-template <typename TR, typename TY> cudaError_t launch_fwd(const BlockCall &c, const Phases &phases, cudaStream_t stream)
-{
-    if (c.T * ((c.d + 1023) / 1024) < 4 * device_sm_count())
-        return launch_fwd_rows<TR, TY, 1, 1024, 1>(c, phases, stream);
-    return launch_fwd_rows<TR, TY, 4, 256, 2>(c, phases, stream);
-}
-
 }  // namespace
 
 bool block_bwd_bias(const BlockGradCall &c) { return c.dbeta_pre || c.dbeta_post || (c.dgate && !c.ldg && c.beta_post); }
@@ -558,7 +300,7 @@ cudaError_t launch_block_fwd(const BlockCall &c, cudaStream_t stream)
         return cudaGetLastError();
     }
     cudaError_t e = cudaSuccess;
-    with_types(c.resid_dtype, c.y_dtype, [&](auto r, auto y) { e = launch_fwd<decltype(r), decltype(y)>(c, phases, stream); });
+    with_types(c.resid_dtype, c.y_dtype, [&](auto r, auto y) { e = launch_block_rows_fwd<decltype(r), decltype(y)>(c, phases, stream); });
     return e;
 }
 

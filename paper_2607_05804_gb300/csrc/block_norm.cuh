@@ -13,28 +13,34 @@ namespace turnopd {
 constexpr int kBlockMaxRow = 8192;   // longest rows that a block of threads holds
 constexpr int kBlockMaxParts = 320;  // CTAs of the backward pass, at most
 
-__device__ __forceinline__ float2 warp_sum2(float2 v)
+__device__ __forceinline__ float add(float a, float b) { return a + b; }
+__device__ __forceinline__ float2 add(float2 a, float2 b) { return fadd2(a, b); }
+__device__ __forceinline__ float from_lane(float v, int o) { return __shfl_xor_sync(~0u, v, o); }
+__device__ __forceinline__ float2 from_lane(float2 v, int o)
+{
+    return make_float2(__shfl_xor_sync(~0u, v.x, o), __shfl_xor_sync(~0u, v.y, o));
+}
+
+// Sum over the `warps` warps of a group, the same value in every thread; red: an entry per warp of the block, free again
+// two sums later.  The warps' sums are added up like the lanes': a lane reads one of them each (a thread that reads all
+// takes 60 instructions for ten warps, this 20).
+template <typename V> __device__ __forceinline__ V group_sum(V v, V *red, int group, int warps)
 {
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1)
-        v = fadd2(v, make_float2(__shfl_xor_sync(~0u, v.x, o), __shfl_xor_sync(~0u, v.y, o)));
-    return v;
-}
-
-// Sum over the `warps` warps of a group, the same values in every thread; red: an entry per warp of the block, free again
-// two sums later.
-__device__ __forceinline__ float2 group_sum2(float2 v, float2 *red, int group, int warps)
-{
-    v = warp_sum2(v);
+        v = add(v, from_lane(v, o));
     if (warps == 1)
         return v;
-    const int first = group * warps;
-    if ((threadIdx.x & 31) == 0)
+    const int lane = threadIdx.x & 31;
+    if (lane == 0)
         red[threadIdx.x >> 5] = v;
     group_barrier(group, warps * 32);
-    v = red[first];
-    for (int w = 1; w < warps; ++w)
-        v = fadd2(v, red[first + w]);
+    v = V{};
+    if (lane < warps)
+        v = red[group * warps + lane];
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1)
+        v = add(v, from_lane(v, o));
     return v;
 }
 
@@ -95,6 +101,9 @@ struct Phases {
         }
     }
 };
+
+// The row kernels of the forward pass, by the types of r and y.
+template <typename TR, typename TY> cudaError_t launch_block_rows_fwd(const BlockCall &c, const Phases &phases, cudaStream_t stream);
 
 // The row kernels of the backward pass, by the types of dr' and of dh; *parts: rows of partial sums that they leave in the
 // workspace, 4 d floats each (dh xh_pre, dh, X xh_post, X; the second and fourth only where block_bwd_bias says).  *taken:
