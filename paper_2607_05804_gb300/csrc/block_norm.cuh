@@ -13,35 +13,62 @@ namespace turnopd {
 constexpr int kBlockMaxRow = 8192;   // longest rows that a block of threads holds
 constexpr int kBlockMaxParts = 320;  // CTAs of the backward pass, at most
 
-__device__ __forceinline__ float add(float a, float b) { return a + b; }
-__device__ __forceinline__ float2 add(float2 a, float2 b) { return fadd2(a, b); }
-__device__ __forceinline__ float from_lane(float v, int o) { return __shfl_xor_sync(~0u, v, o); }
-__device__ __forceinline__ float2 from_lane(float2 v, int o)
+// N numbers that are added up together.
+template <int N> struct Numbers {
+    float v[N];
+};
+// Sums over the warp's lanes.  Of two numbers each half of the warp takes one on after the first exchange, and of four each
+// quarter after the second: 5 + 2 shuffles for two numbers, not 10.
+__device__ __forceinline__ float halve(float a, float b, int lane, int o)
 {
-    return make_float2(__shfl_xor_sync(~0u, v.x, o), __shfl_xor_sync(~0u, v.y, o));
+    const bool upper = lane & o;
+    return (upper ? b : a) + __shfl_xor_sync(~0u, upper ? a : b, o);
+}
+template <int N> __device__ __forceinline__ float spread_sum(const Numbers<N> &x)  // number N lane / 32 of this lane
+{
+    const int lane = threadIdx.x & 31;
+    float v;
+    if constexpr (N == 4)
+        v = halve(halve(x.v[0], x.v[2], lane, 16), halve(x.v[1], x.v[3], lane, 16), lane, 8);
+    else if constexpr (N == 2)
+        v = halve(x.v[0], x.v[1], lane, 16);
+    else
+        v = x.v[0];
+#pragma unroll
+    for (int o = 16 / N; o > 0; o >>= 1)
+        v += __shfl_xor_sync(~0u, v, o);
+    return v;
+}
+template <int N> __device__ __forceinline__ Numbers<N> gather_sums(float v)
+{
+    Numbers<N> x;
+#pragma unroll
+    for (int k = 0; k < N; ++k)
+        x.v[k] = N == 1 ? v : __shfl_sync(~0u, v, k * (32 / N));
+    return x;
 }
 
-// Sum over the `warps` warps of a group, the same value in every thread; red: an entry per warp of the block, free again
+// Sums over the `warps` warps of a group, the same values in every thread; red: an entry per warp of the block, free again
 // two sums later.  The warps' sums are added up like the lanes': a lane reads one of them each (a thread that reads all
 // takes 60 instructions for ten warps, this 20).
-template <typename V> __device__ __forceinline__ V group_sum(V v, V *red, int group, int warps)
+template <int N> __device__ __forceinline__ Numbers<N> group_sum(Numbers<N> x, Numbers<N> *red, int group, int warps)
 {
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1)
-        v = add(v, from_lane(v, o));
-    if (warps == 1)
-        return v;
-    const int lane = threadIdx.x & 31;
-    if (lane == 0)
-        red[threadIdx.x >> 5] = v;
-    group_barrier(group, warps * 32);
-    v = V{};
-    if (lane < warps)
-        v = red[group * warps + lane];
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1)
-        v = add(v, from_lane(v, o));
-    return v;
+    float v = spread_sum(x);
+    if (warps > 1) {
+        const int lane = threadIdx.x & 31;
+        if (lane % (32 / N) == 0)
+            red[threadIdx.x >> 5].v[lane / (32 / N)] = v;
+        group_barrier(group, warps * 32);
+        x = Numbers<N>{};
+        if (lane < warps)
+            x = red[group * warps + lane];
+        v = spread_sum(x);
+    }
+    return gather_sums<N>(v);
+}
+__device__ __forceinline__ float group_sum(float x, float *red, int group, int warps)
+{
+    return group_sum(Numbers<1>{{x}}, reinterpret_cast<Numbers<1> *>(red), group, warps).v[0];
 }
 
 // Column j of row i of an array of any type; 8-bit codes with their exponents.
@@ -109,6 +136,7 @@ template <typename TR, typename TY> cudaError_t launch_block_rows_fwd(const Bloc
 // workspace, 4 d floats each (dh xh_pre, dh, X xh_post, X; the second and fourth only where block_bwd_bias says).  *taken:
 // whether they take such rows.
 bool block_bwd_bias(const BlockGradCall &c);
+bool block_bwd_needs_y(const BlockGradCall &c);
 template <typename TR, typename TY>
 cudaError_t launch_block_rows_bwd(const BlockGradCall &c, int *parts, bool *taken, cudaStream_t stream);
 

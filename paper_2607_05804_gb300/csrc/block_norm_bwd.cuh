@@ -9,18 +9,27 @@
 namespace turnopd {
 namespace {
 
-constexpr int kE = 16;       // columns of a row that one thread holds, in two pieces of eight
-constexpr int kPieces = kE / 8;
-
 __device__ __forceinline__ void cp8(void *smem, const void *gmem)
 {
     asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"((uint32_t)__cvta_generic_to_shared(smem)), "l"(gmem) : "memory");
+}
+// Waits for all but the newest `pending` groups of copies.
+__device__ __forceinline__ void wait_copies(int pending)
+{
+    if (pending == 0)
+        asm volatile("cp.async.wait_group 0;" ::: "memory");
+    else if (pending == 1)
+        asm volatile("cp.async.wait_group 1;" ::: "memory");
+    else if (pending == 2)
+        asm volatile("cp.async.wait_group 2;" ::: "memory");
+    else
+        asm volatile("cp.async.wait_group 3;" ::: "memory");
 }
 
 // One array of a row in the ring.
 struct RingPart {
     const char *p;   // row 0, null: not read
-    int64_t pitch;   // bytes from row to row
+    uint32_t pitch;  // bytes from row to row
     int at;          // bytes into a stage
     int dtype;
     int bytes;       // of one column
@@ -28,8 +37,11 @@ struct RingPart {
 
 struct Ring {
     RingPart resid, y, dh, dro, gate;
-    int stage;  // bytes of a stage of one group
-    int depth;  // rows in flight ahead of the one at hand
+    uint32_t dr, dy, dgate;  // pitches of the results' rows
+    int extra;   // bytes into a stage: for each warp its copy of the row's statistics and of its columns' exponents
+    bool blocks; // rows are whole blocks of 256 columns, whose codes and exponents are copied by the warp
+    int stage;   // bytes of a stage of one group
+    int stages;  // 2 to 5: the row at hand, the next one, and those in flight
 };
 
 // Eight columns from the ring; codes without their scale.
@@ -44,56 +56,87 @@ __device__ __forceinline__ void from_ring(const char *at, int dtype, float2 *v)
         decode8(*reinterpret_cast<const uint2 *>(at), dtype == TURNOPD_E4M3, f);
 }
 
-template <typename T> constexpr int type_code() { return sizeof(T) == 2 ? TURNOPD_BF16 : TURNOPD_F32; }
+constexpr int extra_bytes(int pieces) { return 16 + 2 * 8 * pieces; }  // of a warp: statistics, exponents of r' and of y
 
-// One column of a row of any array, by its type; codes without their scale.
-__device__ __forceinline__ float one_column(const RingPart &p, int64_t i, int j)
+// Most threads of a block with one or two pieces of eight columns to a thread: 96 registers each, or 128.
+constexpr int most_threads(int pieces) { return pieces == 1 ? 640 : 512; }
+
+// What r' and y are stored in: the gradients' types, codes of one kind, or any.
+enum Stored { kGradientTypes, kE4m3, kInt8, kAny };
+template <Stored S, typename T> constexpr int type_code()
 {
-    const char *at = p.p + i * p.pitch + (int64_t)j * p.bytes;
-    const int dtype = p.dtype;
+    return S == kGradientTypes ? (sizeof(T) == 2 ? TURNOPD_BF16 : TURNOPD_F32) : S == kE4m3 ? TURNOPD_E4M3 : TURNOPD_INT8;
+}
+constexpr int type_bytes(int dtype) { return dtype == TURNOPD_F32 ? 4 : dtype == TURNOPD_BF16 ? 2 : 1; }
+
+template <typename T> constexpr int gradient_type() { return sizeof(T) == 2 ? TURNOPD_BF16 : TURNOPD_F32; }
+
+// One column of a row of any array as it is stored, and its value later, so that no instruction waits for the load
+// before the value is needed.
+__device__ __forceinline__ uint32_t raw_column(const RingPart &p, uint32_t i, int j)
+{
+    const char *at = p.p + (uint64_t)i * p.pitch + j * p.bytes;
+    if (p.bytes == 2)
+        return *reinterpret_cast<const unsigned short *>(at);
+    if (p.bytes == 4)
+        return *reinterpret_cast<const uint32_t *>(at);
+    return *reinterpret_cast<const uint8_t *>(at);
+}
+__device__ __forceinline__ float column_value(uint32_t raw, int dtype, uint32_t exponent)
+{
     if (dtype == TURNOPD_BF16)
-        return __bfloat162float(*reinterpret_cast<const __nv_bfloat16 *>(at));
+        return __uint_as_float(raw << 16);
     if (dtype == TURNOPD_F32)
-        return *reinterpret_cast<const float *>(at);
-    const uint8_t b = *reinterpret_cast<const uint8_t *>(at);
-    return dtype == TURNOPD_E4M3 ? decode_e4m3(b) : (float)(int8_t)b;
+        return __uint_as_float(raw);
+    return (dtype == TURNOPD_E4M3 ? decode_e4m3((uint8_t)raw) : (float)(int8_t)raw) * act_scale(exponent);
 }
 
-// A thread keeps its columns of the sums over rows and of the factor after the first norm in registers from row to row, and
-// of gamma_pre in shared memory, in pieces of four (its registers would not hold both).  Group b of all takes rows b,
-// b + groups, ..., so that every sum has a fixed order.  A row's arrays come through a ring in shared memory, in which each
-// thread copies and reads its own pieces only: no barrier but those of the row's two sums.  A warp's pieces lie 256 columns
-// apart, so that they are found at constant offsets.
+// One piece of eight columns to a thread, two in longer rows, whose sums over rows it keeps in registers from row to row.  Group b of all takes
+// rows b, b + groups, ..., so that every sum has a fixed order.  A row's arrays come through a ring in shared memory, in
+// which each thread copies and reads its own pieces only.  The sums over the next row that D needs are taken together with
+// those over the row at hand that dy needs: one barrier to a row.  gamma lies in shared memory, and values are read from
+// the ring once more where they are needed again: a thread's registers would not hold them.  A warp's pieces lie 256
+// columns apart, so that they are found at constant offsets.
 //
 // ENDS: the rows begin anywhere, but in all arrays at the same element of a group of eight.  The groups' number is a multiple
 // of eight then, so all rows of one group begin at the same element, and a thread keeps the same columns from row to row:
 // pieces of eight from the first boundary on, and the first threads one of the elements before and after them each.
-// GENERAL: layer norms, or sums for betas; without it the mean of g and those sums are left out.
-// STORED: r' and y are of the gradients' types; else of any, codes among them.
-template <typename TR, typename TY, bool STORED, bool ENDS, bool GENERAL, int MOST, int PER_SM>
-__global__ void __launch_bounds__(MOST, PER_SM) k_block_bwd(BlockGradCall c, Ring ring, int n, int phase, int phase_step)
+// GENERAL: layer norms, or sums for betas; without it the means of g and those sums are left out.
+// COMMON: dh and dr' come in, dr and dy go out, no gate for every element.
+template <typename TR, typename TY, int kPieces, Stored STORED, bool ENDS, bool GENERAL, bool COMMON>
+__global__ void __launch_bounds__(most_threads(kPieces), 1) k_block_bwd(BlockGradCall c, Ring ring, int n, int phase, int phase_step)
 {
-    using V = std::conditional_t<GENERAL, float2, float>;  // sums over a row: (of g, of g xh) or the second alone
+    // sums over a row: of g xh (and of g) of the norm after the block, and of the norm before the next one
+    constexpr int kRowSums = GENERAL ? 4 : 2, kE = 8 * kPieces, kExtra = extra_bytes(kPieces);
+    constexpr bool kMixed = STORED == kAny, kCodes = STORED == kE4m3 || STORED == kInt8;
+    constexpr int kTypeR = type_code<STORED, TR>(), kTypeY = type_code<STORED, TY>();
     extern __shared__ __align__(128) char shared[];
-    __shared__ V red[2][16];
+    __shared__ Numbers<kRowSums> red[2][most_threads(kPieces) / 32];
     const int t = threadIdx.x % n, group = threadIdx.x / n, warps = n / 32, per = blockDim.x / n, d = (int)c.d;
-    const int64_t groups = (int64_t)gridDim.x * per, b = (int64_t)blockIdx.x * per + group;
-    const bool layer = GENERAL && c.kind == TURNOPD_LAYER_NORM, pre = c.gamma_pre, post = c.gamma_post;
-    const bool token_gate = ring.gate.p, dgate = token_gate && c.dgate;
-    const bool post_sums = c.dgamma_post || c.dbeta_post || (c.dgate && !c.ldg);
-    const bool needs_y = ring.y.p, needs_stream = c.d_resid || c.dy || c.dgate || post_sums;
+    const uint32_t T = (uint32_t)c.T, groups = gridDim.x * per, b = blockIdx.x * per + group;  // rows: 2^31 at most, and a few steps more
+    const bool layer = GENERAL && c.kind == TURNOPD_LAYER_NORM, pre = COMMON || c.gamma_pre, post = c.gamma_post;
+    const bool token_gate = !COMMON && ring.gate.p, dgate = token_gate && c.dgate, has_dro = COMMON || ring.dro.p;
+    const bool put_dr = COMMON || c.d_resid, put_dy = COMMON || c.dy, needs_y = ring.y.p;
+    const bool post_sums = COMMON || c.dgamma_post || c.dbeta_post || (c.dgate && !c.ldg);
+    const bool needs_stream = COMMON || put_dr || put_dy || c.dgate || post_sums;
     const float inv_d = 1.f / (float)d, s = c.branch_scale;
-    const int64_t exps_per_row = (c.d + kActGroup - 1) / kActGroup;
+    const uint32_t exps_per_row = (d + kActGroup - 1) / kActGroup;
     const int head = ENDS ? min((8 - (int)((phase + b * phase_step) & 7)) & 7, d) : 0;
     const int whole = (d - head) / 8, ends = ENDS ? d - whole * 8 : 0;
     const int end = t < head ? t : whole * 8 + t;  // the single column of this thread, where t < ends
     const int piece0 = (t >> 5) * 32 * kPieces + (t & 31);
-    const auto column = [&](int k) { return head + (piece0 + 32 * k) * 8; };  // the first of piece k
+    // the first column of piece k; of a missing one that of the last piece, which is computed once more, with factors of 0,
+    // and not stored
+    int columns[kPieces];
+#pragma unroll
+    for (int k = 0; k < kPieces; ++k)
+        columns[k] = head + min(piece0 + 32 * k, whole - 1) * 8;
+    const auto column = [&](int k) { return columns[k]; };
     const auto there = [&](int k) { return piece0 + 32 * k < whole; };
     const bool at_end = ENDS && t < ends;
 
-    char *own = shared + (size_t)group * ((ring.depth + 1) * ring.stage + n * kE * (int)sizeof(float));
-    float4 *gamma = reinterpret_cast<float4 *>(own + (ring.depth + 1) * ring.stage) + t;  // n apart
+    char *own = shared + (size_t)group * (ring.stages * ring.stage + n * kE * (int)sizeof(float));
+    float4 *gamma = reinterpret_cast<float4 *>(own + ring.stages * ring.stage) + t;  // n apart
     constexpr int kSums = GENERAL ? 4 : 2, kPostSum = GENERAL ? 2 : 1;  // dh xh_pre, (dh,) X xh_post (, X)
     float2 cpost[kE / 2], sums[kSums][kE / 2];
     float sums_end[kSums] = {};
@@ -120,352 +163,407 @@ __global__ void __launch_bounds__(MOST, PER_SM) k_block_bwd(BlockGradCall c, Rin
         gamma[(2 * k + 1) * n] = make_float4(g[4], g[5], g[6], g[7]);
     }
     const float gamma_end = at_end && pre ? param(c.gamma_pre, c.param_dtype, end) : 0.f, cpost_end = at_end ? post_factor(end) : 0.f;
-    // missing pieces are zeros in every stage
-#pragma unroll
-    for (int k = 0; k < kPieces; ++k)
-        if (!there(k))
-            for (int q = 0; q <= ring.depth; ++q)
-                for (const RingPart *p : {&ring.resid, &ring.y, &ring.dh, &ring.dro, &ring.gate})
-                    if (p->p)
-                        for (int h = 0; h < p->bytes; ++h)
-                            *reinterpret_cast<uint2 *>(own + q * ring.stage + p->at + (piece0 + 32 * k) * 8 * p->bytes + 8 * h) =
-                                make_uint2(0u, 0u);
 
-    // One array's pieces of a row: `from` is this thread's first one there, which goes on by a step of the groups.
-    struct Source {
-        const char *from;
-        int64_t step;
-    };
-    const auto source = [&](const RingPart &p) { return Source{p.p + b * p.pitch + column(0) * p.bytes, groups * p.pitch}; };
-    Source resid = source(ring.resid), y = source(ring.y), dh = source(ring.dh), dro = source(ring.dro), gate = source(ring.gate);
-    int64_t ahead = b;  // the next row to copy
-    const auto copy = [&](int stage) {
-        const bool on = ahead < c.T && (!c.mask || c.mask[ahead]);
-        char *to = own + stage * ring.stage;
-        const auto part = [&](Source &src, const RingPart &p, int bytes) {
-            if (!p.p)
-                return;
-#pragma unroll
-            for (int k = 0; k < kPieces; ++k) {
-                if (!on || !there(k))
-                    continue;
-                char *dst = to + p.at + piece0 * 8 * bytes + k * 256 * bytes;
-                const char *at = src.from + k * 256 * bytes;
-                if (bytes == 1) {
-                    cp8(dst, at);
-                } else {
-                    cp16(dst, at);
-                    if (bytes == 4)
-                        cp16(dst + 16, at + 16);
+    uint32_t ahead = b;  // the next row to copy, whose mask has been read before
+    uint32_t ahead_on = ahead < T && c.mask ? c.mask[ahead] : 1u;
+    int ahead_stage = 0;
+    uint32_t ons = 0;  // whether the rows copied last are not masked, the newest in bit 0
+    const bool code_r = kCodes ? pre : kMixed && pre && ring.resid.dtype >= TURNOPD_E4M3;
+    const bool code_y = kCodes ? needs_y : kMixed && needs_y && ring.y.dtype >= TURNOPD_E4M3;
+    const auto copy = [&]() {
+        if (ahead < T && ahead_on) {
+            char *to = own + ahead_stage * ring.stage;
+            const auto part = [&](const RingPart &p, int bytes) {
+                if (!p.p)
+                    return;
+                const char *from = p.p + (uint64_t)ahead * p.pitch;
+                if (bytes == 1 && ring.blocks) {
+                    // a warp's codes together, sixteen at a time: half as many copies, and eight bytes each take longer than
+                    // sixteen (32,768 x 4,096: 500 us so)
+                    const int lane = t & 31;
+                    if (lane < 16 * kPieces)
+                        cp16(to + p.at + (t >> 5) * kPieces * 256 + lane * 16,
+                             from + min(((t >> 5) * kPieces + (lane >> 4)) * 256, d - 256) + (lane & 15) * 16);
+                    return;
                 }
+#pragma unroll
+                for (int k = 0; k < kPieces; ++k) {
+                    char *dst = to + p.at + piece0 * 8 * bytes + k * 256 * bytes;
+                    const char *at = from + column(k) * bytes;
+                    if (bytes == 1) {
+                        cp8(dst, at);
+                    } else {
+                        cp16(dst, at);
+                        if (bytes == 4)
+                            cp16(dst + 16, at + 16);
+                    }
+                }
+            };
+            part(ring.resid, kMixed ? ring.resid.bytes : type_bytes(kTypeR));
+            part(ring.dh, sizeof(TY));
+            part(ring.dro, sizeof(TR));
+            part(ring.y, kMixed ? ring.y.bytes : type_bytes(kTypeY));
+            part(ring.gate, sizeof(TY));
+            char *extra = to + ring.extra + (t >> 5) * kExtra;
+            const int lane = t & 31, block = min((t >> 5) * kPieces + lane, d / 256 - 1);  // of 256 columns
+            if (lane == 0 && (COMMON || c.stats))
+                cp16(extra, c.stats + (uint64_t)ahead * 4);
+            if ((kMixed || kCodes) && ring.blocks && lane < kPieces) {
+                if (code_r)
+                    cp8(extra + 16 + 8 * lane, c.resid_exps + (uint64_t)ahead * exps_per_row + block * 8);
+                if (code_y)
+                    cp8(extra + 16 + 8 * (kPieces + lane), c.y_exps + (uint64_t)ahead * exps_per_row + block * 8);
             }
-            src.from += src.step;
-        };
-        part(resid, ring.resid, STORED ? (int)sizeof(TR) : ring.resid.bytes);
-        part(dh, ring.dh, sizeof(TY));
-        part(dro, ring.dro, sizeof(TR));
-        part(y, ring.y, STORED ? (int)sizeof(TY) : ring.y.bytes);
-        part(gate, ring.gate, sizeof(TY));
+        }
+        ons = ons << 1 | (ahead < T && ahead_on);
         ahead += groups;
+        ahead_stage = ahead_stage + 1 == ring.stages ? 0 : ahead_stage + 1;
+        if (c.mask && ahead < T)
+            ahead_on = c.mask[ahead];
         asm volatile("cp.async.commit_group;" ::: "memory");
     };
-    // a row's statistics, its exponents (a byte to each piece, whose columns may lie in two groups of them: the first's in the
-    // low half) and this thread's single column are read a row ahead
-    struct Numbers {
+    // What a thread needs of a row beside its pieces.  Exponents that do not come through the ring (of each piece, whose columns
+    // may lie in two groups of them) and the thread's single column are read two rows ahead, and looked at when their turn comes.
+    struct Row {
         float4 stats;
-        uint32_t er, ey;
-        float resid, y, dh, dro, gate;
+        uint32_t er[kPieces], er2[ENDS ? kPieces : 1], ey[kPieces], ey2[ENDS ? kPieces : 1];
+        uint32_t resid, y, dh, dro, gate, e_resid, e_y;
         bool fine;
     };
-    const bool code_r = !STORED && pre && ring.resid.dtype >= TURNOPD_E4M3, code_y = !STORED && needs_y && ring.y.dtype >= TURNOPD_E4M3;
-    const auto numbers = [&](int64_t i) {
-        Numbers m{};
-        if (i < c.T) {
-            m.fine = takes_part(c, i, m.stats);
-            if (m.fine) {
-                if (!STORED) {
+    const auto read_row = [&](uint32_t i) {
+        Row m{};
+        if (i >= T)
+            return m;
+        if ((kMixed || kCodes) && !ring.blocks) {
+            const uint64_t at = (uint64_t)i * exps_per_row;
 #pragma unroll
-                    for (int k = 0; k < kPieces; ++k)
-                        if (there(k)) {
-                            const int64_t at = i * exps_per_row;
-                            const int g = column(k) / kActGroup, h = ENDS ? (column(k) + 7) / kActGroup : g;
-                            if (code_r)
-                                m.er |= (uint32_t)c.resid_exps[at + g] << (8 * k) | (ENDS ? (uint32_t)c.resid_exps[at + h] << (8 * k + 16) : 0u);
-                            if (code_y)
-                                m.ey |= (uint32_t)c.y_exps[at + g] << (8 * k) | (ENDS ? (uint32_t)c.y_exps[at + h] << (8 * k + 16) : 0u);
-                        }
+            for (int k = 0; k < kPieces; ++k) {
+                const int g = column(k) / kActGroup, h = (column(k) + 7) / kActGroup;
+                if (code_r) {
+                    m.er[k] = c.resid_exps[at + g];
+                    if (ENDS)
+                        m.er2[ENDS ? k : 0] = c.resid_exps[at + h];
                 }
-                if (at_end) {
-                    const int64_t at = i * exps_per_row + end / kActGroup;
-                    if (pre) {
-                        m.resid = one_column(ring.resid, i, end) * (code_r ? act_scale(c.resid_exps[at]) : 1.f);
-                        m.dh = one_column(ring.dh, i, end);
-                    }
-                    if (ring.dro.p)
-                        m.dro = one_column(ring.dro, i, end);
-                    if (needs_y)
-                        m.y = one_column(ring.y, i, end) * (code_y ? act_scale(c.y_exps[at]) : 1.f);
-                    if (token_gate)
-                        m.gate = one_column(ring.gate, i, end);
+                if (code_y) {
+                    m.ey[k] = c.y_exps[at + g];
+                    if (ENDS)
+                        m.ey2[ENDS ? k : 0] = c.y_exps[at + h];
                 }
             }
+            if (at_end && code_r)
+                m.e_resid = c.resid_exps[at + end / kActGroup];
+            if (at_end && code_y)
+                m.e_y = c.y_exps[at + end / kActGroup];
+        }
+        if (at_end) {
+            if (pre) {
+                m.resid = raw_column(ring.resid, i, end);
+                m.dh = raw_column(ring.dh, i, end);
+            }
+            if (has_dro)
+                m.dro = raw_column(ring.dro, i, end);
+            if (needs_y)
+                m.y = raw_column(ring.y, i, end);
+            if (token_gate)
+                m.gate = raw_column(ring.gate, i, end);
         }
         return m;
     };
-    for (int k = 0; k < ring.depth; ++k)
-        copy(k);
-    Numbers m = numbers(b);
-    int stage = 0, odd = 0;
-    for (int64_t i = b; i < c.T; i += groups) {
-        copy(stage ? stage - 1 : ring.depth);
-        const Numbers next = numbers(i + groups);
-        if (ring.depth == 3)
-            asm volatile("cp.async.wait_group 3;" ::: "memory");
-        else if (ring.depth == 2)
-            asm volatile("cp.async.wait_group 2;" ::: "memory");
-        else if (ring.depth == 1)
-            asm volatile("cp.async.wait_group 1;" ::: "memory");
-        else
-            asm volatile("cp.async.wait_group 0;" ::: "memory");
-        const char *at = own + stage * ring.stage;
-        const float mu0 = m.stats.x, r0 = m.stats.y, mu1 = m.stats.z, r1 = m.stats.w;
-        // eight columns of an array
-        const auto activation = [&](const RingPart &part, int stored, uint32_t exps, int k, float2 *v) {
-            const int dtype = STORED ? stored : part.dtype, bytes = STORED ? (stored == TURNOPD_BF16 ? 2 : 4) : part.bytes;
-            from_ring(at + part.at + piece0 * 8 * bytes + k * 256 * bytes, dtype, v);
-            if (!STORED && dtype >= TURNOPD_E4M3) {
-                const float lo = act_scale(exps >> (8 * k) & 255u), hi = ENDS ? act_scale(exps >> (8 * k + 16) & 255u) : lo;
-                const int first = ENDS ? kActGroup - (column(k) & (kActGroup - 1)) : 8;  // columns of the first group
+    // the rest, from the ring (of a masked row that is of no use); on: the row is there and not masked
+    const auto complete = [&](Row &m, const char *at, bool on) {
+        const char *extra = at + ring.extra + (t >> 5) * kExtra;
+        m.stats = COMMON || c.stats ? *reinterpret_cast<const float4 *>(extra) : make_float4(0.f, 0.f, 0.f, 0.f);
+        m.fine = on && (!post || m.stats.y > 0.f) && (!pre || m.stats.w > 0.f);
+        if ((kMixed || kCodes) && ring.blocks) {
+            const int lane = t & 31;
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    v[e] = fmul2(v[e], make_float2(2 * e < first ? lo : hi, 2 * e + 1 < first ? lo : hi));
+            for (int k = 0; k < kPieces; ++k) {
+                m.er[k] = static_cast<uint8_t>(extra[16 + 8 * k + (lane >> 2)]);
+                m.ey[k] = static_cast<uint8_t>(extra[16 + 8 * (kPieces + k) + (lane >> 2)]);
             }
-        };
-        const auto gradient = [&](auto type, const RingPart &part, int k, float2 *v) {
-            using T = decltype(type);
-            load8(reinterpret_cast<const T *>(at + part.at) + piece0 * 8 + k * 256, reinterpret_cast<float *>(v));
-        };
-        const auto put8 = [&](auto *p, int64_t ld, int k, const float2 *v) {
-            if (there(k))
-                store8(p + i * ld + column(0) + k * 256, reinterpret_cast<const float *>(v));
-        };
-        const auto put1 = [&](auto *p, int64_t ld, float v) {
-            using T = std::remove_reference_t<decltype(*p)>;
-            if (at_end)
-                p[i * ld + end] = from_float<T>(v);
-        };
-        const auto normed = [&](float2 *v, float mu, float r) {
+        }
+    };
+
+    // Eight columns of an activation of the row in a stage, less mu, but for a factor that is returned: the codes' scale, where
+    // it is the same for all eight and nothing is taken off.
+    const auto activation = [&](const char *at, const RingPart &part, int stored, uint32_t exp, uint32_t exp2, float mu, int k, float2 *v) {
+        const int dtype = kMixed ? part.dtype : stored, bytes = kMixed ? part.bytes : type_bytes(stored);
+        from_ring(at + part.at + piece0 * 8 * bytes + k * 256 * bytes, dtype, v);
+        if ((kMixed || kCodes) && dtype >= TURNOPD_E4M3) {
+            const float lo = act_scale(exp);
+            if (!ENDS && !GENERAL)
+                return lo;
+            const float hi = ENDS ? act_scale(exp2) : lo;
+            const int first = ENDS ? kActGroup - (column(k) & (kActGroup - 1)) : 8;  // columns of the first group
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                v[e] = ffma2(v[e], make_float2(2 * e < first ? lo : hi, 2 * e + 1 < first ? lo : hi), splat(-mu));
+        } else if (GENERAL) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                v[e] = fadd2(v[e], splat(-mu));
+        }
+        return 1.f;
+    };
+    const auto gradient = [&](auto type, const char *at, const RingPart &part, int k, float2 *v) {
+        load8(reinterpret_cast<const decltype(type) *>(at + part.at) + piece0 * 8 + k * 256, reinterpret_cast<float *>(v));
+    };
+    const auto centred_r = [&](const char *at, const Row &m, int k, float2 *v) {
+        return activation(at, ring.resid, kTypeR, m.er[k], m.er2[ENDS ? k : 0], m.stats.z, k, v);
+    };
+    const auto centred_y = [&](const char *at, const Row &m, int k, float2 *v) {  // mu is 0 without that norm
+        return activation(at, ring.y, kTypeY, m.ey[k], m.ey2[ENDS ? k : 0], m.stats.x, k, v);
+    };
+    const auto times_gamma = [&](int k, float2 *g) {
+        const float4 a = gamma[2 * k * n], z = gamma[(2 * k + 1) * n];
+        g[0] = fmul2(g[0], make_float2(a.x, a.y));
+        g[1] = fmul2(g[1], make_float2(a.z, a.w));
+        g[2] = fmul2(g[2], make_float2(z.x, z.y));
+        g[3] = fmul2(g[3], make_float2(z.z, z.w));
+    };
+    // sums of g (r' - mu) and of g over a row of the norm before the next block, and the sums over rows
+    const auto first_sums = [&](const char *at, const Row &m, float &sx, float &sg) {
+        const float r1 = m.stats.w;
+        sx = sg = 0.f;
+#pragma unroll
+        for (int k = 0; k < kPieces; ++k) {
+            float2 x[4], g[4], x2 = make_float2(0.f, 0.f), g2 = x2;
+            const float f = centred_r(at, m, k, x);
+            gradient(TY(), at, ring.dh, k, g);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                sums[0][4 * k + e] = ffma2(fmul2(g[e], splat(r1 * f)), x[e], sums[0][4 * k + e]);
+                if (GENERAL)
+                    sums[1][4 * k + e] = fadd2(g[e], sums[1][4 * k + e]);
+            }
+            times_gamma(k, g);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 if (GENERAL)
-                    v[e] = fadd2(v[e], splat(-mu));
-                v[e] = fmul2(v[e], splat(r));
+                    g2 = fadd2(g2, g[e]);
+                x2 = ffma2(g[e], x[e], x2);
             }
-        };
-        const auto xh_pre = [&](int k, float2 *v) {
-            activation(ring.resid, type_code<TR>(), m.er, k, v);
-            normed(v, mu1, r1);
-        };
-        const auto xh_post = [&](int k, float2 *v) {
-            activation(ring.y, type_code<TY>(), m.ey, k, v);
-            if (post)
-                normed(v, mu0, r0);
-        };
-        const auto times_gamma = [&](int k, float2 *g) {
-            const float4 a = gamma[2 * k * n], z = gamma[(2 * k + 1) * n];
-            g[0] = fmul2(g[0], make_float2(a.x, a.y));
-            g[1] = fmul2(g[1], make_float2(a.z, a.w));
-            g[2] = fmul2(g[2], make_float2(z.x, z.y));
-            g[3] = fmul2(g[3], make_float2(z.z, z.w));
-        };
-        const auto row_sum = [&](float2 sg, float2 sx) -> float2 {
-            float2 v;
-            if constexpr (GENERAL) {
-                v = group_sum(make_float2(sg.x + sg.y, sx.x + sx.y), red[odd], group, warps);
-            } else {
-                v = make_float2(0.f, group_sum(sx.x + sx.y, red[odd], group, warps));
-            }
-            odd ^= 1;
-            return v;
-        };
+            sx = fmaf(x2.x + x2.y, f, sx);
+            sg += g2.x + g2.y;
+        }
+        if (at_end) {
+            const float x = column_value(m.resid, kMixed ? ring.resid.dtype : kTypeR, m.e_resid) - m.stats.z;
+            const float g = column_value(m.dh, gradient_type<TY>(), 0u);
+            sums_end[0] = fmaf(g * r1, x, sums_end[0]);
+            if (GENERAL)
+                sums_end[1] += g;
+            sg += g * gamma_end;
+            sx = fmaf(g * gamma_end, x, sx);
+        }
+    };
 
-        // (the sums over the row are taken whatever the mask and the statistics say: no barrier stands under a condition
-        // that every thread reads from the caller's memory for itself)
-        float2 mean = make_float2(0.f, 0.f);
-        const float xe_pre = ENDS && m.fine && at_end ? (m.resid - mu1) * r1 : 0.f;
-        const float xe_post = ENDS && m.fine && at_end ? (post ? (m.y - mu0) * r0 : m.y) : 0.f;
-        if (pre) {
+    for (int k = 0; k + 1 < ring.stages; ++k)
+        copy();
+    Row m = read_row(b), next = read_row(b + groups);
+    int stage = 0, odd = 0;
+    // the sums of the first row are taken by themselves (those of rows that do not take part, of nothing: no barrier stands
+    // under a condition that every thread reads from the caller's memory for itself)
+    Numbers<kRowSums> row_sums{};
+    wait_copies(ring.stages - 2);
+    __syncwarp();  // the warp's copies of the statistics
+    complete(m, own, ons >> (ring.stages - 2) & 1);
+    if (pre && m.fine) {
+        float sx, sg;
+        first_sums(own, m, sx, sg);
+        row_sums.v[1] = sx;
+        if (GENERAL)
+            row_sums.v[kRowSums - 1] = sg;
+    }
+    if (pre && needs_stream) {
+        row_sums = group_sum(row_sums, red[odd], group, warps);
+        odd ^= 1;
+    }
+    for (uint32_t i = b; i < T; i += groups) {
+        copy();
+        Row after = read_row(i + 2 * groups);
+        const char *at = own + stage * ring.stage;
+        const int next_stage = stage + 1 == ring.stages ? 0 : stage + 1;
+        const bool fine = m.fine;
+        const float r0 = m.stats.y, r1 = m.stats.w, scale = post ? r0 : 1.f;
+        const auto put8 = [&](auto type, void *p, uint32_t pitch, int k, const float2 *v) {
+            using R = decltype(type);
+            if (there(k))
+                store8(reinterpret_cast<R *>(static_cast<char *>(p) + (uint64_t)i * pitch) + column(k), reinterpret_cast<const float *>(v));
+        };
+        const auto put1 = [&](auto type, void *p, uint32_t pitch, float v) {
+            using R = decltype(type);
+            if (at_end)
+                reinterpret_cast<R *>(static_cast<char *>(p) + (uint64_t)i * pitch)[end] = from_float<R>(v);
+        };
+        // D = dr' + r (g - mean g - xh mean(g xh)), then X = D times the gate that each token has of its own, and E
+        const float c1 = -(row_sums.v[1] * inv_d * r1) * r1 * r1;  // of r' - mu
+        const float c0 = layer ? -r1 * (row_sums.v[kRowSums - 1] * inv_d) : 0.f;
+        float2 E[kE / 2];
+        float E_end = 0.f, ye = 0.f;
+        row_sums = Numbers<kRowSums>{};
+        if (needs_stream && fine) {
             float2 sg = make_float2(0.f, 0.f), sx = sg;
-            if (m.fine) {
 #pragma unroll
-                for (int k = 0; k < kPieces; ++k) {
-                    float2 x[4], g[4];
-                    xh_pre(k, x);
-                    gradient(TY(), ring.dh, k, g);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        sums[0][4 * k + e] = ffma2(g[e], x[e], sums[0][4 * k + e]);
-                        if (GENERAL)
-                            sums[1][4 * k + e] = fadd2(g[e], sums[1][4 * k + e]);
-                    }
+            for (int k = 0; k < kPieces; ++k) {
+                float2 D[4], x[4];
+                if (has_dro)
+                    gradient(TR(), at, ring.dro, k, D);
+                else
+                    D[0] = D[1] = D[2] = D[3] = make_float2(0.f, 0.f);
+                if (pre) {
+                    float2 g[4];
+                    const float f = c1 * centred_r(at, m, k, x);
+                    gradient(TY(), at, ring.dh, k, g);
                     times_gamma(k, g);
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
+                        D[e] = ffma2(x[e], splat(f), ffma2(g[e], splat(r1), D[e]));
                         if (GENERAL)
-                            sg = fadd2(sg, g[e]);
-                        sx = ffma2(g[e], x[e], sx);
+                            D[e] = fadd2(D[e], splat(c0));
                     }
                 }
-                if (ENDS) {
-                    sums_end[0] = fmaf(m.dh, xe_pre, sums_end[0]);
-                    if (GENERAL)
-                        sums_end[1] += m.dh;
-                    sg.x += m.dh * gamma_end;
-                    sx.x = fmaf(m.dh * gamma_end, xe_pre, sx.x);
-                }
-            }
-            if (needs_stream)
-                mean = row_sum(sg, sx);
-        }
-        if (needs_stream) {
-            // D = dr' + r (g - mean g - xh mean(g xh)), then X = D times the gate that each token has of its own, and E
-            const float2 c0 = splat(layer ? -r1 * (mean.x * inv_d) : 0.f), c1 = splat(-r1 * (mean.y * inv_d));
-            float2 E[kE / 2];
-            float E_end = 0.f;
-            float2 sg = make_float2(0.f, 0.f), sx = sg;
-            if (m.fine) {
-#pragma unroll
-                for (int k = 0; k < kPieces; ++k) {
-                    float2 D[4], x[4];
-                    if (ring.dro.p)
-                        gradient(TR(), ring.dro, k, D);
-                    else
-                        D[0] = D[1] = D[2] = D[3] = make_float2(0.f, 0.f);
-                    if (pre) {
-                        float2 g[4];
-                        xh_pre(k, x);
-                        gradient(TY(), ring.dh, k, g);
-                        times_gamma(k, g);
-#pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            D[e] = fadd2(D[e], ffma2(g[e], splat(r1), GENERAL ? ffma2(x[e], c1, c0) : fmul2(x[e], c1)));
-                    }
-                    if (c.d_resid) {
-                        float2 o[4];
+                if (put_dr) {
+                    float2 o[4];
+                    if (c.resid_scale == 1.f) {
+                        put8(TR(), c.d_resid, ring.dr, k, D);
+                    } else {
 #pragma unroll
                         for (int e = 0; e < 4; ++e)
                             o[e] = fmul2(D[e], splat(c.resid_scale));
-                        put8(static_cast<TR *>(c.d_resid), c.lddr, k, o);
+                        put8(TR(), c.d_resid, ring.dr, k, o);
                     }
-                    if (needs_y)
-                        xh_post(k, x);
-                    if (token_gate) {
-                        float2 g[4];
-                        if (dgate) {
+                }
+                if (needs_y) {
+                    const float f = scale * centred_y(at, m, k, x);
 #pragma unroll
-                            for (int e = 0; e < 8; ++e) {
-                                float w = reinterpret_cast<const float *>(x)[e];
-                                if (post && there(k))
-                                    w = fmaf(w, param(c.gamma_post, c.param_dtype, column(k) + e),
-                                             c.beta_post ? param(c.beta_post, c.param_dtype, column(k) + e) : 0.f);
-                                reinterpret_cast<float *>(g)[e] = s * reinterpret_cast<const float *>(D)[e] * w;
-                            }
-                            put8(static_cast<TY *>(c.dgate), c.lddg, k, g);
+                    for (int e = 0; e < 4; ++e)
+                        x[e] = fmul2(x[e], splat(f));
+                }
+                if (token_gate) {
+                    float2 g[4];
+                    if (dgate) {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            float w = reinterpret_cast<const float *>(x)[e];
+                            if (post && there(k))
+                                w = fmaf(w, param(c.gamma_post, c.param_dtype, column(k) + e),
+                                         c.beta_post ? param(c.beta_post, c.param_dtype, column(k) + e) : 0.f);
+                            reinterpret_cast<float *>(g)[e] = s * reinterpret_cast<const float *>(D)[e] * w;
                         }
-                        gradient(TY(), ring.gate, k, g);
-#pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            D[e] = fmul2(D[e], g[e]);
+                        put8(TY(), c.dgate, ring.dgate, k, g);
                     }
-                    if (post_sums) {
+                    gradient(TY(), at, ring.gate, k, g);
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            if (needs_y)
-                                sums[kPostSum][4 * k + e] = ffma2(D[e], x[e], sums[kPostSum][4 * k + e]);
-                            if (GENERAL)
-                                sums[kSums - 1][4 * k + e] = fadd2(D[e], sums[kSums - 1][4 * k + e]);
-                        }
-                    }
+                    for (int e = 0; e < 4; ++e)
+                        D[e] = fmul2(D[e], g[e]);
+                }
+                if (post_sums) {
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        const float2 g = fmul2(D[e], cpost[4 * k + e]);
-                        E[4 * k + e] = g;
+                        if (needs_y)
+                            sums[kPostSum][4 * k + e] = ffma2(D[e], x[e], sums[kPostSum][4 * k + e]);
                         if (GENERAL)
-                            sg = fadd2(sg, g);
-                        if (post)
-                            sx = ffma2(g, x[e], sx);
+                            sums[kSums - 1][4 * k + e] = fadd2(D[e], sums[kSums - 1][4 * k + e]);
                     }
-                    if (c.dy && !post)
-                        put8(static_cast<TY *>(c.dy), c.lddy, k, E + 4 * k);
                 }
-                if (ENDS) {
-                    float D = m.dro + (pre ? fmaf(m.dh * gamma_end, r1, fmaf(xe_pre, c1.x, c0.x)) : 0.f);
-                    if (c.d_resid)
-                        put1(static_cast<TR *>(c.d_resid), c.lddr, D * c.resid_scale);
-                    if (dgate) {
-                        float w = xe_post;
-                        if (post && at_end)
-                            w = fmaf(w, param(c.gamma_post, c.param_dtype, end), c.beta_post ? param(c.beta_post, c.param_dtype, end) : 0.f);
-                        put1(static_cast<TY *>(c.dgate), c.lddg, s * D * w);
-                    }
-                    if (token_gate)
-                        D *= m.gate;
-                    if (!at_end)
-                        D = 0.f;
-                    sums_end[kPostSum] = fmaf(D, xe_post, sums_end[kPostSum]);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float2 g = fmul2(D[e], cpost[4 * k + e]);
+                    E[4 * k + e] = g;
                     if (GENERAL)
-                        sums_end[kSums - 1] += D;
-                    E_end = D * cpost_end;
-                    sg.x += E_end;
-                    sx.x = fmaf(E_end, xe_post, sx.x);
-                    if (c.dy && !post)
-                        put1(static_cast<TY *>(c.dy), c.lddy, E_end);
+                        sg = fadd2(sg, g);
+                    if (post)
+                        sx = ffma2(g, x[e], sx);
                 }
-            } else {
-                const float2 zero[4] = {};
-#pragma unroll
-                for (int k = 0; k < kPieces; ++k) {
-                    if (c.d_resid)
-                        put8(static_cast<TR *>(c.d_resid), c.lddr, k, zero);
-                    if (c.dy)
-                        put8(static_cast<TY *>(c.dy), c.lddy, k, zero);
-                    if (dgate)
-                        put8(static_cast<TY *>(c.dgate), c.lddg, k, zero);
-                }
-                if (ENDS) {
-                    if (c.d_resid)
-                        put1(static_cast<TR *>(c.d_resid), c.lddr, 0.f);
-                    if (c.dy)
-                        put1(static_cast<TY *>(c.dy), c.lddy, 0.f);
-                    if (dgate)
-                        put1(static_cast<TY *>(c.dgate), c.lddg, 0.f);
-                }
+                if (put_dy && !post)
+                    put8(TY(), c.dy, ring.dy, k, E + 4 * k);
             }
-            if (c.dy && post) {
-                const float2 v = row_sum(sg, sx);
-                if (m.fine) {
-                    const float2 a0 = splat(layer ? -r0 * (v.x * inv_d) : 0.f), a1 = splat(-r0 * (v.y * inv_d));
-#pragma unroll
-                    for (int k = 0; k < kPieces; ++k) {
-                        float2 x[4];
-                        xh_post(k, x);
-#pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            x[e] = ffma2(E[4 * k + e], splat(r0), GENERAL ? ffma2(x[e], a1, a0) : fmul2(x[e], a1));
-                        put8(static_cast<TY *>(c.dy), c.lddy, k, x);
-                    }
-                    if (ENDS)
-                        put1(static_cast<TY *>(c.dy), c.lddy, fmaf(E_end, r0, fmaf(xe_post, a1.x, a0.x)));
+            if (at_end) {
+                float D = has_dro ? column_value(m.dro, gradient_type<TR>(), 0u) : 0.f;
+                if (pre) {
+                    const float x = column_value(m.resid, kMixed ? ring.resid.dtype : kTypeR, m.e_resid) - m.stats.z;
+                    D = fmaf(x, c1, fmaf(column_value(m.dh, gradient_type<TY>(), 0u) * gamma_end, r1, D)) + c0;
                 }
+                if (put_dr)
+                    put1(TR(), c.d_resid, ring.dr, D * c.resid_scale);
+                ye = needs_y ? (column_value(m.y, kMixed ? ring.y.dtype : kTypeY, m.e_y) - m.stats.x) * scale : 0.f;
+                if (dgate) {
+                    float w = ye;
+                    if (post)
+                        w = fmaf(w, param(c.gamma_post, c.param_dtype, end), c.beta_post ? param(c.beta_post, c.param_dtype, end) : 0.f);
+                    put1(TY(), c.dgate, ring.dgate, s * D * w);
+                }
+                if (token_gate)
+                    D *= column_value(m.gate, gradient_type<TY>(), 0u);
+                sums_end[kPostSum] = fmaf(D, ye, sums_end[kPostSum]);
+                if (GENERAL)
+                    sums_end[kSums - 1] += D;
+                E_end = D * cpost_end;
+                sg.x += E_end;
+                sx.x = fmaf(E_end, ye, sx.x);
+                if (put_dy && !post)
+                    put1(TY(), c.dy, ring.dy, E_end);
             }
+            row_sums.v[0] = sx.x + sx.y;
+            if (GENERAL)
+                row_sums.v[kRowSums - 2] = sg.x + sg.y;
+        } else if (needs_stream) {
+            const float2 zero[4] = {};
+#pragma unroll
+            for (int k = 0; k < kPieces; ++k) {
+                if (put_dr)
+                    put8(TR(), c.d_resid, ring.dr, k, zero);
+                if (put_dy)
+                    put8(TY(), c.dy, ring.dy, k, zero);
+                if (dgate)
+                    put8(TY(), c.dgate, ring.dgate, k, zero);
+            }
+            if (put_dr)
+                put1(TR(), c.d_resid, ring.dr, 0.f);
+            if (put_dy)
+                put1(TY(), c.dy, ring.dy, 0.f);
+            if (dgate)
+                put1(TY(), c.dgate, ring.dgate, 0.f);
+        }
+        wait_copies(ring.stages - 2);
+        __syncwarp();
+        complete(next, own + next_stage * ring.stage, ons >> (ring.stages - 2) & 1);
+        if (pre && next.fine) {
+            float sx, sg;
+            first_sums(own + next_stage * ring.stage, next, sx, sg);
+            row_sums.v[1] = sx;
+            if (GENERAL)
+                row_sums.v[kRowSums - 1] = sg;
+        }
+        if (needs_stream) {
+            row_sums = group_sum(row_sums, red[odd], group, warps);
+            odd ^= 1;
+        }
+        if (put_dy && post && fine) {
+            const float a1 = -r0 * r0 * (row_sums.v[0] * inv_d), a0 = layer ? -r0 * (row_sums.v[kRowSums - 2] * inv_d) : 0.f;
+#pragma unroll
+            for (int k = 0; k < kPieces; ++k) {
+                float2 x[4];
+                const float f = a1 * centred_y(at, m, k, x);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    x[e] = ffma2(x[e], splat(f), fmul2(E[4 * k + e], splat(r0)));
+                    if (GENERAL)
+                        x[e] = fadd2(x[e], splat(a0));
+                }
+                put8(TY(), c.dy, ring.dy, k, x);
+            }
+            if (ENDS)
+                put1(TY(), c.dy, ring.dy, fmaf(E_end, r0, -r0 * (row_sums.v[0] * inv_d) * ye) + a0);
         }
         m = next;
-        stage = stage == ring.depth ? 0 : stage + 1;
+        next = after;
+        stage = next_stage;
     }
     if (!c.workspace)
         return;
     // the block's groups are added up in their order, in shared memory: one row of partial sums per block
-    asm volatile("cp.async.wait_all;" ::: "memory");
+    wait_copies(0);
     __syncthreads();
     float *out = static_cast<float *>(c.workspace) + (int64_t)blockIdx.x * 4 * d;
 #pragma unroll
@@ -493,53 +591,49 @@ __global__ void __launch_bounds__(MOST, PER_SM) k_block_bwd(BlockGradCall c, Rin
     }
 }
 
-}  // namespace
-
-template <typename TR, typename TY> cudaError_t launch_block_rows_bwd(const BlockGradCall &given, int *parts, bool *taken, cudaStream_t stream)
+template <typename TR, typename TY, int kPieces> cudaError_t launch_rows(BlockGradCall c, const Phases &phases, int *parts, bool *taken, cudaStream_t stream)
 {
-    BlockGradCall c = given;
     const bool sums = c.dgamma_pre || c.dbeta_pre || c.dgamma_post || c.dbeta_post || (c.dgate && !c.ldg);
-    const bool needs_y = c.gamma_post ? c.dy || c.dgamma_post || c.dgate : c.dgate != nullptr;
-    const bool token_gate = c.gate && c.ldg;
+    const bool needs_y = block_bwd_needs_y(c), token_gate = c.gate && c.ldg, ends = phases.at || phases.step || c.d % 8;
     if (!sums)
         c.workspace = nullptr;
+    constexpr int kE = 8 * kPieces;
     Ring ring{};
-    const int n = (int)((c.d + kE * 32 - 1) / (kE * 32)) * 32, per = std::max(1, 256 / n);
+    ring.dr = (uint32_t)(c.lddr * sizeof(TR));
+    ring.dy = (uint32_t)(c.lddy * sizeof(TY));
+    ring.dgate = (uint32_t)(c.lddg * sizeof(TY));
+    const int n = (int)((c.d + kE * 32 - 1) / (kE * 32)) * 32, per = std::max(1, 256 / n), threads = n * per;
     const auto add = [&](RingPart &part, const void *p, int64_t ld, int32_t dtype) {
         if (!p)
             return;
         part.p = static_cast<const char *>(p);
         part.dtype = dtype;
         part.bytes = stored_bytes(dtype);
-        part.pitch = ld * part.bytes;
+        part.pitch = (uint32_t)(ld * part.bytes);
         part.at = ring.stage;
         ring.stage += n * kE * part.bytes;
     };
-    const void *resid = c.gamma_pre ? c.resid : nullptr, *y = needs_y ? c.y : nullptr, *gate = token_gate ? c.gate : nullptr;
-    add(ring.resid, resid, c.ldr, c.resid_dtype);
+    add(ring.resid, c.gamma_pre ? c.resid : nullptr, c.ldr, c.resid_dtype);
     add(ring.dh, c.dh, c.lddh, c.grad_y_dtype);
     add(ring.dro, c.d_resid_out, c.lddro, c.grad_r_dtype);
-    add(ring.y, y, c.ldy, c.y_dtype);
-    add(ring.gate, gate, c.ldg, c.grad_y_dtype);
-    const Phases phases{Phase(resid, c.ldr, c.resid_dtype),
-                        Phase(c.dh, c.lddh, c.grad_y_dtype),
-                        Phase(c.d_resid_out, c.lddro, c.grad_r_dtype),
-                        Phase(y, c.ldy, c.y_dtype),
-                        Phase(gate, c.ldg, c.grad_y_dtype),
-                        Phase(c.d_resid, c.lddr, c.grad_r_dtype),
-                        Phase(c.dy, c.lddy, c.grad_y_dtype),
-                        Phase(token_gate ? c.dgate : nullptr, c.lddg, c.grad_y_dtype)};
-    *taken = phases.alike;
+    add(ring.y, needs_y ? c.y : nullptr, c.ldy, c.y_dtype);
+    add(ring.gate, token_gate ? c.gate : nullptr, c.ldg, c.grad_y_dtype);
+    ring.extra = ring.stage;
+    ring.stage += n / 32 * extra_bytes(kPieces);
+    const auto in_blocks = [](const RingPart &p, const uint8_t *exps) {
+        return !p.p || p.bytes != 1 ||
+               (reinterpret_cast<uintptr_t>(p.p) % 16 == 0 && p.pitch % 16 == 0 && reinterpret_cast<uintptr_t>(exps) % 8 == 0);
+    };
+    ring.blocks = c.d % 256 == 0 && !ends && in_blocks(ring.resid, c.resid_exps) && in_blocks(ring.y, c.y_exps);
+    // two CTAs per SM up to 256 threads (320 have the registers, but then one), if each has room for a row in flight beside the two at hand
+    constexpr size_t kRoom = 226 * 1024, kHalf = 112 * 1024;
+    const size_t stage = (size_t)per * std::max(ring.stage, 1), gamma = sizeof(float) * kE * threads;
+    const int per_sm = threads <= most_threads(kPieces) / 2 && 3 * stage + gamma <= kHalf ? 2 : 1;
+    ring.stages = (int)std::min<size_t>(5, ((per_sm == 2 ? kHalf : kRoom) - gamma) / stage);
+    *taken = ring.stages >= 2;  // not rows of 8,192 columns of fp32 with a gate of their own
     if (!*taken)
         return cudaSuccess;
-    const bool ends = phases.at || phases.step || c.d % 8;
-    // two CTAs per SM up to 256 threads, if each then has room for a row in flight ahead of the one at hand
-    constexpr size_t kRoom = 220 * 1024;
-    const int threads = n * per;
-    const size_t stage = (size_t)per * std::max(ring.stage, 1), gamma = sizeof(float) * kE * threads;
-    const int per_sm = threads <= 256 && 2 * (2 * stage + gamma) <= kRoom ? 2 : 1;
-    ring.depth = (int)std::min<size_t>(3, (kRoom / per_sm - gamma) / stage - 1);
-    const size_t smem = std::max<size_t>(stage * (ring.depth + 1) + gamma, sums && per > 1 ? sizeof(float) * per * (size_t)c.d : 0);
+    const size_t smem = std::max<size_t>(stage * ring.stages + gamma, sums && per > 1 ? sizeof(float) * per * (size_t)c.d : 0);
     const int64_t blocks = (c.T + per - 1) / per;
     const int64_t most = std::min<int64_t>((int64_t)per_sm * device_sm_count(), kBlockMaxParts);
     int grid = (int)std::min<int64_t>(blocks > device_sm_count() ? (blocks + 1) / 2 : blocks, most);
@@ -547,7 +641,8 @@ template <typename TR, typename TY> cudaError_t launch_block_rows_bwd(const Bloc
         grid = std::min((grid * per + 7) / 8 * 8 / per, kBlockMaxParts);  // a multiple of eight groups
     *parts = grid;
     const bool general = c.kind == TURNOPD_LAYER_NORM || block_bwd_bias(c);
-    const bool stored = (!resid || c.resid_dtype == c.grad_r_dtype) && (!y || c.y_dtype == c.grad_y_dtype);
+    const bool stored = (!ring.resid.p || c.resid_dtype == c.grad_r_dtype) && (!ring.y.p || c.y_dtype == c.grad_y_dtype);
+    const bool common = c.gamma_pre && c.d_resid_out && c.d_resid && c.dy && sums && !token_gate;
     const auto go = [&](auto kernel) {
         const cudaError_t e = allow_shared(kernel, kRoom);
         if (e != cudaSuccess)
@@ -555,17 +650,47 @@ template <typename TR, typename TY> cudaError_t launch_block_rows_bwd(const Bloc
         kernel<<<grid, threads, smem, stream>>>(c, ring, n, phases.at, phases.step);
         return cudaGetLastError();
     };
-    const auto wide = [&](auto is_stored, auto has_ends, auto is_general) {
-        constexpr bool S = decltype(is_stored)::value, E = decltype(has_ends)::value, G = decltype(is_general)::value;
-        return threads <= 256 ? go(k_block_bwd<TR, TY, S, E, G, 256, 2>) : go(k_block_bwd<TR, TY, S, E, G, 512, 1>);
+    const auto with_general = [&](auto stored, auto has_ends, auto is_common) {
+        constexpr Stored S = decltype(stored)::value;
+        constexpr bool E = decltype(has_ends)::value, C = decltype(is_common)::value;
+        return general ? go(k_block_bwd<TR, TY, kPieces, S, E, true, C>) : go(k_block_bwd<TR, TY, kPieces, S, E, false, C>);
     };
-    const auto with_general = [&](auto is_stored, auto has_ends) {
-        return general ? wide(is_stored, has_ends, std::true_type()) : wide(is_stored, has_ends, std::false_type());
-    };
-    const auto with_ends = [&](auto is_stored) {
-        return ends ? with_general(is_stored, std::true_type()) : with_general(is_stored, std::false_type());
-    };
-    return stored ? with_ends(std::true_type()) : with_ends(std::false_type());
+    const std::integral_constant<Stored, kGradientTypes> gradient_types;
+    const std::integral_constant<Stored, kAny> any;
+    if (common && !ends) {
+        if (stored)
+            return with_general(gradient_types, std::false_type(), std::true_type());
+        if (c.resid_dtype == c.y_dtype && c.y_dtype == TURNOPD_E4M3)
+            return with_general(std::integral_constant<Stored, kE4m3>(), std::false_type(), std::true_type());
+        if (c.resid_dtype == c.y_dtype && c.y_dtype == TURNOPD_INT8)
+            return with_general(std::integral_constant<Stored, kInt8>(), std::false_type(), std::true_type());
+    }
+    if (ends)
+        return stored ? with_general(gradient_types, std::true_type(), std::false_type())
+                      : with_general(any, std::true_type(), std::false_type());
+    return stored ? with_general(gradient_types, std::false_type(), std::false_type())
+                  : with_general(any, std::false_type(), std::false_type());
+}
+
+}  // namespace
+
+template <typename TR, typename TY> cudaError_t launch_block_rows_bwd(const BlockGradCall &c, int *parts, bool *taken, cudaStream_t stream)
+{
+    const bool token_gate = c.gate && c.ldg;
+    const Phases phases{Phase(c.gamma_pre ? c.resid : nullptr, c.ldr, c.resid_dtype),
+                        Phase(c.dh, c.lddh, c.grad_y_dtype),
+                        Phase(c.d_resid_out, c.lddro, c.grad_r_dtype),
+                        Phase(block_bwd_needs_y(c) ? c.y : nullptr, c.ldy, c.y_dtype),
+                        Phase(token_gate ? c.gate : nullptr, c.ldg, c.grad_y_dtype),
+                        Phase(c.d_resid, c.lddr, c.grad_r_dtype),
+                        Phase(c.dy, c.lddy, c.grad_y_dtype),
+                        Phase(token_gate ? c.dgate : nullptr, c.lddg, c.grad_y_dtype)};
+    // rows less than 4 GB apart, so that a row's place is one product of 32 bits by 32, with a piece of eight columns at least
+    const int64_t most = std::max({c.ldr, c.lddh, c.lddro, c.ldy, c.ldg, c.lddr, c.lddy, c.lddg});
+    *taken = phases.alike && most < (int64_t)1 << 30 && c.d >= 16;
+    if (!*taken)
+        return cudaSuccess;
+    return c.d <= 8 * most_threads(1) ? launch_rows<TR, TY, 1>(c, phases, parts, taken, stream) : launch_rows<TR, TY, 2>(c, phases, parts, taken, stream);
 }
 
 }  // namespace turnopd

@@ -78,7 +78,8 @@ __device__ __forceinline__ void decode8(uint2 u, bool e4m3, float *v)
         } else {
 #pragma unroll
             for (int k = 0; k < 4; ++k)
-                v[4 * h + k] = (float)(int8_t)(w >> (8 * k));
+                // the byte plus 128 as the last bits of 2^23: no conversion, of which an SM does few at a time
+                v[4 * h + k] = __uint_as_float(__byte_perm(w ^ 0x80808080u, 0x4b000000u, 0x7440 | k)) - 8388736.f;
         }
     }
 }
