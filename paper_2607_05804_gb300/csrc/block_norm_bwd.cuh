@@ -20,10 +20,8 @@ __device__ __forceinline__ void wait_copies(int pending)
         asm volatile("cp.async.wait_group 0;" ::: "memory");
     else if (pending == 1)
         asm volatile("cp.async.wait_group 1;" ::: "memory");
-    else if (pending == 2)
-        asm volatile("cp.async.wait_group 2;" ::: "memory");
     else
-        asm volatile("cp.async.wait_group 3;" ::: "memory");
+        asm volatile("cp.async.wait_group 2;" ::: "memory");
 }
 
 // One array of a row in the ring.
@@ -41,7 +39,7 @@ struct Ring {
     int extra;   // bytes into a stage: for each warp its copy of the row's statistics and of its columns' exponents
     bool blocks; // rows are whole blocks of 256 columns, whose codes and exponents are copied by the warp
     int stage;   // bytes of a stage of one group
-    int stages;  // 2 to 5: the row at hand, the next one, and those in flight
+    int stages;  // 2 to 4: the row at hand, the next one, and those in flight
 };
 
 // Eight columns from the ring; codes without their scale.
@@ -65,7 +63,7 @@ constexpr int most_threads(int pieces) { return pieces == 1 ? 640 : 512; }
 enum Stored { kGradientTypes, kE4m3, kInt8, kAny };
 template <Stored S, typename T> constexpr int type_code()
 {
-    return S == kGradientTypes ? (sizeof(T) == 2 ? TURNOPD_BF16 : TURNOPD_F32) : S == kE4m3 ? TURNOPD_E4M3 : TURNOPD_INT8;
+    return S == kGradientTypes ? (int)(sizeof(T) == 2 ? TURNOPD_BF16 : TURNOPD_F32) : (int)(S == kE4m3 ? TURNOPD_E4M3 : TURNOPD_INT8);
 }
 constexpr int type_bytes(int dtype) { return dtype == TURNOPD_F32 ? 4 : dtype == TURNOPD_BF16 ? 2 : 1; }
 
@@ -629,7 +627,7 @@ template <typename TR, typename TY, int kPieces> cudaError_t launch_rows(BlockGr
     constexpr size_t kRoom = 226 * 1024, kHalf = 112 * 1024;
     const size_t stage = (size_t)per * std::max(ring.stage, 1), gamma = sizeof(float) * kE * threads;
     const int per_sm = threads <= most_threads(kPieces) / 2 && 3 * stage + gamma <= kHalf ? 2 : 1;
-    ring.stages = (int)std::min<size_t>(5, ((per_sm == 2 ? kHalf : kRoom) - gamma) / stage);
+    ring.stages = (int)std::min<size_t>(4, ((per_sm == 2 ? kHalf : kRoom) - gamma) / stage);
     *taken = ring.stages >= 2;  // not rows of 8,192 columns of fp32 with a gate of their own
     if (!*taken)
         return cudaSuccess;
@@ -690,7 +688,11 @@ template <typename TR, typename TY> cudaError_t launch_block_rows_bwd(const Bloc
     *taken = phases.alike && most < (int64_t)1 << 30 && c.d >= 16;
     if (!*taken)
         return cudaSuccess;
-    return c.d <= 8 * most_threads(1) ? launch_rows<TR, TY, 1>(c, phases, parts, taken, stream) : launch_rows<TR, TY, 2>(c, phases, parts, taken, stream);
+    // Two pieces to a thread and two blocks per SM up to 4,096 columns (from 8-bit activations, 32,768 x 4,096: 277 us, one piece
+    // and one block 352); then one piece, whose blocks have twice the warps (16,384 x 5,120 bf16: 192 us, two pieces 203), as
+    // long as a block's threads hold the row.
+    return c.d <= 4096 || c.d > 8 * most_threads(1) ? launch_rows<TR, TY, 2>(c, phases, parts, taken, stream)
+                                                    : launch_rows<TR, TY, 1>(c, phases, parts, taken, stream);
 }
 
 }  // namespace turnopd

@@ -276,12 +276,12 @@ __global__ void __launch_bounds__(MOST, PER_SM) k_block_fwd(BlockCall c, int n, 
     }
 }
 
-template <typename TR, typename TY, int P, int MOST, int PER_SM>
+template <typename TR, typename TY, bool GATE, int P, int MOST, int PER_SM>
 cudaError_t launch_rows(const BlockCall &c, const Phases &phases, cudaStream_t stream)
 {
     const int n = (int)((c.d + P * 256 - 1) / (P * 256)) * 32, per = std::max(1, 256 / n);
     const int64_t blocks = (c.T + per - 1) / per;
-    const bool gate = c.gate && c.ldg, ends = phases.at || phases.step || c.d % 8;
+    const bool ends = phases.at || phases.step || c.d % 8;
     const bool general = c.kind == TURNOPD_LAYER_NORM || c.beta_post || c.beta_pre;
     const auto go = [&](auto kernel, auto has_ends, auto is_general) {
         constexpr bool E = decltype(has_ends)::value;
@@ -299,25 +299,31 @@ cudaError_t launch_rows(const BlockCall &c, const Phases &phases, cudaStream_t s
         kernel<<<(unsigned)grid, n * per, smem, stream>>>(c, n, phases.at, phases.step);
         return cudaGetLastError();
     };
-    const auto with_general = [&](auto has_gate, auto has_ends) {
-        constexpr bool A = decltype(has_gate)::value, E = decltype(has_ends)::value;
-        return general ? go(k_block_fwd<TR, TY, P, A, E, true, MOST, PER_SM>, has_ends, std::true_type())
-                       : go(k_block_fwd<TR, TY, P, A, E, false, MOST, PER_SM>, has_ends, std::false_type());
+    const auto with_general = [&](auto has_ends) {
+        constexpr bool E = decltype(has_ends)::value;
+        return general ? go(k_block_fwd<TR, TY, P, GATE, E, true, MOST, PER_SM>, has_ends, std::true_type())
+                       : go(k_block_fwd<TR, TY, P, GATE, E, false, MOST, PER_SM>, has_ends, std::false_type());
     };
-    const auto with_ends = [&](auto has_gate) {
-        return ends ? with_general(has_gate, std::true_type()) : with_general(has_gate, std::false_type());
-    };
-    return gate ? with_ends(std::true_type()) : with_ends(std::false_type());
+    return ends ? with_general(std::true_type()) : with_general(std::false_type());
+}
+
+// Many rows: as many pieces to a thread as its registers hold, so that many rows are in flight; few rows: one, so that each
+// answers sooner.
+template <typename TR, typename TY, bool GATE> cudaError_t launch_gated(const BlockCall &c, const Phases &phases, cudaStream_t stream)
+{
+    if (c.T * ((c.d + 1023) / 1024) < 4 * device_sm_count())
+        return c.d <= 4096 ? launch_rows<TR, TY, GATE, 1, 512, 1>(c, phases, stream) : launch_rows<TR, TY, GATE, 1, 1024, 1>(c, phases, stream);
+    if constexpr (sizeof(TR) + sizeof(TY) * (GATE ? 2 : 1) <= 6)
+        return launch_rows<TR, TY, GATE, 4, 256, 2>(c, phases, stream);
+    else
+        return launch_rows<TR, TY, GATE, 2, 512, 1>(c, phases, stream);
 }
 
 }  // namespace
 
-// Many rows: four pieces to a thread, so that many rows are in flight; few rows: one, so that each answers sooner.
 template <typename TR, typename TY> cudaError_t launch_block_rows_fwd(const BlockCall &c, const Phases &phases, cudaStream_t stream)
 {
-    if (c.T * ((c.d + 1023) / 1024) < 4 * device_sm_count())
-        return c.d <= 4096 ? launch_rows<TR, TY, 1, 512, 1>(c, phases, stream) : launch_rows<TR, TY, 1, 1024, 1>(c, phases, stream);
-    return launch_rows<TR, TY, 4, 256, 2>(c, phases, stream);
+    return c.gate && c.ldg ? launch_gated<TR, TY, true>(c, phases, stream) : launch_gated<TR, TY, false>(c, phases, stream);
 }
 
 }  // namespace turnopd
