@@ -22,53 +22,53 @@ constexpr int kPieces = 4;                  // pieces of eight columns that a la
 constexpr int kFwdChunk = 256 * kPieces;    // columns that a warp copies at once
 
 // VEC: rows of both arrays begin on 16-byte boundaries.
-template <typename TW, typename TO, bool VEC> __global__ void __launch_bounds__(32 * kFwdWarps) k_embed(EmbedCall c, int64_t chunks)
+template <typename TW, typename TO, bool VEC> __global__ void __launch_bounds__(32 * kFwdWarps) k_embed(EmbedCall c)
 {
     const int lane = threadIdx.x & 31;
-    const int64_t d = c.d, units = c.T * chunks;
-    for (int64_t u = (int64_t)blockIdx.x * kFwdWarps + (threadIdx.x >> 5); u < units; u += (int64_t)gridDim.x * kFwdWarps) {
-        const int64_t i = u / chunks, first = (u - i * chunks) * kFwdChunk;
-        int id = -1;
-        if (!c.mask || c.mask[i]) {
-            id = c.ids[i];
-            if (id < 0 || id >= c.vocab) {
-                if (lane == 0)
-                    set_status(c.status, TURNOPD_ERR_TOKEN_RANGE);
-                id = -1;
-            }
-        }
-        const TW *w = static_cast<const TW *>(c.w) + (int64_t)max(id, 0) * c.ldw;
-        TO *out = static_cast<TO *>(c.out) + i * c.ldo;
-        const auto one = [&](int64_t j) { out[j] = from_float<TO>(id < 0 ? 0.f : to_float(w[j]) * c.scale); };
-        if constexpr (VEC) {
-            float v[kPieces][8] = {};
-#pragma unroll
-            for (int k = 0; k < kPieces; ++k) {
-                const int64_t j = first + k * 256 + lane * 8;
-                if (id >= 0 && j + 8 <= d)
-                    load8(w + j, v[k]);
-            }
-#pragma unroll
-            for (int k = 0; k < kPieces; ++k) {
-                const int64_t j = first + k * 256 + lane * 8;
-                if (j + 8 <= d) {
-#pragma unroll
-                    for (int h = 0; h < 8; ++h)
-                        v[k][h] *= c.scale;
-                    if (id < 0)
-                        for (int h = 0; h < 8; ++h)
-                            v[k][h] = 0.f;
-                    store8(out + j, v[k]);
-                } else {
-                    for (int64_t h = j; h < d; ++h)
-                        one(h);
+    const int64_t d = c.d;
+    for (int64_t first = (int64_t)blockIdx.y * kFwdChunk; first < d; first += (int64_t)gridDim.y * kFwdChunk)
+        for (int64_t i = (int64_t)blockIdx.x * kFwdWarps + (threadIdx.x >> 5); i < c.T; i += (int64_t)gridDim.x * kFwdWarps) {
+            int id = -1;
+            if (!c.mask || c.mask[i]) {
+                id = c.ids[i];
+                if (id < 0 || id >= c.vocab) {
+                    if (lane == 0)
+                        set_status(c.status, TURNOPD_ERR_TOKEN_RANGE);
+                    id = -1;
                 }
             }
-        } else {
+            const TW *w = static_cast<const TW *>(c.w) + (int64_t)max(id, 0) * c.ldw;
+            TO *out = static_cast<TO *>(c.out) + i * c.ldo;
+            const auto one = [&](int64_t j) { out[j] = from_float<TO>(id < 0 ? 0.f : to_float(w[j]) * c.scale); };
+            if constexpr (VEC) {
+                float v[kPieces][8] = {};
+#pragma unroll
+                for (int k = 0; k < kPieces; ++k) {
+                    const int64_t j = first + k * 256 + lane * 8;
+                    if (id >= 0 && j + 8 <= d)
+                        load8(w + j, v[k]);
+                }
+#pragma unroll
+                for (int k = 0; k < kPieces; ++k) {
+                    const int64_t j = first + k * 256 + lane * 8;
+                    if (j + 8 <= d) {
+#pragma unroll
+                        for (int h = 0; h < 8; ++h)
+                            v[k][h] *= c.scale;
+                        if (id < 0)
+                            for (int h = 0; h < 8; ++h)
+                                v[k][h] = 0.f;
+                        store8(out + j, v[k]);
+                    } else {
+                        for (int64_t h = j; h < d; ++h)
+                            one(h);
+                    }
+                }
+            } else {
 #pragma unroll 8
-            for (int64_t j = first + lane; j < min(first + kFwdChunk, d); j += 32)
-                one(j);
-        }
+                for (int64_t j = first + lane; j < min(first + kFwdChunk, d); j += 32)
+                    one(j);
+            }
     }
 }
 
@@ -77,59 +77,105 @@ template <typename TW, typename TO, bool VEC> __global__ void __launch_bounds__(
 constexpr int kSortThreads = 1024, kSortWarps = 32;
 constexpr int kMaxCtas = 8;       // of the sort's cluster
 constexpr int kRadixBits = 9;     // at most, of one pass
+constexpr int kSortBatch = 8;     // keys of a lane in flight
 
 struct SortBuffers {
     uint32_t *key[2];
     int32_t *at[2];
 };
 
-// One cluster sorts all tokens, least significant digits first: each CTA takes a part of the list and each of its warps a part
-// of that, in order.  A warp counts its digits, the counts are summed up over the warps, the CTAs and the digits, and the warp
-// puts its keys where they belong.  Tokens that are masked or whose id is out of range get the key `vocab` and come last.
-// The last pass leaves the list in buffer (passes & 1).  present (or null): a bit for each id that occurs.
-__global__ void __launch_bounds__(kSortThreads) k_sort_tokens(const int32_t *__restrict__ ids, const uint8_t *__restrict__ mask,
-                                                              int64_t T, int64_t vocab, SortBuffers b, int passes, int bits,
-                                                              uint32_t *present, int32_t *status)
+// Zeros from CTA `cta` of `ctas` into all rows of dw.
+template <typename TW> __device__ __forceinline__ void zero_rows(const EmbedGradCall &c, int64_t cta, int64_t ctas)
+{
+    TW *w = static_cast<TW *>(c.dw);
+    constexpr int W = 16 / (int)sizeof(TW);
+    const int64_t thread = cta * blockDim.x + threadIdx.x, threads = ctas * blockDim.x;
+    if (c.ldw == c.d && reinterpret_cast<uintptr_t>(w) % 16 == 0) {
+        const int64_t n = c.vocab * c.d;
+        for (int64_t j = thread; j < n / W; j += threads)
+            __stcs(reinterpret_cast<uint4 *>(w) + j, make_uint4(0u, 0u, 0u, 0u));
+        if (thread < n % W)
+            w[n / W * W + thread] = from_float<TW>(0.f);
+        return;
+    }
+    const int lane = threadIdx.x & 31;
+    const bool vec = reinterpret_cast<uintptr_t>(w) % 16 == 0 && c.ldw % W == 0;
+    for (int64_t v = thread / 32; v < c.vocab; v += threads / 32) {
+        TW *row = w + v * c.ldw;
+        const int64_t whole = vec ? c.d / W : 0;
+        for (int64_t j = lane; j < whole; j += 32)
+            __stcs(reinterpret_cast<uint4 *>(row) + j, make_uint4(0u, 0u, 0u, 0u));
+        for (int64_t j = whole * W + lane; j < c.d; j += 32)
+            row[j] = from_float<TW>(0.f);
+    }
+}
+
+// The first cluster sorts all tokens, least significant digits first: each CTA takes a part of the list and each of its warps a
+// part of that, in order.  A warp counts its digits, the counts are summed up over the warps, the CTAs and the digits, and the
+// warp puts its keys where they belong.  Tokens that are masked or whose id is out of range get the key `vocab` and come last.
+// The last pass leaves the list in buffer (passes & 1).  Meanwhile the other clusters write zeros into the whole table: the
+// rows of ids that occur are written over by the sums, which costs less than to find out first which do (151,936 x 4,096 bf16,
+// 32,768 tokens: 12 us more of writing; the sort's 20 us behind it).
+__global__ void __launch_bounds__(kSortThreads) k_sort_tokens(EmbedGradCall c, SortBuffers b, int passes, int bits, uint32_t ctas)
 {
     extern __shared__ uint32_t counts[];  // [kSortWarps][bins]
     __shared__ uint32_t total[1 << kRadixBits], warp_total[kSortWarps];
+    pdl_begin();
+    if (blockIdx.x >= ctas) {
+        if (c.dw_dtype == TURNOPD_BF16)
+            zero_rows<__nv_bfloat16>(c, blockIdx.x - ctas, gridDim.x - ctas);
+        else
+            zero_rows<float>(c, blockIdx.x - ctas, gridDim.x - ctas);
+        return;
+    }
+    const int64_t T = c.T, vocab = c.vocab;
     const int bins = 1 << bits, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const uint32_t rank = cluster_ctarank(), ctas = gridDim.x;
+    const uint32_t rank = cluster_ctarank();
     const int64_t seg = ((T + (int64_t)ctas * kSortWarps - 1) / ((int64_t)ctas * kSortWarps) + 31) / 32 * 32;
     const int64_t lo = min(T, ((int64_t)rank * kSortWarps + warp) * seg), hi = min(T, lo + seg);
     uint32_t *mine = counts + warp * bins;
-    if (present)
-        for (int64_t w = (int64_t)rank * kSortThreads + threadIdx.x; w < (vocab + 31) / 32; w += (int64_t)ctas * kSortThreads)
-            present[w] = 0;
     for (int p = 0; p < passes; ++p) {
         const uint32_t *from = b.key[p & 1];
         const auto key_of = [&](int64_t i) -> uint32_t {
+            if (i >= hi)
+                return 0u;
             if (p)
                 return __ldcg(from + i);
-            if (mask && !mask[i])
+            if (c.mask && !c.mask[i])
                 return (uint32_t)vocab;
-            const int id = ids[i];
+            const int id = c.ids[i];
             if (id >= 0 && id < vocab)
                 return (uint32_t)id;
-            set_status(status, TURNOPD_ERR_TOKEN_RANGE);
+            set_status(c.status, TURNOPD_ERR_TOKEN_RANGE);
             return (uint32_t)vocab;
         };
         const int shift = p * bits;
         for (int k = lane; k < bins; k += 32)
             mine[k] = 0;
         __syncwarp();
-        for (int64_t i = lo + lane; i - lane < hi; i += 32) {
-            const uint32_t digit = i < hi ? (key_of(i) >> shift) & (bins - 1) : ~0u;
-            const uint32_t peers = __match_any_sync(~0u, digit);
-            if (i < hi && lane == __ffs(peers) - 1)
-                mine[digit] += __popc(peers);
-            __syncwarp();
+        for (int64_t first = lo; first < hi; first += 32 * kSortBatch) {
+            uint32_t key[kSortBatch];
+#pragma unroll
+            for (int k = 0; k < kSortBatch; ++k)
+                key[k] = key_of(first + 32 * k + lane);
+#pragma unroll
+            for (int k = 0; k < kSortBatch; ++k) {
+                const bool there = first + 32 * k + lane < hi;
+                if (first + 32 * k >= hi)
+                    break;
+                const uint32_t digit = there ? (key[k] >> shift) & (bins - 1) : ~0u;
+                const uint32_t peers = __match_any_sync(~0u, digit);
+                if (there && lane == __ffs(peers) - 1)
+                    mine[digit] += __popc(peers);
+                __syncwarp();
+            }
         }
         __syncthreads();
         // per digit: the sum over the warps, and each warp's place in it
         const int bin = threadIdx.x;
         if (bin < bins) {
             uint32_t sum = 0;
+#pragma unroll 8
             for (int w = 0; w < kSortWarps; ++w) {
                 const uint32_t n = counts[w * bins + bin];
                 counts[w * bins + bin] = sum;
@@ -154,41 +200,52 @@ __global__ void __launch_bounds__(kSortThreads) k_sort_tokens(const int32_t *__r
         if (lane == 31)
             warp_total[warp] = scan;
         __syncthreads();
-        for (int w = 0; w < warp; ++w)
-            before += warp_total[w];
-        if (bin < bins)
+        if (bin < bins) {
+            for (int w = 0; w < warp; ++w)
+                before += warp_total[w];
+#pragma unroll 8
             for (int w = 0; w < kSortWarps; ++w)
                 counts[w * bins + bin] += before + scan - all;
+        }
         __syncthreads();
-        for (int64_t i = lo + lane; i - lane < hi; i += 32) {
-            const uint32_t key = i < hi ? key_of(i) : 0u, digit = i < hi ? (key >> shift) & (bins - 1) : ~0u;
-            const uint32_t peers = __match_any_sync(~0u, digit);
-            uint32_t to = 0;
-            if (i < hi)
-                to = mine[digit] + __popc(peers & ((1u << lane) - 1u));
-            __syncwarp();
-            if (i < hi) {
-                if (lane == __ffs(peers) - 1)
-                    mine[digit] += __popc(peers);
-                __stcg(b.key[~p & 1] + to, key);
-                __stcg(b.at[~p & 1] + to, p ? __ldcg(b.at[p & 1] + i) : (int32_t)i);
+        for (int64_t first = lo; first < hi; first += 32 * kSortBatch) {
+            uint32_t key[kSortBatch];
+            int32_t at[kSortBatch];
+#pragma unroll
+            for (int k = 0; k < kSortBatch; ++k) {
+                const int64_t i = first + 32 * k + lane;
+                key[k] = key_of(i);
+                at[k] = p && i < hi ? __ldcg(b.at[p & 1] + i) : (int32_t)i;
             }
-            __syncwarp();
+#pragma unroll
+            for (int k = 0; k < kSortBatch; ++k) {
+                const bool there = first + 32 * k + lane < hi;
+                if (first + 32 * k >= hi)
+                    break;
+                const uint32_t digit = there ? (key[k] >> shift) & (bins - 1) : ~0u;
+                const uint32_t peers = __match_any_sync(~0u, digit);
+                uint32_t to = 0;
+                if (there)
+                    to = mine[digit] + __popc(peers & ((1u << lane) - 1u));
+                __syncwarp();
+                if (there) {
+                    if (lane == __ffs(peers) - 1)
+                        mine[digit] += __popc(peers);
+                    __stcg(b.key[~p & 1] + to, key[k]);
+                    __stcg(b.at[~p & 1] + to, at[k]);
+                }
+                __syncwarp();
+            }
         }
         cluster_sync();
     }
-    if (present)
-        for (int64_t i = (int64_t)rank * kSortThreads + threadIdx.x; i < T; i += (int64_t)ctas * kSortThreads) {
-            const uint32_t key = __ldcg(b.key[passes & 1] + i);
-            if (key < vocab && (i == 0 || __ldcg(b.key[passes & 1] + i - 1) != key))
-                atomicOr(present + key / 32, 1u << (key & 31));
-        }
 }
 
 // ---------------------------------------------------------------- sums
 
 constexpr int kSumThreads = 256;
-constexpr int kMaxTiles = 1024;
+constexpr int kMaxTile = 512;   // positions
+constexpr int kListed = 1024;  // tiles that a block of the last kernel looks at together
 
 // Eight columns of a thread: consecutive ones (VEC), or `step` apart.
 template <bool VEC> struct Columns {
@@ -235,145 +292,221 @@ __device__ __forceinline__ void put_row(const EmbedGradCall &c, const Columns<VE
     cols.store(w, sum);
 }
 
-// CTAs [0, tiles slices): a tile of the sorted list and a slice of the columns each.  A run that lies in the tile goes to dW;
-// one that began before it leaves its sum in partial row 2 t, one that began in it and goes on in 2 t + 1.  The CTAs
-// after them write the zeros of the ids that do not occur.
+constexpr int kRows = 8;  // in flight
+
+// A tile of the sorted list and a slice of the columns.  A tile owns the runs that begin in it, and goes on with its last run
+// through the next tile.  A run that ends by then goes to dW; a longer one leaves the sum of its owner's two tiles in partial
+// row 2 t + 1, and of each later tile that it reaches in that tile's row 2 t.  The rows come through a ring in shared memory,
+// in which each thread copies and reads its own columns (bf16 rows that begin at odd elements: a row ahead, in registers).
 template <typename TG, typename TW, bool VEC>
-__global__ void __launch_bounds__(kSumThreads) k_embed_sums(EmbedGradCall c, const uint32_t *__restrict__ key,
-                                                            const int32_t *__restrict__ at, int tile, int tiles, int slices,
-                                                            float *partial, int64_t ldp, const uint32_t *__restrict__ present)
+__global__ void __launch_bounds__(kSumThreads) k_embed_sums(EmbedGradCall c, const uint32_t *__restrict__ keys,
+                                                            const int32_t *__restrict__ ats, int tile, int slices, float *partial,
+                                                            int64_t ldp)
 {
+    constexpr bool kRing = VEC || sizeof(TG) == 4;
+    extern __shared__ __align__(16) char ring[];
+    __shared__ uint32_t key[2 * kMaxTile + 2];  // from the position before the tile to the one after the next tile
+    __shared__ int32_t at[2 * kMaxTile];
+    pdl_begin();
     const int64_t T = c.T, d = c.d;
-    if (blockIdx.x >= (unsigned)(tiles * slices)) {
-        const int lane = threadIdx.x & 31, nw = blockDim.x >> 5;
-        const int64_t warps = (int64_t)(gridDim.x - tiles * slices) * nw;
-        for (int64_t w = (int64_t)(blockIdx.x - tiles * slices) * nw + (threadIdx.x >> 5); w < (c.vocab + 31) / 32; w += warps) {
-            const int64_t left = c.vocab - w * 32;
-            uint32_t off = ~present[w] & (left < 32 ? (1u << left) - 1u : ~0u);
-            while (off) {
-                const int k = __ffs(off) - 1;
-                off &= off - 1;
-                TW *row = static_cast<TW *>(c.dw) + (w * 32 + k) * c.ldw;
-                const float zero[8] = {};
-                for (int64_t j = VEC ? lane * 8 : lane; j < d; j += 256) {
-                    const Columns<VEC> cols{j, d, 32};
-                    cols.store(row, zero);
+    const uint32_t none = (uint32_t)c.vocab;
+    const int t = blockIdx.x / slices, slice = blockIdx.x % slices;
+    const int64_t base = (int64_t)slice * 8 * blockDim.x, lo = (int64_t)t * tile;
+    const Columns<VEC> cols{base + (VEC ? threadIdx.x * 8 : threadIdx.x), d, (int)blockDim.x};
+    const int size = (int)min(T - lo, (int64_t)tile), most = (int)min(T - lo, (int64_t)2 * tile);  // positions of the tile, and of both
+    for (int q = threadIdx.x; q < most + 2; q += blockDim.x) {
+        const int64_t p = lo - 1 + q;
+        key[q] = p >= 0 && p < T ? keys[p] : none;
+        if (q < most)
+            at[q] = ats[lo + q];
+    }
+    const bool long_ago = t > 1 && keys[lo - tile - 1] == keys[lo];
+    __syncthreads();
+    uint32_t run = key[1];
+    if (run == none)
+        return;
+    const uint32_t last = key[size];
+    bool leading = lo > 0 && key[0] == run;        // begun before this tile:
+    bool skip = leading && !long_ago;              // in the last one, whose it is then
+    const bool all_leading = leading && last == run;
+    const bool skip_first = skip;
+    const uint32_t first = run;
+    const auto wanted = [&](int q) {
+        const uint32_t k = key[q + 1];
+        return q < most && k != none && (q < size || (k == last && !all_leading)) && !(skip_first && k == first);
+    };
+    float sum[8] = {}, ahead[8];
+    const auto issue = [&](int q) {
+        const TG *row = static_cast<const TG *>(c.dout) + (wanted(q) ? (int64_t)at[q] * c.ldg : 0);
+        if constexpr (kRing) {
+            if (wanted(q)) {
+                if (VEC && cols.first + 8 <= d) {
+                    char *to = ring + ((q % kRows) * blockDim.x + threadIdx.x) * 8 * sizeof(TG);
+#pragma unroll
+                    for (int h = 0; h < (int)sizeof(TG) / 2; ++h)
+                        cp16(to + 16 * h, reinterpret_cast<const char *>(row + cols.first) + 16 * h);
+                } else if (!VEC) {
+#pragma unroll
+                    for (int h = 0; h < 8; ++h)
+                        if (cols.at(h) < d)
+                            asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(
+                                             (uint32_t)__cvta_generic_to_shared(ring + (((q % kRows) * 8 + h) * blockDim.x + threadIdx.x) * 4)),
+                                         "l"(row + cols.at(h))
+                                         : "memory");
                 }
             }
+            asm volatile("cp.async.commit_group;" ::: "memory");
+        } else if (wanted(q)) {
+            cols.load(row, ahead);
         }
-        return;
-    }
-    const int t = blockIdx.x / slices, slice = blockIdx.x % slices;
-    const int64_t base = (int64_t)slice * 8 * blockDim.x;
-    const Columns<VEC> cols{base + (VEC ? threadIdx.x * 8 : threadIdx.x), d, (int)blockDim.x};
-    const int64_t lo = (int64_t)t * tile, hi = min(T, lo + tile);
-    float sum[8] = {};
-    uint32_t run = key[lo];
-    bool begun = lo > 0 && key[lo - 1] == run;  // before this tile
-    const auto flush = [&](bool goes_on) {
-        if (begun || goes_on) {
-            float *p = partial + (2 * (int64_t)t + (begun ? 0 : 1)) * ldp;
-            cols.store(p, sum);
-        } else {
-            put_row<TW, VEC>(c, cols, run, sum);
-        }
-#pragma unroll
-        for (int k = 0; k < 8; ++k)
-            sum[k] = 0.f;
-        begun = false;
     };
-    for (int64_t p = lo; p < hi; ++p) {
-        const uint32_t k = key[p];
-        if (k != run) {
-            flush(false);
-            run = k;
-        }
-        if (k >= (uint32_t)c.vocab)
-            return;
+    const auto add = [&](int q) {
         float v[8];
-        cols.load(static_cast<const TG *>(c.dout) + (int64_t)at[p] * c.ldg, v);
+        if constexpr (kRing) {
+            asm volatile("cp.async.wait_group %0;" ::"n"(kRows - 1) : "memory");
+            if (VEC && cols.first + 8 <= d) {
+                load8(reinterpret_cast<const TG *>(ring) + ((q % kRows) * blockDim.x + threadIdx.x) * 8, v);
+            } else if (VEC) {
+                cols.load(static_cast<const TG *>(c.dout) + (int64_t)at[q] * c.ldg, v);  // the last columns of a row
+            } else {
+#pragma unroll
+                for (int h = 0; h < 8; ++h)
+                    v[h] = cols.at(h) < d ? reinterpret_cast<const float *>(ring)[((q % kRows) * 8 + h) * blockDim.x + threadIdx.x] : 0.f;
+            }
+        } else {
+#pragma unroll
+            for (int h = 0; h < 8; ++h)
+                v[h] = ahead[h];
+        }
+        if (kRing || q + 1 < most)
+            issue(kRing ? q + kRows : q + 1);
+        if (!skip)
+#pragma unroll
+            for (int h = 0; h < 8; ++h)
+                sum[h] += v[h];
+    };
+    const auto flush = [&](bool goes_on) {
+        if (!skip) {
+            if (leading || goes_on)
+                cols.store(partial + (2 * (int64_t)t + (leading ? 0 : 1)) * ldp, sum);
+            else
+                put_row<TW, VEC>(c, cols, run, sum);
+        }
 #pragma unroll
         for (int h = 0; h < 8; ++h)
-            sum[h] += v[h];
+            sum[h] = 0.f;
+        leading = skip = false;
+    };
+    for (int q = 0; q < (kRing ? kRows : 1); ++q)
+        issue(q);
+#pragma unroll 1
+    for (int q = 0;; ++q) {
+        const uint32_t k = key[q + 1];  // past both tiles: the position after them
+        const bool over = q >= most || k == none || (q >= size && (k != run || leading || skip));
+        if (k != run || over) {
+            flush(over && k == run);
+            if (over)
+                break;
+            run = k;
+        }
+        add(q);
     }
-    flush(hi < T && key[hi] == run);
+    if (kRing)
+        asm volatile("cp.async.wait_all;" ::: "memory");
 }
 
-// Runs over several tiles: the partial sums of the tile they began in and of those they go on in.  32 threads take 256
+// Runs over more than two tiles: the partial sums of the tile they began in and of those they go on in.  32 threads take 256
 // columns, the block's eight warps share the tiles of a run, and their sums are added up in order.
 template <typename TW>
 __global__ void __launch_bounds__(256) k_embed_join(EmbedGradCall c, const uint32_t *__restrict__ key, int tile, int tiles,
                                                     int slices, const float *__restrict__ partial, int64_t ldp)
 {
-    __shared__ int owner[kMaxTiles], first_of[kMaxTiles / 32 + 1];
+    __shared__ int owner[kListed], first_of[kListed / 32 + 1];
     __shared__ float part[8][256];
+    pdl_begin();
     const int64_t d = c.d;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    static_assert(kMaxTiles == 32 * 32, "one warp adds up the counts");
-    // tile t owns a run that begins in it and goes on in tile t + 1; every block lists the owners in the same order
-    for (int w = warp; w < kMaxTiles / 32; w += 8) {
-        const int t = w * 32 + lane;
-        bool owns = false;
-        if (t + 1 < tiles) {
-            const uint32_t k = key[(int64_t)(t + 1) * tile - 1];
-            owns = k < (uint32_t)c.vocab && key[(int64_t)(t + 1) * tile] == k && (t == 0 || key[(int64_t)t * tile - 1] != k);
-        }
-        const uint32_t owners = __ballot_sync(~0u, owns);
-        if (lane == 0)
-            first_of[w + 1] = (int)owners;
-    }
-    __syncthreads();
-    if (warp == 0) {
-        const uint32_t owners = (uint32_t)first_of[lane + 1];
-        int scan = __popc(owners);
-        for (int o = 1; o < 32; o <<= 1) {
-            const int n = __shfl_up_sync(~0u, scan, o);
-            scan += lane >= o ? n : 0;
-        }
-        int place = scan - __popc(owners);
-        for (uint32_t left = owners; left; left &= left - 1)
-            owner[place++] = lane * 32 + __ffs(left) - 1;
-        __syncwarp();
-        first_of[lane + 1] = scan;
-    }
-    __syncthreads();
-    const int n = first_of[kMaxTiles / 32] * slices;
-    for (int item = blockIdx.x; item < n; item += gridDim.x) {
-        const int t = owner[item / slices], slice = item % slices;
-        const uint32_t k = key[(int64_t)(t + 1) * tile - 1];
-        const Columns<true> cols{(int64_t)slice * 256 + lane * 8, ldp, 1};  // of the partial sums, whose rows are padded
-        float sum[8] = {};
-        for (int s = t + 1 + warp; s < tiles && key[(int64_t)s * tile] == k; s += 8) {
-            float v[8];
-            if (cols.first < ldp) {
-                cols.load(partial + 2 * (int64_t)s * ldp, v);
+    static_assert(kListed == 32 * 32, "one warp adds up the counts");
+    for (int t0 = 0; t0 + 2 < tiles; t0 += kListed) {
+        // tile t owns a run that begins in it and goes on in tile t + 2; every block lists the owners in the same order
+        __syncthreads();
 #pragma unroll
-                for (int h = 0; h < 8; ++h)
-                    sum[h] += v[h];
+        for (int w = warp; w < kListed / 32; w += 8) {
+            const int t = t0 + w * 32 + lane;
+            bool owns = false;
+            if (t + 2 < tiles) {
+                const uint32_t k = key[(int64_t)(t + 1) * tile - 1], later = key[(int64_t)(t + 2) * tile];
+                const uint32_t earlier = t ? key[(int64_t)t * tile - 1] : ~0u;
+                owns = k < (uint32_t)c.vocab && later == k && earlier != k;
             }
-        }
-#pragma unroll
-        for (int h = 0; h < 8; ++h)
-            part[warp][lane * 8 + h] = sum[h];
-        __syncthreads();
-        const int64_t j = (int64_t)slice * 256 + threadIdx.x;
-        if (j < d) {
-            float s = partial[(2 * (int64_t)t + 1) * ldp + j];
-#pragma unroll
-            for (int w = 0; w < 8; ++w)
-                s += part[w][threadIdx.x];
-            TW *w = static_cast<TW *>(c.dw) + (int64_t)k * c.ldw + j;
-            s *= c.scale;
-            *w = from_float<TW>(c.accumulate ? to_float(*w) + s : s);
+            const uint32_t owners = __ballot_sync(~0u, owns);
+            if (lane == 0)
+                first_of[w + 1] = (int)owners;
         }
         __syncthreads();
+        if (warp == 0) {
+            const uint32_t owners = (uint32_t)first_of[lane + 1];
+            int scan = __popc(owners);
+            for (int o = 1; o < 32; o <<= 1) {
+                const int n = __shfl_up_sync(~0u, scan, o);
+                scan += lane >= o ? n : 0;
+            }
+            int place = scan - __popc(owners);
+            for (uint32_t left = owners; left; left &= left - 1)
+                owner[place++] = t0 + lane * 32 + __ffs(left) - 1;
+            __syncwarp();
+            first_of[lane + 1] = scan;
+        }
+        __syncthreads();
+        const int n = first_of[kListed / 32] * slices;
+        for (int item = blockIdx.x; item < n; item += gridDim.x) {
+            const int t = owner[item / slices], slice = item % slices;
+            const uint32_t k = key[(int64_t)(t + 1) * tile - 1];
+            const Columns<true> cols{(int64_t)slice * 256 + lane * 8, ldp, 1};  // of the partial sums, whose rows are padded
+            float sum[8] = {};
+            for (int s0 = t + 2 + warp; s0 < tiles; s0 += 32) {
+                bool in[4];
+                float v[4][8];
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+                    in[q] = s0 + 8 * q < tiles && key[(int64_t)(s0 + 8 * q) * tile] == k;
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+                    if (in[q] && cols.first < ldp)
+                        cols.load(partial + 2 * (int64_t)(s0 + 8 * q) * ldp, v[q]);
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+                    if (in[q] && cols.first < ldp)
+#pragma unroll
+                        for (int h = 0; h < 8; ++h)
+                            sum[h] += v[q][h];
+                if (!in[3])
+                    break;
+            }
+#pragma unroll
+            for (int h = 0; h < 8; ++h)
+                part[warp][h * 32 + lane] = sum[h];
+            __syncthreads();
+            const int64_t j = (int64_t)slice * 256 + threadIdx.x;
+            if (j < d) {
+                float s = partial[(2 * (int64_t)t + 1) * ldp + j];
+#pragma unroll
+                for (int w = 0; w < 8; ++w)
+                    s += part[w][(threadIdx.x & 7) * 32 + (threadIdx.x >> 3)];
+                TW *w = static_cast<TW *>(c.dw) + (int64_t)k * c.ldw + j;
+                s *= c.scale;
+                *w = from_float<TW>(c.accumulate ? to_float(*w) + s : s);
+            }
+            __syncthreads();
+        }
     }
 }
 
+// 1,024 tiles, of 8 to 512 positions
 int tile_size(int64_t T)
 {
     int n = 8;
-    while ((T + n - 1) / n > kMaxTiles)
+    while (n < kMaxTile && (T + n - 1) / n > kListed)
         n *= 2;
     return n;
 }
@@ -385,11 +518,10 @@ bool boundary(const void *p, int64_t ld, int32_t dtype)
 
 struct Workspace {
     SortBuffers sort;
-    uint32_t *present;
     float *partial;
     int64_t ldp;
     size_t bytes;
-    Workspace(void *ws, int64_t T, int64_t d, int64_t vocab) : ldp((d + 7) / 8 * 8)
+    Workspace(void *ws, int64_t T, int64_t d) : ldp((d + 7) / 8 * 8)
     {
         char *p = static_cast<char *>(ws);
         const auto take = [&](size_t n) {
@@ -402,7 +534,6 @@ struct Workspace {
             sort.key[k] = reinterpret_cast<uint32_t *>(take(sizeof(uint32_t) * (size_t)T));
             sort.at[k] = reinterpret_cast<int32_t *>(take(sizeof(int32_t) * (size_t)T));
         }
-        present = reinterpret_cast<uint32_t *>(take(sizeof(uint32_t) * (size_t)((vocab + 31) / 32)));
         const int tile = tile_size(T);
         partial = reinterpret_cast<float *>(take(sizeof(float) * 2 * (size_t)ldp * (size_t)((T + tile - 1) / tile)));
     }
@@ -410,25 +541,26 @@ struct Workspace {
 
 }  // namespace
 
-size_t embed_bwd_workspace_bytes(int64_t T, int64_t d, int64_t vocab) { return Workspace(nullptr, T, d, vocab).bytes; }
+size_t embed_bwd_workspace_bytes(int64_t T, int64_t d) { return std::max<size_t>(Workspace(nullptr, T, d).bytes, 256); }
 
 cudaError_t launch_embed(const EmbedCall &c, cudaStream_t stream)
 {
-    const int64_t chunks = (c.d + kFwdChunk - 1) / kFwdChunk;
-    const unsigned grid = (unsigned)std::min<int64_t>((c.T * chunks + kFwdWarps - 1) / kFwdWarps, (int64_t)device_sm_count() * 16);
+    const int64_t chunks = (c.d + kFwdChunk - 1) / kFwdChunk, blocks = (c.T + kFwdWarps - 1) / kFwdWarps;
+    const dim3 grid((unsigned)std::min<int64_t>(blocks, std::max<int64_t>((int64_t)device_sm_count() * 16 / chunks, 1)),
+                    (unsigned)std::min<int64_t>(chunks, 65535));
     const bool vec = boundary(c.w, c.ldw, c.w_dtype) && boundary(c.out, c.ldo, c.out_dtype);
     with_types(c.w_dtype, c.out_dtype, [&](auto w, auto o) {
         using W = decltype(w);
         using O = decltype(o);
         auto kernel = vec ? k_embed<W, O, true> : k_embed<W, O, false>;
-        kernel<<<grid, 32 * kFwdWarps, 0, stream>>>(c, chunks);
+        kernel<<<grid, 32 * kFwdWarps, 0, stream>>>(c);
     });
     return cudaGetLastError();
 }
 
 cudaError_t launch_embed_bwd(const EmbedGradCall &c, cudaStream_t stream)
 {
-    const Workspace ws(c.workspace, c.T, c.d, c.vocab);
+    const Workspace ws(c.workspace, c.T, c.d);
     int key_bits = 1;
     while ((int64_t)1 << key_bits <= c.vocab)
         ++key_bits;
@@ -436,40 +568,48 @@ cudaError_t launch_embed_bwd(const EmbedGradCall &c, cudaStream_t stream)
     cudaError_t e = allow_shared(k_sort_tokens, sizeof(uint32_t) * kSortWarps << kRadixBits);
     if (e != cudaSuccess)
         return e;
+    // 32 KB of zeros to a CTA at least, and as many CTAs as the device holds
+    const int64_t zeros = c.accumulate ? 0 : c.vocab * c.d * (c.dw_dtype == TURNOPD_BF16 ? 2 : 4);
+    const unsigned ctas = c.T > kSortThreads ? kMaxCtas : 1;
+    const unsigned fill = (unsigned)std::min<int64_t>((zeros + 32767) / 32768, (int64_t)device_sm_count() * 2 - kMaxCtas);
     cudaLaunchConfig_t cfg = {};
-    cudaLaunchAttribute attr[1];
-    cfg.gridDim = c.T > kSortThreads ? kMaxCtas : 1;
+    cudaLaunchAttribute attr[2];
+    cfg.gridDim = (ctas + fill + ctas - 1) / ctas * ctas;
     cfg.blockDim = kSortThreads;
     cfg.dynamicSmemBytes = sizeof(uint32_t) * kSortWarps << bits;
     cfg.stream = stream;
     attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = cfg.gridDim.x;
+    attr[0].val.clusterDim.x = ctas;
     attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    e = cudaLaunchKernelEx(&cfg, k_sort_tokens, c.ids, c.mask, c.T, c.vocab, ws.sort, passes, bits,
-                           c.accumulate ? (uint32_t *)nullptr : ws.present, c.status);
-    if (e != cudaSuccess)
+    cfg.numAttrs = 2;
+    e = cudaLaunchKernelEx(&cfg, k_sort_tokens, c, ws.sort, passes, bits, (uint32_t)ctas);
+    if (e != cudaSuccess || c.T == 0)
         return e;
     const uint32_t *key = ws.sort.key[passes & 1];
     const int32_t *at = ws.sort.at[passes & 1];
     const int tile = tile_size(c.T), tiles = (int)((c.T + tile - 1) / tile);
     const int threads = (int)std::min<int64_t>(kSumThreads, (c.d + 255) / 256 * 32), slices = (int)((c.d + 8 * threads - 1) / (8 * threads));
-    const int zero = c.accumulate ? 0 : (int)std::min<int64_t>((c.vocab + 255) / 256, (int64_t)device_sm_count() * 4);
     const bool vec = boundary(c.dout, c.ldg, c.dout_dtype) && boundary(c.dw, c.ldw, c.dw_dtype);
     with_types(c.dout_dtype, c.dw_dtype, [&](auto g, auto w) {
         using G = decltype(g);
         using W = decltype(w);
+        const size_t smem = vec || sizeof(G) == 4 ? sizeof(G) * 8 * kRows * (size_t)threads : 0;
         auto sums = vec ? k_embed_sums<G, W, true> : k_embed_sums<G, W, false>;
-        if (tiles * slices + zero > 0)
-            sums<<<tiles * slices + zero, threads, 0, stream>>>(c, key, at, tile, tiles, slices, ws.partial, ws.ldp, ws.present);
-        if (tiles > 1) {
+        e = allow_shared(sums, sizeof(G) * 8 * kRows * kSumThreads);
+        if (e != cudaSuccess)
+            return;
+        e = launch_dependent(sums, dim3((unsigned)((int64_t)tiles * slices)), dim3(threads), smem, stream, c, key, at, tile,
+                             slices, ws.partial, ws.ldp);
+        if (e == cudaSuccess && tiles > 2) {
             const int n = (int)((c.d + 255) / 256);
-            const unsigned grid = (unsigned)std::min<int64_t>((int64_t)(tiles - 1) * n, (int64_t)device_sm_count() * 4);
-            k_embed_join<W><<<grid, 256, 0, stream>>>(c, key, tile, tiles, n, ws.partial, ws.ldp);
+            const unsigned grid = (unsigned)std::min<int64_t>((int64_t)(tiles - 2) * n, (int64_t)device_sm_count() * 4);
+            e = launch_dependent(k_embed_join<W>, dim3(grid), dim3(256), 0, stream, c, key, tile, tiles, n, (const float *)ws.partial, ws.ldp);
         }
     });
-    return cudaGetLastError();
+    return e;
 }
 
 }  // namespace turnopd
