@@ -6,18 +6,18 @@
 // of two would spare int8 up to one of its seven bits, but round twice and depend on how the quotient is formed.
 
 #include <algorithm>
+#include <type_traits>
 
 #include "columns.cuh"
 #include "common.cuh"
 #include "kernels.h"
+#include "packed.cuh"
 
 namespace turnopd {
 namespace {
 
 constexpr int kWarps = 8;
-constexpr int kChunk = 256;  // columns of a row that a warp takes at once, eight groups
-constexpr int kUnits = 4;    // chunks of a row that it has in flight
-constexpr int kStrip = kChunk * kUnits;
+constexpr int kChunk = 256;  // columns of a row, eight groups, that a warp takes together
 
 // The exponent byte of a group from the bits of its largest magnitude; 255 where that is infinite or NaN.
 __device__ __forceinline__ uint32_t exponent_byte(uint32_t amax, bool e4m3)
@@ -44,79 +44,140 @@ __device__ __forceinline__ uint32_t encode2(float a, float b, bool e4m3)
 
 __device__ __forceinline__ uint32_t magnitude(float x) { return __float_as_uint(x) & 0x7fffffffu; }
 
-// A warp takes strips of four chunks of a row; a block's strips begin at one column (no division tells a row from its columns:
-// with one for each chunk 32,768 x 4,096 bf16 took 132 us).  VEC (rows of x on 16-byte boundaries, of codes on 8-byte ones):
-// eight columns to a lane, four lanes to a group.  Else a group at a time, a column to a lane.
-template <typename TX, bool VEC> __global__ void __launch_bounds__(32 * kWarps, 4) k_act8_store(Act8Call c)
+// Eight columns as they are stored.
+template <typename TX> struct Raw;
+template <> struct Raw<__nv_bfloat16> {
+    uint4 u;
+    __device__ void load(const __nv_bfloat16 *p) { u = __ldcs(reinterpret_cast<const uint4 *>(p)); }
+    __device__ void put(int k, __nv_bfloat16 x)
+    {
+        const uint32_t b = __bfloat16_as_ushort(x), w = k & 1 ? b << 16 : b;
+        (k < 4 ? (k < 2 ? u.x : u.y) : (k < 6 ? u.z : u.w)) |= w;
+    }
+    // the largest magnitude as the bits of a float; of sixteen bits as whole numbers NaN is the largest
+    __device__ uint32_t largest() const
+    {
+        const uint32_t m = 0x7fff7fffu;
+        const uint32_t a = __vmaxu2(__vmaxu2(u.x & m, u.y & m), __vmaxu2(u.z & m, u.w & m));
+        return max(a << 16, a & 0xffff0000u);
+    }
+    __device__ float2 pair(int k) const { return unpack2(word(u, k)); }
+};
+template <> struct Raw<float> {
+    float4 a, b;
+    __device__ void load(const float *p)
+    {
+        a = __ldcs(reinterpret_cast<const float4 *>(p));
+        b = __ldcs(reinterpret_cast<const float4 *>(p) + 1);
+    }
+    __device__ void put(int k, float x)
+    {
+        float4 &v = k < 4 ? a : b;
+        (k & 2 ? (k & 1 ? v.w : v.z) : (k & 1 ? v.y : v.x)) = x;
+    }
+    __device__ uint32_t largest() const
+    {
+        return max(max(max(magnitude(a.x), magnitude(a.y)), max(magnitude(a.z), magnitude(a.w))),
+                   max(max(magnitude(b.x), magnitude(b.y)), max(magnitude(b.z), magnitude(b.w))));
+    }
+    __device__ float2 pair(int k) const
+    {
+        const float4 &v = k < 2 ? a : b;
+        return k & 1 ? make_float2(v.z, v.w) : make_float2(v.x, v.y);
+    }
+};
+
+// Rows of x on 16-byte boundaries, of codes on 8-byte ones: a warp takes strips of U chunks of a row, eight columns to a lane,
+// four lanes to a group.  A block's strips begin at one column: no division tells a row from its columns (with one for each
+// chunk 32,768 x 4,096 bf16 took 132 us).
+template <typename TX, bool E4M3, int U> __global__ void __launch_bounds__(32 * kWarps) k_act8_store(Act8Call c)
+{
+    const int lane = threadIdx.x & 31;
+    const int64_t d = c.d, groups = (d + kActGroup - 1) / kActGroup;
+    for (int64_t strip = (int64_t)blockIdx.y * U * kChunk; strip < d; strip += (int64_t)gridDim.y * U * kChunk)
+        for (int64_t row = (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5); row < c.T; row += (int64_t)gridDim.x * kWarps) {
+            const bool on = !c.mask || c.mask[row];
+            const int64_t first = strip + lane * 8;
+            const TX *x = static_cast<const TX *>(c.x) + row * c.ldx + first;
+            uint8_t *codes = static_cast<uint8_t *>(c.codes) + row * c.ldc + first, *exps = c.exps + row * groups;
+            Raw<TX> v[U];
+#pragma unroll
+            for (int q = 0; q < U; ++q) {
+                const int64_t left = d - first - q * kChunk;
+                if (on && left >= 8) {
+                    v[q].load(x + q * kChunk);
+                } else {
+                    v[q] = Raw<TX>{};
+#pragma unroll
+                    for (int k = 0; k < 8; ++k)
+                        if (on && k < left)
+                            v[q].put(k, x[q * kChunk + k]);
+                }
+            }
+            uint32_t e[U];
+#pragma unroll
+            for (int q = 0; q < U; ++q) {
+                const int64_t left = d - first - q * kChunk;
+                uint32_t amax = v[q].largest();
+                amax = max(amax, __shfl_xor_sync(~0u, amax, 1));
+                amax = max(amax, __shfl_xor_sync(~0u, amax, 2));
+                e[q] = on ? exponent_byte(amax, E4M3) : 0u;
+                const float s = inverse_scale(e[q]);
+                uint2 w;
+                const float2 p0 = v[q].pair(0), p1 = v[q].pair(1), p2 = v[q].pair(2), p3 = v[q].pair(3);
+                w.x = encode2(p0.x * s, p0.y * s, E4M3) | encode2(p1.x * s, p1.y * s, E4M3) << 16;
+                w.y = encode2(p2.x * s, p2.y * s, E4M3) | encode2(p3.x * s, p3.y * s, E4M3) << 16;
+                if (e[q] == 255u) {
+                    w = make_uint2(0u, 0u);
+                    if (left > 0)
+                        set_status(c.status, TURNOPD_ERR_NONFINITE);
+                }
+                if (left >= 8) {
+                    __stcs(reinterpret_cast<uint2 *>(codes + q * kChunk), w);
+                } else {
+#pragma unroll
+                    for (int k = 0; k < 8; ++k)
+                        if (k < left)
+                            codes[q * kChunk + k] = (uint8_t)((k < 4 ? w.x : w.y) >> (8 * (k & 3)));
+                }
+            }
+            // the strip's 8 U exponents in one store: lane 4 g + q has that of group g of chunk q
+            const int q = lane & 3;
+            const int64_t at = (strip + q * kChunk) / kActGroup + (lane >> 2);
+            if (q < U && at < groups)
+                exps[at] = (uint8_t)(U == 1 || q == 0 ? e[0] : q == 1 ? e[U > 1 ? 1 : 0] : q == 2 ? e[U > 2 ? 2 : 0] : e[U > 3 ? 3 : 0]);
+        }
+}
+
+// Any rows: a column to a lane, a group at a time.
+template <typename TX> __global__ void __launch_bounds__(32 * kWarps) k_act8_store_any(Act8Call c)
 {
     const int lane = threadIdx.x & 31;
     const int64_t d = c.d, groups = (d + kActGroup - 1) / kActGroup;
     const bool e4m3 = c.code_dtype == TURNOPD_E4M3;
-    for (int64_t strip = (int64_t)blockIdx.y * kStrip; strip < d; strip += (int64_t)gridDim.y * kStrip)
+    for (int64_t strip = (int64_t)blockIdx.y * kChunk; strip < d; strip += (int64_t)gridDim.y * kChunk)
         for (int64_t row = (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5); row < c.T; row += (int64_t)gridDim.x * kWarps) {
             const bool on = !c.mask || c.mask[row];
-            float v[kUnits][8];
+            const TX *x = static_cast<const TX *>(c.x) + row * c.ldx;
+            uint8_t *codes = static_cast<uint8_t *>(c.codes) + row * c.ldc, *exps = c.exps + row * groups;
+            float v[8];
 #pragma unroll
-            for (int q = 0; q < kUnits; ++q) {
-                const TX *x = static_cast<const TX *>(c.x) + row * c.ldx;
-                const int64_t j = (strip + q * kChunk) + (VEC ? lane * 8 : lane);
-                if (VEC && on && j + 8 <= d) {
-                    load8(x + j, v[q]);
-                } else {
-#pragma unroll
-                    for (int k = 0; k < 8; ++k)
-                        v[q][k] = on && j + (VEC ? k : k * kActGroup) < d ? to_float(x[j + (VEC ? k : k * kActGroup)]) : 0.f;
-                }
+            for (int g = 0; g < 8; ++g) {
+                const int64_t j = strip + g * kActGroup + lane;
+                v[g] = on && j < d ? to_float(x[j]) : 0.f;
             }
 #pragma unroll
-            for (int q = 0; q < kUnits; ++q) {
-                uint8_t *codes = static_cast<uint8_t *>(c.codes) + row * c.ldc, *exps = c.exps + row * groups;
-                if constexpr (VEC) {
-                    const int64_t j = (strip + q * kChunk) + lane * 8;
-                    uint32_t amax = 0;
-#pragma unroll
-                    for (int k = 0; k < 8; ++k)
-                        amax = max(amax, magnitude(v[q][k]));
-                    amax = max(amax, __shfl_xor_sync(~0u, amax, 1));
-                    amax = max(amax, __shfl_xor_sync(~0u, amax, 2));
-                    const uint32_t e = on ? exponent_byte(amax, e4m3) : 0u;
-                    const float s = inverse_scale(e);
-                    if (e == 255u) {
-#pragma unroll
-                        for (int k = 0; k < 8; ++k)
-                            v[q][k] = 0.f;
-                    }
-                    uint2 w;
-                    w.x = encode2(v[q][0] * s, v[q][1] * s, e4m3) | encode2(v[q][2] * s, v[q][3] * s, e4m3) << 16;
-                    w.y = encode2(v[q][4] * s, v[q][5] * s, e4m3) | encode2(v[q][6] * s, v[q][7] * s, e4m3) << 16;
-                    if (j + 8 <= d) {
-                        __stcs(reinterpret_cast<uint2 *>(codes + j), w);
-                    } else {
-#pragma unroll
-                        for (int k = 0; k < 8; ++k)
-                            if (j + k < d)
-                                codes[j + k] = (uint8_t)((k < 4 ? w.x : w.y) >> (8 * (k & 3)));
-                    }
-                    if ((lane & 3) == 0 && j < d) {
-                        exps[j / kActGroup] = (uint8_t)e;
-                        if (e == 255u)
-                            set_status(c.status, TURNOPD_ERR_NONFINITE);
-                    }
-                } else {
-#pragma unroll
-                    for (int g = 0; g < 8; ++g) {
-                        const int64_t j = (strip + q * kChunk) + g * kActGroup + lane;
-                        const uint32_t amax = __reduce_max_sync(~0u, magnitude(v[q][g]));
-                        const uint32_t e = on ? exponent_byte(amax, e4m3) : 0u;
-                        const float t = e == 255u ? 0.f : v[q][g] * inverse_scale(e);
-                        if (j < d)
-                            codes[j] = (uint8_t)encode2(t, 0.f, e4m3);
-                        if (lane == 0 && j < d) {
-                            exps[j / kActGroup] = (uint8_t)e;
-                            if (e == 255u)
-                                set_status(c.status, TURNOPD_ERR_NONFINITE);
-                        }
-                    }
+            for (int g = 0; g < 8; ++g) {
+                const int64_t j = strip + g * kActGroup + lane;
+                const uint32_t amax = __reduce_max_sync(~0u, magnitude(v[g]));
+                const uint32_t e = on ? exponent_byte(amax, e4m3) : 0u;
+                const float t = e == 255u ? 0.f : v[g] * inverse_scale(e);
+                if (j < d)
+                    codes[j] = (uint8_t)encode2(t, 0.f, e4m3);
+                if (lane == 0 && j < d) {
+                    exps[j / kActGroup] = (uint8_t)e;
+                    if (e == 255u)
+                        set_status(c.status, TURNOPD_ERR_NONFINITE);
                 }
             }
         }
@@ -130,18 +191,18 @@ template <typename TX> __device__ __forceinline__ float worth(float code, float 
     return v > kMost ? kMost : v < -kMost ? -kMost : v;  // NaN stays
 }
 
-template <typename TX, bool VEC> __global__ void __launch_bounds__(32 * kWarps, 4) k_act8_load(Act8Call c)
+template <typename TX, bool VEC, int U> __global__ void __launch_bounds__(32 * kWarps, 4) k_act8_load(Act8Call c)
 {
     const int lane = threadIdx.x & 31;
     const int64_t d = c.d, groups = (d + kActGroup - 1) / kActGroup;
     const bool e4m3 = c.code_dtype == TURNOPD_E4M3;
-    for (int64_t strip = (int64_t)blockIdx.y * kStrip; strip < d; strip += (int64_t)gridDim.y * kStrip)
+    for (int64_t strip = (int64_t)blockIdx.y * U * kChunk; strip < d; strip += (int64_t)gridDim.y * U * kChunk)
         for (int64_t row = (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5); row < c.T; row += (int64_t)gridDim.x * kWarps) {
-            uint2 code[kUnits];
-            uint32_t exp[kUnits];
+            uint2 code[U];
+            uint32_t exp[U];
             if constexpr (VEC) {
 #pragma unroll
-                for (int q = 0; q < kUnits; ++q) {
+                for (int q = 0; q < U; ++q) {
                     const int64_t j = (strip + q * kChunk) + lane * 8;
                     if (j + 8 <= d) {
                         code[q] = __ldcs(reinterpret_cast<const uint2 *>(static_cast<const uint8_t *>(c.codes) + row * c.ldc + j));
@@ -150,7 +211,7 @@ template <typename TX, bool VEC> __global__ void __launch_bounds__(32 * kWarps, 
                 }
             }
 #pragma unroll
-            for (int q = 0; q < kUnits; ++q) {
+            for (int q = 0; q < U; ++q) {
                 TX *x = static_cast<TX *>(c.out) + row * c.ldx;
                 const uint8_t *codes = static_cast<const uint8_t *>(c.codes) + row * c.ldc, *exps = c.exps + row * groups;
                 const auto one = [&](int64_t j) {
@@ -190,19 +251,22 @@ bool on_boundaries(const Act8Call &c)
            c.ldc % 8 == 0;
 }
 
-template <bool STORE> cudaError_t launch(const Act8Call &c, cudaStream_t stream)
+// Strips of four chunks where there are enough for every warp to have several, else of one.
+template <typename F> void with_grid(const Act8Call &c, bool strips_of_four, F &&go)
 {
-    const int64_t strips = (c.d + kStrip - 1) / kStrip, blocks = (c.T + kWarps - 1) / kWarps;
-    const dim3 grid((unsigned)std::min<int64_t>(blocks, std::max<int64_t>((int64_t)device_sm_count() * 8 / strips, 1)),
-                    (unsigned)std::min<int64_t>(strips, 65535));
-    const bool vec = on_boundaries(c);
-    const auto go = [&](auto x) {
-        using X = decltype(x);
-        auto kernel = STORE ? (vec ? k_act8_store<X, true> : k_act8_store<X, false>)
-                            : (vec ? k_act8_load<X, true> : k_act8_load<X, false>);
-        kernel<<<grid, 32 * kWarps, 0, stream>>>(c);
-    };
-    if (c.x_dtype == TURNOPD_BF16)
+    const int64_t chunks = (c.d + kChunk - 1) / kChunk, blocks = (c.T + kWarps - 1) / kWarps, sms = device_sm_count();
+    const bool four = strips_of_four && blocks * ((chunks + 3) / 4) >= 8 * sms;
+    const int64_t strips = four ? (chunks + 3) / 4 : chunks;
+    const dim3 grid((unsigned)std::min<int64_t>(blocks, std::max<int64_t>(sms * 16 / strips, 1)), (unsigned)std::min<int64_t>(strips, 65535));
+    if (four)
+        go(grid, std::integral_constant<int, 4>());
+    else
+        go(grid, std::integral_constant<int, 1>());
+}
+
+template <typename F> cudaError_t with_type(int32_t dtype, F &&go)
+{
+    if (dtype == TURNOPD_BF16)
         go(__nv_bfloat16());
     else
         go(float());
@@ -211,7 +275,32 @@ template <bool STORE> cudaError_t launch(const Act8Call &c, cudaStream_t stream)
 
 }  // namespace
 
-cudaError_t launch_act8_store(const Act8Call &c, cudaStream_t stream) { return launch<true>(c, stream); }
-cudaError_t launch_act8_load(const Act8Call &c, cudaStream_t stream) { return launch<false>(c, stream); }
+cudaError_t launch_act8_store(const Act8Call &c, cudaStream_t stream)
+{
+    const bool vec = on_boundaries(c);
+    return with_type(c.x_dtype, [&](auto x) {
+        with_grid(c, vec, [&](dim3 grid, auto units) {
+            using X = decltype(x);
+            constexpr int U = decltype(units)::value;
+            auto kernel = !vec                             ? k_act8_store_any<X>
+                          : c.code_dtype == TURNOPD_E4M3 ? k_act8_store<X, true, U>
+                                                           : k_act8_store<X, false, U>;
+            kernel<<<grid, 32 * kWarps, 0, stream>>>(c);
+        });
+    });
+}
+
+cudaError_t launch_act8_load(const Act8Call &c, cudaStream_t stream)
+{
+    const bool vec = on_boundaries(c);
+    return with_type(c.x_dtype, [&](auto x) {
+        with_grid(c, vec, [&](dim3 grid, auto units) {
+            using X = decltype(x);
+            constexpr int U = decltype(units)::value;
+            auto kernel = vec ? k_act8_load<X, true, U> : k_act8_load<X, false, 1>;
+            kernel<<<grid, 32 * kWarps, 0, stream>>>(c);
+        });
+    });
+}
 
 }  // namespace turnopd

@@ -75,23 +75,23 @@ template <typename TW, typename TO, bool VEC> __global__ void __launch_bounds__(
 // ---------------------------------------------------------------- tokens sorted by id
 
 constexpr int kSortThreads = 1024, kSortWarps = 32;
-constexpr int kMaxCtas = 8;       // of the sort's cluster
+constexpr int kMaxCtas = 16;      // of the sort's cluster
+constexpr int64_t kZeroBytes = 128 << 20;  // written beside the sort at most
 constexpr int kRadixBits = 9;     // at most, of one pass
 constexpr int kSortBatch = 8;     // keys of a lane in flight
 
 struct SortBuffers {
-    uint32_t *key[2];
-    int32_t *at[2];
+    uint2 *list[2];  // (key, token)
 };
 
-// Zeros from CTA `cta` of `ctas` into all rows of dw.
-template <typename TW> __device__ __forceinline__ void zero_rows(const EmbedGradCall &c, int64_t cta, int64_t ctas)
+// Zeros from CTA `cta` of `ctas` into the first `rows` rows of dw.
+template <typename TW> __device__ __forceinline__ void zero_rows(const EmbedGradCall &c, int64_t rows, int64_t cta, int64_t ctas)
 {
     TW *w = static_cast<TW *>(c.dw);
     constexpr int W = 16 / (int)sizeof(TW);
     const int64_t thread = cta * blockDim.x + threadIdx.x, threads = ctas * blockDim.x;
     if (c.ldw == c.d && reinterpret_cast<uintptr_t>(w) % 16 == 0) {
-        const int64_t n = c.vocab * c.d;
+        const int64_t n = rows * c.d;
         for (int64_t j = thread; j < n / W; j += threads)
             __stcs(reinterpret_cast<uint4 *>(w) + j, make_uint4(0u, 0u, 0u, 0u));
         if (thread < n % W)
@@ -100,7 +100,7 @@ template <typename TW> __device__ __forceinline__ void zero_rows(const EmbedGrad
     }
     const int lane = threadIdx.x & 31;
     const bool vec = reinterpret_cast<uintptr_t>(w) % 16 == 0 && c.ldw % W == 0;
-    for (int64_t v = thread / 32; v < c.vocab; v += threads / 32) {
+    for (int64_t v = thread / 32; v < rows; v += threads / 32) {
         TW *row = w + v * c.ldw;
         const int64_t whole = vec ? c.d / W : 0;
         for (int64_t j = lane; j < whole; j += 32)
@@ -113,21 +113,25 @@ template <typename TW> __device__ __forceinline__ void zero_rows(const EmbedGrad
 // The first cluster sorts all tokens, least significant digits first: each CTA takes a part of the list and each of its warps a
 // part of that, in order.  A warp counts its digits, the counts are summed up over the warps, the CTAs and the digits, and the
 // warp puts its keys where they belong.  Tokens that are masked or whose id is out of range get the key `vocab` and come last.
-// The last pass leaves the list in buffer (passes & 1).  Meanwhile the other clusters write zeros into the whole table: the
-// rows of ids that occur are written over by the sums, which costs less than to find out first which do (151,936 x 4,096 bf16,
-// 32,768 tokens: 12 us more of writing; the sort's 20 us behind it).
-__global__ void __launch_bounds__(kSortThreads) k_sort_tokens(EmbedGradCall c, SortBuffers b, int passes, int bits, uint32_t ctas)
+// The last pass leaves the list in buffer (passes & 1).  Meanwhile the other clusters write zeros into the first rows_zeroed
+// rows of the table; those of them that occur are written over by the sums, which costs less than to wait for the list.
+// present: a bit for each id that occurs from row rows_zeroed on.
+__global__ void __launch_bounds__(kSortThreads) k_sort_tokens(EmbedGradCall c, SortBuffers b, int passes, int bits, uint32_t ctas,
+                                                              int64_t rows_zeroed, uint32_t *present)
 {
     extern __shared__ uint32_t counts[];  // [kSortWarps][bins]
     __shared__ uint32_t total[1 << kRadixBits], warp_total[kSortWarps];
     pdl_begin();
     if (blockIdx.x >= ctas) {
         if (c.dw_dtype == TURNOPD_BF16)
-            zero_rows<__nv_bfloat16>(c, blockIdx.x - ctas, gridDim.x - ctas);
+            zero_rows<__nv_bfloat16>(c, rows_zeroed, blockIdx.x - ctas, gridDim.x - ctas);
         else
-            zero_rows<float>(c, blockIdx.x - ctas, gridDim.x - ctas);
+            zero_rows<float>(c, rows_zeroed, blockIdx.x - ctas, gridDim.x - ctas);
         return;
     }
+    if (rows_zeroed < c.vocab)
+        for (int64_t w = (int64_t)cluster_ctarank() * kSortThreads + threadIdx.x; w < (c.vocab + 31) / 32; w += (int64_t)ctas * kSortThreads)
+            present[w] = 0;
     const int64_t T = c.T, vocab = c.vocab;
     const int bins = 1 << bits, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const uint32_t rank = cluster_ctarank();
@@ -135,12 +139,12 @@ __global__ void __launch_bounds__(kSortThreads) k_sort_tokens(EmbedGradCall c, S
     const int64_t lo = min(T, ((int64_t)rank * kSortWarps + warp) * seg), hi = min(T, lo + seg);
     uint32_t *mine = counts + warp * bins;
     for (int p = 0; p < passes; ++p) {
-        const uint32_t *from = b.key[p & 1];
+        const uint2 *from = b.list[p & 1];
         const auto key_of = [&](int64_t i) -> uint32_t {
             if (i >= hi)
                 return 0u;
             if (p)
-                return __ldcg(from + i);
+                return __ldcg(&from[i].x);
             if (c.mask && !c.mask[i])
                 return (uint32_t)vocab;
             const int id = c.ids[i];
@@ -209,20 +213,18 @@ __global__ void __launch_bounds__(kSortThreads) k_sort_tokens(EmbedGradCall c, S
         }
         __syncthreads();
         for (int64_t first = lo; first < hi; first += 32 * kSortBatch) {
-            uint32_t key[kSortBatch];
-            int32_t at[kSortBatch];
+            uint2 key[kSortBatch];
 #pragma unroll
             for (int k = 0; k < kSortBatch; ++k) {
                 const int64_t i = first + 32 * k + lane;
-                key[k] = key_of(i);
-                at[k] = p && i < hi ? __ldcg(b.at[p & 1] + i) : (int32_t)i;
+                key[k] = p && i < hi ? __ldcg(from + i) : make_uint2(p ? 0u : key_of(i), (uint32_t)i);
             }
 #pragma unroll
             for (int k = 0; k < kSortBatch; ++k) {
                 const bool there = first + 32 * k + lane < hi;
                 if (first + 32 * k >= hi)
                     break;
-                const uint32_t digit = there ? (key[k] >> shift) & (bins - 1) : ~0u;
+                const uint32_t digit = there ? (key[k].x >> shift) & (bins - 1) : ~0u;
                 const uint32_t peers = __match_any_sync(~0u, digit);
                 uint32_t to = 0;
                 if (there)
@@ -231,14 +233,19 @@ __global__ void __launch_bounds__(kSortThreads) k_sort_tokens(EmbedGradCall c, S
                 if (there) {
                     if (lane == __ffs(peers) - 1)
                         mine[digit] += __popc(peers);
-                    __stcg(b.key[~p & 1] + to, key[k]);
-                    __stcg(b.at[~p & 1] + to, at[k]);
+                    __stcg(b.list[~p & 1] + to, key[k]);
                 }
                 __syncwarp();
             }
         }
         cluster_sync();
     }
+    if (rows_zeroed < vocab)
+        for (int64_t i = (int64_t)rank * kSortThreads + threadIdx.x; i < T; i += (int64_t)ctas * kSortThreads) {
+            const uint32_t key = __ldcg(&b.list[passes & 1][i].x);
+            if (key < vocab && (i == 0 || __ldcg(&b.list[passes & 1][i - 1].x) != key))
+                atomicOr(present + key / 32, 1u << (key & 31));
+        }
 }
 
 // ---------------------------------------------------------------- sums
@@ -292,16 +299,19 @@ __device__ __forceinline__ void put_row(const EmbedGradCall &c, const Columns<VE
     cols.store(w, sum);
 }
 
-constexpr int kRows = 8;  // in flight
+constexpr int kRows = 8;       // in flight
+constexpr int kZeroRows = 64;  // of a CTA that writes zeros
 
 // A tile of the sorted list and a slice of the columns.  A tile owns the runs that begin in it, and goes on with its last run
 // through the next tile.  A run that ends by then goes to dW; a longer one leaves the sum of its owner's two tiles in partial
 // row 2 t + 1, and of each later tile that it reaches in that tile's row 2 t.  The rows come through a ring in shared memory,
 // in which each thread copies and reads its own columns (bf16 rows that begin at odd elements: a row ahead, in registers).
+// Every so many CTAs one writes zeros instead, into the rows from rows_zeroed on that do not occur, 64 of them: the sums wait
+// for their rows while the zeros go out.
 template <typename TG, typename TW, bool VEC>
-__global__ void __launch_bounds__(kSumThreads) k_embed_sums(EmbedGradCall c, const uint32_t *__restrict__ keys,
-                                                            const int32_t *__restrict__ ats, int tile, int slices, float *partial,
-                                                            int64_t ldp)
+__global__ void __launch_bounds__(kSumThreads) k_embed_sums(EmbedGradCall c, const uint2 *__restrict__ list, int tile, int slices, float *partial,
+                                                            int64_t ldp, int64_t rows_zeroed, const uint32_t *__restrict__ present,
+                                                            int zero_ctas)
 {
     constexpr bool kRing = VEC || sizeof(TG) == 4;
     extern __shared__ __align__(16) char ring[];
@@ -310,17 +320,33 @@ __global__ void __launch_bounds__(kSumThreads) k_embed_sums(EmbedGradCall c, con
     pdl_begin();
     const int64_t T = c.T, d = c.d;
     const uint32_t none = (uint32_t)c.vocab;
-    const int t = blockIdx.x / slices, slice = blockIdx.x % slices;
+    const int zeros = (int)((int64_t)blockIdx.x * zero_ctas / gridDim.x);  // CTAs before this one that write them
+    if ((int64_t)(blockIdx.x + 1) * zero_ctas / gridDim.x > zeros) {
+        const int lane = threadIdx.x & 31;
+        const int64_t v0 = rows_zeroed + (int64_t)zeros * kZeroRows;
+        for (int64_t v = v0 + (threadIdx.x >> 5); v < min(v0 + kZeroRows, c.vocab); v += blockDim.x >> 5) {
+            if (present[v / 32] >> (v & 31) & 1)
+                continue;
+            const float zero[8] = {};
+            for (int64_t j = VEC ? lane * 8 : lane; j < d; j += 256) {
+                const Columns<VEC> cols{j, d, 32};
+                cols.store(static_cast<TW *>(c.dw) + v * c.ldw, zero);
+            }
+        }
+        return;
+    }
+    const int t = (blockIdx.x - zeros) / slices, slice = (blockIdx.x - zeros) % slices;
     const int64_t base = (int64_t)slice * 8 * blockDim.x, lo = (int64_t)t * tile;
     const Columns<VEC> cols{base + (VEC ? threadIdx.x * 8 : threadIdx.x), d, (int)blockDim.x};
     const int size = (int)min(T - lo, (int64_t)tile), most = (int)min(T - lo, (int64_t)2 * tile);  // positions of the tile, and of both
     for (int q = threadIdx.x; q < most + 2; q += blockDim.x) {
         const int64_t p = lo - 1 + q;
-        key[q] = p >= 0 && p < T ? keys[p] : none;
-        if (q < most)
-            at[q] = ats[lo + q];
+        const uint2 entry = p >= 0 && p < T ? list[p] : make_uint2(none, 0u);
+        key[q] = entry.x;
+        if (q > 0 && q <= most)
+            at[q - 1] = (int)entry.y;
     }
-    const bool long_ago = t > 1 && keys[lo - tile - 1] == keys[lo];
+    const bool long_ago = t > 1 && list[lo - tile - 1].x == list[lo].x;
     __syncthreads();
     uint32_t run = key[1];
     if (run == none)
@@ -416,9 +442,10 @@ __global__ void __launch_bounds__(kSumThreads) k_embed_sums(EmbedGradCall c, con
 }
 
 // Runs over more than two tiles: the partial sums of the tile they began in and of those they go on in.  32 threads take 256
-// columns, the block's eight warps share the tiles of a run, and their sums are added up in order.
+// columns, the block's eight warps share the tiles of a run, and their sums are added up in order.  A row of blocks looks at
+// 1,024 tiles.
 template <typename TW>
-__global__ void __launch_bounds__(256) k_embed_join(EmbedGradCall c, const uint32_t *__restrict__ key, int tile, int tiles,
+__global__ void __launch_bounds__(256) k_embed_join(EmbedGradCall c, const uint2 *__restrict__ list, int tile, int tiles,
                                                     int slices, const float *__restrict__ partial, int64_t ldp)
 {
     __shared__ int owner[kListed], first_of[kListed / 32 + 1];
@@ -427,16 +454,16 @@ __global__ void __launch_bounds__(256) k_embed_join(EmbedGradCall c, const uint3
     const int64_t d = c.d;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     static_assert(kListed == 32 * 32, "one warp adds up the counts");
-    for (int t0 = 0; t0 + 2 < tiles; t0 += kListed) {
+    for (int64_t t0 = (int64_t)blockIdx.y * kListed; t0 + 2 < tiles; t0 += (int64_t)gridDim.y * kListed) {
         // tile t owns a run that begins in it and goes on in tile t + 2; every block lists the owners in the same order
         __syncthreads();
 #pragma unroll
         for (int w = warp; w < kListed / 32; w += 8) {
-            const int t = t0 + w * 32 + lane;
+            const int t = (int)t0 + w * 32 + lane;
             bool owns = false;
             if (t + 2 < tiles) {
-                const uint32_t k = key[(int64_t)(t + 1) * tile - 1], later = key[(int64_t)(t + 2) * tile];
-                const uint32_t earlier = t ? key[(int64_t)t * tile - 1] : ~0u;
+                const uint32_t k = list[(int64_t)(t + 1) * tile - 1].x, later = list[(int64_t)(t + 2) * tile].x;
+                const uint32_t earlier = t ? list[(int64_t)t * tile - 1].x : ~0u;
                 owns = k < (uint32_t)c.vocab && later == k && earlier != k;
             }
             const uint32_t owners = __ballot_sync(~0u, owns);
@@ -453,7 +480,7 @@ __global__ void __launch_bounds__(256) k_embed_join(EmbedGradCall c, const uint3
             }
             int place = scan - __popc(owners);
             for (uint32_t left = owners; left; left &= left - 1)
-                owner[place++] = t0 + lane * 32 + __ffs(left) - 1;
+                owner[place++] = (int)t0 + lane * 32 + __ffs(left) - 1;
             __syncwarp();
             first_of[lane + 1] = scan;
         }
@@ -461,7 +488,7 @@ __global__ void __launch_bounds__(256) k_embed_join(EmbedGradCall c, const uint3
         const int n = first_of[kListed / 32] * slices;
         for (int item = blockIdx.x; item < n; item += gridDim.x) {
             const int t = owner[item / slices], slice = item % slices;
-            const uint32_t k = key[(int64_t)(t + 1) * tile - 1];
+            const uint32_t k = list[(int64_t)(t + 1) * tile - 1].x;
             const Columns<true> cols{(int64_t)slice * 256 + lane * 8, ldp, 1};  // of the partial sums, whose rows are padded
             float sum[8] = {};
             for (int s0 = t + 2 + warp; s0 < tiles; s0 += 32) {
@@ -469,7 +496,7 @@ __global__ void __launch_bounds__(256) k_embed_join(EmbedGradCall c, const uint3
                 float v[4][8];
 #pragma unroll
                 for (int q = 0; q < 4; ++q)
-                    in[q] = s0 + 8 * q < tiles && key[(int64_t)(s0 + 8 * q) * tile] == k;
+                    in[q] = s0 + 8 * q < tiles && list[(int64_t)(s0 + 8 * q) * tile].x == k;
 #pragma unroll
                 for (int q = 0; q < 4; ++q)
                     if (in[q] && cols.first < ldp)
@@ -502,11 +529,16 @@ __global__ void __launch_bounds__(256) k_embed_join(EmbedGradCall c, const uint3
     }
 }
 
-// 1,024 tiles, of 8 to 512 positions
-int tile_size(int64_t T)
+int sum_threads(int64_t d) { return (int)std::min<int64_t>(kSumThreads, (d + 255) / 256 * 32); }
+int sum_slices(int64_t d) { return (int)((d + 8 * sum_threads(d) - 1) / (8 * sum_threads(d))); }
+
+// Positions of a tile: as many as leave 8,192 warps, which keep the device's memory busy; each run that passes two tiles'
+// ends costs partial sums (32,768 x 4,096: 64 positions).
+int tile_size(int64_t T, int64_t d)
 {
+    const int64_t warps = (int64_t)sum_slices(d) * (sum_threads(d) / 32);
     int n = 8;
-    while (n < kMaxTile && (T + n - 1) / n > kListed)
+    while (n < kMaxTile && (T + 2 * n - 1) / (2 * n) * warps >= 8192)
         n *= 2;
     return n;
 }
@@ -518,10 +550,11 @@ bool boundary(const void *p, int64_t ld, int32_t dtype)
 
 struct Workspace {
     SortBuffers sort;
+    uint32_t *present;
     float *partial;
     int64_t ldp;
     size_t bytes;
-    Workspace(void *ws, int64_t T, int64_t d) : ldp((d + 7) / 8 * 8)
+    Workspace(void *ws, int64_t T, int64_t d, int64_t vocab) : ldp((d + 7) / 8 * 8)
     {
         char *p = static_cast<char *>(ws);
         const auto take = [&](size_t n) {
@@ -530,18 +563,17 @@ struct Workspace {
             return at;
         };
         bytes = 0;
-        for (int k = 0; k < 2; ++k) {
-            sort.key[k] = reinterpret_cast<uint32_t *>(take(sizeof(uint32_t) * (size_t)T));
-            sort.at[k] = reinterpret_cast<int32_t *>(take(sizeof(int32_t) * (size_t)T));
-        }
-        const int tile = tile_size(T);
+        for (uint2 *&list : sort.list)
+            list = reinterpret_cast<uint2 *>(take(sizeof(uint2) * (size_t)T));
+        present = reinterpret_cast<uint32_t *>(take(sizeof(uint32_t) * (size_t)((vocab + 31) / 32)));
+        const int tile = tile_size(T, d);
         partial = reinterpret_cast<float *>(take(sizeof(float) * 2 * (size_t)ldp * (size_t)((T + tile - 1) / tile)));
     }
 };
 
 }  // namespace
 
-size_t embed_bwd_workspace_bytes(int64_t T, int64_t d) { return std::max<size_t>(Workspace(nullptr, T, d).bytes, 256); }
+size_t embed_bwd_workspace_bytes(int64_t T, int64_t d, int64_t vocab) { return Workspace(nullptr, T, d, vocab).bytes; }
 
 cudaError_t launch_embed(const EmbedCall &c, cudaStream_t stream)
 {
@@ -560,18 +592,24 @@ cudaError_t launch_embed(const EmbedCall &c, cudaStream_t stream)
 
 cudaError_t launch_embed_bwd(const EmbedGradCall &c, cudaStream_t stream)
 {
-    const Workspace ws(c.workspace, c.T, c.d);
+    const Workspace ws(c.workspace, c.T, c.d, c.vocab);
     int key_bits = 1;
     while ((int64_t)1 << key_bits <= c.vocab)
         ++key_bits;
     const int passes = (key_bits + kRadixBits - 1) / kRadixBits, bits = (key_bits + passes - 1) / passes;
     cudaError_t e = allow_shared(k_sort_tokens, sizeof(uint32_t) * kSortWarps << kRadixBits);
+    if (e == cudaSuccess)
+        e = cudaFuncSetAttribute(k_sort_tokens, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
     if (e != cudaSuccess)
         return e;
-    // 32 KB of zeros to a CTA at least, and as many CTAs as the device holds
-    const int64_t zeros = c.accumulate ? 0 : c.vocab * c.d * (c.dw_dtype == TURNOPD_BF16 ? 2 : 4);
-    const unsigned ctas = c.T > kSortThreads ? kMaxCtas : 1;
-    const unsigned fill = (unsigned)std::min<int64_t>((zeros + 32767) / 32768, (int64_t)device_sm_count() * 2 - kMaxCtas);
+    // As many zeros beside the sort as go out in its time (a small table whole), 32 KB to a CTA at least.
+    const int64_t row_bytes = c.d * (c.dw_dtype == TURNOPD_BF16 ? 2 : 4);
+    const unsigned ctas = c.T > 8 * kSortThreads ? kMaxCtas : c.T > kSortThreads ? 8 : 1;
+    int64_t rows_zeroed = c.accumulate ? 0 : c.vocab;
+    if (c.T > 0 && rows_zeroed * row_bytes > kZeroBytes)
+        rows_zeroed = kZeroBytes / row_bytes / kZeroRows * kZeroRows;
+    const int zero_ctas = c.accumulate ? 0 : (int)((c.vocab - rows_zeroed + kZeroRows - 1) / kZeroRows);
+    const unsigned fill = (unsigned)std::min<int64_t>((rows_zeroed * row_bytes + 32767) / 32768, (int64_t)device_sm_count() * 2 - kMaxCtas);
     cudaLaunchConfig_t cfg = {};
     cudaLaunchAttribute attr[2];
     cfg.gridDim = (ctas + fill + ctas - 1) / ctas * ctas;
@@ -585,13 +623,12 @@ cudaError_t launch_embed_bwd(const EmbedGradCall &c, cudaStream_t stream)
     attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 2;
-    e = cudaLaunchKernelEx(&cfg, k_sort_tokens, c, ws.sort, passes, bits, (uint32_t)ctas);
+    e = cudaLaunchKernelEx(&cfg, k_sort_tokens, c, ws.sort, passes, bits, (uint32_t)ctas, c.accumulate ? c.vocab : rows_zeroed, ws.present);
     if (e != cudaSuccess || c.T == 0)
         return e;
-    const uint32_t *key = ws.sort.key[passes & 1];
-    const int32_t *at = ws.sort.at[passes & 1];
-    const int tile = tile_size(c.T), tiles = (int)((c.T + tile - 1) / tile);
-    const int threads = (int)std::min<int64_t>(kSumThreads, (c.d + 255) / 256 * 32), slices = (int)((c.d + 8 * threads - 1) / (8 * threads));
+    const uint2 *list = ws.sort.list[passes & 1];
+    const int tile = tile_size(c.T, c.d), tiles = (int)((c.T + tile - 1) / tile);
+    const int threads = sum_threads(c.d), slices = sum_slices(c.d);
     const bool vec = boundary(c.dout, c.ldg, c.dout_dtype) && boundary(c.dw, c.ldw, c.dw_dtype);
     with_types(c.dout_dtype, c.dw_dtype, [&](auto g, auto w) {
         using G = decltype(g);
@@ -601,12 +638,14 @@ cudaError_t launch_embed_bwd(const EmbedGradCall &c, cudaStream_t stream)
         e = allow_shared(sums, sizeof(G) * 8 * kRows * kSumThreads);
         if (e != cudaSuccess)
             return;
-        e = launch_dependent(sums, dim3((unsigned)((int64_t)tiles * slices)), dim3(threads), smem, stream, c, key, at, tile,
-                             slices, ws.partial, ws.ldp);
+        e = launch_dependent(sums, dim3((unsigned)((int64_t)tiles * slices + zero_ctas)), dim3(threads), smem, stream, c,
+                             list, tile, slices, ws.partial, ws.ldp, rows_zeroed, (const uint32_t *)ws.present, zero_ctas);
         if (e == cudaSuccess && tiles > 2) {
             const int n = (int)((c.d + 255) / 256);
-            const unsigned grid = (unsigned)std::min<int64_t>((int64_t)(tiles - 2) * n, (int64_t)device_sm_count() * 4);
-            e = launch_dependent(k_embed_join<W>, dim3(grid), dim3(256), 0, stream, c, key, tile, tiles, n, (const float *)ws.partial, ws.ldp);
+            const int64_t lists = std::min<int64_t>((tiles - 2 + kListed - 1) / kListed, 65535);
+            const int64_t items = (int64_t)std::min(tiles - 2, kListed) * n, most = std::max<int64_t>(device_sm_count() * 4 / lists, 1);
+            const dim3 grid((unsigned)std::min(items, most), (unsigned)lists);
+            e = launch_dependent(k_embed_join<W>, grid, dim3(256), 0, stream, c, list, tile, tiles, n, (const float *)ws.partial, ws.ldp);
         }
     });
     return e;

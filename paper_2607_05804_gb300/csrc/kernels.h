@@ -360,7 +360,7 @@ struct EmbedGradCall {
     int32_t *status;
 };
 
-size_t embed_bwd_workspace_bytes(int64_t T, int64_t d);
+size_t embed_bwd_workspace_bytes(int64_t T, int64_t d, int64_t vocab);
 cudaError_t launch_embed(const EmbedCall &c, cudaStream_t stream);
 cudaError_t launch_embed_bwd(const EmbedGradCall &c, cudaStream_t stream);
 

@@ -607,7 +607,7 @@ size_t turnopd_embedding_bwd_workspace_bytes(int64_t num_tokens, int64_t d, int6
 {
     if (bad_count(num_tokens, d) || vocab < 1 || vocab > INT32_MAX)
         return 0;
-    return embed_bwd_workspace_bytes(num_tokens, d);
+    return embed_bwd_workspace_bytes(num_tokens, d, vocab);
 }
 
 turnopd_status turnopd_embedding_bwd(const void *dout, int32_t dout_dtype, int64_t ldg, const int32_t *token_ids,
@@ -623,7 +623,7 @@ turnopd_status turnopd_embedding_bwd(const void *dout, int32_t dout_dtype, int64
     if (bad_count(num_tokens, d) || vocab < 1 || vocab > INT32_MAX || bad_rows(dout, dtype_size(dout_dtype), ldg, d) ||
         bad_rows(dw, dtype_size(dw_dtype), ldw, d) || misaligned(token_ids, 4) || !finite_f32(scale))
         return TURNOPD_ERR_SHAPE;
-    if (!workspace || misaligned(workspace, 256) || workspace_bytes < embed_bwd_workspace_bytes(num_tokens, d))
+    if (!workspace || misaligned(workspace, 256) || workspace_bytes < embed_bwd_workspace_bytes(num_tokens, d, vocab))
         return TURNOPD_ERR_WORKSPACE;
     const bool accumulate = (flags & TURNOPD_ACCUMULATE_GRAD) != 0;
     if (num_tokens == 0 && accumulate)
