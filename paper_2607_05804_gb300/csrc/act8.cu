@@ -166,19 +166,26 @@ template <typename TX> __global__ void __launch_bounds__(32 * kWarps) k_act8_sto
                 const int64_t j = strip + g * kActGroup + lane;
                 v[g] = on && j < d ? to_float(x[j]) : 0.f;
             }
+            // lane g has group g's largest magnitude, makes its exponent and writes it
+            uint32_t mine = 0;
+#pragma unroll
+            for (int g = 0; g < 8; ++g) {
+                const uint32_t amax = __reduce_max_sync(~0u, magnitude(v[g]));
+                mine = lane == g ? amax : mine;
+            }
+            const uint32_t e = on ? exponent_byte(mine, e4m3) : 0u;
+            const float s = inverse_scale(e);
+            if (lane < 8 && strip + lane * kActGroup < d) {
+                exps[strip / kActGroup + lane] = (uint8_t)e;
+                if (e == 255u)
+                    set_status(c.status, TURNOPD_ERR_NONFINITE);
+            }
 #pragma unroll
             for (int g = 0; g < 8; ++g) {
                 const int64_t j = strip + g * kActGroup + lane;
-                const uint32_t amax = __reduce_max_sync(~0u, magnitude(v[g]));
-                const uint32_t e = on ? exponent_byte(amax, e4m3) : 0u;
-                const float t = e == 255u ? 0.f : v[g] * inverse_scale(e);
+                const float scale = __shfl_sync(~0u, s, g);
                 if (j < d)
-                    codes[j] = (uint8_t)encode2(t, 0.f, e4m3);
-                if (lane == 0 && j < d) {
-                    exps[j / kActGroup] = (uint8_t)e;
-                    if (e == 255u)
-                        set_status(c.status, TURNOPD_ERR_NONFINITE);
-                }
+                    codes[j] = (uint8_t)encode2(scale == 0.f ? 0.f : v[g] * scale, 0.f, e4m3);
             }
         }
 }

@@ -31,6 +31,7 @@ struct RingPart {
     int at;          // bytes into a stage
     int dtype;
     int bytes;       // of one column
+    bool direct;     // does not come through the ring: read from global memory when it is needed
 };
 
 struct Ring {
@@ -56,8 +57,8 @@ __device__ __forceinline__ void from_ring(const char *at, int dtype, float2 *v)
 
 constexpr int extra_bytes(int pieces) { return 16 + 2 * 8 * pieces; }  // of a warp: statistics, exponents of r' and of y
 
-// Most threads of a block with one or two pieces of eight columns to a thread: 96 registers each, or 128.
-constexpr int most_threads(int pieces) { return pieces == 1 ? 640 : 512; }
+// Most threads of a block: 512 with 128 registers each, or 640 with 96, which one piece of eight columns to a thread will do with.
+constexpr int kFew = 512, kMany = 640;
 
 // What r' and y are stored in: the gradients' types, codes of one kind, or any.
 enum Stored { kGradientTypes, kE4m3, kInt8, kAny };
@@ -101,15 +102,15 @@ __device__ __forceinline__ float column_value(uint32_t raw, int dtype, uint32_t 
 // pieces of eight from the first boundary on, and the first threads one of the elements before and after them each.
 // GENERAL: layer norms, or sums for betas; without it the means of g and those sums are left out.
 // COMMON: dh and dr' come in, dr and dy go out, no gate for every element.
-template <typename TR, typename TY, int kPieces, Stored STORED, bool ENDS, bool GENERAL, bool COMMON>
-__global__ void __launch_bounds__(most_threads(kPieces), 1) k_block_bwd(BlockGradCall c, Ring ring, int n, int phase, int phase_step)
+template <typename TR, typename TY, int kPieces, int MOST, Stored STORED, bool ENDS, bool GENERAL, bool COMMON>
+__global__ void __launch_bounds__(MOST, 1) k_block_bwd(BlockGradCall c, Ring ring, int n, int phase, int phase_step)
 {
     // sums over a row: of g xh (and of g) of the norm after the block, and of the norm before the next one
     constexpr int kRowSums = GENERAL ? 4 : 2, kE = 8 * kPieces, kExtra = extra_bytes(kPieces);
     constexpr bool kMixed = STORED == kAny, kCodes = STORED == kE4m3 || STORED == kInt8;
     constexpr int kTypeR = type_code<STORED, TR>(), kTypeY = type_code<STORED, TY>();
     extern __shared__ __align__(128) char shared[];
-    __shared__ Numbers<kRowSums> red[2][most_threads(kPieces) / 32];
+    __shared__ Numbers<kRowSums> red[2][MOST / 32];
     const int t = threadIdx.x % n, group = threadIdx.x / n, warps = n / 32, per = blockDim.x / n, d = (int)c.d;
     const uint32_t T = (uint32_t)c.T, groups = gridDim.x * per, b = blockIdx.x * per + group;  // rows: 2^31 at most, and a few steps more
     const bool layer = GENERAL && c.kind == TURNOPD_LAYER_NORM, pre = COMMON || c.gamma_pre, post = c.gamma_post;
@@ -172,7 +173,7 @@ __global__ void __launch_bounds__(most_threads(kPieces), 1) k_block_bwd(BlockGra
         if (ahead < T && ahead_on) {
             char *to = own + ahead_stage * ring.stage;
             const auto part = [&](const RingPart &p, int bytes) {
-                if (!p.p)
+                if (!p.p || (!COMMON && p.direct))
                     return;
                 const char *from = p.p + (uint64_t)ahead * p.pitch;
                 if (bytes == 1 && ring.blocks) {
@@ -284,9 +285,13 @@ __global__ void __launch_bounds__(most_threads(kPieces), 1) k_block_bwd(BlockGra
 
     // Eight columns of an activation of the row in a stage, less mu, but for a factor that is returned: the codes' scale, where
     // it is the same for all eight and nothing is taken off.
-    const auto activation = [&](const char *at, const RingPart &part, int stored, uint32_t exp, uint32_t exp2, float mu, int k, float2 *v) {
+    const auto activation = [&](const char *at, uint32_t i, const RingPart &part, int stored, uint32_t exp, uint32_t exp2, float mu, int k,
+                                float2 *v) {
         const int dtype = kMixed ? part.dtype : stored, bytes = kMixed ? part.bytes : type_bytes(stored);
-        from_ring(at + part.at + piece0 * 8 * bytes + k * 256 * bytes, dtype, v);
+        if (!COMMON && part.direct)
+            from_ring(part.p + (uint64_t)i * part.pitch + column(k) * bytes, dtype, v);
+        else
+            from_ring(at + part.at + piece0 * 8 * bytes + k * 256 * bytes, dtype, v);
         if ((kMixed || kCodes) && dtype >= TURNOPD_E4M3) {
             const float lo = act_scale(exp);
             if (!ENDS && !GENERAL)
@@ -303,14 +308,18 @@ __global__ void __launch_bounds__(most_threads(kPieces), 1) k_block_bwd(BlockGra
         }
         return 1.f;
     };
-    const auto gradient = [&](auto type, const char *at, const RingPart &part, int k, float2 *v) {
+    const auto gradient = [&](auto type, const char *at, uint32_t i, const RingPart &part, int k, float2 *v) {
+        if (!COMMON && part.direct) {
+            load8(reinterpret_cast<const decltype(type) *>(part.p + (uint64_t)i * part.pitch) + column(k), reinterpret_cast<float *>(v));
+            return;
+        }
         load8(reinterpret_cast<const decltype(type) *>(at + part.at) + piece0 * 8 + k * 256, reinterpret_cast<float *>(v));
     };
     const auto centred_r = [&](const char *at, const Row &m, int k, float2 *v) {
-        return activation(at, ring.resid, kTypeR, m.er[k], m.er2[ENDS ? k : 0], m.stats.z, k, v);
+        return activation(at, 0u, ring.resid, kTypeR, m.er[k], m.er2[ENDS ? k : 0], m.stats.z, k, v);
     };
-    const auto centred_y = [&](const char *at, const Row &m, int k, float2 *v) {  // mu is 0 without that norm
-        return activation(at, ring.y, kTypeY, m.ey[k], m.ey2[ENDS ? k : 0], m.stats.x, k, v);
+    const auto centred_y = [&](const char *at, uint32_t i, const Row &m, int k, float2 *v) {  // mu is 0 without that norm
+        return activation(at, i, ring.y, kTypeY, m.ey[k], m.ey2[ENDS ? k : 0], m.stats.x, k, v);
     };
     const auto times_gamma = [&](int k, float2 *g) {
         const float4 a = gamma[2 * k * n], z = gamma[(2 * k + 1) * n];
@@ -327,7 +336,7 @@ __global__ void __launch_bounds__(most_threads(kPieces), 1) k_block_bwd(BlockGra
         for (int k = 0; k < kPieces; ++k) {
             float2 x[4], g[4], x2 = make_float2(0.f, 0.f), g2 = x2;
             const float f = centred_r(at, m, k, x);
-            gradient(TY(), at, ring.dh, k, g);
+            gradient(TY(), at, 0u, ring.dh, k, g);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 sums[0][4 * k + e] = ffma2(fmul2(g[e], splat(r1 * f)), x[e], sums[0][4 * k + e]);
@@ -405,13 +414,13 @@ __global__ void __launch_bounds__(most_threads(kPieces), 1) k_block_bwd(BlockGra
             for (int k = 0; k < kPieces; ++k) {
                 float2 D[4], x[4];
                 if (has_dro)
-                    gradient(TR(), at, ring.dro, k, D);
+                    gradient(TR(), at, 0u, ring.dro, k, D);
                 else
                     D[0] = D[1] = D[2] = D[3] = make_float2(0.f, 0.f);
                 if (pre) {
                     float2 g[4];
                     const float f = c1 * centred_r(at, m, k, x);
-                    gradient(TY(), at, ring.dh, k, g);
+                    gradient(TY(), at, 0u, ring.dh, k, g);
                     times_gamma(k, g);
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
@@ -432,7 +441,7 @@ __global__ void __launch_bounds__(most_threads(kPieces), 1) k_block_bwd(BlockGra
                     }
                 }
                 if (needs_y) {
-                    const float f = scale * centred_y(at, m, k, x);
+                    const float f = scale * centred_y(at, i, m, k, x);
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
                         x[e] = fmul2(x[e], splat(f));
@@ -440,17 +449,20 @@ __global__ void __launch_bounds__(most_threads(kPieces), 1) k_block_bwd(BlockGra
                 if (token_gate) {
                     float2 g[4];
                     if (dgate) {
+                        // s D (gamma xh + beta): the factor after that norm is s gamma here
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) {
-                            float w = reinterpret_cast<const float *>(x)[e];
-                            if (post && there(k))
-                                w = fmaf(w, param(c.gamma_post, c.param_dtype, column(k) + e),
-                                         c.beta_post ? param(c.beta_post, c.param_dtype, column(k) + e) : 0.f);
-                            reinterpret_cast<float *>(g)[e] = s * reinterpret_cast<const float *>(D)[e] * w;
-                        }
+                        for (int e = 0; e < 4; ++e)
+                            g[e] = fmul2(x[e], cpost[4 * k + e]);
+                        if (GENERAL && c.beta_post)
+#pragma unroll
+                            for (int e = 0; e < 8; ++e)
+                                reinterpret_cast<float *>(g)[e] += s * param(c.beta_post, c.param_dtype, column(k) + e);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            g[e] = fmul2(g[e], D[e]);
                         put8(TY(), c.dgate, ring.dgate, k, g);
                     }
-                    gradient(TY(), at, ring.gate, k, g);
+                    gradient(TY(), at, i, ring.gate, k, g);
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
                         D[e] = fmul2(D[e], g[e]);
@@ -486,10 +498,10 @@ __global__ void __launch_bounds__(most_threads(kPieces), 1) k_block_bwd(BlockGra
                     put1(TR(), c.d_resid, ring.dr, D * c.resid_scale);
                 ye = needs_y ? (column_value(m.y, kMixed ? ring.y.dtype : kTypeY, m.e_y) - m.stats.x) * scale : 0.f;
                 if (dgate) {
-                    float w = ye;
-                    if (post)
-                        w = fmaf(w, param(c.gamma_post, c.param_dtype, end), c.beta_post ? param(c.beta_post, c.param_dtype, end) : 0.f);
-                    put1(TY(), c.dgate, ring.dgate, s * D * w);
+                    float w = ye * cpost_end;
+                    if (GENERAL && c.beta_post)
+                        w += s * param(c.beta_post, c.param_dtype, end);
+                    put1(TY(), c.dgate, ring.dgate, D * w);
                 }
                 if (token_gate)
                     D *= column_value(m.gate, gradient_type<TY>(), 0u);
@@ -542,7 +554,7 @@ __global__ void __launch_bounds__(most_threads(kPieces), 1) k_block_bwd(BlockGra
 #pragma unroll
             for (int k = 0; k < kPieces; ++k) {
                 float2 x[4];
-                const float f = a1 * centred_y(at, m, k, x);
+                const float f = a1 * centred_y(at, i, m, k, x);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     x[e] = ffma2(x[e], splat(f), fmul2(E[4 * k + e], splat(r0)));
@@ -589,7 +601,7 @@ __global__ void __launch_bounds__(most_threads(kPieces), 1) k_block_bwd(BlockGra
     }
 }
 
-template <typename TR, typename TY, int kPieces> cudaError_t launch_rows(BlockGradCall c, const Phases &phases, int *parts, bool *taken, cudaStream_t stream)
+template <typename TR, typename TY, int kPieces, int MOST> cudaError_t launch_rows(BlockGradCall c, const Phases &phases, int *parts, bool *taken, cudaStream_t stream)
 {
     const bool sums = c.dgamma_pre || c.dbeta_pre || c.dgamma_post || c.dbeta_post || (c.dgate && !c.ldg);
     const bool needs_y = block_bwd_needs_y(c), token_gate = c.gate && c.ldg, ends = phases.at || phases.step || c.d % 8;
@@ -601,7 +613,7 @@ template <typename TR, typename TY, int kPieces> cudaError_t launch_rows(BlockGr
     ring.dy = (uint32_t)(c.lddy * sizeof(TY));
     ring.dgate = (uint32_t)(c.lddg * sizeof(TY));
     const int n = (int)((c.d + kE * 32 - 1) / (kE * 32)) * 32, per = std::max(1, 256 / n), threads = n * per;
-    const auto add = [&](RingPart &part, const void *p, int64_t ld, int32_t dtype) {
+    const auto add = [&](RingPart &part, const void *p, int64_t ld, int32_t dtype, bool direct) {
         if (!p)
             return;
         part.p = static_cast<const char *>(p);
@@ -609,26 +621,34 @@ template <typename TR, typename TY, int kPieces> cudaError_t launch_rows(BlockGr
         part.bytes = stored_bytes(dtype);
         part.pitch = (uint32_t)(ld * part.bytes);
         part.at = ring.stage;
-        ring.stage += n * kE * part.bytes;
+        part.direct = direct;
+        ring.stage += direct ? 0 : n * kE * part.bytes;
     };
-    add(ring.resid, c.gamma_pre ? c.resid : nullptr, c.ldr, c.resid_dtype);
-    add(ring.dh, c.dh, c.lddh, c.grad_y_dtype);
-    add(ring.dro, c.d_resid_out, c.lddro, c.grad_r_dtype);
-    add(ring.y, needs_y ? c.y : nullptr, c.ldy, c.y_dtype);
-    add(ring.gate, token_gate ? c.gate : nullptr, c.ldg, c.grad_y_dtype);
-    ring.extra = ring.stage;
-    ring.stage += n / 32 * extra_bytes(kPieces);
+    constexpr size_t kRoom = 226 * 1024, kHalf = 112 * 1024;
+    const size_t gamma = sizeof(float) * kE * threads;
+    // y and a gate of its own for every element are read from global memory where two rows do not fit otherwise
+    for (const bool direct : {false, true}) {
+        ring.stage = 0;
+        add(ring.resid, c.gamma_pre ? c.resid : nullptr, c.ldr, c.resid_dtype, false);
+        add(ring.dh, c.dh, c.lddh, c.grad_y_dtype, false);
+        add(ring.dro, c.d_resid_out, c.lddro, c.grad_r_dtype, false);
+        add(ring.y, needs_y ? c.y : nullptr, c.ldy, c.y_dtype, direct);
+        add(ring.gate, token_gate ? c.gate : nullptr, c.ldg, c.grad_y_dtype, direct);
+        ring.extra = ring.stage;
+        ring.stage += n / 32 * extra_bytes(kPieces);
+        if (2 * (size_t)per * ring.stage + gamma <= kRoom)
+            break;
+    }
     const auto in_blocks = [](const RingPart &p, const uint8_t *exps) {
         return !p.p || p.bytes != 1 ||
                (reinterpret_cast<uintptr_t>(p.p) % 16 == 0 && p.pitch % 16 == 0 && reinterpret_cast<uintptr_t>(exps) % 8 == 0);
     };
     ring.blocks = c.d % 256 == 0 && !ends && in_blocks(ring.resid, c.resid_exps) && in_blocks(ring.y, c.y_exps);
-    // two CTAs per SM up to 256 threads (320 have the registers, but then one), if each has room for a row in flight beside the two at hand
-    constexpr size_t kRoom = 226 * 1024, kHalf = 112 * 1024;
-    const size_t stage = (size_t)per * std::max(ring.stage, 1), gamma = sizeof(float) * kE * threads;
-    const int per_sm = threads <= most_threads(kPieces) / 2 && 3 * stage + gamma <= kHalf ? 2 : 1;
+    // two CTAs per SM up to 256 threads, if each then has room for a row in flight beside the two at hand
+    const size_t stage = (size_t)per * ring.stage;
+    const int per_sm = threads <= 256 && 3 * stage + gamma <= kHalf ? 2 : 1;
     ring.stages = (int)std::min<size_t>(4, ((per_sm == 2 ? kHalf : kRoom) - gamma) / stage);
-    *taken = ring.stages >= 2;  // not rows of 8,192 columns of fp32 with a gate of their own
+    *taken = ring.stages >= 2;
     if (!*taken)
         return cudaSuccess;
     const size_t smem = std::max<size_t>(stage * ring.stages + gamma, sums && per > 1 ? sizeof(float) * per * (size_t)c.d : 0);
@@ -640,7 +660,7 @@ template <typename TR, typename TY, int kPieces> cudaError_t launch_rows(BlockGr
     *parts = grid;
     const bool general = c.kind == TURNOPD_LAYER_NORM || block_bwd_bias(c);
     const bool stored = (!ring.resid.p || c.resid_dtype == c.grad_r_dtype) && (!ring.y.p || c.y_dtype == c.grad_y_dtype);
-    const bool common = c.gamma_pre && c.d_resid_out && c.d_resid && c.dy && sums && !token_gate;
+    const bool common = c.gamma_pre && c.d_resid_out && c.d_resid && c.dy && sums && !token_gate && !ring.y.direct;
     const auto go = [&](auto kernel) {
         const cudaError_t e = allow_shared(kernel, kRoom);
         if (e != cudaSuccess)
@@ -651,7 +671,7 @@ template <typename TR, typename TY, int kPieces> cudaError_t launch_rows(BlockGr
     const auto with_general = [&](auto stored, auto has_ends, auto is_common) {
         constexpr Stored S = decltype(stored)::value;
         constexpr bool E = decltype(has_ends)::value, C = decltype(is_common)::value;
-        return general ? go(k_block_bwd<TR, TY, kPieces, S, E, true, C>) : go(k_block_bwd<TR, TY, kPieces, S, E, false, C>);
+        return general ? go(k_block_bwd<TR, TY, kPieces, MOST, S, E, true, C>) : go(k_block_bwd<TR, TY, kPieces, MOST, S, E, false, C>);
     };
     const std::integral_constant<Stored, kGradientTypes> gradient_types;
     const std::integral_constant<Stored, kAny> any;
@@ -690,9 +710,13 @@ template <typename TR, typename TY> cudaError_t launch_block_rows_bwd(const Bloc
         return cudaSuccess;
     // Two pieces to a thread and two blocks per SM up to 4,096 columns (from 8-bit activations, 32,768 x 4,096: 277 us, one piece
     // and one block 352); then one piece, whose blocks have twice the warps (16,384 x 5,120 bf16: 192 us, two pieces 203), as
-    // long as a block's threads hold the row.
-    return c.d <= 4096 || c.d > 8 * most_threads(1) ? launch_rows<TR, TY, 2>(c, phases, parts, taken, stream)
-                                                    : launch_rows<TR, TY, 1>(c, phases, parts, taken, stream);
+    // long as a block's threads hold the row.  With the sums of layer norms or betas, or rows that begin anywhere, two pieces
+    // are more than the registers hold.
+    const bool few = c.kind != TURNOPD_LAYER_NORM && !block_bwd_bias(c) && !phases.at && !phases.step && c.d % 8 == 0;
+    if (c.d > 8 * kMany || (few && c.d > 256 && c.d <= 4096))
+        return launch_rows<TR, TY, 2, kFew>(c, phases, parts, taken, stream);
+    return c.d <= 8 * kFew ? launch_rows<TR, TY, 1, kFew>(c, phases, parts, taken, stream)
+                           : launch_rows<TR, TY, 1, kMany>(c, phases, parts, taken, stream);
 }
 
 }  // namespace turnopd

@@ -289,7 +289,7 @@ cudaError_t launch_rows(const BlockCall &c, const Phases &phases, cudaStream_t s
         const auto bytes = [&](int64_t d) { return P == 1 ? (size_t)0 : kVectorBytes * (size_t)(E ? d / 8 + 2 : (d + 7) / 8); };
         // as many CTAs as are resident at once, of which each SM's shared memory limits some
         const size_t smem = bytes(c.d);
-        const int resident = std::min<int>(std::max(PER_SM * MOST / (n * per), 1), (int)(220 * 1024 / (smem + 1024)));
+        const int resident = std::min<int>(std::max((P == 1 && n == 32 ? 1024 : PER_SM * MOST) / (n * per), 1), (int)(220 * 1024 / (smem + 1024)));
         int64_t grid = std::min<int64_t>(blocks, (int64_t)device_sm_count() * resident);
         if (E)
             grid = (grid * per + 7) / 8 * 8 / per;  // a multiple of eight groups
@@ -301,22 +301,29 @@ cudaError_t launch_rows(const BlockCall &c, const Phases &phases, cudaStream_t s
     };
     const auto with_general = [&](auto has_ends) {
         constexpr bool E = decltype(has_ends)::value;
-        return general ? go(k_block_fwd<TR, TY, P, GATE, E, true, MOST, PER_SM>, has_ends, std::true_type())
-                       : go(k_block_fwd<TR, TY, P, GATE, E, false, MOST, PER_SM>, has_ends, std::false_type());
+        if (general)
+            return go(k_block_fwd<TR, TY, P, GATE, E, true, MOST, PER_SM>, has_ends, std::true_type());
+        return go(k_block_fwd<TR, TY, P, GATE, E, false, MOST, PER_SM>, has_ends, std::false_type());
     };
     return ends ? with_general(std::true_type()) : with_general(std::false_type());
 }
 
-// Many rows: as many pieces to a thread as its registers hold, so that many rows are in flight; few rows: one, so that each
-// answers sooner.
+// Many rows: as many pieces to a thread as its registers hold (and the row has), so that many rows are in flight; few rows:
+// one, so that each answers sooner.
 template <typename TR, typename TY, bool GATE> cudaError_t launch_gated(const BlockCall &c, const Phases &phases, cudaStream_t stream)
 {
-    if (c.T * ((c.d + 1023) / 1024) < 4 * device_sm_count())
-        return c.d <= 4096 ? launch_rows<TR, TY, GATE, 1, 512, 1>(c, phases, stream) : launch_rows<TR, TY, GATE, 1, 1024, 1>(c, phases, stream);
+    const bool few = c.T * ((c.d + 1023) / 1024) < 4 * device_sm_count();
+    if (c.d <= 256 || (few && c.d <= 4096))
+        return launch_rows<TR, TY, GATE, 1, 512, 1>(c, phases, stream);
+    if (few)
+        return launch_rows<TR, TY, GATE, 1, 1024, 1>(c, phases, stream);
+    // bf16 layer norms with a gate per channel, 32,768 x 512: 42 us with four pieces, 31 with two; 32,768 x 4,096: 223, 268;
+    // 16,384 x 8,192: 374, 287 (two copies of their four vectors do not fit beside each other)
+    const bool general = c.kind == TURNOPD_LAYER_NORM || c.beta_post || c.beta_pre;
     if constexpr (sizeof(TR) + sizeof(TY) * (GATE ? 2 : 1) <= 6)
-        return launch_rows<TR, TY, GATE, 4, 256, 2>(c, phases, stream);
-    else
-        return launch_rows<TR, TY, GATE, 2, 512, 1>(c, phases, stream);
+        if (c.d > 512 && (!general || c.d <= 5120))
+            return launch_rows<TR, TY, GATE, 4, 256, 2>(c, phases, stream);
+    return launch_rows<TR, TY, GATE, 2, 512, 1>(c, phases, stream);
 }
 
 }  // namespace

@@ -327,11 +327,13 @@ __global__ void __launch_bounds__(kSumThreads) k_embed_sums(EmbedGradCall c, con
         for (int64_t v = v0 + (threadIdx.x >> 5); v < min(v0 + kZeroRows, c.vocab); v += blockDim.x >> 5) {
             if (present[v / 32] >> (v & 31) & 1)
                 continue;
-            const float zero[8] = {};
-            for (int64_t j = VEC ? lane * 8 : lane; j < d; j += 256) {
-                const Columns<VEC> cols{j, d, 32};
-                cols.store(static_cast<TW *>(c.dw) + v * c.ldw, zero);
-            }
+            TW *row = static_cast<TW *>(c.dw) + v * c.ldw;
+            constexpr int W = 16 / (int)sizeof(TW);
+            const int64_t pieces = VEC ? d / W : 0;
+            for (int64_t j = lane; j < pieces; j += 32)
+                __stcs(reinterpret_cast<uint4 *>(row) + j, make_uint4(0u, 0u, 0u, 0u));
+            for (int64_t j = pieces * W + lane; j < d; j += 32)
+                row[j] = from_float<TW>(0.f);
         }
         return;
     }

@@ -3,7 +3,7 @@ between the blocks their norms, gates and residual connections.  With policy.Pol
 
 Everything outside of the blocks runs in libturnopd's kernels.  A block is any callable [T, d] -> [T, d]; it runs without a
 record in the forward pass and once more, from the input that was kept, in the backward pass, where autograd gives its
-gradients.  What is kept in between -- each block's input and output and the residual stream after it -- can be kept in 8
+gradients; it may not write into its input.  What is kept in between -- each block's input and output and the residual stream after it -- can be kept in 8
 bits (turnopd_act8_store): 1.03 bytes an element instead of two or four, at the price of the codes' rounding in the gradients.
 """
 from __future__ import annotations
@@ -100,6 +100,9 @@ class PolicyTrunk:
         """dx [T, d], of the residual stream's type: dL/dx.  It is used up; once after each forward pass that was saved."""
         if self.saved is None:
             raise RuntimeError("PolicyTrunk.backward needs a saved forward pass of its own")
+        if torch.cuda.is_current_stream_capturing():
+            raise RuntimeError("PolicyTrunk.backward cannot be captured: autograd runs the blocks, whose parameters may have "
+                               "other graphs' nodes")
         saved, self.saved = self.saved, None
         T, d, dev, bt = dx.shape[0], dx.shape[1], dx.device, self.embedding.dtype
         f32 = dict(dtype=torch.float32, device=dev)
