@@ -120,7 +120,7 @@ __global__ void __launch_bounds__(kSortThreads) k_sort_tokens(EmbedGradCall c, S
                                                               int64_t rows_zeroed, uint32_t *present)
 {
     extern __shared__ uint32_t counts[];  // [kSortWarps][bins]
-    __shared__ uint32_t total[1 << kRadixBits], warp_total[kSortWarps];
+    __shared__ uint32_t total[1 << kRadixBits], base[1 << kRadixBits], warp_total[kSortWarps];
     pdl_begin();
     if (blockIdx.x >= ctas) {
         if (c.dw_dtype == TURNOPD_BF16)
@@ -140,34 +140,37 @@ __global__ void __launch_bounds__(kSortThreads) k_sort_tokens(EmbedGradCall c, S
     uint32_t *mine = counts + warp * bins;
     for (int p = 0; p < passes; ++p) {
         const uint2 *from = b.list[p & 1];
-        const auto key_of = [&](int64_t i) -> uint32_t {
+        const auto entry = [&](int64_t i) -> uint2 {
             if (i >= hi)
-                return 0u;
+                return make_uint2(0u, 0u);
             if (p)
-                return __ldcg(&from[i].x);
-            if (c.mask && !c.mask[i])
-                return (uint32_t)vocab;
-            const int id = c.ids[i];
-            if (id >= 0 && id < vocab)
-                return (uint32_t)id;
-            set_status(c.status, TURNOPD_ERR_TOKEN_RANGE);
-            return (uint32_t)vocab;
+                return __ldcg(from + i);
+            uint32_t key = (uint32_t)vocab;
+            if (!c.mask || c.mask[i]) {
+                const int id = c.ids[i];
+                if (id >= 0 && id < vocab)
+                    key = (uint32_t)id;
+                else
+                    set_status(c.status, TURNOPD_ERR_TOKEN_RANGE);
+            }
+            return make_uint2(key, (uint32_t)i);
         };
+        uint2 list[kSortBatch];  // the last batch read, which is the only one up to 256 keys to a warp
+        const bool once = seg <= 32 * kSortBatch;
         const int shift = p * bits;
         for (int k = lane; k < bins; k += 32)
             mine[k] = 0;
         __syncwarp();
         for (int64_t first = lo; first < hi; first += 32 * kSortBatch) {
-            uint32_t key[kSortBatch];
 #pragma unroll
             for (int k = 0; k < kSortBatch; ++k)
-                key[k] = key_of(first + 32 * k + lane);
+                list[k] = entry(first + 32 * k + lane);
 #pragma unroll
             for (int k = 0; k < kSortBatch; ++k) {
                 const bool there = first + 32 * k + lane < hi;
                 if (first + 32 * k >= hi)
                     break;
-                const uint32_t digit = there ? (key[k] >> shift) & (bins - 1) : ~0u;
+                const uint32_t digit = there ? (list[k].x >> shift) & (bins - 1) : ~0u;
                 const uint32_t peers = __match_any_sync(~0u, digit);
                 if (there && lane == __ffs(peers) - 1)
                     mine[digit] += __popc(peers);
@@ -178,24 +181,33 @@ __global__ void __launch_bounds__(kSortThreads) k_sort_tokens(EmbedGradCall c, S
         // per digit: the sum over the warps, and each warp's place in it
         const int bin = threadIdx.x;
         if (bin < bins) {
-            uint32_t sum = 0;
-#pragma unroll 8
+            uint32_t n[kSortWarps], sum = 0;
+#pragma unroll
+            for (int w = 0; w < kSortWarps; ++w)
+                n[w] = counts[w * bins + bin];
+#pragma unroll
             for (int w = 0; w < kSortWarps; ++w) {
-                const uint32_t n = counts[w * bins + bin];
                 counts[w * bins + bin] = sum;
-                sum += n;
+                sum += n[w];
             }
             total[bin] = sum;
         }
         cluster_sync();
         uint32_t before = 0, all = 0;
-        if (bin < bins)
-            for (uint32_t r = 0; r < ctas; ++r) {
-                uint32_t n;
-                asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(n) : "r"(mapa(smem_u32(total + bin), r)) : "memory");
-                before += r < rank ? n : 0u;
-                all += n;
+        if (bin < bins) {
+            uint32_t n[kMaxCtas];
+#pragma unroll
+            for (uint32_t r = 0; r < kMaxCtas; ++r) {
+                n[r] = 0;
+                if (r < ctas)
+                    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(n[r]) : "r"(mapa(smem_u32(total + bin), r)));
             }
+#pragma unroll
+            for (uint32_t r = 0; r < kMaxCtas; ++r) {
+                before += r < rank ? n[r] : 0u;
+                all += n[r];
+            }
+        }
         uint32_t scan = all;
         for (int o = 1; o < 32; o <<= 1) {
             const uint32_t n = __shfl_up_sync(~0u, scan, o);
@@ -207,33 +219,29 @@ __global__ void __launch_bounds__(kSortThreads) k_sort_tokens(EmbedGradCall c, S
         if (bin < bins) {
             for (int w = 0; w < warp; ++w)
                 before += warp_total[w];
-#pragma unroll 8
-            for (int w = 0; w < kSortWarps; ++w)
-                counts[w * bins + bin] += before + scan - all;
+            base[bin] = before + scan - all;
         }
         __syncthreads();
         for (int64_t first = lo; first < hi; first += 32 * kSortBatch) {
-            uint2 key[kSortBatch];
+            if (!once)
 #pragma unroll
-            for (int k = 0; k < kSortBatch; ++k) {
-                const int64_t i = first + 32 * k + lane;
-                key[k] = p && i < hi ? __ldcg(from + i) : make_uint2(p ? 0u : key_of(i), (uint32_t)i);
-            }
+                for (int k = 0; k < kSortBatch; ++k)
+                    list[k] = entry(first + 32 * k + lane);
 #pragma unroll
             for (int k = 0; k < kSortBatch; ++k) {
                 const bool there = first + 32 * k + lane < hi;
                 if (first + 32 * k >= hi)
                     break;
-                const uint32_t digit = there ? (key[k].x >> shift) & (bins - 1) : ~0u;
+                const uint32_t digit = there ? (list[k].x >> shift) & (bins - 1) : ~0u;
                 const uint32_t peers = __match_any_sync(~0u, digit);
                 uint32_t to = 0;
                 if (there)
-                    to = mine[digit] + __popc(peers & ((1u << lane) - 1u));
+                    to = base[digit] + mine[digit] + __popc(peers & ((1u << lane) - 1u));
                 __syncwarp();
                 if (there) {
                     if (lane == __ffs(peers) - 1)
                         mine[digit] += __popc(peers);
-                    __stcg(b.list[~p & 1] + to, key[k]);
+                    __stcg(b.list[~p & 1] + to, list[k]);
                 }
                 __syncwarp();
             }
