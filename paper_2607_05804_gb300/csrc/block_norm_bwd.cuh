@@ -144,25 +144,6 @@ __global__ void __launch_bounds__(MOST, 1) k_block_bwd(BlockGradCall c, Ring rin
 #pragma unroll
         for (int q = 0; q < kSums; ++q)
             sums[q][k] = make_float2(0.f, 0.f);
-    // s gamma_post gate of a column (without those that there are not)
-    const auto post_factor = [&](int j) {
-        float p = s * (post ? param(c.gamma_post, c.param_dtype, j) : 1.f);
-        return c.gate && !c.ldg ? p * param(c.gate, c.param_dtype, j) : p;
-    };
-#pragma unroll
-    for (int k = 0; k < kPieces; ++k) {
-        float g[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const int j = column(k) + e;
-            g[e] = there(k) && pre ? param(c.gamma_pre, c.param_dtype, j) : 0.f;
-            reinterpret_cast<float *>(cpost)[k * 8 + e] = there(k) ? post_factor(j) : 0.f;
-        }
-        gamma[2 * k * n] = make_float4(g[0], g[1], g[2], g[3]);
-        gamma[(2 * k + 1) * n] = make_float4(g[4], g[5], g[6], g[7]);
-    }
-    const float gamma_end = at_end && pre ? param(c.gamma_pre, c.param_dtype, end) : 0.f, cpost_end = at_end ? post_factor(end) : 0.f;
-
     uint32_t ahead = b;  // the next row to copy, whose mask has been read before
     uint32_t ahead_on = ahead < T && c.mask ? c.mask[ahead] : 1u;
     int ahead_stage = 0;
@@ -221,6 +202,28 @@ __global__ void __launch_bounds__(MOST, 1) k_block_bwd(BlockGradCall c, Ring rin
             ahead_on = c.mask[ahead];
         asm volatile("cp.async.commit_group;" ::: "memory");
     };
+    for (int k = 0; k + 1 < ring.stages; ++k)
+        copy();
+
+    // s gamma_post gate of a column (without those that there are not)
+    const auto post_factor = [&](int j) {
+        float p = s * (post ? param(c.gamma_post, c.param_dtype, j) : 1.f);
+        return c.gate && !c.ldg ? p * param(c.gate, c.param_dtype, j) : p;
+    };
+#pragma unroll
+    for (int k = 0; k < kPieces; ++k) {
+        float g[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const int j = column(k) + e;
+            g[e] = there(k) && pre ? param(c.gamma_pre, c.param_dtype, j) : 0.f;
+            reinterpret_cast<float *>(cpost)[k * 8 + e] = there(k) ? post_factor(j) : 0.f;
+        }
+        gamma[2 * k * n] = make_float4(g[0], g[1], g[2], g[3]);
+        gamma[(2 * k + 1) * n] = make_float4(g[4], g[5], g[6], g[7]);
+    }
+    const float gamma_end = at_end && pre ? param(c.gamma_pre, c.param_dtype, end) : 0.f, cpost_end = at_end ? post_factor(end) : 0.f;
+
     // What a thread needs of a row beside its pieces.  Exponents that do not come through the ring (of each piece, whose columns
     // may lie in two groups of them) and the thread's single column are read two rows ahead, and looked at when their turn comes.
     struct Row {
@@ -364,8 +367,6 @@ __global__ void __launch_bounds__(MOST, 1) k_block_bwd(BlockGradCall c, Ring rin
         }
     };
 
-    for (int k = 0; k + 1 < ring.stages; ++k)
-        copy();
     Row m = read_row(b), next = read_row(b + groups);
     int stage = 0, odd = 0;
     // the sums of the first row are taken by themselves (those of rows that do not take part, of nothing: no barrier stands

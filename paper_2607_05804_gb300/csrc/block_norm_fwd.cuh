@@ -79,6 +79,35 @@ __global__ void __launch_bounds__(MOST, PER_SM) k_block_fwd(BlockCall c, int n, 
     const auto column = [&](int k) { return head + (piece0 + 32 * k) * 8; };  // the first of piece k
     const auto there = [&](int k) { return piece0 + 32 * k < whole; };
 
+    Raw8<TR> r[P];
+    Raw8<TY> y[P], g[GATE ? P : 1];
+    float re = 0.f, ye = 0.f, ge = 0.f;
+    bool on = false;
+    const auto load = [&](int64_t i) {
+        on = i < c.T && (!c.mask || c.mask[i]);
+        const TR *rr = static_cast<const TR *>(c.resid) + i * c.ldr;
+        const TY *yy = static_cast<const TY *>(c.y) + i * c.ldy, *gg = static_cast<const TY *>(c.gate) + i * c.ldg;
+#pragma unroll
+        for (int k = 0; k < P; ++k)
+            if (on && there(k)) {
+                y[k].load(yy + column(0) + k * 256);
+                r[k].load(rr + column(0) + k * 256);
+                if (GATE)
+                    g[GATE ? k : 0].load(gg + column(0) + k * 256);
+            } else {
+                r[k].clear();
+                y[k].clear();
+                if (GATE)
+                    g[GATE ? k : 0].clear();
+            }
+        if (ENDS) {
+            re = on && at_end ? to_float(rr[end]) : 0.f;
+            ye = on && at_end ? to_float(yy[end]) : 0.f;
+            ge = GATE && on && at_end ? to_float(gg[end]) : 0.f;
+        }
+    };
+    load(b);
+
     const int plane = ENDS ? d / 8 + 2 : (d + 7) / 8;  // floats, or groups of four
     constexpr int kPlanes = ENDS ? 8 : 2, kWidth = ENDS ? 1 : 4;
     float2 held[kHeld ? kVectors : 1][4];
@@ -121,33 +150,6 @@ __global__ void __launch_bounds__(MOST, PER_SM) k_block_fwd(BlockCall c, int n, 
         }
     };
 
-    Raw8<TR> r[P];
-    Raw8<TY> y[P], g[GATE ? P : 1];
-    float re = 0.f, ye = 0.f, ge = 0.f;
-    bool on = false;
-    const auto load = [&](int64_t i) {
-        on = i < c.T && (!c.mask || c.mask[i]);
-        const TR *rr = static_cast<const TR *>(c.resid) + i * c.ldr;
-        const TY *yy = static_cast<const TY *>(c.y) + i * c.ldy, *gg = static_cast<const TY *>(c.gate) + i * c.ldg;
-#pragma unroll
-        for (int k = 0; k < P; ++k)
-            if (on && there(k)) {
-                y[k].load(yy + column(0) + k * 256);
-                r[k].load(rr + column(0) + k * 256);
-                if (GATE)
-                    g[GATE ? k : 0].load(gg + column(0) + k * 256);
-            } else {
-                r[k].clear();
-                y[k].clear();
-                if (GATE)
-                    g[GATE ? k : 0].clear();
-            }
-        if (ENDS) {
-            re = on && at_end ? to_float(rr[end]) : 0.f;
-            ye = on && at_end ? to_float(yy[end]) : 0.f;
-            ge = GATE && on && at_end ? to_float(gg[end]) : 0.f;
-        }
-    };
     // mu and rho of the columns that x(k, e) gives in pairs, and of a single one; missing columns are zeros.  The sums are
     // taken for rows that do not take part too: no barrier stands under a condition that every thread reads from the
     // caller's memory for itself.
@@ -175,7 +177,6 @@ __global__ void __launch_bounds__(MOST, PER_SM) k_block_fwd(BlockCall c, int n, 
         rho = rsqrtf(group_sum(q.x + q.y, red[sums++ & 3], group, warps) * inv_d + c.eps);  // within two units of the last place
         return isfinite(mu) && isfinite(rho) && rho > 0.f;
     };
-    load(b);
     for (int64_t i = b; i < c.T; i += groups) {
         bool fine = on;
         float mu0 = 0.f, rho0 = 0.f, mu1 = 0.f, rho1 = 0.f;
