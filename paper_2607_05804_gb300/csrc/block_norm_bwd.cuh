@@ -55,7 +55,7 @@ __device__ __forceinline__ void from_ring(const char *at, int dtype, float2 *v)
         decode8(*reinterpret_cast<const uint2 *>(at), dtype == TURNOPD_E4M3, f);
 }
 
-constexpr int extra_bytes(int pieces) { return 16 + 2 * 8 * pieces; }  // of a warp: statistics, exponents of r' and of y
+constexpr int extra_bytes(int pieces, bool codes) { return 16 + (codes ? 2 * 8 * pieces : 0); }  // of a warp: statistics, exponents
 
 // Most threads of a block: 512 with 128 registers each, or 640 with 96, which one piece of eight columns to a thread will do with.
 constexpr int kFew = 512, kMany = 640;
@@ -106,7 +106,7 @@ template <typename TR, typename TY, int kPieces, int MOST, Stored STORED, bool E
 __global__ void __launch_bounds__(MOST, 1) k_block_bwd(BlockGradCall c, Ring ring, int n, int phase, int phase_step)
 {
     // sums over a row: of g xh (and of g) of the norm after the block, and of the norm before the next one
-    constexpr int kRowSums = GENERAL ? 4 : 2, kE = 8 * kPieces, kExtra = extra_bytes(kPieces);
+    constexpr int kRowSums = GENERAL ? 4 : 2, kE = 8 * kPieces, kExtra = extra_bytes(kPieces, STORED != kGradientTypes);
     constexpr bool kMixed = STORED == kAny, kCodes = STORED == kE4m3 || STORED == kInt8;
     constexpr int kTypeR = type_code<STORED, TR>(), kTypeY = type_code<STORED, TY>();
     extern __shared__ __align__(128) char shared[];
@@ -625,7 +625,9 @@ template <typename TR, typename TY, int kPieces, int MOST> cudaError_t launch_ro
         part.direct = direct;
         ring.stage += direct ? 0 : n * kE * part.bytes;
     };
-    constexpr size_t kRoom = 226 * 1024, kHalf = 112 * 1024;
+    const bool stored = (!c.gamma_pre || c.resid_dtype == c.grad_r_dtype) && (!needs_y || c.y_dtype == c.grad_y_dtype);
+    // of a block that has an SM's shared memory to itself, or half of it beside a block's own kilobyte and its static arrays
+    constexpr size_t kRoom = 226 * 1024, kHalf = 114 * 1024 - 1024 - 512;
     const size_t gamma = sizeof(float) * kE * threads;
     // y and a gate of its own for every element are read from global memory where two rows do not fit otherwise
     for (const bool direct : {false, true}) {
@@ -636,7 +638,7 @@ template <typename TR, typename TY, int kPieces, int MOST> cudaError_t launch_ro
         add(ring.y, needs_y ? c.y : nullptr, c.ldy, c.y_dtype, direct);
         add(ring.gate, token_gate ? c.gate : nullptr, c.ldg, c.grad_y_dtype, direct);
         ring.extra = ring.stage;
-        ring.stage += n / 32 * extra_bytes(kPieces);
+        ring.stage += n / 32 * extra_bytes(kPieces, !stored);
         if (2 * (size_t)per * ring.stage + gamma <= kRoom)
             break;
     }
@@ -655,12 +657,14 @@ template <typename TR, typename TY, int kPieces, int MOST> cudaError_t launch_ro
     const size_t smem = std::max<size_t>(stage * ring.stages + gamma, sums && per > 1 ? sizeof(float) * per * (size_t)c.d : 0);
     const int64_t blocks = (c.T + per - 1) / per;
     const int64_t most = std::min<int64_t>((int64_t)per_sm * device_sm_count(), kBlockMaxParts);
-    int grid = (int)std::min<int64_t>(blocks > device_sm_count() ? (blocks + 1) / 2 : blocks, most);
+    // six rows to a group at least, once there is one for every SM: each block's partial sums are written and read again
+    // (512 rows x 4,096: 152 blocks 18 us, 256 blocks 22)
+    const int64_t sms = device_sm_count();
+    int grid = (int)std::min<int64_t>(blocks > sms ? std::max(sms, (blocks + 5) / 6) : blocks, most);
     if (ends)
         grid = std::min((grid * per + 7) / 8 * 8 / per, kBlockMaxParts);  // a multiple of eight groups
     *parts = grid;
     const bool general = c.kind == TURNOPD_LAYER_NORM || block_bwd_bias(c);
-    const bool stored = (!ring.resid.p || c.resid_dtype == c.grad_r_dtype) && (!ring.y.p || c.y_dtype == c.grad_y_dtype);
     const bool common = c.gamma_pre && c.d_resid_out && c.d_resid && c.dy && sums && !token_gate && !ring.y.direct;
     const auto go = [&](auto kernel) {
         const cudaError_t e = allow_shared(kernel, kRoom);
