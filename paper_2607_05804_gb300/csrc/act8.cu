@@ -149,43 +149,47 @@ template <typename TX, bool E4M3, int U> __global__ void __launch_bounds__(32 * 
         }
 }
 
-// Any rows: a column to a lane, a group at a time.
-template <typename TX> __global__ void __launch_bounds__(32 * kWarps) k_act8_store_any(Act8Call c)
+// Any rows: a column to a lane, a group at a time, U chunks of a row at once.
+template <typename TX, int U> __global__ void __launch_bounds__(32 * kWarps) k_act8_store_any(Act8Call c)
 {
     const int lane = threadIdx.x & 31;
     const int64_t d = c.d, groups = (d + kActGroup - 1) / kActGroup;
     const bool e4m3 = c.code_dtype == TURNOPD_E4M3;
-    for (int64_t strip = (int64_t)blockIdx.y * kChunk; strip < d; strip += (int64_t)gridDim.y * kChunk)
+    for (int64_t strip = (int64_t)blockIdx.y * U * kChunk; strip < d; strip += (int64_t)gridDim.y * U * kChunk)
         for (int64_t row = (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5); row < c.T; row += (int64_t)gridDim.x * kWarps) {
             const bool on = !c.mask || c.mask[row];
-            const TX *x = static_cast<const TX *>(c.x) + row * c.ldx;
-            uint8_t *codes = static_cast<uint8_t *>(c.codes) + row * c.ldc, *exps = c.exps + row * groups;
-            float v[8];
+            const int left = (int)min(d - strip, (int64_t)U * kChunk);
+            const TX *x = static_cast<const TX *>(c.x) + row * c.ldx + strip;
+            uint8_t *codes = static_cast<uint8_t *>(c.codes) + row * c.ldc + strip, *exps = c.exps + row * groups + strip / kActGroup;
+            // (a column past the end counts as the last one, whose group is the same or is not written)
+            TX raw[U * 8];
+            float v[U * 8];
 #pragma unroll
-            for (int g = 0; g < 8; ++g) {
-                const int64_t j = strip + g * kActGroup + lane;
-                v[g] = on && j < d ? to_float(x[j]) : 0.f;
-            }
+            for (int g = 0; g < U * 8; ++g)
+                if (on)
+                    raw[g] = x[min(g * kActGroup + lane, left - 1)];
+#pragma unroll
+            for (int g = 0; g < U * 8; ++g)
+                v[g] = on && g * kActGroup < left ? to_float(raw[g]) : 0.f;
             // lane g has group g's largest magnitude, makes its exponent and writes it
             uint32_t mine = 0;
 #pragma unroll
-            for (int g = 0; g < 8; ++g) {
+            for (int g = 0; g < U * 8; ++g) {
                 const uint32_t amax = __reduce_max_sync(~0u, magnitude(v[g]));
                 mine = lane == g ? amax : mine;
             }
             const uint32_t e = on ? exponent_byte(mine, e4m3) : 0u;
             const float s = inverse_scale(e);
-            if (lane < 8 && strip + lane * kActGroup < d) {
-                exps[strip / kActGroup + lane] = (uint8_t)e;
+            if (lane < U * 8 && lane * kActGroup < left) {
+                exps[lane] = (uint8_t)e;
                 if (e == 255u)
                     set_status(c.status, TURNOPD_ERR_NONFINITE);
             }
 #pragma unroll
-            for (int g = 0; g < 8; ++g) {
-                const int64_t j = strip + g * kActGroup + lane;
+            for (int g = 0; g < U * 8; ++g) {
                 const float scale = __shfl_sync(~0u, s, g);
-                if (j < d)
-                    codes[j] = (uint8_t)encode2(scale == 0.f ? 0.f : v[g] * scale, 0.f, e4m3);
+                if (g * kActGroup + lane < left)
+                    codes[g * kActGroup + lane] = (uint8_t)encode2(scale == 0.f ? 0.f : v[g] * scale, 0.f, e4m3);
             }
         }
 }
@@ -198,54 +202,73 @@ template <typename TX> __device__ __forceinline__ float worth(float code, float 
     return v > kMost ? kMost : v < -kMost ? -kMost : v;  // NaN stays
 }
 
-template <typename TX, bool VEC, int U> __global__ void __launch_bounds__(32 * kWarps, 4) k_act8_load(Act8Call c)
+// The same two layouts as for storing.
+template <typename TX, int U> __global__ void __launch_bounds__(32 * kWarps, 4) k_act8_load(Act8Call c)
 {
     const int lane = threadIdx.x & 31;
     const int64_t d = c.d, groups = (d + kActGroup - 1) / kActGroup;
     const bool e4m3 = c.code_dtype == TURNOPD_E4M3;
     for (int64_t strip = (int64_t)blockIdx.y * U * kChunk; strip < d; strip += (int64_t)gridDim.y * U * kChunk)
         for (int64_t row = (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5); row < c.T; row += (int64_t)gridDim.x * kWarps) {
+            const int64_t first = strip + lane * 8;
+            const uint8_t *codes = static_cast<const uint8_t *>(c.codes) + row * c.ldc + first, *exps = c.exps + row * groups;
+            TX *x = static_cast<TX *>(c.out) + row * c.ldx + first;
             uint2 code[U];
             uint32_t exp[U];
-            if constexpr (VEC) {
 #pragma unroll
-                for (int q = 0; q < U; ++q) {
-                    const int64_t j = (strip + q * kChunk) + lane * 8;
-                    if (j + 8 <= d) {
-                        code[q] = __ldcs(reinterpret_cast<const uint2 *>(static_cast<const uint8_t *>(c.codes) + row * c.ldc + j));
-                        exp[q] = c.exps[row * groups + j / kActGroup];
-                    }
-                }
+            for (int q = 0; q < U; ++q) {
+                const int64_t left = d - first - q * kChunk;
+                code[q] = make_uint2(0u, 0u);
+                exp[q] = left > 0 ? exps[(first + q * kChunk) / kActGroup] : 0u;
+                if (left >= 8)
+                    code[q] = __ldcs(reinterpret_cast<const uint2 *>(codes + q * kChunk));
+                else
+                    for (int k = 0; k < left; ++k)
+                        (k < 4 ? code[q].x : code[q].y) |= (uint32_t)codes[q * kChunk + k] << (8 * (k & 3));
             }
 #pragma unroll
             for (int q = 0; q < U; ++q) {
-                TX *x = static_cast<TX *>(c.out) + row * c.ldx;
-                const uint8_t *codes = static_cast<const uint8_t *>(c.codes) + row * c.ldc, *exps = c.exps + row * groups;
-                const auto one = [&](int64_t j) {
-                    const float v = e4m3 ? decode_e4m3(codes[j]) : (float)(int8_t)codes[j];
-                    x[j] = from_float<TX>(worth<TX>(v, act_scale(exps[j / kActGroup])));
-                };
-                if constexpr (VEC) {
-                    const int64_t j = (strip + q * kChunk) + lane * 8;
-                    if (j + 8 <= d) {
-                        float v[8];
-                        decode8(code[q], e4m3, v);
-                        const float s = act_scale(exp[q]);
+                const int64_t left = d - first - q * kChunk;
+                float v[8];
+                decode8(code[q], e4m3, v);
+                const float s = act_scale(exp[q]);
 #pragma unroll
-                        for (int k = 0; k < 8; ++k)
-                            v[k] = worth<TX>(v[k], s);
-                        store8(x + j, v);
-                    } else {
-                        for (int k = 0; k < 8; ++k)
-                            if (j + k < d)
-                                one(j + k);
-                    }
+                for (int k = 0; k < 8; ++k)
+                    v[k] = worth<TX>(v[k], s);
+                if (left >= 8) {
+                    store8(x + q * kChunk, v);
                 } else {
 #pragma unroll
-                    for (int g = 0; g < 8; ++g)
-                        if ((strip + q * kChunk) + g * kActGroup + lane < d)
-                            one((strip + q * kChunk) + g * kActGroup + lane);
+                    for (int k = 0; k < 8; ++k)
+                        if (k < left)
+                            x[q * kChunk + k] = from_float<TX>(v[k]);
                 }
+            }
+        }
+}
+
+template <typename TX, int U> __global__ void __launch_bounds__(32 * kWarps) k_act8_load_any(Act8Call c)
+{
+    const int lane = threadIdx.x & 31;
+    const int64_t d = c.d, groups = (d + kActGroup - 1) / kActGroup;
+    const bool e4m3 = c.code_dtype == TURNOPD_E4M3;
+    for (int64_t strip = (int64_t)blockIdx.y * U * kChunk; strip < d; strip += (int64_t)gridDim.y * U * kChunk)
+        for (int64_t row = (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5); row < c.T; row += (int64_t)gridDim.x * kWarps) {
+            const int left = (int)min(d - strip, (int64_t)U * kChunk);
+            const uint8_t *codes = static_cast<const uint8_t *>(c.codes) + row * c.ldc + strip;
+            TX *x = static_cast<TX *>(c.out) + row * c.ldx + strip;
+            uint8_t code[U * 8];
+#pragma unroll
+            for (int g = 0; g < U * 8; ++g)
+                code[g] = codes[min(g * kActGroup + lane, left - 1)];
+            float s = 0.f;
+            if (lane < U * 8 && lane * kActGroup < left)
+                s = act_scale(c.exps[row * groups + strip / kActGroup + lane]);
+#pragma unroll
+            for (int g = 0; g < U * 8; ++g) {
+                const float scale = __shfl_sync(~0u, s, g);
+                if (g * kActGroup + lane < left)
+                    x[g * kActGroup + lane] = from_float<TX>(worth<TX>(e4m3 ? decode_e4m3(code[g]) : (float)(int8_t)code[g], scale));
             }
         }
 }
@@ -259,10 +282,10 @@ bool on_boundaries(const Act8Call &c)
 }
 
 // Strips of four chunks where there are enough for every warp to have several, else of one.
-template <typename F> void with_grid(const Act8Call &c, bool strips_of_four, F &&go)
+template <typename F> void with_grid(const Act8Call &c, F &&go)
 {
     const int64_t chunks = (c.d + kChunk - 1) / kChunk, blocks = (c.T + kWarps - 1) / kWarps, sms = device_sm_count();
-    const bool four = strips_of_four && blocks * ((chunks + 3) / 4) >= 8 * sms;
+    const bool four = chunks >= 3 && blocks * ((chunks + 3) / 4) >= 8 * sms;
     const int64_t strips = four ? (chunks + 3) / 4 : chunks;
     const dim3 grid((unsigned)std::min<int64_t>(blocks, std::max<int64_t>(sms * 16 / strips, 1)), (unsigned)std::min<int64_t>(strips, 65535));
     if (four)
@@ -286,10 +309,10 @@ cudaError_t launch_act8_store(const Act8Call &c, cudaStream_t stream)
 {
     const bool vec = on_boundaries(c);
     return with_type(c.x_dtype, [&](auto x) {
-        with_grid(c, vec, [&](dim3 grid, auto units) {
+        with_grid(c, [&](dim3 grid, auto units) {
             using X = decltype(x);
             constexpr int U = decltype(units)::value;
-            auto kernel = !vec                             ? k_act8_store_any<X>
+            auto kernel = !vec                             ? k_act8_store_any<X, U>
                           : c.code_dtype == TURNOPD_E4M3 ? k_act8_store<X, true, U>
                                                            : k_act8_store<X, false, U>;
             kernel<<<grid, 32 * kWarps, 0, stream>>>(c);
@@ -301,10 +324,10 @@ cudaError_t launch_act8_load(const Act8Call &c, cudaStream_t stream)
 {
     const bool vec = on_boundaries(c);
     return with_type(c.x_dtype, [&](auto x) {
-        with_grid(c, vec, [&](dim3 grid, auto units) {
+        with_grid(c, [&](dim3 grid, auto units) {
             using X = decltype(x);
             constexpr int U = decltype(units)::value;
-            auto kernel = vec ? k_act8_load<X, true, U> : k_act8_load<X, false, 1>;
+            auto kernel = vec ? k_act8_load<X, U> : k_act8_load_any<X, U>;
             kernel<<<grid, 32 * kWarps, 0, stream>>>(c);
         });
     });

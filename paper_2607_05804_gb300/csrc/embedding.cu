@@ -65,11 +65,22 @@ template <typename TW, typename TO, bool VEC> __global__ void __launch_bounds__(
                     }
                 }
             } else {
-#pragma unroll 8
-                for (int64_t j = first + lane; j < min(first + kFwdChunk, d); j += 32)
-                    one(j);
+                // sixteen loads before the first store: the compiler cannot know that the arrays do not overlap
+                const int n = (int)min((int64_t)kFwdChunk, d - first);
+                const TW *from = w + first;
+                TO *to = out + first;
+                for (int j = lane; j < n; j += 16 * 32) {
+                    TW v[16];
+#pragma unroll
+                    for (int k = 0; k < 16; ++k)
+                        v[k] = from[min(j + 32 * k, n - 1)];
+#pragma unroll
+                    for (int k = 0; k < 16; ++k)
+                        if (j + 32 * k < n)
+                            to[j + 32 * k] = from_float<TO>(id < 0 ? 0.f : to_float(v[k]) * c.scale);
+                }
             }
-    }
+        }
 }
 
 // ---------------------------------------------------------------- tokens sorted by id
@@ -371,7 +382,13 @@ __global__ void __launch_bounds__(kSumThreads) k_embed_sums(EmbedGradCall c, con
         const uint32_t k = key[q + 1];
         return q < most && k != none && (q < size || (k == last && !all_leading)) && !(skip_first && k == first);
     };
-    float sum[8] = {}, ahead[8];
+    float sum[8] = {};
+    TG ahead[kRing ? 1 : 8];  // as it is stored: converting it would wait for it
+    int32_t places[kRing ? 1 : 8];
+    if (!kRing)
+#pragma unroll
+        for (int h = 0; h < (kRing ? 1 : 8); ++h)
+            places[h] = (int32_t)(min(cols.at(h), d - 1));
     const auto issue = [&](int q) {
         const TG *row = static_cast<const TG *>(c.dout) + (wanted(q) ? (int64_t)at[q] * c.ldg : 0);
         if constexpr (kRing) {
@@ -393,7 +410,9 @@ __global__ void __launch_bounds__(kSumThreads) k_embed_sums(EmbedGradCall c, con
             }
             asm volatile("cp.async.commit_group;" ::: "memory");
         } else if (wanted(q)) {
-            cols.load(row, ahead);
+#pragma unroll
+            for (int h = 0; h < (kRing ? 1 : 8); ++h)
+                ahead[h] = row[places[h]];
         }
     };
     const auto add = [&](int q) {
@@ -412,7 +431,7 @@ __global__ void __launch_bounds__(kSumThreads) k_embed_sums(EmbedGradCall c, con
         } else {
 #pragma unroll
             for (int h = 0; h < 8; ++h)
-                v[h] = ahead[h];
+                v[h] = cols.at(h) < d ? to_float(ahead[kRing ? 0 : h]) : 0.f;
         }
         if (kRing || q + 1 < most)
             issue(kRing ? q + kRows : q + 1);
