@@ -71,6 +71,30 @@ __device__ __forceinline__ float group_sum(float x, float *red, int group, int w
     return group_sum(Numbers<1>{{x}}, reinterpret_cast<Numbers<1> *>(red), group, warps).v[0];
 }
 
+// Eight columns of a parameter from j on (those past the last one are some numbers), without conditions between the loads, or
+// one would wait for another.
+template <typename T> __device__ __forceinline__ void eight_of(const T *p, int j, int d, float *v)
+{
+    if (j + 8 <= d && (reinterpret_cast<uintptr_t>(p + j) & 15) == 0) {
+        load8(p + j, v);
+        return;
+    }
+    T raw[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        raw[e] = p[min(j + e, d - 1)];
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        v[e] = to_float(raw[e]);
+}
+__device__ __forceinline__ void param8(const void *p, int32_t dtype, int j, int d, float *v)
+{
+    if (dtype == TURNOPD_BF16)
+        eight_of(static_cast<const __nv_bfloat16 *>(p), j, d, v);
+    else
+        eight_of(static_cast<const float *>(p), j, d, v);
+}
+
 // Column j of row i of an array of any type; 8-bit codes with their exponents.
 __device__ __forceinline__ float element(const void *p, int32_t dtype, int64_t ld, const uint8_t *exps, int64_t d, int64_t i, int64_t j)
 {

@@ -205,19 +205,27 @@ __global__ void __launch_bounds__(MOST, 1) k_block_bwd(BlockGradCall c, Ring rin
     for (int k = 0; k + 1 < ring.stages; ++k)
         copy();
 
-    // s gamma_post gate of a column (without those that there are not)
+    // gamma_pre, and s gamma_post gate (without those that there are not): 0 for missing pieces
     const auto post_factor = [&](int j) {
         float p = s * (post ? param(c.gamma_post, c.param_dtype, j) : 1.f);
         return c.gate && !c.ldg ? p * param(c.gate, c.param_dtype, j) : p;
     };
 #pragma unroll
     for (int k = 0; k < kPieces; ++k) {
-        float g[8];
+        float g[8] = {}, p[8], a[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            p[e] = a[e] = 1.f;
+        if (pre)
+            param8(c.gamma_pre, c.param_dtype, column(k), d, g);
+        if (post)
+            param8(c.gamma_post, c.param_dtype, column(k), d, p);
+        if (c.gate && !c.ldg)
+            param8(c.gate, c.param_dtype, column(k), d, a);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            const int j = column(k) + e;
-            g[e] = there(k) && pre ? param(c.gamma_pre, c.param_dtype, j) : 0.f;
-            reinterpret_cast<float *>(cpost)[k * 8 + e] = there(k) ? post_factor(j) : 0.f;
+            g[e] = there(k) ? g[e] : 0.f;
+            reinterpret_cast<float *>(cpost)[k * 8 + e] = there(k) ? s * p[e] * a[e] : 0.f;
         }
         gamma[2 * k * n] = make_float4(g[0], g[1], g[2], g[3]);
         gamma[(2 * k + 1) * n] = make_float4(g[4], g[5], g[6], g[7]);

@@ -49,6 +49,40 @@ __device__ __forceinline__ float vector_column(const BlockCall &c, int v, int j)
     return c.beta_post ? s * param(c.beta_post, c.param_dtype, j) : 0.f;
 }
 
+// Eight columns of them from j on.
+template <int N> __device__ __forceinline__ void vector_columns(const BlockCall &c, int j, int d, float2 (&o)[N][4])
+{
+    float g[8], gate[8], beta[8];
+    float *f[4];
+#pragma unroll
+    for (int v = 0; v < N; ++v)
+        f[v] = reinterpret_cast<float *>(o[v]);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        g[e] = gate[e] = 1.f;
+        beta[e] = f[kGamma][e] = 0.f;
+        if (N > 2)
+            f[N > 2 ? kBeta : 0][e] = 0.f;
+    }
+    if (c.gamma_post)
+        param8(c.gamma_post, c.param_dtype, j, d, g);
+    if (c.gate && !c.ldg)
+        param8(c.gate, c.param_dtype, j, d, gate);
+    if (N > 2 && c.beta_post)
+        param8(c.beta_post, c.param_dtype, j, d, beta);
+    if (c.gamma_pre)
+        param8(c.gamma_pre, c.param_dtype, j, d, f[kGamma]);
+    if (N > 2 && c.beta_pre)
+        param8(c.beta_pre, c.param_dtype, j, d, f[N > 2 ? kBeta : 0]);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const float s = c.branch_scale * gate[e];
+        f[kFactor][e] = s * g[e];
+        if (N > 2)
+            f[N > 2 ? kShift : 0][e] = s * beta[e];
+    }
+}
+
 // n threads take a row, P pieces of eight columns to a thread, kept as they were read until r' is there; then the loads of
 // the group's next row go out, and that row's bytes arrive while this one's second norm is taken and its results are written.
 // With several pieces the vectors lie in shared memory: the halves of the pieces in a plane each, so that neighbouring
@@ -109,20 +143,27 @@ __global__ void __launch_bounds__(MOST, PER_SM) k_block_fwd(BlockCall c, int n, 
     load(b);
 
     const int plane = ENDS ? d / 8 + 2 : (d + 7) / 8;  // floats, or groups of four
-    constexpr int kPlanes = ENDS ? 8 : 2, kWidth = ENDS ? 1 : 4;
     float2 held[kHeld ? kVectors : 1][4];
     if constexpr (kHeld) {
-#pragma unroll
-        for (int v = 0; v < kVectors; ++v)
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                reinterpret_cast<float *>(held[v])[e] = there(0) ? vector_column(c, v, column(0) + e) : 0.f;
+        vector_columns<kVectors>(c, whole > 0 ? min(column(0), d - 8) : 0, d, held);
     } else {
-        for (int v = 0; v < kVectors; ++v)
-            for (int j = threadIdx.x; j < d; j += blockDim.x) {
-                const int at = ENDS ? (j & 7) * plane + j / 8 : (j / 4 % 2) * plane * 4 + j / 8 * 4 + j % 4;
-                vectors[v * kPlanes * kWidth * plane + at] = vector_column(c, v, j);
+        for (int piece = threadIdx.x; piece < (d + 7) / 8; piece += blockDim.x) {
+            float2 o[kVectors][4];
+            vector_columns<kVectors>(c, piece * 8, d, o);
+#pragma unroll
+            for (int v = 0; v < kVectors; ++v) {
+                const float *f = reinterpret_cast<const float *>(o[v]);
+                if constexpr (ENDS) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        vectors[(v * 8 + e) * plane + piece] = f[e];
+                } else {
+                    float4 *to = reinterpret_cast<float4 *>(vectors) + v * 2 * plane + piece;
+                    to[0] = make_float4(f[0], f[1], f[2], f[3]);
+                    to[plane] = make_float4(f[4], f[5], f[6], f[7]);
+                }
             }
+        }
         __syncthreads();
     }
     float end_of[kVectors];
