@@ -212,20 +212,12 @@ __global__ void __launch_bounds__(MOST, 1) k_block_bwd(BlockGradCall c, Ring rin
     };
 #pragma unroll
     for (int k = 0; k < kPieces; ++k) {
-        float g[8] = {}, p[8], a[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-            p[e] = a[e] = 1.f;
-        if (pre)
-            param8(c.gamma_pre, c.param_dtype, column(k), d, g);
-        if (post)
-            param8(c.gamma_post, c.param_dtype, column(k), d, p);
-        if (c.gate && !c.ldg)
-            param8(c.gate, c.param_dtype, column(k), d, a);
+        float g[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            g[e] = there(k) ? g[e] : 0.f;
-            reinterpret_cast<float *>(cpost)[k * 8 + e] = there(k) ? s * p[e] * a[e] : 0.f;
+            const int j = column(k) + e;
+            g[e] = there(k) && pre ? param(c.gamma_pre, c.param_dtype, j) : 0.f;
+            reinterpret_cast<float *>(cpost)[k * 8 + e] = there(k) ? post_factor(j) : 0.f;
         }
         gamma[2 * k * n] = make_float4(g[0], g[1], g[2], g[3]);
         gamma[(2 * k + 1) * n] = make_float4(g[4], g[5], g[6], g[7]);
@@ -725,8 +717,10 @@ template <typename TR, typename TY> cudaError_t launch_block_rows_bwd(const Bloc
     // and one block 352); then one piece, whose blocks have twice the warps (16,384 x 5,120 bf16: 192 us, two pieces 203), as
     // long as a block's threads hold the row.  With the sums of layer norms or betas, or rows that begin anywhere, two pieces
     // are more than the registers hold.
-    const bool few = c.kind != TURNOPD_LAYER_NORM && !block_bwd_bias(c) && !phases.at && !phases.step && c.d % 8 == 0;
-    if (c.d > 8 * kMany || (few && c.d > 256 && c.d <= 4096))
+    // Nor are they for few rows, where each row's time counts (512 x 4,096: 18 us with two pieces, 16.6 with one).
+    const bool two = c.kind != TURNOPD_LAYER_NORM && !block_bwd_bias(c) && !phases.at && !phases.step && c.d % 8 == 0 && c.d > 256 &&
+                     c.d <= 4096 && c.T >= 8 * device_sm_count();
+    if (c.d > 8 * kMany || two)
         return launch_rows<TR, TY, 2, kFew>(c, phases, parts, taken, stream);
     return c.d <= 8 * kFew ? launch_rows<TR, TY, 1, kFew>(c, phases, parts, taken, stream)
                            : launch_rows<TR, TY, 1, kMany>(c, phases, parts, taken, stream);
