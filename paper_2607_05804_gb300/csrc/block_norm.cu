@@ -224,37 +224,35 @@ __global__ void __launch_bounds__(kThreads) k_block_params(BlockGradCall c, cons
         part[k * c.d + j] = s[k];
 }
 
-// The parameters' gradients from n rows of partial sums: 32 columns to a block, the rows shared by its eight warps.
-__global__ void __launch_bounds__(256) k_block_bwd_sum(BlockGradCall c, int n, bool bias)
+// The parameters' gradients from n rows of partial sums: 32 columns to a block, the rows shared by its 32 warps (152 rows of
+// 4 x 5,120: 10 us with eight).
+__global__ void __launch_bounds__(1024) k_block_bwd_sum(BlockGradCall c, int n, bool bias)
 {
-    __shared__ float part[4][8][32];
+    __shared__ float part[4][32][33];
     pdl_begin();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int64_t j = (int64_t)blockIdx.x * 32 + lane;
-    float s[4] = {0.f, 0.f, 0.f, 0.f};
-    if (j < c.d) {
+    const int64_t first = (int64_t)blockIdx.x * 32;
+    {
+        const float *p = static_cast<const float *>(c.workspace) + min(first + lane, c.d - 1);
+        float s[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
-        for (int k = warp; k < n; k += 8) {
-            const float *p = static_cast<const float *>(c.workspace) + (int64_t)k * 4 * c.d + j;
+        for (int k = warp; k < n; k += 32)
 #pragma unroll
             for (int q = 0; q < 4; ++q)
                 if (bias || !(q & 1))
-                    s[q] += p[q * c.d];
-        }
+                    s[q] += p[((int64_t)k * 4 + q) * c.d];
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+            part[q][warp][lane] = s[q];
     }
+    __syncthreads();
+    const int64_t j = first + warp;  // a column to each warp
+    float s[4];
 #pragma unroll
     for (int q = 0; q < 4; ++q)
-        part[q][warp][lane] = s[q];
-    __syncthreads();
-    if (warp || j >= c.d)
+        s[q] = warp_sum_f(part[q][lane][warp]);
+    if (lane || j >= c.d)
         return;
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-        s[q] = part[q][0][lane];
-#pragma unroll
-        for (int w = 1; w < 8; ++w)
-            s[q] += part[q][w][lane];
-    }
     if (c.dgamma_pre)
         c.dgamma_pre[j] = s[0];
     if (c.dbeta_pre)
@@ -331,7 +329,7 @@ cudaError_t launch_block_bwd(const BlockGradCall &c, cudaStream_t stream)
         e = cudaGetLastError();
     }
     if (e == cudaSuccess && sums)
-        e = launch_dependent(k_block_bwd_sum, dim3((unsigned)((c.d + 31) / 32)), dim3(256), 0, stream, c, parts, bias);
+        e = launch_dependent(k_block_bwd_sum, dim3((unsigned)((c.d + 31) / 32)), dim3(1024), 0, stream, c, parts, bias);
     return e;
 }
 
