@@ -680,19 +680,16 @@ template <typename TR, typename TY, int kPieces, int MOST> cudaError_t launch_ro
     };
     const std::integral_constant<Stored, kGradientTypes> gradient_types;
     const std::integral_constant<Stored, kAny> any;
-    if (common && !ends) {
-        if (stored)
-            return with_general(gradient_types, std::false_type(), std::true_type());
-        if (c.resid_dtype == c.y_dtype && c.y_dtype == TURNOPD_E4M3)
-            return with_general(std::integral_constant<Stored, kE4m3>(), std::false_type(), std::true_type());
-        if (c.resid_dtype == c.y_dtype && c.y_dtype == TURNOPD_INT8)
-            return with_general(std::integral_constant<Stored, kInt8>(), std::false_type(), std::true_type());
-    }
-    if (ends)
-        return stored ? with_general(gradient_types, std::true_type(), std::false_type())
-                      : with_general(any, std::true_type(), std::false_type());
-    return stored ? with_general(gradient_types, std::false_type(), std::false_type())
-                  : with_general(any, std::false_type(), std::false_type());
+    const auto with_ends = [&](auto stored_as, auto is_common) {
+        return ends ? with_general(stored_as, std::true_type(), is_common) : with_general(stored_as, std::false_type(), is_common);
+    };
+    if (common && stored)
+        return with_ends(gradient_types, std::true_type());
+    if (common && c.resid_dtype == c.y_dtype && c.y_dtype == TURNOPD_E4M3)
+        return with_ends(std::integral_constant<Stored, kE4m3>(), std::true_type());
+    if (common && c.resid_dtype == c.y_dtype && c.y_dtype == TURNOPD_INT8)
+        return with_ends(std::integral_constant<Stored, kInt8>(), std::true_type());
+    return stored ? with_ends(gradient_types, std::false_type()) : with_ends(any, std::false_type());
 }
 
 }  // namespace
