@@ -37,8 +37,10 @@ __device__ __forceinline__ float2 block_sum2(float2 v, float2 *red)
 
 // ---------------------------------------------------------------- rows of any length, column by column
 
-// A block to a row, whose columns are computed anew for each of its four passes; each thread comes back to its own columns,
-// so r' may be written over r.
+// For rows of more than 8,192 columns, and arrays whose rows begin at different elements of a group of eight: a block to a row,
+// whose columns are computed anew for each of its four passes; each thread comes back to its own columns, so r' may be
+// written over r.  Bound: instruction issue (every element asks for its arrays' types); 4,096 x 12,288 bf16 540 us, the
+// backward pass 1,815 (0.11 and 0.05 of the copy rate).
 __global__ void __launch_bounds__(kThreads) k_block_fwd_long(BlockCall c)
 {
     __shared__ float2 red[kThreads / 32];

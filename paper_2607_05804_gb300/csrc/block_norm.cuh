@@ -49,8 +49,7 @@ template <int N> __device__ __forceinline__ Numbers<N> gather_sums(float v)
 }
 
 // Sums over the `warps` warps of a group, the same values in every thread; red: an entry per warp of the block, free again
-// two sums later.  The warps' sums are added up like the lanes': a lane reads one of them each (a thread that reads all
-// takes 60 instructions for ten warps, this 20).
+// two sums later.  The warps' sums are added up like the lanes': a lane reads one of them each.
 template <int N> __device__ __forceinline__ Numbers<N> group_sum(Numbers<N> x, Numbers<N> *red, int group, int warps)
 {
     float v = spread_sum(x);

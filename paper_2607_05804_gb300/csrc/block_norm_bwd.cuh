@@ -90,18 +90,24 @@ __device__ __forceinline__ float column_value(uint32_t raw, int dtype, uint32_t 
     return (dtype == TURNOPD_E4M3 ? decode_e4m3((uint8_t)raw) : (float)(int8_t)raw) * act_scale(exponent);
 }
 
-// One piece of eight columns to a thread, two in longer rows, whose sums over rows it keeps in registers from row to row.  Group b of all takes
-// rows b, b + groups, ..., so that every sum has a fixed order.  A row's arrays come through a ring in shared memory, in
+// One or two pieces of eight columns to a thread, which keeps their sums over rows in registers from row to row.  Group b of all
+// takes rows b, b + groups, ..., so that every sum has a fixed order.  A row's arrays come through a ring in shared memory, in
 // which each thread copies and reads its own pieces only.  The sums over the next row that D needs are taken together with
 // those over the row at hand that dy needs: one barrier to a row.  gamma lies in shared memory, and values are read from
 // the ring once more where they are needed again: a thread's registers would not hold them.  A warp's pieces lie 256
 // columns apart, so that they are found at constant offsets.
 //
+// Bound: instruction issue and its latencies beside HBM (ncu, 8,192 rows: 0.58 of the issue slots with 15 to 20 warps per SM).
+// An element takes four arrays' unpacking, partly twice, 14 multiply-adds and a share of the row's sums, 40 to 52 instructions.
+// 32,768 x 4,096 bf16 284 us with both norms (0.84 of the copy rate), 16,384 x 5,120 190 with a gate per channel (0.78), fp32
+// stream 389 and 265 (0.91, 0.84), layer norms 345 and 271 (0.69, 0.55), from 8-bit codes 275 (0.72).  Rows that begin
+// anywhere, 16,384 x 3,001: 177, where 3,000 columns take 133.
+//
 // ENDS: the rows begin anywhere, but in all arrays at the same element of a group of eight.  The groups' number is a multiple
 // of eight then, so all rows of one group begin at the same element, and a thread keeps the same columns from row to row:
 // pieces of eight from the first boundary on, and the first threads one of the elements before and after them each.
 // GENERAL: layer norms, or sums for betas; without it the means of g and those sums are left out.
-// COMMON: dh and dr' come in, dr and dy go out, no gate for every element.
+// COMMON: dh and dr' come in, dr and dy go out, no gate for every element, so that nothing asks which there are.
 template <typename TR, typename TY, int kPieces, int MOST, Stored STORED, bool ENDS, bool GENERAL, bool COMMON>
 __global__ void __launch_bounds__(MOST, 1) k_block_bwd(BlockGradCall c, Ring ring, int n, int phase, int phase_step)
 {
@@ -158,8 +164,7 @@ __global__ void __launch_bounds__(MOST, 1) k_block_bwd(BlockGradCall c, Ring rin
                     return;
                 const char *from = p.p + (uint64_t)ahead * p.pitch;
                 if (bytes == 1 && ring.blocks) {
-                    // a warp's codes together, sixteen at a time: half as many copies, and eight bytes each take longer than
-                    // sixteen (32,768 x 4,096: 500 us so)
+                    // a warp's codes together, sixteen at a time: half as many copies
                     const int lane = t & 31;
                     if (lane < 16 * kPieces)
                         cp16(to + p.at + (t >> 5) * kPieces * 256 + lane * 16,
@@ -712,9 +717,9 @@ template <typename TR, typename TY> cudaError_t launch_block_rows_bwd(const Bloc
         return cudaSuccess;
     // Two pieces to a thread and two blocks per SM up to 4,096 columns (from 8-bit activations, 32,768 x 4,096: 277 us, one piece
     // and one block 352); then one piece, whose blocks have twice the warps (16,384 x 5,120 bf16: 192 us, two pieces 203), as
-    // long as a block's threads hold the row.  With the sums of layer norms or betas, or rows that begin anywhere, two pieces
-    // are more than the registers hold.
-    // Nor are they for few rows, where each row's time counts (512 x 4,096: 18 us with two pieces, 16.6 with one).
+    // long as a block's threads hold the row.  With the sums of layer norms or betas (32,768 x 4,096: two pieces 742 us, one 345),
+    // or in rows that begin anywhere (16,384 x 3,001: 452 and 226), two pieces are more than the registers hold.  For few rows
+    // one piece answers sooner (512 x 4,096: 18 us with two, 16.6 with one).
     const bool two = c.kind != TURNOPD_LAYER_NORM && !block_bwd_bias(c) && !phases.at && !phases.step && c.d % 8 == 0 && c.d > 256 &&
                      c.d <= 4096 && c.T >= 8 * device_sm_count();
     if (c.d > 8 * kMany || two)

@@ -88,6 +88,10 @@ template <int N> __device__ __forceinline__ void vector_columns(const BlockCall 
 // With several pieces the vectors lie in shared memory: the halves of the pieces in a plane each, so that neighbouring
 // threads' lie next to each other.  With one piece, for few rows, a thread keeps its columns of them in registers.
 //
+// Bound: HBM.  32,768 x 4,096 bf16 with both norms and a gate per channel 171 us (6,270 GB/s, 0.92 of the copy rate), with an
+// fp32 stream 269 (0.88), layer norms 205 (0.77: two more sums and two more vectors to a row), a gate for every element 221
+// (0.90); 16,384 x 8,192 167 (0.95); 32,768 x 1,001 60 (0.65); one row of 4,096 3.0 on the device.
+//
 // ENDS: the rows begin anywhere, but in all arrays at the same element of a group of eight: pieces from the row's first
 // boundary on, and the first threads one of the elements before and after them each.  The groups' number is a multiple of
 // eight, so that all rows of one group begin at the same element.  The vectors lie in eight planes of every eighth column then.

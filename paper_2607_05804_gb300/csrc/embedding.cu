@@ -21,7 +21,9 @@ constexpr int kFwdWarps = 4;
 constexpr int kPieces = 4;                  // pieces of eight columns that a lane has in flight
 constexpr int kFwdChunk = 256 * kPieces;    // columns that a warp copies at once
 
-// VEC: rows of both arrays begin on 16-byte boundaries.
+// A warp copies a row, or 1,024 columns of it, four pieces of a lane in flight.  VEC: rows of both arrays begin on 16-byte
+// boundaries.  Bound: HBM.  32,768 x 5,120 bf16 of 14,100 distinct rows 77 us on the device (480 MB, 6,200 GB/s); 64 rows of
+// 4,096 2.0; 32,768 x 1,001, off boundaries, 30 (0.44 of the copy rate).
 template <typename TW, typename TO, bool VEC> __global__ void __launch_bounds__(32 * kFwdWarps) k_embed(EmbedCall c)
 {
     const int lane = threadIdx.x & 31;
@@ -127,6 +129,9 @@ template <typename TW> __device__ __forceinline__ void zero_rows(const EmbedGrad
 // The last pass leaves the list in buffer (passes & 1).  Meanwhile the other clusters write zeros into the first rows_zeroed
 // rows of the table; those of them that occur are written over by the sums, which costs less than to wait for the list.
 // present: a bit for each id that occurs from row rows_zeroed on.
+//
+// Bound: latency, a chain of some six round trips to the L2 cache or to the cluster's shared memory for each of two digits.
+// 256 tokens 10 us under ncu, 8,192 15, 32,768 22 (eight CTAs 29), 131,072 43.
 __global__ void __launch_bounds__(kSortThreads) k_sort_tokens(EmbedGradCall c, SortBuffers b, int passes, int bits, uint32_t ctas,
                                                               int64_t rows_zeroed, uint32_t *present)
 {
@@ -327,6 +332,8 @@ constexpr int kZeroRows = 64;  // of a CTA that writes zeros
 // in which each thread copies and reads its own columns (bf16 rows that begin at odd elements: a row ahead, in registers).
 // Every so many CTAs one writes zeros instead, into the rows from rows_zeroed on that do not occur, 64 of them: the sums wait
 // for their rows while the zeros go out.
+//
+// Bound: HBM.  151,936 x 4,096 bf16 from 32,768 tokens, the rest of the zeros among them, 228 us (1.33 GB, 5,850 GB/s).
 template <typename TG, typename TW, bool VEC>
 __global__ void __launch_bounds__(kSumThreads) k_embed_sums(EmbedGradCall c, const uint2 *__restrict__ list, int tile, int slices, float *partial,
                                                             int64_t ldp, int64_t rows_zeroed, const uint32_t *__restrict__ present,
@@ -472,7 +479,7 @@ __global__ void __launch_bounds__(kSumThreads) k_embed_sums(EmbedGradCall c, con
 
 // Runs over more than two tiles: the partial sums of the tile they began in and of those they go on in.  32 threads take 256
 // columns, the block's eight warps share the tiles of a run, and their sums are added up in order.  A row of blocks looks at
-// 1,024 tiles.
+// 1,024 tiles.  Bound: latency (10 us for 512 tiles of 4,096 columns: the list of runs, then few rows each).
 template <typename TW>
 __global__ void __launch_bounds__(256) k_embed_join(EmbedGradCall c, const uint2 *__restrict__ list, int tile, int tiles,
                                                     int slices, const float *__restrict__ partial, int64_t ldp)
