@@ -292,6 +292,30 @@ def test_backward_from_8_bits(T, d, pad, code):
     c.check_backward(c.backward(kr, ky, stats), kr, ky, stats)
 
 
+@pytest.mark.parametrize("code", [E4M3, INT8])
+@pytest.mark.parametrize("T,d,pad", [(1300, 512, 0), (1300, 1000, 0), (1300, 2048, 16), (1300, 4096, 0), (300, 1001, 0), (1300, 1000, 3),
+                                     (20, 4608, 0), (20, 6144, 0), (20, 6144, 3), (5, 8192, 0), (40, 16, 0), (40, 40, 8)])
+def test_backward_from_8_bits_without_betas(T, d, pad, code):
+    """The kernels for root-mean-square norms, by rows and width; types of stream and block that differ."""
+    for layout, gate in (((BF, BF, BF, pad, 0), "none"), ((F, BF, F, pad, 0), "channel")):
+        c = case(T, d, layout, gate=gate, kind=RMS, masked=0.2)
+        resid, _, stats, _ = c.forward()
+        kr, ky = c.kept(resid, code), c.kept(c.y, code)
+        c.check_backward(c.backward(kr, ky, stats), kr, ky, stats)
+        o = c.backward(resid, ky, stats)
+        c.check_backward(o, resid, ky, stats)
+
+
+@pytest.mark.parametrize("d", [6000, 7168, 8192])
+def test_wide_rows_of_four_bytes(d):
+    """Rows of which two do not fit in shared memory with everything: y and the gate are read beside it."""
+    for gate, kind in (("token", LAYER), ("none", RMS), ("token", RMS)):
+        c = case(310, d, (F, F, BF, 0, 0), gate=gate, kind=kind, masked=0.2)
+        out = c.forward()
+        c.check_forward(*out)
+        c.check_backward(c.backward(out[0], c.y, out[2]), out[0], c.y, out[2])
+
+
 @pytest.mark.parametrize("d", [96, 1001, 4096, 9000])
 def test_outputs_left_out(d):
     """Each output by itself is what it is among all others."""

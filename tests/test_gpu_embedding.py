@@ -129,6 +129,18 @@ def test_runs_that_end_at_tile_ends():
     assert torch.equal(dw, torch.zeros((120, 33), device="cuda").index_add_(0, ids.long(), dout))
 
 
+@pytest.mark.parametrize("T,d,V,pad,wdt", [(1, 520, 70_001, 0, F), (3000, 520, 70_001, 0, F), (20_000, 1001, 70_033, 0, BF),
+                                           (3000, 1000, 70_000, 3, BF), (9000, 2056, 33_001, 8, BF)])
+def test_tables_beyond_what_is_zeroed_beside_the_sort(T, d, V, pad, wdt):
+    """The rest of the zeros goes out beside the sums: absent rows only, whatever the table held."""
+    dout = torch.randint(-3, 4, (T, d), device="cuda").to(BF)
+    ids = (V ** torch.rand(T, device="cuda", dtype=torch.float64)).long().clamp(1, V).sub_(1)
+    ids = torch.randperm(V, device="cuda")[ids].int()
+    dw, st = backward(dout, ids, V, 1.0, wdt, ldw=d + pad)
+    assert st.item() == 0
+    check_backward(dw, dout, ids, V, 1.0)
+
+
 def test_gradient_masks_and_ids_out_of_range():
     T, d, V = 500, 48, 60
     dout = torch.randn((T, d), device="cuda")
