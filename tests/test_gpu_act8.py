@@ -163,3 +163,21 @@ def test_many_rows_other_stream_and_graph():
     P.turnopd_act8_store(x, None, q, exps, st)
     P.turnopd_act8_load(q, exps, out)
     assert torch.equal(got, out) and not torch.equal(got, first) and st.item() == 0
+
+
+@pytest.mark.parametrize("d", [64, 1001])
+def test_rows_far_apart(d):
+    """Offsets beyond 32 bits in values and codes."""
+    ld, T = 600_000_000, 5
+    x = strided(T, d, ld, 0, BF, 0.0)
+    x.copy_(torch.randn((T, d), device="cuda"))
+    q, exps, st = store(x, INT8, ldc=1_200_000_000)
+    q2, exps2, _ = store(x.contiguous(), INT8)
+    out = strided(T, d, ld, 0, BF, 0.0)
+    P.turnopd_act8_load(q, exps, out)
+    assert st.item() == 0 and torch.equal(q, q2) and torch.equal(exps, exps2)
+    near = torch.empty((T, d), device="cuda", dtype=BF)
+    P.turnopd_act8_load(q2, exps2, near)
+    assert torch.equal(out, near)
+    del x, q, out
+    torch.cuda.empty_cache()

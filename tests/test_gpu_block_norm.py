@@ -376,6 +376,19 @@ def test_large_means_and_constant_rows(d):
     assert st.item() == 0 and torch.equal(resid, c.beta_post.expand(12, d))
 
 
+@pytest.mark.parametrize("d", [64, 1001])
+def test_rows_far_apart(d):
+    """Offsets beyond 32 bits: the numbers of the same rows next to each other."""
+    far = Case(5, d, BF, BF, F, kind=LAYER, gate="channel", ld=600_000_000)
+    near = Case(5, d, BF, BF, F, kind=LAYER, gate="channel", ld=d if d % 8 == 0 else 1008)
+    a, b = far.forward(), near.forward()
+    assert all(torch.equal(x, y) for x, y in zip(a, b))
+    o, p = far.backward(a[0], far.y, a[2]), near.backward(b[0], near.y, b[2])
+    assert all(torch.equal(o[k], p[k]) for k in o)
+    del far, a, o
+    torch.cuda.empty_cache()
+
+
 def test_parameters_of_any_alignment():
     for pdt in (BF, F):
         a, b = (case(200, 1024, (BF, BF, pdt, 0, 0), kind=LAYER, gate="channel") for _ in range(2))

@@ -210,3 +210,19 @@ def test_gradient_against_differences():
     dw, _ = backward(c, ids, V, 2.5, F)
     got, want = (dw.double() * v.double()).sum(), (outs[0] - outs[1]) / 2
     assert abs(got - want) <= 1e-5 * (dw.double().abs() * (v.double().abs() + w.double().abs())).sum()
+
+
+@pytest.mark.parametrize("d", [64, 1001])
+def test_rows_far_apart(d):
+    """Offsets beyond 32 bits in the table, its gradient and the tokens' rows."""
+    ld, n = 600_000_000, 5
+    ids = torch.tensor([4, 0, 4, 2, 1], dtype=torch.int32, device="cuda")
+    w, out = strided(n, d, ld, 0, BF), strided(n, d, ld, 0, BF)
+    w.copy_(torch.randn((n, d), device="cuda"))
+    st = torch.zeros(1, dtype=torch.int32, device="cuda")
+    P.turnopd_embedding_fwd(w, ids, None, 1.0, out, st)
+    assert torch.equal(out, w[ids.long()])
+    dw, _ = backward(out, ids, n, 1.0, BF, dw=w)  # over the table, which is no longer needed
+    check_backward(dw, out, ids, n, 1.0)
+    del w, out, dw
+    torch.cuda.empty_cache()
