@@ -619,6 +619,9 @@ def _rows_like(t, name, shape, dtype=None):
     """Pointer and row stride of a 2-D CUDA tensor of a given shape and type (None stays None)."""
     if t is None:
         return None, shape[1]
+    # the common case first: these calls are made between any two blocks of a decoding step
+    if t.shape == shape and t.is_cuda and t.is_contiguous() and (dtype is None or t.dtype is dtype):
+        return t.data_ptr(), shape[1]
     ld = _rows_2d(t, name)
     if t.shape != shape:
         raise ValueError(f"{name} must have shape {tuple(shape)}, has {tuple(t.shape)}")
@@ -632,11 +635,13 @@ def turnopd_embedding_fwd(w, token_ids, mask, scale, out, dev_status, stream=Non
     out [T, d]; rows of masked tokens are zero."""
     import torch
 
+    if w.dim() != 2:
+        raise ValueError("w must be a 2-D CUDA tensor with unit column stride")
     T, (V, d) = token_ids.numel(), w.shape
-    ldw = _rows_2d(w, "w")
+    pw, ldw = _rows_like(w, "w", w.shape)
     po, ldo = _rows_like(out, "out", (T, d))
     code = load().turnopd_embedding_fwd(
-        w.data_ptr(), _dtype_code(w, "w"), ldw, V, _arg(token_ids, "token_ids", torch.int32, T),
+        pw, _dtype_code(w, "w"), ldw, V, _arg(token_ids, "token_ids", torch.int32, T),
         _arg(mask, "mask", torch.uint8, T), T, d, float(scale), po, _dtype_code(out, "out"), ldo,
         _arg(dev_status, "dev_status", torch.int32, 1), _handle(stream, w))
     if code:
@@ -676,10 +681,14 @@ def _param_dtype(*params):
     """The dtype of the parameters that are given, which have to share one."""
     import torch
 
-    types = {p.dtype for p in params if p is not None}
-    if len(types) > 1:
-        raise ValueError("the norms' parameters and a gate per channel must have one dtype")
-    t = types.pop() if types else torch.float32
+    t = None
+    for p in params:
+        if p is not None:
+            if t is not None and p.dtype is not t:
+                raise ValueError("the norms' parameters and a gate per channel must have one dtype")
+            t = p.dtype
+    if t is None:
+        return torch.float32
     if t is not torch.float32 and t is not torch.bfloat16:
         raise ValueError("the norms' parameters and a gate per channel must be float32 or bfloat16")
     return t
@@ -699,16 +708,17 @@ def turnopd_block_norm_fwd(resid, y, gamma_post, beta_post, gate, gamma_pre, bet
     or None."""
     import torch
 
-    ldr, ldy = _rows_2d(resid, "resid"), _rows_2d(y, "y")
-    T, d = resid.shape
-    if y.shape != resid.shape:
-        raise ValueError("y must match resid in shape")
+    if resid.dim() != 2:
+        raise ValueError("resid must be a 2-D CUDA tensor with unit column stride")
+    T, d = shape = resid.shape
+    pr, ldr = _rows_like(resid, "resid", shape)
+    py, ldy = _rows_like(y, "y", shape)
     pt = _param_dtype(gamma_post, beta_post, gamma_pre, beta_pre, gate if gate is not None and gate.dim() == 1 else None)
     pg, ldg = _gate_arg(gate, T, d, y.dtype, pt)
-    po, ldro = _rows_like(resid_out, "resid_out", resid.shape, resid.dtype)
-    ph, ldh = _rows_like(h_out, "h_out", resid.shape, y.dtype)
+    po, ldro = _rows_like(resid_out, "resid_out", shape, resid.dtype)
+    ph, ldh = _rows_like(h_out, "h_out", shape, y.dtype)
     code = load().turnopd_block_norm_fwd(
-        resid.data_ptr(), _dtype_code(resid, "resid"), ldr, y.data_ptr(), _dtype_code(y, "y"), ldy,
+        pr, _dtype_code(resid, "resid"), ldr, py, _dtype_code(y, "y"), ldy,
         _arg(gamma_post, "gamma_post", pt, d), _arg(beta_post, "beta_post", pt, d), pg, ldg,
         _arg(gamma_pre, "gamma_pre", pt, d), _arg(beta_pre, "beta_pre", pt, d), _code_of(pt),
         _arg(mask, "mask", torch.uint8, T), T, d, int(kind), float(eps), float(resid_scale), float(branch_scale), po, ldro,
