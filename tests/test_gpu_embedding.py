@@ -167,8 +167,8 @@ def test_gradient_masks_and_ids_out_of_range():
     assert torch.equal(dw, old)
 
 
-def test_same_bits_every_time_and_in_a_graph():
-    T, d, V = 6000, 520, 3001
+@pytest.mark.parametrize("T,d,V", [(700, 520, 3001), (6000, 520, 3001), (20_000, 520, 70_001)])
+def test_same_bits_every_time_and_in_a_graph(T, d, V):
     dout = torch.randn((T, d), device="cuda")
     ids = (V ** torch.rand(T, device="cuda")).long().clamp(1, V).sub_(1).int()
     first, _ = backward(dout, ids, V, 1.0, F)
