@@ -285,6 +285,11 @@ int64_t partial_rows(int64_t T, int64_t d)
 
 bool block_bwd_bias(const BlockGradCall &c) { return c.dbeta_pre || c.dbeta_post || (c.dgate && !c.ldg && c.beta_post); }
 
+bool block_bwd_general(const BlockGradCall &c)
+{
+    return c.kind == TURNOPD_LAYER_NORM || block_bwd_bias(c) || (c.dgate && c.ldg && c.beta_post);
+}
+
 bool block_bwd_needs_y(const BlockGradCall &c) { return c.gamma_post ? c.dy || c.dgamma_post || c.dgate : c.dgate != nullptr; }
 
 size_t block_bwd_workspace_bytes(int64_t T, int64_t d)

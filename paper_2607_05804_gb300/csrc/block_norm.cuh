@@ -159,6 +159,9 @@ template <typename TR, typename TY> cudaError_t launch_block_rows_fwd(const Bloc
 // workspace, 4 d floats each (dh xh_pre, dh, X xh_post, X; the second and fourth only where block_bwd_bias says).  *taken:
 // whether they take such rows.
 bool block_bwd_bias(const BlockGradCall &c);
+// whether a row needs more than the sums of g xh: the means of layer norms, the sums for betas, or beta in the gate's own
+// gradient for every element, whose kernels add it
+bool block_bwd_general(const BlockGradCall &c);
 bool block_bwd_needs_y(const BlockGradCall &c);
 template <typename TR, typename TY>
 cudaError_t launch_block_rows_bwd(const BlockGradCall &c, int *parts, bool *taken, cudaStream_t stream);

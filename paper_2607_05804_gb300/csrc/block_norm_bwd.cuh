@@ -106,7 +106,8 @@ __device__ __forceinline__ float column_value(uint32_t raw, int dtype, uint32_t 
 // ENDS: the rows begin anywhere, but in all arrays at the same element of a group of eight.  The groups' number is a multiple
 // of eight then, so all rows of one group begin at the same element, and a thread keeps the same columns from row to row:
 // pieces of eight from the first boundary on, and the first threads one of the elements before and after them each.
-// GENERAL: layer norms, or sums for betas; without it the means of g and those sums are left out.
+// GENERAL: layer norms, sums for betas, or beta in the gradient of a gate for every element; without it the means of g, those
+// sums and that beta are left out.
 // COMMON: dh and dr' come in, dr and dy go out, no gate for every element, so that nothing asks which there are.
 template <typename TR, typename TY, int kPieces, int MOST, Stored STORED, bool ENDS, bool GENERAL, bool COMMON>
 __global__ void __launch_bounds__(MOST, 1) k_block_bwd(BlockGradCall c, Ring ring, int n, int phase, int phase_step)
@@ -669,7 +670,7 @@ template <typename TR, typename TY, int kPieces, int MOST> cudaError_t launch_ro
     if (ends)
         grid = std::min((grid * per + 7) / 8 * 8 / per, kBlockMaxParts);  // a multiple of eight groups
     *parts = grid;
-    const bool general = c.kind == TURNOPD_LAYER_NORM || block_bwd_bias(c);
+    const bool general = block_bwd_general(c);
     const bool common = c.gamma_pre && c.d_resid_out && c.d_resid && c.dy && sums && !token_gate && !ring.y.direct;
     const auto go = [&](auto kernel) {
         const cudaError_t e = allow_shared(kernel, kRoom);
@@ -720,7 +721,7 @@ template <typename TR, typename TY> cudaError_t launch_block_rows_bwd(const Bloc
     // long as a block's threads hold the row.  With the sums of layer norms or betas (32,768 x 4,096: two pieces 742 us, one 345),
     // or in rows that begin anywhere (16,384 x 3,001: 452 and 226), two pieces are more than the registers hold.  For few rows
     // one piece answers sooner (512 x 4,096: 18 us with two, 16.6 with one).
-    const bool two = c.kind != TURNOPD_LAYER_NORM && !block_bwd_bias(c) && !phases.at && !phases.step && c.d % 8 == 0 && c.d > 256 &&
+    const bool two = !block_bwd_general(c) && !phases.at && !phases.step && c.d % 8 == 0 && c.d > 256 &&
                      c.d <= 4096 && c.T >= 8 * device_sm_count();
     if (c.d > 8 * kMany || two)
         return launch_rows<TR, TY, 2, kFew>(c, phases, parts, taken, stream);

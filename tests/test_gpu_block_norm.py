@@ -470,3 +470,21 @@ def test_gradients_against_autograd_and_differences(kind, gate):
         setattr(c, n, own[n])
         got, want = float((o[back[n]].double() * v.double()).sum()), float((losses[0] - losses[1]) / (2 * eps))
         assert abs(got - want) <= 0.02 * float((o[back[n]].double() ** 2).sum().sqrt()), n
+
+
+@pytest.mark.parametrize("gate", ["channel", "token"])
+@pytest.mark.parametrize("d,pad", [(16, 0), (96, 0), (1001, 0), (1000, 3), (4096, 0), (5120, 0), (6144, 0), (9000, 0)])
+def test_betas_without_their_gradients(d, pad, gate):
+    """Root-mean-square norms with betas whose own gradients are not asked for: beta is in the gate's gradient all the same,
+    with all other outputs and by itself, in rows that begin alike and in rows that do not."""
+    for T, layout in ((130, (BF, BF, F, pad, 0)), (130, (F, F, BF, pad, 0)), (1300, (BF, BF, BF, pad, 0))):
+        c = case(T, d, layout, gate=gate, kind=RMS, beta=True, masked=0.2, s=0.5)
+        resid, _, stats, _ = c.forward()
+        frozen = ("dbeta_post", "dbeta_pre")
+        alike = c.y
+        for y in (alike, strided(T, d, c.ld + 5, 1, c.ydt).copy_(alike)):
+            c.y = y
+            o = c.backward(resid, y, stats, skip=frozen)
+            c.check_backward(o, resid, y, stats)
+            alone = c.backward(resid, y, stats, skip=[k for k in o if k != "dgate"])
+            c.check_backward(alone, resid, y, stats)
