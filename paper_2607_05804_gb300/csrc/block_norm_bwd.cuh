@@ -92,7 +92,7 @@ __device__ __forceinline__ float column_value(uint32_t raw, int dtype, uint32_t 
 
 // One or two pieces of eight columns to a thread, which keeps their sums over rows in registers from row to row.  Group b of all
 // takes rows b, b + groups, ..., so that every sum has a fixed order.  A row's arrays come through a ring in shared memory, in
-// which each thread copies and reads its own pieces only.  The sums over the next row that D needs are taken together with
+// which each thread copies and reads its own pieces only (of codes in whole blocks each warp).  The sums over the next row that D needs are taken together with
 // those over the row at hand that dy needs: one barrier to a row.  gamma lies in shared memory, and values are read from
 // the ring once more where they are needed again: a thread's registers would not hold them.  A warp's pieces lie 256
 // columns apart, so that they are found at constant offsets.
@@ -393,6 +393,9 @@ __global__ void __launch_bounds__(MOST, 1) k_block_bwd(BlockGradCall c, Ring rin
         odd ^= 1;
     }
     for (uint32_t i = b; i < T; i += groups) {
+        // the warp's codes of the last row, which any of its lanes may have read until now, lie in the stage that is filled next
+        if (!ENDS && (kMixed || kCodes))
+            __syncwarp();
         copy();
         Row after = read_row(i + 2 * groups);
         const char *at = own + stage * ring.stage;

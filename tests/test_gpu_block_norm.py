@@ -488,3 +488,17 @@ def test_betas_without_their_gradients(d, pad, gate):
             c.check_backward(o, resid, y, stats)
             alone = c.backward(resid, y, stats, skip=[k for k in o if k != "dgate"])
             c.check_backward(alone, resid, y, stats)
+
+
+@pytest.mark.parametrize("code", [E4M3, INT8])
+@pytest.mark.parametrize("T,d,kind", [(3000, 512, RMS), (3000, 4096, RMS), (1500, 5120, RMS), (3000, 2048, LAYER), (1500, 6144, LAYER)])
+def test_backward_from_8_bits_same_bits_every_time(T, d, kind, code):
+    """Codes that a warp copies together, over many rows to a group: each is read before the next row's come into its place."""
+    c = case(T, d, (BF, BF, BF, 0, 0), gate="channel", kind=kind, masked=0.1)
+    resid, _, stats, _ = c.forward()
+    kr, ky = c.kept(resid, code), c.kept(c.y, code)
+    first = c.backward(kr, ky, stats)
+    c.check_backward(first, kr, ky, stats)
+    for _ in range(10):
+        again = c.backward(kr, ky, stats)
+        assert all(torch.equal(first[k], again[k]) for k in first)
