@@ -3,8 +3,13 @@ between the blocks their norms, gates and residual connections.  With policy.Pol
 
 Everything outside of the blocks runs in libturnopd's kernels.  A block is any callable [T, d] -> [T, d]; it runs without a
 record in the forward pass and once more, from the input that was kept, in the backward pass, where autograd gives its
-gradients; it may not write into its input.  What is kept in between -- each block's input and output and the residual stream after it -- can be kept in 8
-bits (turnopd_act8_store): 1.03 bytes an element instead of two or four, at the price of the codes' rounding in the gradients.
+gradients.  It may not write into its input, nor into an output that it gave before.  What it draws from torch's default
+generators it draws again the second time (a forward pass captured into a CUDA graph cannot keep their states: backward refuses
+blocks that draw then); on anything else that changes between its two runs -- a generator of its own, running statistics -- its
+result may not depend.
+
+What is kept in between -- each block's input and output and the residual stream after it -- can be kept in 8 bits
+(turnopd_act8_store): 1.03 bytes an element instead of two or four, at the price of the codes' rounding in the gradients.
 """
 from __future__ import annotations
 
@@ -18,6 +23,40 @@ from . import (TURNOPD_ACCUMULATE_GRAD, TURNOPD_RMS_NORM, turnopd_act8_load, tur
                turnopd_embedding_bwd_workspace_bytes, turnopd_embedding_fwd, turnopd_norm_fwd)
 
 CODES = {"e4m3": torch.float8_e4m3fn, "int8": torch.int8}
+
+
+class _Generators:
+    """The states of torch's default generators, on the host and on one device, when it was made.  As a context: them again,
+    and afterwards those that it found."""
+
+    def __init__(self, device):
+        self.device, self.states = device, (torch.get_rng_state(), torch.cuda.get_rng_state(device))
+
+    def _set(self, states):
+        torch.set_rng_state(states[0])
+        torch.cuda.set_rng_state(states[1], self.device)
+
+    def __enter__(self):
+        self.found = _Generators(self.device).states
+        self._set(self.states)
+
+    def __exit__(self, *_):
+        self._set(self.found)
+
+
+class _NoDraws:
+    """A context that draws nothing from torch's default generators, or raises."""
+
+    def __init__(self, device):
+        self.device = device
+
+    def __enter__(self):
+        self.found = _Generators(self.device).states
+
+    def __exit__(self, error, *_):
+        if error is None and not all(map(torch.equal, self.found, _Generators(self.device).states)):
+            raise RuntimeError("PolicyTrunk.backward: a block draws random numbers, and its forward pass was captured into a CUDA "
+                               "graph, which kept no generator's state to draw them again")
 
 
 @dataclass
@@ -82,6 +121,8 @@ class PolicyTrunk:
         saved = [dict(r=self._put_away(r), stats=stats)] if save else None
         for k, block in enumerate(self.blocks):
             n, after = self.norms[k], self.norms[k + 1] if k + 1 < len(self.blocks) else None
+            if save:
+                drawn = _NoDraws(dev) if torch.cuda.is_current_stream_capturing() else _Generators(dev)
             y = block(h)
             r_next, stats = torch.empty_like(r), torch.empty((T, 4), **f32)
             h_next = torch.empty_like(h) if after else None
@@ -91,7 +132,7 @@ class PolicyTrunk:
             if save:
                 needs_y = n.gamma_post is not None or n.gate is not None
                 saved.append(dict(h=self._put_away(h), y=self._put_away(y) if needs_y else None,
-                                  r=self._put_away(r_next) if after else None, stats=stats))
+                                  r=self._put_away(r_next) if after else None, stats=stats, drawn=drawn))
             r, h = r_next, h_next
         self.saved = saved
         return r
@@ -123,7 +164,7 @@ class PolicyTrunk:
             if after:
                 norm_grads[k + 1].update(pre)
             h = self._take_back(s["h"], bt).detach().requires_grad_()
-            with torch.enable_grad():
+            with torch.enable_grad(), s["drawn"]:
                 y = self.blocks[k](h)
             dh, *block_grads[k] = torch.autograd.grad(y, [h, *self.params[k]], dy, allow_unused=True)
             dh = torch.zeros_like(h) if dh is None else dh.contiguous()

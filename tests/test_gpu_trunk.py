@@ -157,3 +157,70 @@ def test_what_does_not_fit():
         PolicyTrunk(t, [], [])
     with pytest.raises(ValueError):
         PolicyTrunk(t, [lambda h: h], [BlockNorms(t[0])], keep="fp4")
+
+
+class Drawing:
+    """A block that draws from torch's generators, on the device and on the host, or has its draws given."""
+
+    def __init__(self, block, given=None):
+        self.w1, self.w2, self.given, self.drawn = block.w1, block.w2, given, []
+
+    def __call__(self, h):
+        m, a = self.given if self.given else (2.0 * (torch.rand(h.shape, device=h.device) < 0.5), torch.rand(()))
+        self.drawn.append((m, a))
+        return torch.tanh((h * m) @ self.w1) @ self.w2 * float(a)
+
+
+def test_blocks_that_draw_random_numbers():
+    """The backward pass draws what the forward pass drew, whatever was drawn in between, and leaves the generators alone.  The
+    same kernels run on the same numbers as with the draws given, up to the order of a product's sums."""
+    kind, d, V = RMS, 200, 300
+    b, T, table, ids, blocks, norms, params, _, rand = make(kind, d, V, torch.float32)
+    drawing = [Drawing(blk) for blk in blocks]
+    g = rand(T, d)
+    trunk = PolicyTrunk(table, drawing, norms, params, kind=kind)
+    x = trunk.forward(ids)
+    torch.rand(7, device="cuda"), torch.rand(3)
+    states = torch.get_rng_state(), torch.cuda.get_rng_state()
+    out = trunk.backward(g.clone())
+    assert torch.equal(torch.get_rng_state(), states[0]) and torch.equal(torch.cuda.get_rng_state(), states[1])
+    for blk in drawing:
+        (m, a), (m2, a2) = blk.drawn
+        assert torch.equal(m, m2) and torch.equal(a, a2)
+    assert not torch.equal(drawing[0].drawn[0][0], drawing[1].drawn[0][0])
+    fixed = PolicyTrunk(table, [Drawing(blk, blk.drawn[0]) for blk in drawing], norms, params, kind=kind)
+    assert relative(fixed.forward(ids), x) < 1e-5
+    want = fixed.backward(g.clone())
+    assert relative(out["embedding"], want["embedding"]) < 1e-5
+    for k in range(2):
+        assert relative(out["norms"][k]["gamma_pre"], want["norms"][k]["gamma_pre"]) < 1e-5
+        assert all(relative(p, q) < 1e-5 for p, q in zip(out["blocks"][k], want["blocks"][k]))
+    # a forward pass that keeps nothing draws what it draws without the trunk
+    torch.manual_seed(5)
+    trunk.forward(ids, save=False)
+    torch.manual_seed(5)
+    assert torch.equal(drawing[0].drawn[-1][0], 2.0 * (torch.rand((T, d), device="cuda") < 0.5))
+
+
+def test_backward_of_a_captured_forward_pass():
+    """Blocks that repeat themselves are taken back through from the values of the last replay; blocks that draw are refused."""
+    kind, d, V = RMS, 200, 300
+    b, T, table, ids, blocks, norms, params, _, rand = make(kind, d, V, torch.float32)
+    g = rand(T, d)
+    for own, draws in ((blocks, False), ([Drawing(blk) for blk in blocks], True)):
+        trunk = PolicyTrunk(table, own, norms, params, kind=kind)
+        trunk.forward(ids, save=False)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            x = trunk.forward(ids)
+        graph.replay()
+        if draws:
+            with pytest.raises(RuntimeError, match="draws random numbers"):
+                trunk.backward(g.clone())
+            continue
+        out = trunk.backward(g.clone())
+        eager = PolicyTrunk(table, own, norms, params, kind=kind)
+        assert relative(x, eager.forward(ids)) < 1e-5
+        want = eager.backward(g.clone())
+        assert relative(out["embedding"], want["embedding"]) < 1e-5
+        assert all(relative(p, q) < 1e-5 for k in range(2) for p, q in zip(out["blocks"][k], want["blocks"][k]))
