@@ -6,13 +6,14 @@ record in the forward pass and once more, from the input that was kept, in the b
 gradients.  It may not write into its input, nor into an output that it gave before.  What it draws from torch's default
 generators it draws again the second time (a forward pass captured into a CUDA graph cannot keep their states: backward refuses
 blocks that draw then); on anything else that changes between its two runs -- a generator of its own, running statistics -- its
-result may not depend.
+result may not depend.  It runs under the autocast that is on around forward, in both runs.
 
 What is kept in between -- each block's input and output and the residual stream after it -- can be kept in 8 bits
 (turnopd_act8_store): 1.03 bytes an element instead of two or four, at the price of the codes' rounding in the gradients.
 """
 from __future__ import annotations
 
+from contextlib import nullcontext
 from dataclasses import dataclass
 from typing import Any
 
@@ -42,6 +43,19 @@ class _Generators:
 
     def __exit__(self, *_):
         self._set(self.found)
+
+
+class _Autocast:
+    """Autocast as it was when this was made.  Without its cache: what it casts of a parameter in the forward pass, where nothing
+    is recorded, would be taken for the backward pass's, and the parameter would have no gradient."""
+
+    def __init__(self):
+        self.on, self.dtype = torch.is_autocast_enabled("cuda"), torch.get_autocast_dtype("cuda")
+
+    def __call__(self):
+        if not self.on and not torch.is_autocast_enabled("cuda"):
+            return nullcontext()
+        return torch.autocast("cuda", dtype=self.dtype, enabled=self.on, cache_enabled=False)
 
 
 class _NoDraws:
@@ -118,12 +132,14 @@ class PolicyTrunk:
         n = self.norms[0]
         turnopd_norm_fwd(r, n.gamma_pre, n.beta_pre, mask, self.kind, self.eps, h, mean, rstd, self.dev_status)
         stats[:, 2], stats[:, 3] = mean, rstd
-        saved = [dict(r=self._put_away(r), stats=stats)] if save else None
+        autocast = _Autocast()
+        saved = [dict(autocast=autocast, r=self._put_away(r), stats=stats)] if save else None
         for k, block in enumerate(self.blocks):
             n, after = self.norms[k], self.norms[k + 1] if k + 1 < len(self.blocks) else None
             if save:
                 drawn = _NoDraws(dev) if torch.cuda.is_current_stream_capturing() else _Generators(dev)
-            y = block(h)
+            with autocast():
+                y = block(h)
             r_next, stats = torch.empty_like(r), torch.empty((T, 4), **f32)
             h_next = torch.empty_like(h) if after else None
             turnopd_block_norm_fwd(r, y, n.gamma_post, n.beta_post, n.gate, after.gamma_pre if after else None,
@@ -164,7 +180,7 @@ class PolicyTrunk:
             if after:
                 norm_grads[k + 1].update(pre)
             h = self._take_back(s["h"], bt).detach().requires_grad_()
-            with torch.enable_grad(), s["drawn"]:
+            with torch.enable_grad(), s["drawn"], saved[0]["autocast"]():
                 y = self.blocks[k](h)
             dh, *block_grads[k] = torch.autograd.grad(y, [h, *self.params[k]], dy, allow_unused=True)
             dh = torch.zeros_like(h) if dh is None else dh.contiguous()

@@ -224,3 +224,34 @@ def test_backward_of_a_captured_forward_pass():
         want = eager.backward(g.clone())
         assert relative(out["embedding"], want["embedding"]) < 1e-5
         assert all(relative(p, q) < 1e-5 for k in range(2) for p, q in zip(out["blocks"][k], want["blocks"][k]))
+
+
+@pytest.mark.parametrize("inside", [False, True])
+def test_blocks_under_autocast(inside):
+    """The backward pass runs a block as the forward pass ran it, called inside of the autocast context or outside of it."""
+    kind, d, V = RMS, 200, 300
+    b, T, table, ids, blocks, norms, params, _, rand = make(kind, d, V, torch.float32)
+    seen = []
+
+    def cast(blk):
+        def run(h):
+            y = torch.tanh(h @ blk.w1) @ blk.w2
+            seen.append(y.dtype)
+            return y.float()
+        return run
+
+    trunk = PolicyTrunk(table, [cast(blk) for blk in blocks], norms, params, kind=kind)
+    g = rand(T, d)
+    with torch.autocast("cuda", dtype=torch.bfloat16):
+        trunk.forward(ids)
+        out = trunk.backward(g.clone()) if inside else None
+    out = out or trunk.backward(g.clone())
+    assert seen == [torch.bfloat16] * 4
+    assert all(p is not None and p.dtype is torch.float32 and bool(p.any()) for k in range(2) for p in out["blocks"][k])
+    # and the other way round
+    seen.clear()
+    trunk.forward(ids)
+    with torch.autocast("cuda", dtype=torch.bfloat16):
+        trunk.backward(g.clone())
+        assert torch.is_autocast_enabled() and torch.is_autocast_cache_enabled()
+    assert seen == [torch.float32] * 4
