@@ -89,7 +89,7 @@ class PolicyTrunk:
     residual stream after the last block (padding tokens: mask 0, zero rows), and keeps what backward(dx) needs; with
     save=False (a decoding step, say) it keeps nothing.  backward gives a dict: "embedding" (or, with dhead, the tied head's
     gradient, to which it is added), "norms" (a dict for each block) and "blocks" (for each block the gradients of the
-    tensors in `params[l]`, in order)."""
+    tensors in `params[l]`, in order, None where its output does not depend on one)."""
 
     def __init__(self, embedding, blocks, norms, params=None, *, kind=TURNOPD_RMS_NORM, eps=1e-6, scale=1.0, resid_scale=1.0,
                  branch_scale=1.0, resid_dtype=None, keep=None):
@@ -182,7 +182,9 @@ class PolicyTrunk:
             h = self._take_back(s["h"], bt).detach().requires_grad_()
             with torch.enable_grad(), s["drawn"], saved[0]["autocast"]():
                 y = self.blocks[k](h)
-            dh, *block_grads[k] = torch.autograd.grad(y, [h, *self.params[k]], dy, allow_unused=True)
+            leaves = [h, *self.params[k]]
+            dh, *block_grads[k] = (torch.autograd.grad(y, leaves, dy, allow_unused=True) if y.requires_grad
+                                   else [None] * len(leaves))  # its output depends on none of them
             dh = torch.zeros_like(h) if dh is None else dh.contiguous()
             saved[k + 1] = None
         n, s = self.norms[0], saved[0]

@@ -255,3 +255,17 @@ def test_blocks_under_autocast(inside):
         trunk.backward(g.clone())
         assert torch.is_autocast_enabled() and torch.is_autocast_cache_enabled()
     assert seen == [torch.float32] * 4
+
+
+def test_a_block_whose_output_depends_on_nothing():
+    """What comes back goes on through the residual stream alone; the parameters of such a block have no gradient."""
+    kind, d, V = RMS, 200, 300
+    b, T, table, ids, _, norms, params, _, rand = make(kind, d, V, torch.float32)
+    dx = rand(T, d)
+    trunk = PolicyTrunk(table, [torch.ones_like] * 2, norms, params, kind=kind, scale=2.0, resid_scale=0.5)
+    trunk.forward(ids)
+    out = trunk.backward(dx.clone())
+    assert trunk.status() == 0 and out["blocks"] == [[None, None], [None, None]]
+    want = torch.zeros((V, d), dtype=torch.float64, device="cuda").index_add_(0, ids.long(), dx.double()) * 0.5
+    assert relative(out["embedding"], want) < 1e-5
+    assert not out["norms"][0]["gamma_pre"].any() and out["norms"][0]["gate"].any()
