@@ -76,7 +76,8 @@ class _NoDraws:
 @dataclass
 class BlockNorms:
     """The vectors [d] around one block: the norm in front of it, and behind it a norm (gamma_post may be None) and a gate
-    (None for none) of what it adds to the residual stream."""
+    (None for none) of what it adds to the residual stream.  A gate may also have a value for every element of a batch, [T, d] in
+    the embedding's type; its gradient has that shape and type then."""
     gamma_pre: torch.Tensor
     beta_pre: Any = None
     gamma_post: Any = None
@@ -170,7 +171,8 @@ class PolicyTrunk:
         for k in reversed(range(len(self.blocks))):
             n, s, after = self.norms[k], saved[k + 1], self.norms[k + 1] if dh is not None else None
             dy = torch.empty((T, d), dtype=bt, device=dev)
-            g = dict(gate=vector(n.gate), gamma_post=vector(n.gamma_post), beta_post=vector(n.beta_post))
+            gate = torch.empty((T, d), dtype=bt, device=dev) if n.gate is not None and n.gate.dim() == 2 else vector(n.gate)
+            g = dict(gate=gate, gamma_post=vector(n.gamma_post), beta_post=vector(n.beta_post))
             pre = dict(gamma_pre=vector(after.gamma_pre), beta_pre=vector(after.beta_pre)) if after else dict(gamma_pre=None, beta_pre=None)
             with torch.no_grad():
                 turnopd_block_norm_bwd(s["r"], s["y"], n.gamma_post, n.beta_post, n.gate, after.gamma_pre if after else None,

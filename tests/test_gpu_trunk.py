@@ -269,3 +269,40 @@ def test_a_block_whose_output_depends_on_nothing():
     want = torch.zeros((V, d), dtype=torch.float64, device="cuda").index_add_(0, ids.long(), dx.double()) * 0.5
     assert relative(out["embedding"], want) < 1e-5
     assert not out["norms"][0]["gamma_pre"].any() and out["norms"][0]["gate"].any()
+
+
+@pytest.mark.parametrize("dtype,keep,tol", [(torch.float32, None, 1e-3), (torch.bfloat16, None, 0.04), (torch.float32, "int8", 0.1)])
+def test_a_gate_for_every_element(dtype, keep, tol):
+    """Gates [T, d], on a block with a norm behind it and on one without, with a mask: every gradient against autograd."""
+    kind, d, V = RMS, 200, 300
+    b, T, table, ids, blocks, norms, params, _, rand = make(kind, d, V, dtype)
+    mask = torch.from_numpy(b.loss_mask).cuda()
+    on = mask.bool()
+    for n in norms:
+        n.gate = torch.sigmoid(rand(T, d)).to(dtype).requires_grad_()
+    norms[0].beta_post = (0.2 * rand(d)).to(dtype).requires_grad_()
+    blocks = [lambda h, blk=blk: torch.tanh(h @ blk.w1) @ blk.w2 for blk in blocks]  # each token by itself
+    trunk = PolicyTrunk(table, blocks, norms, params, kind=kind, branch_scale=0.5, keep=keep)
+    x = trunk.forward(ids, mask)
+    g = rand(T, d).to(dtype)
+    g64 = g.double()[on]
+    out = trunk.backward(g)
+    assert trunk.status() == 0
+    leaves = {}
+    wide = lambda t: leaves.setdefault(id(t), t.detach().double().requires_grad_()) if t is not None else None  # noqa: E731
+    r = wide(table)[ids.long()][on]
+    for (w1, w2), n in zip(params, norms):
+        v = torch.tanh(norm64(r, wide(n.gamma_pre), None, kind, 1e-6) @ wide(w1)) @ wide(w2)
+        if n.gamma_post is not None:
+            v = norm64(v, wide(n.gamma_post), wide(n.beta_post), kind, 1e-6)
+        r = r + 0.5 * wide(n.gate)[on] * v
+    assert relative(x[on], r.detach()) < (0.02 if dtype is torch.bfloat16 else 1e-4)
+    (g64 * r).sum().backward()
+    assert relative(out["embedding"], leaves[id(table)].grad) < tol
+    for k, n in enumerate(norms):
+        assert out["norms"][k]["gate"].shape == (T, d) and not out["norms"][k]["gate"][~on].any()
+        for name in VECTORS:
+            if getattr(n, name) is not None:
+                assert relative(out["norms"][k][name], leaves[id(getattr(n, name))].grad) < tol, (k, name)
+        for got, p in zip(out["blocks"][k], params[k]):
+            assert relative(got, leaves[id(p)].grad) < tol
