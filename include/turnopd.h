@@ -549,7 +549,8 @@ turnopd_status turnopd_embedding_fwd(const void *w, int32_t w_dtype, int64_t ldw
  *   rows of ids that do not occur are neither read nor written: a head tied to the
  *   embedding has its own gradient there already.
  * Flags: TURNOPD_ACCUMULATE_GRAD only.
- * Workspace: turnopd_embedding_bwd_workspace_bytes(num_tokens, d, vocab), 256-byte aligned.
+ * Workspace: turnopd_embedding_bwd_workspace_bytes(num_tokens, d, vocab), 256-byte aligned; that
+ *   of a larger batch will do.
  * Device errors: TURNOPD_ERR_TOKEN_RANGE (token ignored).
  * Precision: fp32 sums in a fixed order.
  */

@@ -275,7 +275,8 @@ __global__ void __launch_bounds__(kSortThreads) k_sort_tokens(EmbedGradCall c, S
 // ---------------------------------------------------------------- sums
 
 constexpr int kSumThreads = 256;
-constexpr int kMaxTile = 512;   // positions
+constexpr int kMinTile = 8, kMaxTile = 512;  // positions
+constexpr int kBusyWarps = 8192;             // that keep the device's memory busy
 constexpr int kListed = 1024;  // tiles that a block of the last kernel looks at together
 
 // Eight columns of a thread: consecutive ones (VEC), or `step` apart.
@@ -568,15 +569,24 @@ __global__ void __launch_bounds__(256) k_embed_join(EmbedGradCall c, const uint2
 int sum_threads(int64_t d) { return (int)std::min<int64_t>(kSumThreads, (d + 255) / 256 * 32); }
 int sum_slices(int64_t d) { return (int)((d + 8 * sum_threads(d) - 1) / (8 * sum_threads(d))); }
 
-// Positions of a tile: as many as leave 8,192 warps, which keep the device's memory busy; each run that passes two tiles'
-// ends costs partial sums (32,768 x 4,096: 64 positions).
+int64_t tile_warps(int64_t d) { return (int64_t)sum_slices(d) * (sum_threads(d) / 32); }
+
+// Positions of a tile: as many as leave 8,192 warps; each run that passes two tiles' ends costs partial sums
+// (32,768 x 4,096: 64 positions).
 int tile_size(int64_t T, int64_t d)
 {
-    const int64_t warps = (int64_t)sum_slices(d) * (sum_threads(d) / 32);
-    int n = 8;
-    while (n < kMaxTile && (T + 2 * n - 1) / (2 * n) * warps >= 8192)
+    int n = kMinTile;
+    while (n < kMaxTile && (T + 2 * n - 1) / (2 * n) * tile_warps(d) >= kBusyWarps)
         n *= 2;
     return n;
+}
+
+// Tiles of T tokens, or of any fewer, at most: tiles stay shorter than kMaxTile only while `doubled` tiles of twice their
+// length hold all tokens.  (Fewer tokens can be more tiles: of 4,096 columns 8,176 tokens are 1,022, 8,192 are 512.)
+int64_t most_tiles(int64_t T, int64_t d)
+{
+    const int64_t doubled = (kBusyWarps - 1) / tile_warps(d);
+    return std::min((T + kMinTile - 1) / kMinTile, std::max(2 * doubled, (T + kMaxTile - 1) / kMaxTile));
 }
 
 bool boundary(const void *p, int64_t ld, int32_t dtype)
@@ -602,8 +612,7 @@ struct Workspace {
         for (uint2 *&list : sort.list)
             list = reinterpret_cast<uint2 *>(take(sizeof(uint2) * (size_t)T));
         present = reinterpret_cast<uint32_t *>(take(sizeof(uint32_t) * (size_t)((vocab + 31) / 32)));
-        const int tile = tile_size(T, d);
-        partial = reinterpret_cast<float *>(take(sizeof(float) * 2 * (size_t)ldp * (size_t)((T + tile - 1) / tile)));
+        partial = reinterpret_cast<float *>(take(sizeof(float) * 2 * (size_t)ldp * (size_t)most_tiles(T, d)));
     }
 };
 

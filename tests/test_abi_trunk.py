@@ -133,3 +133,15 @@ def test_binding_refuses_what_does_not_fit():
         P._param_dtype(v.half())
     with pytest.raises(ValueError):
         P._act8_code(x, "codes")
+
+
+def test_workspace_of_a_larger_batch_will_do(lib):
+    """No batch needs more than a larger one, wherever the lengths of the tiles double."""
+    for d in (1, 256, 1001, 4096, 8200, 3_000_000):
+        for vocab in (100, 151_936):
+            sizes = [lib.turnopd_embedding_bwd_workspace_bytes(T, d, vocab)
+                     for T in sorted({k * n + j for n in (1, 2, 4, 8, 16, 32, 64) for k in (1, 97, 511, 1022, 4095, 8191, 8192, 65_536)
+                                      for j in (0, 1, 15, 16)})]
+            assert sizes == sorted(sizes) and sizes[0] > 0
+    # partial sums of two rows of 4,096 columns for each of 1,022 tiles at most, beside the list of tokens
+    assert lib.turnopd_embedding_bwd_workspace_bytes(32_768, 4096, 100) <= 1022 * 2 * 4096 * 4 + 32_768 * 16 + 1024

@@ -226,3 +226,18 @@ def test_rows_far_apart(d):
     check_backward(dw, out, ids, n, 1.0)
     del w, out, dw
     torch.cuda.empty_cache()
+
+
+def test_one_workspace_for_batches_of_any_size():
+    """A workspace made for the largest batch, filled with other bits, serves every smaller one."""
+    d, V = 4096, 300
+    ws = torch.empty(P.turnopd_embedding_bwd_workspace_bytes(9000, d, V), dtype=torch.uint8, device="cuda")
+    st = torch.zeros(1, dtype=torch.int32, device="cuda")
+    for T in (8176, 8192, 9000, 40, 1):
+        ids = torch.randint(V, (T,), device="cuda").int()
+        dout = torch.randint(-3, 4, (T, d), device="cuda").to(BF)
+        dw = torch.full((V, d), 3.0, device="cuda")
+        ws.fill_(255)
+        P.turnopd_embedding_bwd(dout, ids, None, 1.0, dw, 0, ws, st)
+        assert st.item() == 0
+        check_backward(dw, dout, ids, V, 1.0)
