@@ -548,7 +548,8 @@ turnopd_status turnopd_embedding_fwd(const void *w, int32_t w_dtype, int64_t ldw
  *   With TURNOPD_ACCUMULATE_GRAD the sums are added to dw (in fp32, rounded once), and
  *   rows of ids that do not occur are neither read nor written: a head tied to the
  *   embedding has its own gradient there already.
- * Flags: TURNOPD_ACCUMULATE_GRAD only.
+ * Flags: TURNOPD_ACCUMULATE_GRAD; TURNOPD_FORCE_PORTABLE (diagnostic: the tokens are sorted by
+ *   clusters of a portable size, as where larger ones cannot be placed; the same bits).
  * Workspace: turnopd_embedding_bwd_workspace_bytes(num_tokens, d, vocab), 256-byte aligned; that
  *   of a larger batch will do.
  * Device errors: TURNOPD_ERR_TOKEN_RANGE (token ignored).

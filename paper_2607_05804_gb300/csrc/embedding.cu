@@ -6,6 +6,7 @@
 // the batch repeats thousands of times (a chat template's) is shared by as many tiles.
 
 #include <algorithm>
+#include <atomic>
 
 #include "columns.cuh"
 #include "common.cuh"
@@ -88,7 +89,7 @@ template <typename TW, typename TO, bool VEC> __global__ void __launch_bounds__(
 // ---------------------------------------------------------------- tokens sorted by id
 
 constexpr int kSortThreads = 1024, kSortWarps = 32;
-constexpr int kMaxCtas = 16;      // of the sort's cluster
+constexpr int kMaxCtas = 16, kPortableCtas = 8;  // of the sort's cluster, and where one of 16 cannot be placed
 constexpr int64_t kZeroBytes = 128 << 20;  // written beside the sort at most
 constexpr int kRadixBits = 9;     // at most, of one pass
 constexpr int kSortBatch = 8;     // keys of a lane in flight
@@ -589,6 +590,39 @@ int64_t most_tiles(int64_t T, int64_t d)
     return std::min((T + kMinTile - 1) / kMinTile, std::max(2 * doubled, (T + kMaxTile - 1) / kMaxTile));
 }
 
+// Whether the sort's largest cluster, of a size that is not portable, can be placed: a part of a device may have too few SMs.
+cudaError_t largest_cluster_fits(bool *fits)
+{
+    static std::atomic<int> known[64];  // by device: 1 no, 2 yes
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess)
+        return e;
+    if (dev >= 64)
+        return cudaErrorInvalidDevice;
+    if (!known[dev]) {
+        cudaLaunchConfig_t cfg = {};
+        cudaLaunchAttribute attr[1];
+        attr[0].id = cudaLaunchAttributeClusterDimension;
+        attr[0].val.clusterDim.x = kMaxCtas;
+        attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+        cfg.attrs = attr;
+        cfg.numAttrs = 1;
+        cfg.gridDim = dim3(kMaxCtas);
+        cfg.blockDim = dim3(kSortThreads);
+        cfg.dynamicSmemBytes = sizeof(uint32_t) * kSortWarps << kRadixBits;
+        int clusters = 0;
+        e = cudaOccupancyMaxActiveClusters(&clusters, k_sort_tokens, &cfg);
+        if (e != cudaSuccess && e != cudaErrorInvalidClusterSize)
+            return e;
+        if (e != cudaSuccess)
+            cudaGetLastError();  // that is the answer
+        known[dev] = e == cudaSuccess && clusters > 0 ? 2 : 1;
+    }
+    *fits = known[dev] == 2;
+    return cudaSuccess;
+}
+
 bool boundary(const void *p, int64_t ld, int32_t dtype)
 {
     return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld * (dtype == TURNOPD_BF16 ? 2 : 4) % 16 == 0;
@@ -649,7 +683,15 @@ cudaError_t launch_embed_bwd(const EmbedGradCall &c, cudaStream_t stream)
         return e;
     // As many zeros beside the sort as go out in its time (a small table whole), 32 KB to a CTA at least.
     const int64_t row_bytes = c.d * (c.dw_dtype == TURNOPD_BF16 ? 2 : 4);
-    const unsigned ctas = c.T > 8 * kSortThreads ? kMaxCtas : c.T > kSortThreads ? 8 : 1;
+    unsigned ctas = c.T > 8 * kSortThreads ? kMaxCtas : c.T > kSortThreads ? kPortableCtas : 1;
+    if (ctas > kPortableCtas) {
+        bool fits = false;
+        e = largest_cluster_fits(&fits);
+        if (e != cudaSuccess)
+            return e;
+        if (!fits || c.portable)
+            ctas = kPortableCtas;
+    }
     int64_t rows_zeroed = c.accumulate ? 0 : c.vocab;
     if (c.T > 0 && rows_zeroed * row_bytes > kZeroBytes)
         rows_zeroed = kZeroBytes / row_bytes / kZeroRows * kZeroRows;

@@ -355,7 +355,7 @@ struct EmbedGradCall {
     void *dw;
     int32_t dw_dtype;
     int64_t ldw, vocab;
-    bool accumulate;
+    bool accumulate, portable;
     void *workspace;
     int32_t *status;
 };

@@ -618,7 +618,7 @@ turnopd_status turnopd_embedding_bwd(const void *dout, int32_t dout_dtype, int64
     NvtxRange nvtx("turnopd_embedding_bwd");
     if (!dev_status || !dw || (num_tokens > 0 && (!dout || !token_ids)))
         return TURNOPD_ERR_NULL;
-    if (!is_dtype(dout_dtype) || !is_dtype(dw_dtype) || (flags & ~(uint32_t)TURNOPD_ACCUMULATE_GRAD))
+    if (!is_dtype(dout_dtype) || !is_dtype(dw_dtype) || (flags & ~(uint32_t)(TURNOPD_ACCUMULATE_GRAD | TURNOPD_FORCE_PORTABLE)))
         return TURNOPD_ERR_UNSUPPORTED;
     if (bad_count(num_tokens, d) || vocab < 1 || vocab > INT32_MAX || bad_rows(dout, dtype_size(dout_dtype), ldg, d) ||
         bad_rows(dw, dtype_size(dw_dtype), ldw, d) || misaligned(token_ids, 4) || !finite_f32(scale))
@@ -629,7 +629,7 @@ turnopd_status turnopd_embedding_bwd(const void *dout, int32_t dout_dtype, int64
     if (num_tokens == 0 && accumulate)
         return TURNOPD_OK;
     EmbedGradCall c{dout, dout_dtype, ldg, token_ids, mask, num_tokens, d, (float)scale, dw, dw_dtype, ldw, vocab, accumulate,
-                    workspace, dev_status};
+                    (flags & TURNOPD_FORCE_PORTABLE) != 0, workspace, dev_status};
     return cuda_status(launch_embed_bwd(c, (cudaStream_t)stream));
 }
 

@@ -241,3 +241,19 @@ def test_one_workspace_for_batches_of_any_size():
         P.turnopd_embedding_bwd(dout, ids, None, 1.0, dw, 0, ws, st)
         assert st.item() == 0
         check_backward(dw, dout, ids, V, 1.0)
+
+
+@pytest.mark.parametrize("T,V", [(8193, 70_001), (20_000, 513), (70_001, 262_150)])
+def test_sort_by_clusters_of_a_portable_size(T, V):
+    """Where a cluster of sixteen CTAs cannot be placed eight sort the tokens: the same bits."""
+    d = 40
+    dout = torch.randn((T, d), device="cuda")
+    ids = (V ** torch.rand(T, device="cuda", dtype=torch.float64)).long().clamp(1, V).sub_(1).int()
+    mask = (torch.rand(T, device="cuda") < 0.8).to(torch.uint8)
+    ref, _ = backward(dout, ids, V, 1.0, F, mask=mask)
+    got, st = backward(dout, ids, V, 1.0, F, mask=mask, flags=P.TURNOPD_FORCE_PORTABLE)
+    assert st.item() == 0 and torch.equal(got, ref)
+    check_backward(got, dout, ids, V, 1.0, on=mask.bool())
+    old = torch.randn((V, d), device="cuda")
+    both = [backward(dout, ids, V, 1.0, F, mask=mask, dw=old.clone(), flags=P.TURNOPD_ACCUMULATE_GRAD | f)[0] for f in (0, P.TURNOPD_FORCE_PORTABLE)]
+    assert torch.equal(*both)
