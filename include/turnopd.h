@@ -654,8 +654,11 @@ size_t turnopd_block_norm_bwd_workspace_bytes(int64_t num_tokens, int64_t d);
  *         group that holds NaN or inf gets 255 and codes of 0, and loads as NaN.
  * Device errors: TURNOPD_ERR_NONFINITE (such a group).
  *
- * turnopd_act8_load -- takes them back: out[i, j] = code 2^k of out_dtype, exact in either
- * type (what lies beyond the type's largest value becomes that value).
+ * turnopd_act8_load -- takes them back: out[i, j] = code 2^k of out_dtype, exact but at the
+ * type's ends: what lies beyond its largest value becomes that value, and BF16, whose smallest
+ * step is 2^-133, rounds E4M3 values that are no multiple of it (they reach down to 2^-135) to
+ * the nearest one, ties to even.  turnopd_block_norm_bwd takes code 2^k in fp32, where codes
+ * that stand for 2^128 or more are infinite.
  */
 turnopd_status turnopd_act8_store(const void *x, int32_t x_dtype, int64_t ldx, const uint8_t *mask,
                                   int64_t num_tokens, int64_t d, void *codes, int32_t code_dtype, int64_t ldc,

@@ -181,3 +181,19 @@ def test_rows_far_apart(d):
     assert torch.equal(out, near)
     del x, q, out
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("d", [32, 33])
+def test_values_below_the_smallest_of_bf16(d):
+    """e4m3 codes reach down to 2^-135, bf16 to 2^-133: what lies between is rounded to the nearest one, ties to even."""
+    n = torch.arange(-16, d - 16, dtype=torch.float64)
+    x = (n * 2.0 ** -135).float()[None].repeat(2, 1).cuda()  # codes up to sixteen of the smallest steps: exact
+    for code in (E4M3, INT8):
+        q, exps, st = store(x, code)
+        wide, out = torch.empty_like(x), torch.empty((2, d), device="cuda", dtype=BF)
+        P.turnopd_act8_load(q, exps, wide)
+        P.turnopd_act8_load(q, exps, out)
+        assert st.item() == 0 and bool((exps == 1).all())
+        exact = (n if code is E4M3 else torch.zeros_like(n)) * 2.0 ** -135
+        assert same(wide[0], exact)
+        assert same(out[0], torch.round(exact * 2.0 ** 133) * 2.0 ** -133) and torch.equal(out[0], out[1])
