@@ -524,9 +524,9 @@ size_t turnopd_norm_bwd_workspace_bytes(int64_t num_tokens, int64_t d);
  * What stands outside a policy model's matrix products on the other side of its blocks:
  * the embedding, and the norms, gate and residual connection between two blocks.  `mask`
  * is uint8[num_tokens] or NULL (every token takes part): rows of tokens with mask 0 (the
- * padding of a batch, say) are not read, and their rows of the outputs are zero.  Columns
- * [d, ld) of an output are not written, and outputs may not overlap inputs unless the
- * entry says so.
+ * padding of a batch, say) are of no effect, whatever they hold, though some of their
+ * elements may be read; their rows of the outputs are zero.  Columns [d, ld) of an output
+ * are not written, and outputs may not overlap inputs unless the entry says so.
  *
  * turnopd_embedding_fwd -- rows of an embedding table, scaled:
  *   out[i, j] = scale w[token_ids[i], j]

@@ -502,3 +502,26 @@ def test_backward_from_8_bits_same_bits_every_time(T, d, kind, code):
     for _ in range(10):
         again = c.backward(kr, ky, stats)
         assert all(torch.equal(first[k], again[k]) for k in first)
+
+
+@pytest.mark.parametrize("code", [None, E4M3, INT8])
+@pytest.mark.parametrize("d,pad", [(512, 0), (1000, 0), (1001, 0), (1000, 3), (8201, 0)])
+def test_masked_rows_are_of_no_effect(d, pad, code):
+    """Whatever they hold: codes and exponents of any bits, statistics and gradients that are not finite."""
+    for gate, kind in (("channel", RMS), ("token", LAYER)):
+        c = case(700, d, (BF, BF, BF, pad, 0), gate=gate, kind=kind, masked=0.4)
+        resid, _, stats, _ = c.forward()
+        kr, ky = c.kept(resid, code), c.kept(c.y, code)
+        first = c.backward(kr, ky, stats)
+        c.check_backward(first, kr, ky, stats)
+        off = ~c.on
+        for x in (kr, ky):
+            if code is None:
+                x[off] = float("inf")
+            else:
+                x[0].view(torch.uint8)[off] = 127  # NaN among e4m3 codes
+                x[1][off] = 255
+        stats[off] = float("nan")
+        c.dh[off], c.d_resid_out[off] = -float("inf"), float("inf")
+        again = c.backward(kr, ky, stats)
+        assert all(torch.equal(first[k], again[k]) for k in first)
