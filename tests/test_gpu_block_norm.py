@@ -525,3 +525,42 @@ def test_masked_rows_are_of_no_effect(d, pad, code):
         c.dh[off], c.d_resid_out[off] = -float("inf"), float("inf")
         again = c.backward(kr, ky, stats)
         assert all(torch.equal(first[k], again[k]) for k in first)
+
+
+NO_BETAS = ("dbeta_post", "dbeta_pre")
+
+
+@pytest.mark.parametrize("gate", ["none", "channel", "token"])
+@pytest.mark.parametrize("T,d,pad", [(40, 16, 0), (1300, 256, 0), (1300, 264, 0), (1300, 512, 0), (1300, 2048, 8), (1300, 4096, 0), (700, 4104, 0),
+                                     (700, 5120, 0), (330, 6144, 0), (330, 8192, 0), (1300, 1001, 0), (330, 1000, 3), (330, 3001, 0),
+                                     (330, 4101, 0), (330, 6147, 0), (330, 8191, 0)])
+def test_backward_of_root_mean_square_norms_alone(T, d, pad, gate):
+    """No betas and no gradients of any: the kernels without the means of layer norms and the sums for betas -- two pieces to a
+    thread from 1,216 rows of 257 to 4,096 columns, 640 threads above that, two pieces again above 5,120 -- by what r' and y
+    are stored in, and rows that begin anywhere."""
+    for k, (rdt, ydt) in enumerate(((BF, BF), (F, BF), (BF, F), (F, F))):
+        c = case(T, d, (rdt, ydt, (BF, F)[k % 2], pad, 0), gate=gate, kind=RMS, masked=0.2 if k else 0.0, s=0.5, alpha=(1.0, 0.7)[k // 2])
+        resid, _, stats, _ = c.forward()
+        for r_code, y_code in ((None, None), (E4M3, E4M3), (INT8, INT8), (None, E4M3), (INT8, None)):
+            kr, ky = c.kept(resid, r_code), c.kept(c.y, y_code)
+            c.check_backward(c.backward(kr, ky, stats, skip=NO_BETAS), kr, ky, stats)
+
+
+@pytest.mark.parametrize("code", [None, E4M3, INT8])
+@pytest.mark.parametrize("T,d,pad", [(1300, 512, 0), (1300, 4096, 0), (330, 5120, 0), (330, 8192, 0), (330, 1001, 0), (330, 6147, 0)])
+def test_root_mean_square_norms_with_parts_missing(T, d, pad, code):
+    """The same without the stream's gradient, without one norm or its gradients, and each output by itself."""
+    for post, pre in ((True, True), (False, True), (True, False)):
+        for gate in ("none", "channel", "token"):
+            c = case(T, d, (BF, BF, F, pad, 0), gate=gate, kind=RMS, post=post, pre=pre, masked=0.2)
+            resid, _, stats, _ = c.forward()
+            kr = c.kept(resid, code) if pre else None
+            ky = c.kept(c.y, code) if post or gate != "none" else None
+            whole = c.backward(kr, ky, stats, skip=NO_BETAS)
+            c.check_backward(whole, kr, ky, stats)
+            if pre:
+                c.check_backward(c.backward(kr, ky, stats, skip=NO_BETAS, d_resid_out=None), kr, ky, stats, dro=None)
+            for name in whole:
+                if whole[name] is not None:
+                    alone = c.backward(kr, ky, stats, skip=[k for k in whole if k != name])
+                    c.check_backward(alone, kr, ky, stats)
