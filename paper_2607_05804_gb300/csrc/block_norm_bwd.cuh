@@ -92,10 +92,10 @@ __device__ __forceinline__ float column_value(uint32_t raw, int dtype, uint32_t 
 
 // One or two pieces of eight columns to a thread, which keeps their sums over rows in registers from row to row.  Group b of all
 // takes rows b, b + groups, ..., so that every sum has a fixed order.  A row's arrays come through a ring in shared memory, in
-// which each thread copies and reads its own pieces only (of codes in whole blocks each warp).  The sums over the next row that D needs are taken together with
-// those over the row at hand that dy needs: one barrier to a row.  gamma lies in shared memory, and values are read from
-// the ring once more where they are needed again: a thread's registers would not hold them.  A warp's pieces lie 256
-// columns apart, so that they are found at constant offsets.
+// which each thread copies and reads its own pieces only (codes of r', and of y where it keeps them, in whole blocks each warp).
+// The sums over the next row that D needs are taken together with those over the row at hand that dy needs: one barrier to a
+// row.  gamma lies in shared memory, and values are read from the ring once more where they are needed again: a thread's
+// registers would not hold them.  A warp's pieces lie 256 columns apart, so that they are found at constant offsets.
 //
 // Bound: instruction issue and its latencies beside HBM (ncu, 8,192 rows: 0.58 of the issue slots with 15 to 20 warps per SM).
 // An element takes four arrays' unpacking, partly twice, 14 multiply-adds and a share of the row's sums, 40 to 52 instructions.
@@ -115,6 +115,12 @@ __global__ void __launch_bounds__(MOST, 1) k_block_bwd(BlockGradCall c, Ring rin
     // sums over a row: of g xh (and of g) of the norm after the block, and of the norm before the next one
     constexpr int kRowSums = GENERAL ? 4 : 2, kE = 8 * kPieces, kExtra = extra_bytes(kPieces, STORED != kGradientTypes);
     constexpr bool kMixed = STORED == kAny, kCodes = STORED == kE4m3 || STORED == kInt8;
+    // Codes that a warp copied together are read before the warp meets in the middle of a row, since the next row's copies come
+    // into their place from the row's end on.  y's are needed once more behind that, for dy: two pieces' are kept in registers
+    // (32,768 x 4,096 from e4m3 275 us; copied by each thread for itself 296; with the warp meeting once more 282, and 526 with
+    // an fp32 stream, which takes 410); one piece's, for which the registers are too few, and those of arrays of any type are
+    // copied by each thread for itself (16,384 x 5,120 layer norms from int8 380 us; in registers 440; meeting once more 442).
+    constexpr bool kKeepY = kCodes && !ENDS && kPieces == 2;
     constexpr int kTypeR = type_code<STORED, TR>(), kTypeY = type_code<STORED, TY>();
     extern __shared__ __align__(128) char shared[];
     __shared__ Numbers<kRowSums> red[2][MOST / 32];
@@ -157,14 +163,15 @@ __global__ void __launch_bounds__(MOST, 1) k_block_bwd(BlockGradCall c, Ring rin
     uint32_t ons = 0;  // whether the rows copied last are not masked, the newest in bit 0
     const bool code_r = kCodes ? pre : kMixed && pre && ring.resid.dtype >= TURNOPD_E4M3;
     const bool code_y = kCodes ? needs_y : kMixed && needs_y && ring.y.dtype >= TURNOPD_E4M3;
+    const bool held_y = kKeepY && code_y && put_dy && post;  // wherever y is read for dy
     const auto copy = [&]() {
         if (ahead < T && ahead_on) {
             char *to = own + ahead_stage * ring.stage;
-            const auto part = [&](const RingPart &p, int bytes) {
+            const auto part = [&](const RingPart &p, int bytes, bool by_warp) {
                 if (!p.p || (!COMMON && p.direct))
                     return;
                 const char *from = p.p + (uint64_t)ahead * p.pitch;
-                if (bytes == 1 && ring.blocks) {
+                if (bytes == 1 && by_warp) {
                     // a warp's codes together, sixteen at a time: half as many copies
                     const int lane = t & 31;
                     if (lane < 16 * kPieces)
@@ -185,11 +192,11 @@ __global__ void __launch_bounds__(MOST, 1) k_block_bwd(BlockGradCall c, Ring rin
                     }
                 }
             };
-            part(ring.resid, kMixed ? ring.resid.bytes : type_bytes(kTypeR));
-            part(ring.dh, sizeof(TY));
-            part(ring.dro, sizeof(TR));
-            part(ring.y, kMixed ? ring.y.bytes : type_bytes(kTypeY));
-            part(ring.gate, sizeof(TY));
+            part(ring.resid, kMixed ? ring.resid.bytes : type_bytes(kTypeR), ring.blocks);
+            part(ring.dh, sizeof(TY), false);
+            part(ring.dro, sizeof(TR), false);
+            part(ring.y, kMixed ? ring.y.bytes : type_bytes(kTypeY), kKeepY && ring.blocks);
+            part(ring.gate, sizeof(TY), false);
             char *extra = to + ring.extra + (t >> 5) * kExtra;
             const int lane = t & 31, block = min((t >> 5) * kPieces + lane, d / 256 - 1);  // of 256 columns
             if (lane == 0 && (COMMON || c.stats))
@@ -332,6 +339,17 @@ __global__ void __launch_bounds__(MOST, 1) k_block_bwd(BlockGradCall c, Ring rin
     const auto centred_y = [&](const char *at, uint32_t i, const Row &m, int k, float2 *v) {  // mu is 0 without that norm
         return activation(at, i, ring.y, kTypeY, m.ey[k], m.ey2[ENDS ? k : 0], m.stats.x, k, v);
     };
+    // the same from y's codes in registers
+    const auto centred_codes = [&](uint2 codes, const Row &m, int k, float2 *v) {
+        decode8(codes, kTypeY == TURNOPD_E4M3, reinterpret_cast<float *>(v));
+        const float scale = act_scale(m.ey[k]);
+        if (!GENERAL)
+            return scale;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            v[e] = ffma2(v[e], splat(scale), splat(-m.stats.x));
+        return 1.f;
+    };
     const auto times_gamma = [&](int k, float2 *g) {
         const float4 a = gamma[2 * k * n], z = gamma[(2 * k + 1) * n];
         g[0] = fmul2(g[0], make_float2(a.x, a.y));
@@ -395,9 +413,6 @@ __global__ void __launch_bounds__(MOST, 1) k_block_bwd(BlockGradCall c, Ring rin
         odd ^= 1;
     }
     for (uint32_t i = b; i < T; i += groups) {
-        // the warp's codes of the last row, which any of its lanes may have read until now, lie in the stage that is filled next
-        if (!ENDS && (kMixed || kCodes))
-            __syncwarp();
         copy();
         Row after = read_row(i + 2 * groups);
         const char *at = own + stage * ring.stage;
@@ -547,6 +562,11 @@ __global__ void __launch_bounds__(MOST, 1) k_block_bwd(BlockGradCall c, Ring rin
             if (dgate)
                 put1(TY(), c.dgate, ring.dgate, 0.f);
         }
+        uint2 y_codes[kKeepY ? kPieces : 1];
+        if (held_y)
+#pragma unroll
+            for (int k = 0; k < kPieces; ++k)
+                y_codes[kKeepY ? k : 0] = *reinterpret_cast<const uint2 *>(at + ring.y.at + piece0 * 8 + k * 256);
         wait_copies(ring.stages - 2);
         __syncwarp();
         complete(next, own + next_stage * ring.stage, ons >> (ring.stages - 2) & 1);
@@ -566,7 +586,7 @@ __global__ void __launch_bounds__(MOST, 1) k_block_bwd(BlockGradCall c, Ring rin
 #pragma unroll
             for (int k = 0; k < kPieces; ++k) {
                 float2 x[4];
-                const float f = a1 * centred_y(at, i, m, k, x);
+                const float f = a1 * (held_y ? centred_codes(y_codes[kKeepY ? k : 0], m, k, x) : centred_y(at, i, m, k, x));
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     x[e] = ffma2(x[e], splat(f), fmul2(E[4 * k + e], splat(r0)));
@@ -721,11 +741,13 @@ template <typename TR, typename TY> cudaError_t launch_block_rows_bwd(const Bloc
     *taken = phases.alike && most < (int64_t)1 << 30 && c.d >= 16;
     if (!*taken)
         return cudaSuccess;
-    // Two pieces to a thread and two blocks per SM up to 4,096 columns (from 8-bit activations, 32,768 x 4,096: 277 us, one piece
-    // and one block 352); then one piece, whose blocks have twice the warps (16,384 x 5,120 bf16: 192 us, two pieces 203), as
-    // long as a block's threads hold the row.  With the sums of layer norms or betas (32,768 x 4,096: two pieces 742 us, one 345),
-    // or in rows that begin anywhere (16,384 x 3,001: 452 and 226), two pieces are more than the registers hold.  For few rows
-    // one piece answers sooner (512 x 4,096: 18 us with two, 16.6 with one).
+    // Two pieces to a thread up to 4,096 columns, with two blocks per SM where both have room, as beside four bf16 arrays (from
+    // 8-bit activations, 32,768 x 4,096: 275 us, one piece and one block 352).  With a gate for every element mostly one block
+    // of 256 threads has: 32,768 x 4,096 481 us, 0.66 of the copy rate, where two have 0.84 without such a gate.  Then one piece,
+    // whose blocks have twice the warps (16,384 x 5,120 bf16: 192 us, two pieces 203), as long as a block's threads hold the row.
+    // With the sums of layer norms or betas (32,768 x 4,096: two pieces 742 us, one 345), or in rows that begin anywhere
+    // (16,384 x 3,001: 452 and 226), two pieces are more than the registers hold.  For few rows one piece answers sooner
+    // (512 x 4,096: 18 us with two, 16.6 with one).
     const bool two = !block_bwd_general(c) && !phases.at && !phases.step && c.d % 8 == 0 && c.d > 256 &&
                      c.d <= 4096 && c.T >= 8 * device_sm_count();
     if (c.d > 8 * kMany || two)
