@@ -363,8 +363,9 @@ template <typename TR, typename TY, bool GATE> cudaError_t launch_gated(const Bl
         return launch_rows<TR, TY, GATE, 1, 512, 1>(c, phases, stream);
     if (few)
         return launch_rows<TR, TY, GATE, 1, 1024, 1>(c, phases, stream);
-    // bf16 layer norms with a gate per channel, 32,768 x 512: 42 us with four pieces, 31 with two; 32,768 x 4,096: 223, 268;
-    // 16,384 x 8,192: 374, 287 (two copies of their four vectors do not fit beside each other)
+    // bf16 layer norms with a gate per channel, rows on boundaries, 32,768 x 512: 40 us with four pieces, 29 with two; x 1,024:
+    // 50, 63; x 4,096: 204, 251; 16,384 x 5,120: 185, 220; x 8,192: 317, 268 (two copies of their four vectors do not fit beside
+    // each other)
     const bool general = c.kind == TURNOPD_LAYER_NORM || c.beta_post || c.beta_pre;
     if constexpr (sizeof(TR) + sizeof(TY) * (GATE ? 2 : 1) <= 6)
         if (c.d > 512 && (!general || c.d <= 5120))
