@@ -306,3 +306,20 @@ def test_a_gate_for_every_element(dtype, keep, tol):
                 assert relative(out["norms"][k][name], leaves[id(getattr(n, name))].grad) < tol, (k, name)
         for got, p in zip(out["blocks"][k], params[k]):
             assert relative(got, leaves[id(p)].grad) < tol
+
+
+def test_decoding_step_in_a_graph():
+    """A step captured once gives the hidden states of whatever tokens its buffer holds; products of the same sizes, fp32."""
+    kind, d, V = RMS, 256, 700
+    b, T, table, ids, blocks, norms, params, _, _ = make(kind, d, V, torch.float32)
+    trunk = PolicyTrunk(table, blocks, norms, params, kind=kind)
+    step = ids[:4].clone()
+    trunk.forward(step, save=False)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        x = trunk.forward(step, save=False)
+    for k in (4, 100, 200):
+        step.copy_(ids[k:k + 4])
+        graph.replay()
+        assert relative(x, PolicyTrunk(table, blocks, norms, params, kind=kind).forward(step, save=False)) < 1e-5
+    assert trunk.status() == 0
